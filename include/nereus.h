@@ -68,9 +68,11 @@ extern "C" {
 #define NEREUS_ERR_ALIAS         -4   /* a destination buffer overlaps a source or another destination     */
 #define NEREUS_ERR_CUDA          -5   /* a CUDA call failed; see nereus_last_cuda_error                    */
 #define NEREUS_ERR_NOMEM         -6   /* host allocation failed                                            */
-#define NEREUS_ERR_MISMATCH      -7   /* parts of a chained fuse do not connect (buffer count or sizes)    */
-#define NEREUS_ERR_ALIGN         -8   /* a shard pointer is not 16-byte aligned                            */
-#define NEREUS_ERR_TOO_LARGE     -9   /* more tasks than the fixed scratch of nereus_transition_run_static */
+#define NEREUS_ERR_MISMATCH      -7   /* parts of a chained fuse do not connect (buffer count or sizes);    */
+                                      /* a written logits view is cut otherwise than the read one          */
+#define NEREUS_ERR_ALIGN         -8   /* a shard pointer is not 16-byte aligned (logits: to its element)   */
+#define NEREUS_ERR_TOO_LARGE     -9   /* more tasks than the fixed scratch of nereus_transition_run_static; */
+                                      /* a logits call beyond the limits named with it                     */
 /* -10 is NEREUS_ERR_INFEASIBLE, declared with the transition DAG below */
 #define NEREUS_ERR_TABLE         -11  /* the task table failed the host-side check that precedes every upload */
 #define NEREUS_ERR_TOO_SMALL     -12  /* a buffer handed to nereus_transition_run_sized is shorter than required */
@@ -426,6 +428,116 @@ int nereus_transition_run_static(nereus_transition_t t, const void* const* src_p
  * caller must have synchronised the stream of those runs.  Allocates nothing; copies a few bytes from the
  * device synchronously.  Like the entry point it serves, it has no counterpart in the paper. */
 int nereus_static_status(int* device_status);
+
+/* ---- the model-stages' own steps on the LM head's logits ----------------------------------------------- */
+
+/* What the head of a plan answers with: rows x vocab logits, cut into tp column shards exactly as the head's rows
+ * are cut over the TP ranks, every shard a device buffer of its own.  Shard s holds columns
+ * [s*shard_cols, min((s+1)*shard_cols, vocab)), row r of it at shard[s] + r*row_stride elements.  Under a padded
+ * plan (NEREUS_VOCAB_PADDED) shard_cols is V_pad/tp: columns at or past `vocab` are padding, they never count and
+ * are never written, and a shard that lies wholly past `vocab` may be NULL.
+ * One tensor [rows, vocab] is tp = 1; a tensor cut into column slices is tp slices with the tensor's row_stride.
+ * Pointers are aligned to an element.  Any vocab >= 1 and any row_stride work; rows whose starts are congruent
+ * modulo 16 bytes on the read and the written side are moved in 16-byte vectors.
+ * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and
+ * may be captured into a CUDA graph (after a first call on the device).  rows = 0 is a call that does nothing.
+ * Common errors: ARG (null pointer, non-positive size, a shard or stride too small for its columns), UNSUPPORTED
+ * (dtype), ALIGN (a pointer that is not aligned to its element), MISMATCH (the written view has other rows,
+ * vocabulary or cut than the read one), ALIAS (a written view overlaps a read one without being it, or itself),
+ * TOO_LARGE (limits named with each call), CUDA. */
+#define NEREUS_VOCAB_MAX_TP 64
+typedef struct {
+    int32_t dtype;                 /* NEREUS_BF16 or NEREUS_FP32 */
+    int32_t tp;                    /* column shards, 1..NEREUS_VOCAB_MAX_TP */
+    int64_t rows, vocab;
+    int64_t shard_cols;            /* columns per shard, tp * shard_cols >= vocab */
+    int64_t row_stride;            /* elements between two rows of a shard */
+    void*   shard[NEREUS_VOCAB_MAX_TP];    /* device */
+} nereus_logits_t;
+
+/* GENERATION: penalties for repeated tokens, biases and grammar masks on a batch of rows, and of the processed row
+ * the greedy token and the log-sum-exp that its sampler needs.  With x the logit of token v in fp32, each step
+ * rounded on its own:
+ *   seen in the history:          x = x > 0 ? x / repetition : x * repetition
+ *   generated `n` times:          x = x - frequency * n ; x = x - (n > 0 ? presence : 0)
+ *   in the row's bias list:       x = x + bias
+ *   not allowed by the row's mask: x = -inf, whatever it was
+ * and the result is rounded to the written type (out->dtype: in->dtype or NEREUS_FP32).  token[r] = the lowest id of
+ * the largest written value, -1 when no value is above -inf; lse[r] = log of the sum of exp of the written values
+ * (-inf when all are, NaN when one is).
+ * All arrays are on the device.  Optional parts are NULL. */
+#define NEREUS_BIAS_MAX    1023
+#define NEREUS_HISTORY_MAX 1048576
+typedef struct {
+    const int32_t* history;        /* [rows, history_stride] token ids, the prompt and then what was generated; ids */
+    int64_t history_stride;        /* outside [0, vocab) count for nothing; or NULL */
+    int64_t history_len;           /* columns in use, at most history_stride and NEREUS_HISTORY_MAX */
+    const int32_t* prompt_len;     /* [rows] or NULL = 0: the first prompt_len[r] tokens count for `seen` only */
+    const int32_t* total_len;      /* [rows] or NULL = history_len; clamped to [0, history_len] */
+    const float*   repetition;     /* [rows] > 0, or NULL = 1 */
+    const float*   presence;       /* [rows], or NULL = 0 */
+    const float*   frequency;      /* [rows], or NULL = 0 */
+    const int32_t* bias_ids;       /* [rows, bias_count], ids outside [0, vocab) are unused entries; of entries of one */
+    const float*   bias_values;    /* id the last counts; or NULL */
+    int64_t bias_count;            /* at most NEREUS_BIAS_MAX */
+    const int32_t* mask;           /* [mask_rows, mask_stride] bit words: token v is allowed when bit v % 32 of word */
+    int64_t mask_stride;           /* v / 32 is set; mask_stride >= ceil(vocab / 32); or NULL */
+    int64_t mask_rows;
+    const int32_t* mask_row;       /* [rows]: row r's mask, none when outside [0, mask_rows); NULL = mask r for row r */
+} nereus_penalties_t;
+/* out == in (same buffers, strides and type) processes in place.  token, lse (device, [rows]) may be NULL.
+ * Errors: common, TOO_LARGE (history, biases, vocab > 2^24). */
+int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out, const nereus_penalties_t* how,
+                          int32_t* token, float* lse, void* cuda_stream);
+
+/* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
+ * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of
+ * exp(x / temperature).  NaN is never taken; a row with fewer than k other logits ends in (-inf, -1).
+ * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite), TOO_LARGE (vocab). */
+#define NEREUS_TOP_MAX_K 256
+int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, float* values, int32_t* ids, float* lse,
+                       void* cuda_stream);
+
+/* TRAINING: distillation from a teacher's top logits.  A row's tokens fall into the groups of its entries, one token
+ * each, and one group `rest` of all other tokens.  With z = x / T, m = max x, S = sum exp((x - m) / T), S_rest the same
+ * over the rest, the student gives the groups Q_k = exp((x_k - m) / T) / S and Q_rest = S_rest / S.  The teacher gives
+ *   lse != NULL   P_k = exp(value_k / T - lse), P_rest = max(0, 1 - sum P_k)
+ *   lse == NULL   P = softmax over the entries of value / T, P_rest = 0        (forward KL only)
+ * and the divergence of the row is, with 0 log 0 = 0,
+ *   NEREUS_FORWARD_KL   D = sum_g P_g log(P_g / Q_g)
+ *   NEREUS_REVERSE_KL   D = sum_g Q_g log(Q_g / P_g), P_rest at least 2^-24 (the resolution of its sum)
+ *   NEREUS_JENSEN       D = beta KL(P || M) + (1 - beta) KL(Q || M), M = beta P + (1 - beta) Q, 0 < beta < 1
+ * Its gradient is dD/dx_v = Q_v (f_g(v) - sum_g Q_g f_g) / T with f = -P/Q, log(Q/P), (1 - beta) log(Q/M).
+ * loss[r] = weight[r] * D.  A row of weight 0 is not read: its loss, saved sums and gradient are 0, whatever it holds.
+ * Entries of one row have distinct ids; ids outside [0, vocab) are unused entries; a row without entries has no loss.
+ * A student that gives an entry no mass at all where the teacher does has loss +inf in the forward KL (and a finite
+ * gradient); a teacher that gives an entry none where the student does, in the reverse KL, loss +inf and gradient NaN. */
+#define NEREUS_FORWARD_KL 0
+#define NEREUS_REVERSE_KL 1
+#define NEREUS_JENSEN     2
+typedef struct {
+    int32_t k;                     /* entries per row, 1..NEREUS_TOP_MAX_K */
+    int32_t divergence;
+    float   beta;                  /* NEREUS_JENSEN only */
+    float   temperature;
+    const float*   values;         /* device [rows, k]: the teacher's logits, as nereus_teacher_top leaves them */
+    const int32_t* ids;            /* device [rows, k] */
+    const float*   lse;            /* device [rows]: the teacher's log-sum-exp of logit / T, or NULL */
+    const float*   weight;         /* device [rows], or NULL = 1 */
+} nereus_distill_t;
+/* The loss alone: loss (device, [rows]) and the sums a backward pass needs, saved (device, [rows, 4]): m, S, S_rest, D. */
+int nereus_distill_forward(const nereus_logits_t* in, const nereus_distill_t* how, float* loss, float* saved,
+                           void* cuda_stream);
+/* The gradient from the saved sums: grad = weight[r] * grad_loss[r] * dD/dx, in the logits' type (grad->dtype ==
+ * in->dtype).  grad_loss (device, [rows]) or NULL = 1.  grad == in is allowed. */
+int nereus_distill_backward(const nereus_logits_t* in, const nereus_distill_t* how, const float* saved,
+                            const float* grad_loss, const nereus_logits_t* grad, void* cuda_stream);
+/* Both in one launch, the row kept on the chip between its sums and its gradient: loss, and grad = weight[r] * dD/dx,
+ * the gradient of the sum of the losses.  grad == in is allowed.
+ * Errors of the three: common, ARG (k, divergence, beta, temperature), UNSUPPORTED (lse == NULL with another divergence
+ * than the forward KL; grad->dtype), TOO_LARGE (vocab). */
+int nereus_distill_step(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
+                        const nereus_logits_t* grad, void* cuda_stream);
 
 const char* nereus_strerror(int code);
 /* cudaError_t of the last failed CUDA call made by this library on the calling thread (0 if none). */

@@ -30,6 +30,8 @@ GENERATION, INFERENCE, TRAINING = 0, 1, 2
 OP_SPLIT, OP_DESTROY, OP_EXTEND, OP_MERGE = 0, 1, 2, 3
 STATIC_MAX_RECTS = 4096
 DEV_OK, DEV_BOUNDS, DEV_TIMEOUT = 0, 1, 2
+VOCAB_MAX_TP, TOP_MAX_K, BIAS_MAX, HISTORY_MAX = 64, 256, 1023, 1048576
+FORWARD_KL, REVERSE_KL, JENSEN = 0, 1, 2
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_34645_b200.build` "
@@ -92,6 +94,29 @@ class PrimInfo(ctypes.Structure):
                                               "order", "level")]
 
 
+class Logits(ctypes.Structure):
+    """nereus_logits_t: rows x vocab logits cut into tp column shards."""
+    _fields_ = [("dtype", ctypes.c_int32), ("tp", ctypes.c_int32), ("rows", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("shard_cols", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("shard", ctypes.c_void_p * VOCAB_MAX_TP)]
+
+
+class Penalties(ctypes.Structure):
+    """nereus_penalties_t."""
+    _fields_ = [("history", ctypes.c_void_p), ("history_stride", ctypes.c_int64), ("history_len", ctypes.c_int64),
+                ("prompt_len", ctypes.c_void_p), ("total_len", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+                ("bias_values", ctypes.c_void_p), ("bias_count", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_int64), ("mask_rows", ctypes.c_int64), ("mask_row", ctypes.c_void_p)]
+
+
+class Distill(ctypes.Structure):
+    """nereus_distill_t."""
+    _fields_ = [("k", ctypes.c_int32), ("divergence", ctypes.c_int32), ("beta", ctypes.c_float),
+                ("temperature", ctypes.c_float), ("values", ctypes.c_void_p), ("ids", ctypes.c_void_p),
+                ("lse", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
+
+
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 _P = ctypes.POINTER
 _SIGS = {
@@ -145,6 +170,11 @@ _SIGS = {
     "nereus_static_status": [_P(_i)],
     "nereus_transition_validate": [_vp],
     "nereus_debug_set_rect": [_vp, _i, _P(Rect)],
+    "nereus_logits_process": [_P(Logits), _P(Logits), _P(Penalties), _vp, _vp, _vp],
+    "nereus_teacher_top": [_P(Logits), _i, ctypes.c_float, _vp, _vp, _vp, _vp],
+    "nereus_distill_forward": [_P(Logits), _P(Distill), _vp, _vp, _vp],
+    "nereus_distill_backward": [_P(Logits), _P(Distill), _vp, _vp, _P(Logits), _vp],
+    "nereus_distill_step": [_P(Logits), _P(Distill), _vp, _P(Logits), _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)          # AttributeError here = the library does not export a declared symbol
@@ -471,6 +501,31 @@ def admit(l_tran, l_step_current, l_step_target, gamma=0.5, h_x=1.0, urgent=Fals
     _ck(_lib.nereus_admit(l_tran, l_step_current, l_step_target, gamma, h_x, int(urgent), ctypes.byref(a),
                           ctypes.byref(pb)), "nereus_admit")
     return bool(a.value), pb.value
+
+
+def logits_process(src: Logits, out: Logits, how: Penalties, token=0, lse=0, stream=0) -> None:
+    """nereus_logits_process; token, lse: device addresses or 0."""
+    _ck(_lib.nereus_logits_process(src, out, how, token, lse, stream), "nereus_logits_process")
+
+
+def teacher_top(src: Logits, k: int, temperature: float, values, ids, lse, stream=0) -> None:
+    """nereus_teacher_top; values, ids, lse: device addresses."""
+    _ck(_lib.nereus_teacher_top(src, k, temperature, values, ids, lse, stream), "nereus_teacher_top")
+
+
+def distill_forward(src: Logits, how: Distill, loss, saved, stream=0) -> None:
+    """nereus_distill_forward; loss, saved: device addresses."""
+    _ck(_lib.nereus_distill_forward(src, how, loss, saved, stream), "nereus_distill_forward")
+
+
+def distill_backward(src: Logits, how: Distill, saved, grad_loss, grad: Logits, stream=0) -> None:
+    """nereus_distill_backward; saved, grad_loss: device addresses, grad_loss may be 0."""
+    _ck(_lib.nereus_distill_backward(src, how, saved, grad_loss, grad, stream), "nereus_distill_backward")
+
+
+def distill_step(src: Logits, how: Distill, loss, grad: Logits, stream=0) -> None:
+    """nereus_distill_step; loss: device address."""
+    _ck(_lib.nereus_distill_step(src, how, loss, grad, stream), "nereus_distill_step")
 
 
 def static_status() -> int:

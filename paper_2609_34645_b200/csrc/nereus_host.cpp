@@ -882,10 +882,10 @@ const char* nereus_strerror(int code) {
     case NEREUS_ERR_ALIAS:       return "a destination buffer overlaps a source or another destination";
     case NEREUS_ERR_CUDA:        return "a CUDA call failed";
     case NEREUS_ERR_NOMEM:       return "out of host memory";
-    case NEREUS_ERR_MISMATCH:    return "chained parts do not connect";
-    case NEREUS_ERR_ALIGN:       return "a shard pointer is not 16-byte aligned";
+    case NEREUS_ERR_MISMATCH:    return "chained parts do not connect, or a written view is cut otherwise than the read one";
+    case NEREUS_ERR_ALIGN:       return "a shard pointer is not 16-byte aligned, or a logits pointer not aligned to its element";
     case NEREUS_ERR_INFEASIBLE:  return "the transition DAG cannot be scheduled: an acquisition stays blocked";
-    case NEREUS_ERR_TOO_LARGE:   return "the transition has more tasks than the fixed scratch of run_static holds";
+    case NEREUS_ERR_TOO_LARGE:   return "the transition has more tasks than the fixed scratch of run_static holds, or a logits call is beyond its limits";
     case NEREUS_ERR_TABLE:       return "the task table failed validation: a task leaves its buffers or two tasks collide";
     case NEREUS_ERR_TOO_SMALL:   return "a shard buffer is shorter than the transition requires";
     default:                     return "unknown error";
