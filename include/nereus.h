@@ -440,7 +440,8 @@ int nereus_static_status(int* device_status);
  * Pointers are aligned to an element.  Any vocab >= 1 and any row_stride work; rows whose starts are congruent
  * modulo 16 bytes on the read and the written side are moved in 16-byte vectors.
  * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and
- * may be captured into a CUDA graph (after a first call on the device).  rows = 0 is a call that does nothing.
+ * may be captured into a CUDA graph.  rows = 0 is a call that does nothing.  A row's results are the same, bit for
+ * bit, whatever other rows the call has and wherever the row stands among them.
  * Common errors: ARG (null pointer, non-positive size, a shard or stride too small for its columns), UNSUPPORTED
  * (dtype), ALIGN (a pointer that is not aligned to its element), MISMATCH (the written view has other rows,
  * vocabulary or cut than the read one), ALIAS (a written view overlaps a read one without being it, or itself),

@@ -5,13 +5,14 @@
 // Logits come cut by vocabulary into column shards, one device buffer each.  All three walk rows of some 100,000
 // elements with a handful of operations on each, so their floor is HBM bandwidth: every logit read once, every written
 // one stored once.  The common frame:
-//   * A row belongs to one thread-block cluster of C = 1, 2, 4 or 8 blocks of 512 threads; its 16-byte vectors are dealt
-//     out in layers of 512 (8 KiB), layer l to block l % C.  A layer lies inside one shard, so that everything about it
+//   * A row belongs to one thread-block cluster of C = 1, 2, 4 or 8 blocks of 256 threads; its 16-byte vectors are dealt
+//     out in layers of 512 (8 KiB, two vectors a thread), layer l to block l % C.  A layer lies inside one shard, so that everything about it
 //     but the thread's own vector is the same for the block: one 32-byte record per layer in shared memory.
 //   * A block's share of the row stays in shared memory (cp.async, every thread reads back only the vectors that it
 //     copied itself, so arrival needs no barrier and no wait that could hang), because the result needs the row's sums
 //     before the first element can be written.  C is the smallest for which three blocks fit on an SM, so that one
-//     block loads while another reduces and a third stores; few rows get more blocks each.
+//     block loads while another reduces and a third stores.  The number of rows has no part in it, so that a row's
+//     result is the same, bit for bit, in any batch.
 //   * The blocks of a cluster exchange a few numbers through distributed shared memory and one cluster barrier.
 //   * Rows of any alignment: vectors that a row fills only in part (its ends, where it does not start on a 16-byte
 //     boundary) are read and written element by element; what lies outside the row is -inf in shared memory.
@@ -50,12 +51,13 @@ struct Deal {
     int32_t aligned;      // every row of every shard starts on a 16-byte boundary
 };
 
-constexpr int kThreads  = 512;
+constexpr int kThreads  = 256;
+constexpr int kVecs     = 2 * kThreads;           // vectors of a layer
 constexpr int kWarps    = kThreads / 32;
 constexpr int kMaxCtas  = 8;                      // portable cluster size
 constexpr float kLog2e  = 1.4426950408889634f;
 
-// One layer of the block's share: positions 0 .. 512 * (elements per vector) - 1, of which [lo, hi) are the row's.
+// One layer of the block's share: positions 0 .. kPerLayer - 1, of which [lo, hi) are the row's.
 struct __align__(16) Layer {
     const char* in;       // address of position 0, 16-byte aligned; may lie before the row where lo > 0
     char*       out;      // ... of the written view, congruent to `in` or not
@@ -66,7 +68,7 @@ struct __align__(16) Layer {
 static_assert(sizeof(Layer) == 32, "Layer is read as two 16-byte words");
 
 template <class T> constexpr int kPerVec = 16 / (int)sizeof(T);
-template <class T> constexpr int kPerLayer = kThreads * kPerVec<T>;
+template <class T> constexpr int kPerLayer = kVecs * kPerVec<T>;
 
 template <class T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
@@ -105,54 +107,102 @@ __device__ __forceinline__ Layer layer_of(const LogitsCut& in, const LogitsCut& 
     return r;
 }
 
-// A 16-byte vector as floats, and back (bf16: round to nearest even).
-template <class T> struct Vec;
-template <> struct Vec<float> {
-    static __device__ __forceinline__ void unpack(uint4 v, float (&f)[4]) {
-        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-    }
-    static __device__ __forceinline__ float max(uint4 v) {           // NaN is passed over
-        float f[4];
-        unpack(v, f);
-        return fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3]));
-    }
-};
-template <> struct Vec<__nv_bfloat16> {
-    static __device__ __forceinline__ void unpack(uint4 v, float (&f)[8]) {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
-    static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
-        uint32_t r;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-        return r;
-    }
-    static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
-        return make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
-    }
-    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
-        uint32_t r;
-        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-        return r;
-    }
-    static __device__ __forceinline__ float max(uint4 v) {
-        const uint32_t m = max2(max2(v.x, v.y), max2(v.z, v.w));
-        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-    }
-};
-
+// Two fp32 in one 64-bit register: sm_100 has add, mul and fma on pairs, which halves the instructions of the loops.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(Pair p) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 __device__ __forceinline__ float exp2_approx(float x) {              // relative error 2^-22, 0 at -inf
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+__device__ __forceinline__ Pair exp2_pair(Pair p) {
+    const float2 f = halves(p);
+    return pair(exp2_approx(f.x), exp2_approx(f.y));
+}
+
+// A 16-byte vector as pairs of fp32, and back (bf16: round to nearest even).  `Max` accumulates maxima without
+// unpacking; NaN is passed over.
+template <class T> struct Vec;
+template <> struct Vec<float> {
+    static constexpr int kPairs = 2;
+    typedef float Max;
+    static __device__ __forceinline__ Max lowest() { return -INFINITY; }
+    static __device__ __forceinline__ void unpack(uint4 v, Pair (&p)[2]) {
+        p[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
+        p[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
+    }
+    static __device__ __forceinline__ uint4 pack(const Pair (&p)[2]) {
+        const float2 a = halves(p[0]), b = halves(p[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
+    }
+    static __device__ __forceinline__ Max max(Max m, uint4 v) {
+        return fmaxf(m, fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))));
+    }
+    static __device__ __forceinline__ Max join(Max a, Max b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ float value(Max m) { return m; }
+};
+template <> struct Vec<__nv_bfloat16> {
+    static constexpr int kPairs = 4;
+    typedef uint32_t Max;
+    static __device__ __forceinline__ Max lowest() { return 0xff80ff80u; }
+    static __device__ __forceinline__ Pair open(uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+    static __device__ __forceinline__ uint32_t close(Pair p) {
+        const float2 f = halves(p);
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(f.y), "f"(f.x));
+        return r;
+    }
+    static __device__ __forceinline__ void unpack(uint4 v, Pair (&p)[4]) {
+        p[0] = open(v.x); p[1] = open(v.y); p[2] = open(v.z); p[3] = open(v.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const Pair (&p)[4]) {
+        return make_uint4(close(p[0]), close(p[1]), close(p[2]), close(p[3]));
+    }
+    static __device__ __forceinline__ Max join(Max a, Max b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    static __device__ __forceinline__ Max max(Max m, uint4 v) { return join(m, join(join(v.x, v.y), join(v.z, v.w))); }
+    static __device__ __forceinline__ float value(Max m) {
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+};
+template <class T> __device__ __forceinline__ void unpack(uint4 v, float (&f)[kPerVec<T>]) {
+    Pair p[Vec<T>::kPairs];
+    Vec<T>::unpack(v, p);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kPairs; ++i) {
+        const float2 h = halves(p[i]);
+        f[2 * i] = h.x;
+        f[2 * i + 1] = h.y;
+    }
+}
+
 __device__ __forceinline__ uint32_t smem_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -175,57 +225,95 @@ __device__ __forceinline__ unsigned long long peer_load64(uint32_t at) {
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ float warp_max(float v) {                 // NaN is passed over
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
 
-// Starts the copies of the block's share into slots [layer][thread], in four commit groups of `quarter` layers.
+// f(layer, vector of the layer) for every vector of this thread in layers [a, b) that holds elements of the row.
+template <class T, class F> __device__ __forceinline__ void for_vectors(const Layer* table, int a, int b, F f) {
+    const int t = threadIdx.x;
+    for (int i = a; i < b; ++i) {
+        const int lo = table[i].lo, hi = table[i].hi;
+        if (hi - lo == kPerLayer<T>) {
+            f(i, t);
+            f(i, t + kThreads);
+        } else {
+#pragma unroll 1
+            for (int v = t; v < kVecs; v += kThreads)
+                if (v * kPerVec<T> < hi && (v + 1) * kPerVec<T> > lo) f(i, v);
+        }
+    }
+}
+
+// Starts the copies of the block's share into its slots, in four commit groups of `quarter` layers.
 template <class T>
 __device__ __forceinline__ void load_share(const Layer* table, uint4* slots, int n, int quarter) {
-    const int t = threadIdx.x, p = t * kPerVec<T>;
-    int i = 0;
+    const int t = threadIdx.x;
+    bool      part = false;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-        const int end = min(n, (g + 1) * quarter);
-        for (; i < end; ++i) {
-            const int lo = table[i].lo, hi = table[i].hi;
-            if (p >= lo && p + kPerVec<T> <= hi) copy_async(smem_address(&slots[i * kThreads + t]), table[i].in + t * 16);
+        for (int i = g * quarter; i < min(n, (g + 1) * quarter); ++i) {
+            const int   lo = table[i].lo, hi = table[i].hi;
+            const char* from = table[i].in + t * 16;
+            const uint32_t to = smem_address(&slots[i * kVecs + t]);
+            if (hi - lo == kPerLayer<T>) {
+                copy_async(to, from);
+                copy_async(to + kThreads * 16, from + kThreads * 16);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int p = (t + h * kThreads) * kPerVec<T>;
+                    if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + h * kThreads * 16, from + h * kThreads * 16);
+                    else part |= p < hi && p + kPerVec<T> > lo;
+                }
+            }
         }
         copy_commit();
     }
-    for (i = 0; i < n; ++i) {                 // vectors that the row fills in part
-        const int lo = table[i].lo, hi = table[i].hi;
-        if (p < hi && p + kPerVec<T> > lo && (p < lo || p + kPerVec<T> > hi)) {
-            T e[kPerVec<T>];
+    if (part) {                               // vectors that the row fills in part: its ends
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int lo = table[i].lo, hi = table[i].hi;
+#pragma unroll 1
+            for (int v = t; v < kVecs; v += kThreads) {
+                const int p = v * kPerVec<T>;
+                if (p >= hi || p + kPerVec<T> <= lo || (p >= lo && p + kPerVec<T> <= hi)) continue;
+                T e[kPerVec<T>];
 #pragma unroll
-            for (int j = 0; j < kPerVec<T>; ++j)
-                e[j] = p + j >= lo && p + j < hi ? reinterpret_cast<const T*>(table[i].in)[p + j] : from_float<T>(-INFINITY);
+                for (int j = 0; j < kPerVec<T>; ++j)
+                    e[j] = p + j >= lo && p + j < hi ? reinterpret_cast<const T*>(table[i].in)[p + j] : from_float<T>(-INFINITY);
 #pragma unroll
-            for (int j = 0; j < kPerVec<T>; ++j) reinterpret_cast<T*>(&slots[i * kThreads + t])[j] = e[j];
+                for (int j = 0; j < kPerVec<T>; ++j) reinterpret_cast<T*>(&slots[i * kVecs + v])[j] = e[j];
+            }
         }
     }
 }
 
-// f(layer index) for every layer in which this thread has a vector of the row, in the order of arrival.
+// for_vectors over the block's share, in the order of arrival.
 template <class T, class F>
 __device__ __forceinline__ void on_arrival(const Layer* table, int n, int quarter, F f) {
-    const int p = threadIdx.x * kPerVec<T>;
-    auto some = [&](int a, int b) {
-        for (int i = a; i < min(b, n); ++i)
-            if (p < table[i].hi && p + kPerVec<T> > table[i].lo) f(i);
-    };
-    copy_wait<3>();
-    some(0, quarter);
-    copy_wait<2>();
-    some(quarter, 2 * quarter);
-    copy_wait<1>();
-    some(2 * quarter, 3 * quarter);
-    copy_wait<0>();
-    some(3 * quarter, 4 * quarter);
+#pragma unroll 1
+    for (int g = 0; g < 4; ++g) {
+        if (g == 0) copy_wait<3>();
+        else if (g == 1) copy_wait<2>();
+        else if (g == 2) copy_wait<1>();
+        else copy_wait<0>();
+        for_vectors<T>(table, g * quarter, min(n, (g + 1) * quarter), f);
+    }
 }
 
 template <class T>
-__device__ __forceinline__ void store_vector(const Layer& l, uint4 v) {
-    const int p = threadIdx.x * kPerVec<T>;
+__device__ __forceinline__ void store_vector(const Layer& l, int vec, uint4 v) {
+    const int p = vec * kPerVec<T>;
     if (l.vec_out && p >= l.lo && p + kPerVec<T> <= l.hi) {
-        __stcs(reinterpret_cast<uint4*>(l.out + threadIdx.x * 16), v);
+        __stcs(reinterpret_cast<uint4*>(l.out + vec * 16), v);
     } else {
         T* o = reinterpret_cast<T*>(l.out);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -238,95 +326,46 @@ __device__ __forceinline__ void store_vector(const Layer& l, uint4 v) {
     }
 }
 
-// Sum of two values over the block, in the same order for every thread.
-__device__ __forceinline__ float2 block_sum2(float a, float b, float2* scratch) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, o);
-        b += __shfl_xor_sync(0xffffffffu, b, o);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_float2(a, b);
-    __syncthreads();
-    float2 r = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) { r.x += scratch[i].x; r.y += scratch[i].y; }
-    return r;
+// Sums of exponentials are kept as (m, sum of 2^((x - m) c)), c = log2(e) / T.  An element costs one fma: with
+// mc = round(m c), 2^(x c - mc) has no rounding but the fma's own, and the sum of these is put right once by 2^(mc - m c).
+// A maximum of -inf goes with a sum of 0 (or NaN), one of +inf with the number of such elements.
+struct Base {
+    Pair  c, minus_mc;
+    float right;
+};
+__device__ __forceinline__ Base base_of(float m, float c) {
+    const float b = m == -INFINITY ? 0.f : m, mc = b * c;
+    return {pair(c, c), pair(-mc, -mc), exp2_approx(fmaf(-b, c, mc))};
 }
-__device__ __forceinline__ float block_max(float v, float2* scratch) {
+template <class T> __device__ __forceinline__ Pair exp_sum(Pair sum, uint4 v, const Base& b) {
+    Pair p[Vec<T>::kPairs];
+    Vec<T>::unpack(v, p);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].x = v;
-    __syncthreads();
-    float r = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kWarps; ++i) r = fmaxf(r, scratch[i].x);
+    for (int i = 0; i < Vec<T>::kPairs; ++i) sum = add2(sum, exp2_pair(fma2(p[i], b.c, b.minus_mc)));
+    return sum;
+}
+template <class T> __device__ __noinline__ float exp_sum_inf(uint4 v) {
+    float f[kPerVec<T>], r = 0.f;
+    unpack<T>(v, f);
+    for (int j = 0; j < kPerVec<T>; ++j) r += f[j] == INFINITY ? 1.f : f[j] == f[j] ? 0.f : f[j];
     return r;
 }
 
-// A maximum m and the sum of 2^((x - m) c): two of them joined.  A maximum of -inf goes with a sum of 0 (or NaN).
+// Two such sums joined, the same whichever comes first (no product is contracted into the sum).
 __device__ __forceinline__ float scale_to(float m, float to, float c) {
     return m == to ? 1.f : exp2_approx((m - to) * c);
 }
 __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
     const float m = fmaxf(a.x, b.x);
-    // the same whichever comes first: no product is contracted into the sum
     return make_float2(m, __fadd_rn(__fmul_rn(a.y, scale_to(a.x, m, c)), __fmul_rn(b.y, scale_to(b.x, m, c))));
 }
-
-// The whole cluster's (maximum, sum), the same on every thread: warp shuffles, the block's 16 warps, and the blocks'
-// results through distributed shared memory.  The caller has arrived at the cluster barrier once since the kernel's
-// start (so that the peers run) and not waited; nothing touches a peer's memory after the call.
-__device__ float2 cluster_join(float2 v, float c, int rank, int log_c, float2* scratch, float2* from_peers) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), c);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    __syncthreads();                              // the last reader of scratch is done
-    if (lane == 0) scratch[warp] = v;
-    __syncthreads();
-    v = scratch[lane % kWarps];
-#pragma unroll
-    for (int o = kWarps / 2; o; o >>= 1)
-        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), c);
-    if (log_c == 0) return v;
-    cluster_wait();
-    if (threadIdx.x < 1 << log_c) peer_store(peer_address(&from_peers[rank], threadIdx.x), v.x, v.y);
-    cluster_arrive();
-    cluster_wait();
-    v = from_peers[0];
-    for (int i = 1; i < 1 << log_c; ++i) v = join(v, from_peers[i], c);
-    return v;
-}
-
 // log of a sum of exponentials from its maximum, the scaled maximum and the sum of exp(x - max)
 __device__ __forceinline__ float log_sum(float m, float scaled_m, float sum) {
     if (sum != sum) return sum;
     return m == -INFINITY || m == INFINITY ? m : scaled_m + logf(sum);
 }
 
-// The sum of 2^((x - m) c) over a vector, m >= all of x, m finite; NaN stays NaN.
-template <class T> __device__ __forceinline__ float exp_sum(uint4 v, float m, float c) {
-    float f[kPerVec<T>];
-    Vec<T>::unpack(v, f);
-#pragma unroll
-    for (int j = 0; j < kPerVec<T>; ++j) f[j] = exp2_approx((f[j] - m) * c);
-#pragma unroll
-    for (int w = kPerVec<T> / 2; w; w /= 2)
-#pragma unroll
-        for (int j = 0; j < w; ++j) f[j] += f[j + w];
-    return f[0];
-}
-// ... for a maximum of +inf: the infinite ones count 1
-template <class T> __device__ __noinline__ float exp_sum_inf(uint4 v) {
-    float f[kPerVec<T>], r = 0.f;
-    Vec<T>::unpack(v, f);
-    for (int j = 0; j < kPerVec<T>; ++j) r += f[j] == INFINITY ? 1.f : f[j] == f[j] ? 0.f : f[j];
-    return r;
-}
-
-// Where a token of the row lies: its layer, and its position there.
+// Where a token of the row lies: its block, its layer there, and its position in the layer.
 struct Place {
     int rank, layer, position;
 };
@@ -339,12 +378,6 @@ __device__ __forceinline__ Place place_of(const LogitsCut& in, const Deal& d, in
     return {l & ((1 << d.log_c) - 1), l >> d.log_c, q % kPerLayer<T>};
 }
 __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0, (d.layers - rank + (1 << d.log_c) - 1) >> d.log_c); }
-
-// One bit per element of the block's share, a byte per vector, for the few elements that need more than the others.
-__device__ __forceinline__ void set_flag(uint32_t* flags, int layer, int vec, int element) {
-    const int byte = layer * kThreads + vec;
-    atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + element));
-}
 
 // ---- penalties, biases, masks --------------------------------------------------------------------------------
 //
@@ -384,7 +417,7 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
 
     Layer*    table = reinterpret_cast<Layer*>(dynamic);
     uint32_t* flags = reinterpret_cast<uint32_t*>(table + deal.mine);
-    uint32_t* hash = flags + (how.bias_ids ? deal.mine * kThreads / 4 : 0);
+    uint32_t* hash = flags + (how.bias_ids ? deal.mine * kVecs / 4 : 0);   // flags: a bit per element, a byte per vector
     uint32_t* counters = hash + (how.bias_ids ? 2 * kHash : 0);
     int32_t*  hash_id = reinterpret_cast<int32_t*>(hash);
     int32_t*  hash_entry = hash_id + kHash;
@@ -409,10 +442,10 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
         __syncthreads();
         if (tid < n) table[tid] = layer_of<TI, TO>(in, out, deal, row, rank, first + tid);
         if (total > 0)
-            for (int i = tid; i < n * kThreads * E * (int)sizeof(Count) / 16; i += kThreads)
+            for (int i = tid; i < n * kPerLayer<TI> * (int)sizeof(Count) / 16; i += kThreads)
                 reinterpret_cast<uint4*>(counters)[i] = make_uint4(0, 0, 0, 0);
         if (how.bias_ids) {
-            for (int i = tid; i < n * kThreads / 4; i += kThreads) flags[i] = 0;
+            for (int i = tid; i < n * kVecs / 4; i += kThreads) flags[i] = 0;
             for (int i = tid; i < 2 * kHash; i += kThreads) hash_id[i] = -1;
         }
         __syncthreads();
@@ -430,7 +463,8 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 const Place p = place_of<TI>(in, deal, row, id);
                 const int   l = p.layer - first;
                 if (p.rank != rank || (uint32_t)l >= (uint32_t)n) continue;
-                set_flag(flags, l, p.position / E, p.position % E);
+                const int byte = l * kVecs + p.position / E;
+                atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + p.position % E));
                 uint32_t h = (uint32_t)id * 2654435761u % kHash;
                 for (int probe = 0; probe < kHash; ++probe, h = (h + 1) % kHash) {
                     const int was = atomicCAS(&hash_id[h], -1, id);
@@ -438,15 +472,13 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 }
             }
         __syncthreads();
-        const int p0 = tid * E;
-#pragma unroll 2
-        for (int l = 0; l < n; ++l) {
-            const Layer L = table[l];
-            if (p0 >= L.hi || p0 + E <= L.lo) continue;
-            const bool whole = p0 >= L.lo && p0 + E <= L.hi;
+        for_vectors<TI>(table, 0, n, [&](int l, int vec) {
+            const Layer& L = table[l];
+            const int    p0 = vec * E;
+            const bool   whole = p0 >= L.lo && p0 + E <= L.hi;
             float x[E];
             if (whole) {
-                Vec<TI>::unpack(__ldcs(reinterpret_cast<const uint4*>(L.in + tid * 16)), x);
+                unpack<TI>(__ldcs(reinterpret_cast<const uint4*>(L.in + vec * 16)), x);
             } else {
 #pragma unroll
                 for (int j = 0; j < E; ++j)
@@ -472,7 +504,7 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 }
             }
             if (how.bias_ids) {
-                if (const uint32_t f = reinterpret_cast<const uint8_t*>(flags)[l * kThreads + tid]) {
+                if (const uint32_t f = reinterpret_cast<const uint8_t*>(flags)[l * kVecs + vec]) {
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
                         if (!(f >> j & 1)) continue;
@@ -529,7 +561,7 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 for (int j = 0; j < E; ++j) part += exp2_approx((x[j] - base) * kLog2e);
                 sum += part;
             }
-        }
+        });
     }
 
     // the block's result, and the cluster's on its first block
@@ -628,39 +660,58 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const __grid_constant__ L
     __syncthreads();
     load_share<T>(table, slots, n, quarter);
 
-    float m = -INFINITY, sum = 0.f;
-    on_arrival<T>(table, n, quarter, [&](int i) { m = fmaxf(m, Vec<T>::max(slots[i * kThreads + tid])); });
-    const int p0 = tid * E;
-    if (m == INFINITY) {
-        for (int i = 0; i < n; ++i)
-            if (p0 < table[i].hi && p0 + E > table[i].lo) sum += exp_sum_inf<T>(slots[i * kThreads + tid]);
+    typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;
+    on_arrival<T>(table, n, quarter, [&](int i, int vec) {
+        const uint4 v = slots[i * kVecs + vec];
+        if (vec < kThreads) m0 = Vec<T>::max(m0, v); else m1 = Vec<T>::max(m1, v);
+    });
+    const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1), m = fmaxf(f0, f1), m_warp = warp_max(m);
+    float sum = 0.f;
+    if (m_warp == INFINITY) {
+        for_vectors<T>(table, 0, n, [&](int i, int vec) { sum += exp_sum_inf<T>(slots[i * kVecs + vec]); });
     } else {
-        const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 2
-        for (int i = 0; i < n; ++i)
-            if (p0 < table[i].hi && p0 + E > table[i].lo) sum += exp_sum<T>(slots[i * kThreads + tid], base, c);
+        const Base b = base_of(m_warp, c);
+        Pair s0 = 0, s1 = 0;
+        for_vectors<T>(table, 0, n, [&](int i, int vec) {
+            if (vec < kThreads) s0 = exp_sum<T>(s0, slots[i * kVecs + vec], b);
+            else s1 = exp_sum<T>(s1, slots[i * kVecs + vec], b);
+        });
+        const float2 h = halves(add2(s0, s1));
+        sum = (h.x + h.y) * b.right;
     }
+    sum = warp_sum(sum);
+    if ((tid & 31) == 0) scratch[tid >> 5] = make_float2(m_warp, sum);
 
-    // the k-th largest of the threads' maxima, to 16 bits from below
+    // the k-th largest of the threads' maxima (of both halves of each for a large k), to 16 bits from below
+    const bool     two = k > 96;
+    const uint32_t key0 = key_of(two ? f0 : m), key1 = key_of(f1);
     uint32_t       t = 0;
-    const uint32_t key = key_of(m);
 #pragma unroll 1
-    for (int bit = 31; bit >= 16; --bit)
-        if (__syncthreads_count(key >= (t | 1u << bit)) >= k) t |= 1u << bit;
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t u = t | 1u << bit;
+        int reach = __syncthreads_count(key0 >= u);
+        if (two) reach += __syncthreads_count(key1 >= u);
+        if (reach >= k) t = u;
+    }
     t = max(t, kKeyMinusInf);
     const float bound = value_of(t);
-    // every element of this thread's share that is not NaN: f(key, token)
+    // every element of this thread's share that reaches `least` (so is not NaN): f(key, token)
     auto each = [&](float least, auto f) {
+#pragma unroll 1
         for (int i = 0; i < n; ++i) {
             const Layer& L = table[i];
-            if (p0 >= L.hi || p0 + E <= L.lo) continue;
-            const uint4 v = slots[i * kThreads + tid];
-            if (!(Vec<T>::max(v) >= least)) continue;
-            float x[E];
-            Vec<T>::unpack(v, x);
+#pragma unroll 1
+            for (int vec = tid; vec < kVecs; vec += kThreads) {
+                const int p0 = vec * E;
+                if (p0 >= L.hi || p0 + E <= L.lo) continue;
+                const uint4 v = slots[i * kVecs + vec];
+                if (!(Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), v)) >= least)) continue;
+                float x[E];
+                unpack<T>(v, x);
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (x[j] >= least && p0 + j >= L.lo && p0 + j < L.hi) f(key_of(x[j]), L.token + p0 + j);
+                for (int j = 0; j < E; ++j)
+                    if (x[j] >= least && p0 + j >= L.lo && p0 + j < L.hi) f(key_of(x[j]), L.token + p0 + j);
+            }
         }
     };
     auto push = [&](uint32_t kk, int v) {
@@ -668,14 +719,8 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const __grid_constant__ L
         if (i < kCandidates) found[i] = (unsigned long long)kk << 32 | (0xffffffffu - (uint32_t)v);
     };
     if (m >= bound) each(bound, push);
-
-    // meanwhile the block's sum
-    float2 v = make_float2(m, sum);
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), c);
-    if ((tid & 31) == 0) scratch[tid >> 5] = v;
     __syncthreads();
+    float2 v;
     if (tid == 0) {
         v = scratch[0];
         for (int i = 1; i < kWarps; ++i) v = join(v, scratch[i], c);
@@ -766,176 +811,202 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const __grid_constant__ L
 
 // ---- distillation --------------------------------------------------------------------------------------------
 //
-// The sum over the rest is taken on its own, with the entries' elements left out (one flag bit per element): as the
-// difference of the whole sum and the entries' it would lose its digits where the entries hold nearly all of the mass.
-// The gradient of a token of the rest is exp((x - m) / T) times one number per row; the entries' gradients are worked out
-// by one thread each and left in the elements' places in shared memory, from where they go out with the others.
+// The sum over the rest is taken on its own, with -inf put in the entries' places in shared memory: as the difference
+// of the whole sum and the entries' it would lose its digits where the entries hold nearly all of the mass.  The
+// gradient of a token of the rest is exp((x - m) / T) times one number per row.  The entries, k <= 256, are worked out
+// by one thread each on the block's first k / 32 warps (every block of the cluster works out all of them rather than
+// wait for another exchange), and their gradients are stored after the others.
 
 enum Pass { kForward, kBackward, kStep };
+
+// Sum of two values over the first `warps` warps, the only ones to call it; the same on every thread.
+__device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2* scratch) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, o);
+        b += __shfl_xor_sync(0xffffffffu, b, o);
+    }
+    if (warps == 1) return make_float2(a, b);
+    asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_float2(a, b);
+    asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+    float2 r = scratch[0];
+    for (int i = 1; i < warps; ++i) { r.x += scratch[i].x; r.y += scratch[i].y; }
+    return r;
+}
 
 template <class T, int kPass>
 __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant__ LogitsCut in,
                                                            const __grid_constant__ LogitsCut grad, Deal deal,
                                                            const __grid_constant__ nereus_distill_t how, float* loss,
                                                            float* saved, const float* grad_loss) {
-    constexpr int E = kPerVec<T>;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2 scratch[kWarps], from_peers[kMaxCtas];
-    const int     k = how.k, tid = threadIdx.x, rank = blockIdx.x & ((1 << deal.log_c) - 1), p0 = tid * E;
+    __shared__ float2 scratch[kWarps], entry_scratch[kWarps], from_peers[kMaxCtas];
+    __shared__ float  rest_scale_of_row;
+    const int     k = how.k, tid = threadIdx.x, warp = tid >> 5, entry_warps = (k + 31) >> 5;
+    const int     ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
     const int     n = layers_of(deal, rank), quarter = (n + 3) / 4;
     float         weight = how.weight ? how.weight[row] : 1.f;
 
-    Layer*    table = reinterpret_cast<Layer*>(dynamic);
-    uint4*    slots = reinterpret_cast<uint4*>(table + deal.mine);
-    uint32_t* flags = reinterpret_cast<uint32_t*>(slots + deal.mine * kThreads);
+    Layer* table = reinterpret_cast<Layer*>(dynamic);
+    uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
     if (tid < n) table[tid] = layer_of<T, T>(in, grad, deal, row, rank, tid);
+    __syncthreads();
     if (weight == 0.f) {
         if (rank == 0 && tid == 0 && kPass != kBackward) loss[row] = 0.f;
         if (rank == 0 && tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
-        if (kPass != kForward) {
-            __syncthreads();
-            for (int i = 0; i < n; ++i)
-                if (p0 < table[i].hi && p0 + E > table[i].lo) store_vector<T>(table[i], make_uint4(0, 0, 0, 0));
-        }
+        if (kPass != kForward)
+            for_vectors<T>(table, 0, n, [&](int i, int vec) { store_vector<T>(table[i], vec, make_uint4(0, 0, 0, 0)); });
         return;
     }
-    if (kPass != kBackward && deal.log_c) cluster_arrive();       // the peers run, for cluster_join
-    for (int i = tid; i < n * kThreads / 4; i += kThreads) flags[i] = 0;
-    __syncthreads();
+    if (kPass != kBackward && deal.log_c) cluster_arrive();       // the peers run: their shared memory may be written
     load_share<T>(table, slots, n, quarter);
 
-    // entry `tid`: teacher and student, and its place if the block holds it
+    // entry `tid`: the teacher's side of it, the student's logit, and its place if the block holds it
     const float t = how.temperature, c = kLog2e / t;
-    int id = tid < k ? how.ids[row * k + tid] : -1;
-    if ((uint32_t)id >= (uint32_t)in.vocab) id = -1;
-    const float y = id >= 0 ? how.values[row * k + tid] : 0.f;
-    float x = 0.f;
-    T*    slot = nullptr;
-    if (id >= 0) {
-        const Place p = place_of<T>(in, deal, row, id);
-        const int   s = in.tp == 1 ? 0 : id / in.cols;
-        x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
-        if (p.rank == rank) {
-            slot = reinterpret_cast<T*>(slots + p.layer * kThreads) + p.position;
-            set_flag(flags, p.layer, p.position / E, p.position % E);
+    int   id = -1, entries = 0;
+    float x = 0.f, log_p = 0.f, p = 0.f, p_rest = 0.f, mass = 1.f;
+    int   place = -1, place_vec = 0;              // layer, position
+    if (warp < entry_warps) {
+        if (tid < k) id = how.ids[row * k + tid];
+        if ((uint32_t)id >= (uint32_t)in.vocab) id = -1;
+        float y = 0.f;
+        if (id >= 0) {
+            y = how.values[row * k + tid];
+            const Place at = place_of<T>(in, deal, row, id);
+            const int   s = in.tp == 1 ? 0 : id / in.cols;
+            x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
+            if (at.rank == rank) { place = at.layer; place_vec = at.position; }
+        }
+        if (how.lse) {
+            log_p = y / t - how.lse[row];
+            p = id >= 0 ? expf(log_p) : 0.f;
+            const float2 s = entry_sum(p, id >= 0 ? 1.f : 0.f, entry_warps, entry_scratch);
+            entries = (int)s.y;
+            p_rest = entries < in.vocab ? fmaxf(0.f, 1.f - s.x) : 0.f;
+        } else {
+            float top = warp_max(id >= 0 ? y : -INFINITY);
+            if (entry_warps > 1) {
+                if ((tid & 31) == 0) scratch[warp].x = top;
+                asm volatile("bar.sync 1, %0;" ::"r"(entry_warps * 32) : "memory");
+                for (int i = 0; i < entry_warps; ++i) top = fmaxf(top, scratch[i].x);
+            }
+            const float  e = id >= 0 ? expf((y - top) / t) : 0.f;
+            const float2 s = entry_sum(e, id >= 0 ? 1.f : 0.f, entry_warps, entry_scratch);
+            entries = (int)s.y;
+            log_p = (y - top) / t - logf(s.x);
+            p = entries ? e / s.x : 0.f;
+            if (!entries) mass = 0.f;
         }
     }
-    // a block may overwrite the logits once all blocks have read the entries' (cluster_join orders the other passes)
+    // a block may overwrite the logits once all blocks have read the entries' (the exchange orders the other passes)
     if (kPass == kBackward && deal.log_c) cluster_arrive();
-    const float lse = how.lse ? how.lse[row] : block_max(id >= 0 ? y : -INFINITY, scratch);
-    float log_p, p, p_rest, mass = 1.f;
-    int   entries;
-    if (how.lse) {
-        log_p = y / t - lse;
-        p = id >= 0 ? expf(log_p) : 0.f;
-        const float2 s = block_sum2(p, id >= 0 ? 1.f : 0.f, scratch);
-        entries = (int)s.y;
-        p_rest = entries < in.vocab ? fmaxf(0.f, 1.f - s.x) : 0.f;
-    } else {
-        const float  e = id >= 0 ? expf((y - lse) / t) : 0.f;
-        const float2 s = block_sum2(e, id >= 0 ? 1.f : 0.f, scratch);
-        entries = (int)s.y;
-        log_p = (y - lse) / t - logf(s.x);
-        p = entries ? e / s.x : 0.f;
-        p_rest = 0.f;
-        if (!entries) mass = 0.f;
-    }                                             // (the sums' barriers also publish the flags)
 
-    const uint8_t* flag_of = reinterpret_cast<const uint8_t*>(flags) + tid;
-    float m, total, rest;
+    float m, total = 0.f, rest;
     if (kPass == kBackward) {
         m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
         copy_wait<0>();
-        __syncthreads();
     } else {
-        m = -INFINITY;
-        on_arrival<T>(table, n, quarter, [&](int i) { m = fmaxf(m, Vec<T>::max(slots[i * kThreads + tid])); });
-        const float base = m == -INFINITY ? 0.f : m;
-        float       sum = 0.f;
-#pragma unroll 2
-        for (int i = 0; i < n; ++i) {
-            if (p0 >= table[i].hi || p0 + E <= table[i].lo) continue;
-            uint4 v = slots[i * kThreads + tid];
-            if (const uint32_t f = flag_of[i * kThreads]) {
-                float e[E];
-                Vec<T>::unpack(v, e);
+        typename Vec<T>::Max top = Vec<T>::lowest();
+        on_arrival<T>(table, n, quarter, [&](int i, int vec) { top = Vec<T>::max(top, slots[i * kVecs + vec]); });
+        m = warp_max(Vec<T>::value(top));
+        __syncthreads();                          // the elements are there; scratch is free
+        if ((tid & 31) == 0) scratch[warp].x = m;
+        if (place >= 0) reinterpret_cast<T*>(slots + place * kVecs)[place_vec] = from_float<T>(-INFINITY);
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (f >> j & 1) e[j] = -INFINITY;
-                v = Vec<T>::pack(e);
-            }
-            sum += exp_sum<T>(v, base, c);
+        for (int i = 0; i < kWarps; ++i) m = fmaxf(m, scratch[i].x);
+        const Base b = base_of(m, c);
+        Pair s0 = 0, s1 = 0;
+        for_vectors<T>(table, 0, n, [&](int i, int vec) {
+            if (vec < kThreads) s0 = exp_sum<T>(s0, slots[i * kVecs + vec], b);
+            else s1 = exp_sum<T>(s1, slots[i * kVecs + vec], b);
+        });
+        const float2 h = halves(add2(s0, s1));
+        const float  sum = warp_sum(h.x + h.y) * b.right;
+        if ((tid & 31) == 0) scratch[warp].y = sum;
+        __syncthreads();
+        rest = scratch[0].y;
+#pragma unroll
+        for (int i = 1; i < kWarps; ++i) rest += scratch[i].y;
+        if (deal.log_c) {
+            cluster_wait();
+            if (tid < ctas) peer_store(peer_address(&from_peers[rank], tid), m, rest);
+            cluster_arrive();
+            cluster_wait();
+            float2 all = from_peers[0];
+            for (int i = 1; i < ctas; ++i) all = join(all, from_peers[i], c);
+            m = all.x;
+            rest = all.y;
         }
-        const float2 all = cluster_join(make_float2(m, sum), c, rank, deal.log_c, scratch, from_peers);
-        m = all.x;
-        rest = all.y;
-        total = rest + block_sum2(id >= 0 ? expf((x - m) / t) : 0.f, 0.f, scratch).x;
+        if (kPass == kForward && rank) return;
     }
 
-    // the groups: entry `tid` on its thread, the rest on all
-    const float log_total = logf(total);
-    const float log_q = (x - m) / t - log_total, q = expf(log_q);
-    const float log_q_rest = logf(rest) - log_total, q_rest = rest / total;
-    float term = 0.f, qf = 0.f, slope = 0.f, term_rest = 0.f, qf_rest = 0.f, slope_rest = 0.f;
-    if (how.divergence == NEREUS_FORWARD_KL) {
-        if (p > 0.f) term = p * (log_p - log_q);
-        if (p_rest > 0.f) term_rest = p_rest * (logf(p_rest) - log_q_rest);
-    } else if (how.divergence == NEREUS_REVERSE_KL) {
-        p_rest = fmaxf(p_rest, 5.9604644775390625e-8f);
-        if (q > 0.f && id >= 0) { slope = log_q - log_p; term = qf = q * slope; }
-        if (q_rest > 0.f) { slope_rest = log_q_rest - logf(p_rest); term_rest = qf_rest = q_rest * slope_rest; }
-    } else {
-        const float a = how.beta, b = 1.f - how.beta;
-        if (id >= 0) {
-            const float log_m = logf(a * p + b * q);
-            if (q > 0.f) { slope = b * (log_q - log_m); qf = q * slope; }
-            term = qf + (p > 0.f ? a * p * (log_p - log_m) : 0.f);
+    // the groups: an entry on its thread, the rest on all of them
+    float g = 0.f;
+    if (warp < entry_warps) {
+        if (kPass != kBackward) total = rest + entry_sum(id >= 0 ? expf((x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+        const float log_total = logf(total);
+        const float log_q = (x - m) / t - log_total, q = expf(log_q);
+        const float log_q_rest = logf(rest) - log_total, q_rest = rest / total;
+        float term = 0.f, qf = 0.f, slope = 0.f, term_rest = 0.f, qf_rest = 0.f, slope_rest = 0.f;
+        if (how.divergence == NEREUS_FORWARD_KL) {
+            if (p > 0.f) term = p * (log_p - log_q);
+            if (p_rest > 0.f) term_rest = p_rest * (logf(p_rest) - log_q_rest);
+        } else if (how.divergence == NEREUS_REVERSE_KL) {
+            p_rest = fmaxf(p_rest, 5.9604644775390625e-8f);
+            if (q > 0.f && id >= 0) { slope = log_q - log_p; term = qf = q * slope; }
+            if (q_rest > 0.f) { slope_rest = log_q_rest - logf(p_rest); term_rest = qf_rest = q_rest * slope_rest; }
+        } else {
+            const float a = how.beta, b = 1.f - how.beta;
+            if (id >= 0) {
+                const float log_m = logf(a * p + b * q);
+                if (q > 0.f) { slope = b * (log_q - log_m); qf = q * slope; }
+                term = qf + (p > 0.f ? a * p * (log_p - log_m) : 0.f);
+            }
+            const float log_m = logf(a * p_rest + b * q_rest);
+            if (q_rest > 0.f) { slope_rest = b * (log_q_rest - log_m); qf_rest = q_rest * slope_rest; }
+            term_rest = qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
         }
-        const float log_m = logf(a * p_rest + b * q_rest);
-        if (q_rest > 0.f) { slope_rest = b * (log_q_rest - log_m); qf_rest = q_rest * slope_rest; }
-        term_rest = qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
-    }
-    const float2 sums = block_sum2(id >= 0 ? term : 0.f, qf, scratch);
-    const float  d = sums.x + term_rest, mean = sums.y + qf_rest;
-    if (rank == 0 && tid == 0) {
-        if (kPass != kBackward) loss[row] = weight * d;
-        if (kPass == kForward) {
-            float* const o = saved + row * 4;
-            o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
+        const float2 sums = entry_sum(id >= 0 ? term : 0.f, qf, entry_warps, entry_scratch);
+        const float  d = sums.x + term_rest, mean = sums.y + qf_rest;
+        if (rank == 0 && tid == 0) {
+            if (kPass != kBackward) loss[row] = weight * d;
+            if (kPass == kForward) {
+                float* const o = saved + row * 4;
+                o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
+            }
         }
+        if (kPass == kBackward && grad_loss) weight *= grad_loss[row];
+        const float scale = weight / t;
+        float rest_scale;
+        if (how.divergence == NEREUS_FORWARD_KL) {    // Q f and Q sum Q f, which stay finite where Q is 0
+            g = (mass * q - p) * scale;
+            rest_scale = (mass - (p_rest > 0.f && rest > 0.f ? p_rest / q_rest : 0.f)) * scale / total;
+        } else {
+            g = q > 0.f ? q * (slope - mean) * scale : 0.f;
+            rest_scale = (slope_rest - mean) * scale / total;
+        }
+        if (tid == 0) rest_scale_of_row = rest_scale;
     }
     if (kPass == kForward) return;
-    if (kPass == kBackward && grad_loss) weight *= grad_loss[row];
-    const float scale = weight / t;
-    float g, rest_scale;
-    if (how.divergence == NEREUS_FORWARD_KL) {    // Q f and Q sum Q f, which stay finite where Q is 0
-        g = (mass * q - p) * scale;
-        rest_scale = (mass - (p_rest > 0.f && rest > 0.f ? p_rest / q_rest : 0.f)) * scale / total;
-    } else {
-        g = q > 0.f ? q * (slope - mean) * scale : 0.f;
-        rest_scale = (slope_rest - mean) * scale / total;
-    }
-    if (slot) *slot = from_float<T>(g);
     if (kPass == kBackward && deal.log_c) cluster_wait();
     __syncthreads();
-#pragma unroll 2
-    for (int i = 0; i < n; ++i) {
-        if (p0 >= table[i].hi || p0 + E <= table[i].lo) continue;
-        const uint4 raw = slots[i * kThreads + tid];
-        float       e[E];
-        Vec<T>::unpack(raw, e);
+    {
+        const Base  b = base_of(m, c);
+        const float scale = rest_scale_of_row * b.right;
+        const Pair  s = pair(scale, scale);
+        for_vectors<T>(table, 0, n, [&](int i, int vec) {
+            Pair e[Vec<T>::kPairs];
+            Vec<T>::unpack(slots[i * kVecs + vec], e);
 #pragma unroll
-        for (int j = 0; j < E; ++j) e[j] = exp2_approx((e[j] - m) * c) * rest_scale;
-        if (const uint32_t f = flag_of[i * kThreads]) {
-            float ready[E];
-            Vec<T>::unpack(raw, ready);
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (f >> j & 1) e[j] = ready[j];
-        }
-        store_vector<T>(table[i], Vec<T>::pack(e));
+            for (int j = 0; j < Vec<T>::kPairs; ++j) e[j] = mul2(exp2_pair(fma2(e[j], b.c, b.minus_mc)), s);
+            store_vector<T>(table[i], vec, Vec<T>::pack(e));
+        });
     }
+    __syncthreads();                                  // the entries' places have been written as of the rest
+    if (place >= 0) reinterpret_cast<T*>(table[place].out)[place_vec] = from_float<T>(g);
 }
 
 // ---- host side: the checks of the arguments ------------------------------------------------------------------
@@ -1040,30 +1111,26 @@ constexpr int kMaxDevices = 64;
 constexpr int kSmemShare  = 73 * 1024;      // shared memory per block for which three blocks fit on an SM
 
 struct Device {
-    int sms = 0, smem = 0;
+    int id = 0, smem = 0;      // dynamic shared memory that a block may have
 };
-// The current device's numbers, looked up once.
+// The current device; its shared memory is looked up once.
 int device_of(Device* d) {
-    static std::atomic<int> sms[kMaxDevices], smem[kMaxDevices];
-    int dev = 0, n = 0, m = 0;
-    NEREUS_CUDA(cudaGetDevice(&dev));
-    if (dev < 0 || dev >= kMaxDevices) return NEREUS_ERR_UNSUPPORTED;
-    n = sms[dev].load();
-    m = smem[dev].load();
-    if (!n || !m) {
-        NEREUS_CUDA(cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev));
-        NEREUS_CUDA(cudaDeviceGetAttribute(&m, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev));
-        sms[dev].store(n);
-        smem[dev].store(m);
+    static std::atomic<int> smem[kMaxDevices];
+    NEREUS_CUDA(cudaGetDevice(&d->id));
+    if (d->id < 0 || d->id >= kMaxDevices) return NEREUS_ERR_UNSUPPORTED;
+    d->smem = smem[d->id].load();
+    if (!d->smem) {
+        int most = 0;
+        NEREUS_CUDA(cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, d->id));
+        d->smem = most - 16384;                                   // 16 KiB: the kernels' static part
+        smem[d->id].store(d->smem);
     }
-    d->sms = n;
-    d->smem = m;
     return NEREUS_OK;
 }
 
-// Deals a row out so that a block's share takes at most kSmemShare bytes at `per_layer` a layer and `fixed` once, and
-// further while rows x blocks stay within the SMs.
-Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int sms) {
+// Deals a row out over the fewest blocks whose share takes at most kSmemShare bytes at `per_layer` a layer and `fixed`
+// once.  The number of rows has no part in it: a row's sums come out the same in any batch.
+Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed) {
     Deal d;
     const int64_t e = 16 / size_of(v.dtype), w = held_cols(v, 0), bytes = v.row_stride * size_of(v.dtype);
     d.aligned = v.rows < 2 || bytes % 16 == 0;
@@ -1071,25 +1138,23 @@ Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int sms
         if (held_cols(v, s) && (uintptr_t)v.shard[s] % 16) d.aligned = 0;
     const int64_t vecs = d.aligned ? (w + e - 1) / e : (w + 2 * e - 2) / e;
     const int64_t used = (v.vocab + v.shard_cols - 1) / v.shard_cols;
-    d.per_shard = (int)((vecs + kThreads - 1) / kThreads);
+    d.per_shard = (int)((vecs + kVecs - 1) / kVecs);
     d.layers = (int)(d.per_shard * used);
     d.log_c = 0;
     auto share = [&] { return (int64_t)(d.layers + (1 << d.log_c) - 1) >> d.log_c; };
     while (d.log_c < 3 && share() * per_layer + fixed > kSmemShare) ++d.log_c;
-    while (d.log_c < 3 && (2 << d.log_c) <= d.layers && (v.rows << d.log_c) * 2 <= sms) ++d.log_c;
     d.mine = (int)share();
     return d;
 }
 
 // Launches a kernel with a cluster of blocks per row.
 template <class... P, class... A>
-int launch(void (*kernel)(P...), std::atomic<int>* opted, int64_t rows, const Deal& d, int64_t smem, const Device& dev,
+int launch(void (*kernel)(P...), std::atomic<bool>* opted, int64_t rows, const Deal& d, int64_t smem, const Device& dev,
            cudaStream_t stream, A... args) {
-    if (smem > dev.smem - 16384) return NEREUS_ERR_TOO_LARGE;          // 16 KiB: the kernels' static part
-    if (smem > 32768 && opted->load() < smem) {
-        // the largest any call will ask for, so that this happens once
-        NEREUS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - 16384));
-        opted->store(dev.smem);
+    if (smem > dev.smem) return NEREUS_ERR_TOO_LARGE;
+    if (!opted[dev.id].load()) {
+        NEREUS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem));
+        opted[dev.id].store(true);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(rows << d.log_c));
@@ -1111,14 +1176,12 @@ int launch(void (*kernel)(P...), std::atomic<int>* opted, int64_t rows, const De
 template <class T, int kPass>
 int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
                    const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
-    static std::atomic<int> opted[kMaxDevices];
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    int id = 0;
-    NEREUS_CUDA(cudaGetDevice(&id));
-    const int64_t per_layer = sizeof(Layer) + kThreads * 17;
-    const Deal    d = deal_of(in, per_layer, 0, dev.sms);
-    return launch(distill_kernel<T, kPass>, &opted[id], in.rows, d, d.mine * per_layer, dev, stream,
+    const int64_t per_layer = sizeof(Layer) + kVecs * 16;
+    const Deal    d = deal_of(in, per_layer, 0);
+    return launch(distill_kernel<T, kPass>, opted, in.rows, d, d.mine * per_layer, dev, stream,
                   cut_of(in), kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
 }
 
@@ -1140,32 +1203,28 @@ int distill(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
 template <class TI, class TO, class Count>
 int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const nereus_penalties_t& how, int32_t* token,
                    float* lse, cudaStream_t stream) {
-    static std::atomic<int> opted[kMaxDevices];
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    int id = 0;
-    NEREUS_CUDA(cudaGetDevice(&id));
-    const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) + (how.bias_ids ? kThreads : 0);
+    const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) + (how.bias_ids ? kVecs : 0);
     const int64_t fixed = how.bias_ids ? 2 * kHash * 4 : 0;
-    Deal d = deal_of(in, per_layer, fixed, dev.sms);
+    Deal d = deal_of(in, per_layer, fixed);
     // what does not fit is done in rounds
-    while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem - 16384 || d.mine > kThreads)) d.mine = (d.mine + 1) / 2;
-    return launch(process_kernel<TI, TO, Count>, &opted[id], in.rows, d, d.mine * per_layer + fixed, dev, stream,
+    while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > kThreads)) d.mine = (d.mine + 1) / 2;
+    return launch(process_kernel<TI, TO, Count>, opted, in.rows, d, d.mine * per_layer + fixed, dev, stream,
                   cut_of(in), cut_of(out), d, how, token, lse);
 }
 
 template <class T>
 int top_launch(const nereus_logits_t& in, int k, float temperature, float* values, int32_t* ids, float* lse, cudaStream_t stream) {
-    static std::atomic<int> opted[kMaxDevices];
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    int id = 0;
-    NEREUS_CUDA(cudaGetDevice(&id));
-    const int64_t per_layer = sizeof(Layer) + kThreads * 16;
-    const Deal    d = deal_of(in, per_layer, 0, dev.sms);
+    const int64_t per_layer = sizeof(Layer) + kVecs * 16;
+    const Deal    d = deal_of(in, per_layer, 0);
     // the slots also take the lists of all blocks of the cluster
     const int64_t lists = d.log_c ? ((int64_t)k << d.log_c) * 8 + d.mine * (int64_t)sizeof(Layer) : 0;
-    return launch(top_kernel<T>, &opted[id], in.rows, d, std::max(d.mine * per_layer, lists), dev, stream, cut_of(in),
+    return launch(top_kernel<T>, opted, in.rows, d, std::max(d.mine * per_layer, lists), dev, stream, cut_of(in),
                   d, k, 1.f / temperature, values, ids, lse);
 }
 
