@@ -236,41 +236,76 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// f(layer, vector of the layer) for every vector of this thread in layers [a, b) that holds elements of the row.
-template <class T, class F> __device__ __forceinline__ void for_vectors(const Layer* table, int a, int b, F f) {
-    const int t = threadIdx.x;
-    for (int i = a; i < b; ++i) {
-        const int lo = table[i].lo, hi = table[i].hi;
-        if (hi - lo == kPerLayer<T>) {
-            f(i, t);
-            f(i, t + kThreads);
-        } else {
-#pragma unroll 1
-            for (int v = t; v < kVecs; v += kThreads)
-                if (v * kPerVec<T> < hi && (v + 1) * kPerVec<T> > lo) f(i, v);
-        }
+// Fills the block's table; all of its first `n` threads' layers, n <= 32.  Returned through `masks`: which layers lie
+// wholly inside the row, and which of these can also be written in 16-byte vectors.  Ends in a barrier.
+template <class TI, class TO>
+__device__ __forceinline__ uint2 fill_table(Layer* table, uint2* masks, const LogitsCut& in, const LogitsCut& out, const Deal& d,
+                                            int64_t row, int rank, int n) {
+    if (threadIdx.x < 32) {
+        Layer l = {nullptr, nullptr, 0, 0, 0, 0};
+        if ((int)threadIdx.x < n) table[threadIdx.x] = l = layer_of<TI, TO>(in, out, d, row, rank, threadIdx.x);
+        const bool     whole = l.hi - l.lo == kPerLayer<TI>;
+        const uint32_t a = __ballot_sync(0xffffffffu, whole), b = __ballot_sync(0xffffffffu, whole && l.vec_out);
+        if (threadIdx.x == 0) *masks = make_uint2(a, b);
     }
+    __syncthreads();
+    return *masks;
 }
 
+// f(layer, vector of the layer) for every vector of this thread in a layer that the row fills in part.
+template <class T, class F> __device__ __forceinline__ void for_edges(const Layer* table, int i, F f) {
+    const int lo = table[i].lo, hi = table[i].hi;
+#pragma unroll 1
+    for (int v = threadIdx.x; v < kVecs; v += kThreads)
+        if (v * kPerVec<T> < hi && (v + 1) * kPerVec<T> > lo) f(i, v);
+}
+template <int N> struct Batch {
+    enum { n = N };
+    uint4 v[N];
+};
+// The block's share from shared memory, layers [a, b): f(layer, vector, value) one at a time where the row fills a layer
+// in part; otherwise g(layer, batch) with the thread's four values of two layers, so that four independent vectors are
+// in work at a time, or its two of one layer where the next is not whole.
+template <class T, class F, class G>
+__device__ __forceinline__ void sweep(const Layer* table, const uint4* slots, uint32_t whole, int a, int b, F f, G g) {
+    const uint4* mine = slots + threadIdx.x;
+    for (int i = a; i < b;) {
+        const uint4* s = mine + i * kVecs;
+        if (i + 1 < b && (whole >> i & 3u) == 3u) {
+            const Batch<4> v = {{s[0], s[kThreads], s[kVecs], s[kVecs + kThreads]}};
+            g(i, v);
+            i += 2;
+            continue;
+        }
+        if (whole >> i & 1u) {
+            const Batch<2> v = {{s[0], s[kThreads]}};
+            g(i, v);
+        } else {
+            for_edges<T>(table, i, [&](int l, int vec) { f(l, vec, slots[l * kVecs + vec]); });
+        }
+        ++i;
+    }
+}
 // Starts the copies of the block's share into its slots, in four commit groups of `quarter` layers.
 template <class T>
-__device__ __forceinline__ void load_share(const Layer* table, uint4* slots, int n, int quarter) {
-    const int t = threadIdx.x;
-    bool      part = false;
+__device__ __forceinline__ void load_share(const Layer* table, uint4* slots, uint32_t whole, int n, int quarter) {
+    const int      t = threadIdx.x;
+    const uint32_t to = smem_address(slots + t);
+    bool           part = false;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
+#pragma unroll 2
         for (int i = g * quarter; i < min(n, (g + 1) * quarter); ++i) {
-            const int   lo = table[i].lo, hi = table[i].hi;
             const char* from = table[i].in + t * 16;
-            const uint32_t to = smem_address(&slots[i * kVecs + t]);
-            if (hi - lo == kPerLayer<T>) {
-                copy_async(to, from);
-                copy_async(to + kThreads * 16, from + kThreads * 16);
+            if (whole >> i & 1u) {
+                copy_async(to + i * (kVecs * 16), from);
+                copy_async(to + i * (kVecs * 16) + kThreads * 16, from + kThreads * 16);
             } else {
+                const int lo = table[i].lo, hi = table[i].hi;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int p = (t + h * kThreads) * kPerVec<T>;
-                    if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + h * kThreads * 16, from + h * kThreads * 16);
+                    if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + i * (kVecs * 16) + h * kThreads * 16, from + h * kThreads * 16);
                     else part |= p < hi && p + kPerVec<T> > lo;
                 }
             }
@@ -280,32 +315,31 @@ __device__ __forceinline__ void load_share(const Layer* table, uint4* slots, int
     if (part) {                               // vectors that the row fills in part: its ends
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
-            const int lo = table[i].lo, hi = table[i].hi;
-#pragma unroll 1
-            for (int v = t; v < kVecs; v += kThreads) {
-                const int p = v * kPerVec<T>;
-                if (p >= hi || p + kPerVec<T> <= lo || (p >= lo && p + kPerVec<T> <= hi)) continue;
+            if (whole >> i & 1u) continue;
+            for_edges<T>(table, i, [&](int, int v) {
+                const int lo = table[i].lo, hi = table[i].hi, p = v * kPerVec<T>;
+                if (p >= lo && p + kPerVec<T> <= hi) return;
                 T e[kPerVec<T>];
 #pragma unroll
                 for (int j = 0; j < kPerVec<T>; ++j)
                     e[j] = p + j >= lo && p + j < hi ? reinterpret_cast<const T*>(table[i].in)[p + j] : from_float<T>(-INFINITY);
 #pragma unroll
                 for (int j = 0; j < kPerVec<T>; ++j) reinterpret_cast<T*>(&slots[i * kVecs + v])[j] = e[j];
-            }
+            });
         }
     }
 }
 
-// for_vectors over the block's share, in the order of arrival.
-template <class T, class F>
-__device__ __forceinline__ void on_arrival(const Layer* table, int n, int quarter, F f) {
+// sweep over the block's share, in the order of arrival.
+template <class T, class F, class G>
+__device__ __forceinline__ void on_arrival(const Layer* table, const uint4* slots, uint32_t whole, int n, int quarter, F f, G g) {
 #pragma unroll 1
-    for (int g = 0; g < 4; ++g) {
-        if (g == 0) copy_wait<3>();
-        else if (g == 1) copy_wait<2>();
-        else if (g == 2) copy_wait<1>();
+    for (int q = 0; q < 4; ++q) {
+        if (q == 0) copy_wait<3>();
+        else if (q == 1) copy_wait<2>();
+        else if (q == 2) copy_wait<1>();
         else copy_wait<0>();
-        for_vectors<T>(table, g * quarter, min(n, (g + 1) * quarter), f);
+        sweep<T>(table, slots, whole, q * quarter, min(n, (q + 1) * quarter), f, g);
     }
 }
 
@@ -343,6 +377,17 @@ template <class T> __device__ __forceinline__ Pair exp_sum(Pair sum, uint4 v, co
 #pragma unroll
     for (int i = 0; i < Vec<T>::kPairs; ++i) sum = add2(sum, exp2_pair(fma2(p[i], b.c, b.minus_mc)));
     return sum;
+}
+// ... over the thread's part of the block's share
+template <class T> __device__ __forceinline__ float exp_sums(const Layer* table, const uint4* slots, uint32_t whole, int n, const Base& b) {
+    Pair s[4] = {0, 0, 0, 0};
+    sweep<T>(table, slots, whole, 0, n, [&](int, int, uint4 v) { s[0] = exp_sum<T>(s[0], v, b); },
+             [&](int, const auto& v) {
+#pragma unroll
+                 for (int j = 0; j < v.n; ++j) s[j] = exp_sum<T>(s[j], v.v[j], b);
+             });
+    const float2 h = halves(add2(add2(s[0], s[1]), add2(s[2], s[3])));
+    return (h.x + h.y) * b.right;
 }
 template <class T> __device__ __noinline__ float exp_sum_inf(uint4 v) {
     float f[kPerVec<T>], r = 0.f;
@@ -403,7 +448,7 @@ template <class Count> __device__ __forceinline__ void count_token(uint32_t* wor
 }
 
 template <class TI, class TO, class Count>
-__global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant__ LogitsCut in,
+__global__ void __launch_bounds__(kThreads, 4) process_kernel(const __grid_constant__ LogitsCut in,
                                                            const __grid_constant__ LogitsCut out, Deal deal,
                                                            const __grid_constant__ nereus_penalties_t how, int32_t* token,
                                                            float* lse) {
@@ -472,7 +517,7 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 }
             }
         __syncthreads();
-        for_vectors<TI>(table, 0, n, [&](int l, int vec) {
+        auto work = [&](int l, int vec) {
             const Layer& L = table[l];
             const int    p0 = vec * E;
             const bool   whole = p0 >= L.lo && p0 + E <= L.hi;
@@ -561,7 +606,9 @@ __global__ void __launch_bounds__(kThreads) process_kernel(const __grid_constant
                 for (int j = 0; j < E; ++j) part += exp2_approx((x[j] - base) * kLog2e);
                 sum += part;
             }
-        });
+        };
+#pragma unroll 1
+        for (int l = 0; l < n; ++l) for_edges<TI>(table, l, work);
     }
 
     // the block's result, and the cluster's on its first block
@@ -637,7 +684,7 @@ __device__ __forceinline__ int block_count(int v, int* scratch) {
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, float inv_t,
+__global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, float inv_t,
                                                        float* values, int32_t* ids, float* lse) {
     constexpr int E = kPerVec<T>;
     extern __shared__ __align__(16) unsigned char dynamic[];
@@ -654,30 +701,29 @@ __global__ void __launch_bounds__(kThreads) top_kernel(const __grid_constant__ L
 
     Layer* table = reinterpret_cast<Layer*>(dynamic);
     uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    if (tid < n) table[tid] = layer_of<T, T>(in, LogitsCut(), deal, row, rank, tid);
+    __shared__ uint2 masks;
     if (tid == 0) n_found = 0;
     if (tid < k) best[tid] = 0;
-    __syncthreads();
-    load_share<T>(table, slots, n, quarter);
+    const uint32_t whole = fill_table<T, T>(table, &masks, in, LogitsCut(), deal, row, rank, n).x;
+    load_share<T>(table, slots, whole, n, quarter);
 
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;
-    on_arrival<T>(table, n, quarter, [&](int i, int vec) {
-        const uint4 v = slots[i * kVecs + vec];
-        if (vec < kThreads) m0 = Vec<T>::max(m0, v); else m1 = Vec<T>::max(m1, v);
-    });
+    on_arrival<T>(table, slots, whole, n, quarter,
+                  [&](int, int vec, uint4 v) { if (vec < kThreads) m0 = Vec<T>::max(m0, v); else m1 = Vec<T>::max(m1, v); },
+                  [&](int, const auto& v) {
+#pragma unroll
+                      for (int j = 0; j < v.n; j += 2) {
+                          m0 = Vec<T>::max(m0, v.v[j]);
+                          m1 = Vec<T>::max(m1, v.v[j + 1]);
+                      }
+                  });
     const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1), m = fmaxf(f0, f1), m_warp = warp_max(m);
     float sum = 0.f;
     if (m_warp == INFINITY) {
-        for_vectors<T>(table, 0, n, [&](int i, int vec) { sum += exp_sum_inf<T>(slots[i * kVecs + vec]); });
+        for (int i = 0; i < n; ++i) for_edges<T>(table, i, [&](int l, int vec) { sum += exp_sum_inf<T>(slots[l * kVecs + vec]); });
     } else {
         const Base b = base_of(m_warp, c);
-        Pair s0 = 0, s1 = 0;
-        for_vectors<T>(table, 0, n, [&](int i, int vec) {
-            if (vec < kThreads) s0 = exp_sum<T>(s0, slots[i * kVecs + vec], b);
-            else s1 = exp_sum<T>(s1, slots[i * kVecs + vec], b);
-        });
-        const float2 h = halves(add2(s0, s1));
-        sum = (h.x + h.y) * b.right;
+        sum = exp_sums<T>(table, slots, whole, n, b);
     }
     sum = warp_sum(sum);
     if ((tid & 31) == 0) scratch[tid >> 5] = make_float2(m_warp, sum);
@@ -836,7 +882,7 @@ __device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2*
 }
 
 template <class T, int kPass>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant__ LogitsCut in,
+__global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_constant__ LogitsCut in,
                                                            const __grid_constant__ LogitsCut grad, Deal deal,
                                                            const __grid_constant__ nereus_distill_t how, float* loss,
                                                            float* saved, const float* grad_loss) {
@@ -851,36 +897,38 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
 
     Layer* table = reinterpret_cast<Layer*>(dynamic);
     uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    if (tid < n) table[tid] = layer_of<T, T>(in, grad, deal, row, rank, tid);
-    __syncthreads();
+    __shared__ uint2 masks;
+    int id = -1;                                  // entry `tid`
+    if (tid < k) id = how.ids[row * k + tid];
+    const uint2 whole = fill_table<T, T>(table, &masks, in, grad, deal, row, rank, n);
     if (weight == 0.f) {
         if (rank == 0 && tid == 0 && kPass != kBackward) loss[row] = 0.f;
         if (rank == 0 && tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
         if (kPass != kForward)
-            for_vectors<T>(table, 0, n, [&](int i, int vec) { store_vector<T>(table[i], vec, make_uint4(0, 0, 0, 0)); });
+            for (int i = 0; i < n; ++i)
+                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
         return;
     }
     if (kPass != kBackward && deal.log_c) cluster_arrive();       // the peers run: their shared memory may be written
-    load_share<T>(table, slots, n, quarter);
-
-    // entry `tid`: the teacher's side of it, the student's logit, and its place if the block holds it
+    // the teacher's side of the entry, the student's logit, and its place if the block holds it
     const float t = how.temperature, c = kLog2e / t;
-    int   id = -1, entries = 0;
-    float x = 0.f, log_p = 0.f, p = 0.f, p_rest = 0.f, mass = 1.f;
-    int   place = -1, place_vec = 0;              // layer, position
+    int   entries = 0, place = -1, place_at = 0;  // layer, position
+    float x = 0.f, y = 0.f, teacher_lse = 0.f, log_p = 0.f, p = 0.f, p_rest = 0.f, mass = 1.f;
+    if ((uint32_t)id >= (uint32_t)in.vocab) id = -1;
     if (warp < entry_warps) {
-        if (tid < k) id = how.ids[row * k + tid];
-        if ((uint32_t)id >= (uint32_t)in.vocab) id = -1;
-        float y = 0.f;
+        if (how.lse) teacher_lse = how.lse[row];
         if (id >= 0) {
             y = how.values[row * k + tid];
             const Place at = place_of<T>(in, deal, row, id);
             const int   s = in.tp == 1 ? 0 : id / in.cols;
             x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
-            if (at.rank == rank) { place = at.layer; place_vec = at.position; }
+            if (at.rank == rank) { place = at.layer; place_at = at.position; }
         }
+    }
+    load_share<T>(table, slots, whole.x, n, quarter);
+    if (warp < entry_warps) {
         if (how.lse) {
-            log_p = y / t - how.lse[row];
+            log_p = y / t - teacher_lse;
             p = id >= 0 ? expf(log_p) : 0.f;
             const float2 s = entry_sum(p, id >= 0 ? 1.f : 0.f, entry_warps, entry_scratch);
             entries = (int)s.y;
@@ -909,22 +957,20 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
         copy_wait<0>();
     } else {
         typename Vec<T>::Max top = Vec<T>::lowest();
-        on_arrival<T>(table, n, quarter, [&](int i, int vec) { top = Vec<T>::max(top, slots[i * kVecs + vec]); });
+        on_arrival<T>(table, slots, whole.x, n, quarter, [&](int, int, uint4 v) { top = Vec<T>::max(top, v); },
+                      [&](int, const auto& v) {
+#pragma unroll
+                          for (int j = 0; j < v.n; ++j) top = Vec<T>::max(top, v.v[j]);
+                      });
         m = warp_max(Vec<T>::value(top));
         __syncthreads();                          // the elements are there; scratch is free
         if ((tid & 31) == 0) scratch[warp].x = m;
-        if (place >= 0) reinterpret_cast<T*>(slots + place * kVecs)[place_vec] = from_float<T>(-INFINITY);
+        if (place >= 0) reinterpret_cast<T*>(slots + place * kVecs)[place_at] = from_float<T>(-INFINITY);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) m = fmaxf(m, scratch[i].x);
         const Base b = base_of(m, c);
-        Pair s0 = 0, s1 = 0;
-        for_vectors<T>(table, 0, n, [&](int i, int vec) {
-            if (vec < kThreads) s0 = exp_sum<T>(s0, slots[i * kVecs + vec], b);
-            else s1 = exp_sum<T>(s1, slots[i * kVecs + vec], b);
-        });
-        const float2 h = halves(add2(s0, s1));
-        const float  sum = warp_sum(h.x + h.y) * b.right;
+        const float sum = warp_sum(exp_sums<T>(table, slots, whole.x, n, b));
         if ((tid & 31) == 0) scratch[warp].y = sum;
         __syncthreads();
         rest = scratch[0].y;
@@ -944,7 +990,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     }
 
     // the groups: an entry on its thread, the rest on all of them
-    float g = 0.f;
+    float g = 0.f, divergence = 0.f, divergence_rest = 0.f;
     if (warp < entry_warps) {
         if (kPass != kBackward) total = rest + entry_sum(id >= 0 ? expf((x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
         const float log_total = logf(total);
@@ -969,19 +1015,22 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
             if (q_rest > 0.f) { slope_rest = b * (log_q_rest - log_m); qf_rest = q_rest * slope_rest; }
             term_rest = qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
         }
-        const float2 sums = entry_sum(id >= 0 ? term : 0.f, qf, entry_warps, entry_scratch);
-        const float  d = sums.x + term_rest, mean = sums.y + qf_rest;
-        if (rank == 0 && tid == 0) {
-            if (kPass != kBackward) loss[row] = weight * d;
-            if (kPass == kForward) {
-                float* const o = saved + row * 4;
-                o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
-            }
+        // of the forward KL the gradient takes Q f and Q sum Q f, which stay finite where Q is 0 and need no sum: its
+        // loss is summed after the gradient has gone out
+        const bool early = how.divergence == NEREUS_FORWARD_KL && kPass != kForward;
+        float2 sums = make_float2(0.f, 0.f);
+        if (!early) sums = entry_sum(id >= 0 ? term : 0.f, qf, entry_warps, entry_scratch);
+        divergence = early ? (id >= 0 ? term : 0.f) : sums.x;
+        divergence_rest = term_rest;
+        if (kPass == kForward && tid == 0) {
+            const float d = divergence + divergence_rest;
+            loss[row] = weight * d;
+            float* const o = saved + row * 4;
+            o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
         }
-        if (kPass == kBackward && grad_loss) weight *= grad_loss[row];
-        const float scale = weight / t;
+        const float scale = (kPass == kBackward && grad_loss ? weight * grad_loss[row] : weight) / t, mean = sums.y + qf_rest;
         float rest_scale;
-        if (how.divergence == NEREUS_FORWARD_KL) {    // Q f and Q sum Q f, which stay finite where Q is 0
+        if (how.divergence == NEREUS_FORWARD_KL) {
             g = (mass * q - p) * scale;
             rest_scale = (mass - (p_rest > 0.f && rest > 0.f ? p_rest / q_rest : 0.f)) * scale / total;
         } else {
@@ -997,16 +1046,32 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
         const Base  b = base_of(m, c);
         const float scale = rest_scale_of_row * b.right;
         const Pair  s = pair(scale, scale);
-        for_vectors<T>(table, 0, n, [&](int i, int vec) {
+        auto gradient = [&](uint4 v) {
             Pair e[Vec<T>::kPairs];
-            Vec<T>::unpack(slots[i * kVecs + vec], e);
+            Vec<T>::unpack(v, e);
 #pragma unroll
             for (int j = 0; j < Vec<T>::kPairs; ++j) e[j] = mul2(exp2_pair(fma2(e[j], b.c, b.minus_mc)), s);
-            store_vector<T>(table[i], vec, Vec<T>::pack(e));
-        });
+            return Vec<T>::pack(e);
+        };
+        sweep<T>(table, slots, whole.y, 0, n, [&](int l, int vec, uint4 v) { store_vector<T>(table[l], vec, gradient(v)); },
+                 [&](int l, const auto& v) {
+                     uint4 o[v.n];
+#pragma unroll
+                     for (int j = 0; j < v.n; ++j) o[j] = gradient(v.v[j]);
+#pragma unroll
+                     for (int j = 0; j < v.n; j += 2) {
+                         uint4* const to = reinterpret_cast<uint4*>(table[l + j / 2].out) + tid;
+                         __stcs(to, o[j]);
+                         __stcs(to + kThreads, o[j + 1]);
+                     }
+                 });
     }
     __syncthreads();                                  // the entries' places have been written as of the rest
-    if (place >= 0) reinterpret_cast<T*>(table[place].out)[place_vec] = from_float<T>(g);
+    if (place >= 0) reinterpret_cast<T*>(table[place].out)[place_at] = from_float<T>(g);
+    if (kPass == kStep && rank == 0 && warp < entry_warps) {
+        if (how.divergence == NEREUS_FORWARD_KL) divergence = entry_sum(divergence, 0.f, entry_warps, entry_scratch).x;
+        if (tid == 0) loss[row] = weight * (divergence + divergence_rest);
+    }
 }
 
 // ---- host side: the checks of the arguments ------------------------------------------------------------------
