@@ -23,6 +23,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "nereus_internal.hpp"
 
@@ -42,6 +43,7 @@ struct LogitsCut {
     char*   shard[NEREUS_VOCAB_MAX_TP];
     int64_t row_bytes;
     int32_t tp, cols, vocab;
+    float   per_col;      // 1 / cols
 };
 
 // How rows are dealt out: `per_shard` layers in every shard, `layers` in all, 1 << log_c blocks per row, `mine` layers
@@ -236,14 +238,14 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// Fills the block's table; all of its first `n` threads' layers, n <= 32.  Returned through `masks`: which layers lie
+// Fills the block's table with its layers first .. first + n - 1, n <= 32.  Returned through `masks`: which layers lie
 // wholly inside the row, and which of these can also be written in 16-byte vectors.  Ends in a barrier.
 template <class TI, class TO>
 __device__ __forceinline__ uint2 fill_table(Layer* table, uint2* masks, const LogitsCut& in, const LogitsCut& out, const Deal& d,
-                                            int64_t row, int rank, int n) {
+                                            int64_t row, int rank, int first, int n) {
     if (threadIdx.x < 32) {
         Layer l = {nullptr, nullptr, 0, 0, 0, 0};
-        if ((int)threadIdx.x < n) table[threadIdx.x] = l = layer_of<TI, TO>(in, out, d, row, rank, threadIdx.x);
+        if ((int)threadIdx.x < n) table[threadIdx.x] = l = layer_of<TI, TO>(in, out, d, row, rank, first + (int)threadIdx.x);
         const bool     whole = l.hi - l.lo == kPerLayer<TI>;
         const uint32_t a = __ballot_sync(0xffffffffu, whole), b = __ballot_sync(0xffffffffu, whole && l.vec_out);
         if (threadIdx.x == 0) *masks = make_uint2(a, b);
@@ -362,14 +364,20 @@ __device__ __forceinline__ void store_vector(const Layer& l, int vec, uint4 v) {
 
 // Sums of exponentials are kept as (m, sum of 2^((x - m) c)), c = log2(e) / T.  An element costs one fma: with
 // mc = round(m c), 2^(x c - mc) has no rounding but the fma's own, and the sum of these is put right once by 2^(mc - m c).
+// Where m c is too large for that (a row of the type's lowest value, an infinity) the elements' differences are taken.
 // A maximum of -inf goes with a sum of 0 (or NaN), one of +inf with the number of such elements.
 struct Base {
     Pair  c, minus_mc;
-    float right;
+    float m, right;
+    bool  far;
 };
+__device__ __forceinline__ bool is_far(float mc) { return !(fabsf(mc) < 0x1p100f); }
 __device__ __forceinline__ Base base_of(float m, float c) {
     const float b = m == -INFINITY ? 0.f : m, mc = b * c;
-    return {pair(c, c), pair(-mc, -mc), exp2_approx(fmaf(-b, c, mc))};
+    return {pair(c, c), pair(-mc, -mc), b, exp2_approx(fmaf(-b, c, mc)), is_far(mc)};
+}
+__device__ __forceinline__ float scale_to(float m, float to, float c) {
+    return m == to ? 1.f : exp2_approx((m - to) * c);
 }
 template <class T> __device__ __forceinline__ Pair exp_sum(Pair sum, uint4 v, const Base& b) {
     Pair p[Vec<T>::kPairs];
@@ -378,8 +386,20 @@ template <class T> __device__ __forceinline__ Pair exp_sum(Pair sum, uint4 v, co
     for (int i = 0; i < Vec<T>::kPairs; ++i) sum = add2(sum, exp2_pair(fma2(p[i], b.c, b.minus_mc)));
     return sum;
 }
+template <class T> __device__ __noinline__ float exp_sum_far(uint4 v, float m, float c) {
+    float f[kPerVec<T>], r = 0.f;
+    unpack<T>(v, f);
+    for (int j = 0; j < kPerVec<T>; ++j) r += scale_to(f[j], m, c);
+    return r;
+}
 // ... over the thread's part of the block's share
 template <class T> __device__ __forceinline__ float exp_sums(const Layer* table, const uint4* slots, uint32_t whole, int n, const Base& b) {
+    if (b.far) {
+        float r = 0.f;
+        for (int i = 0; i < n; ++i)
+            for_edges<T>(table, i, [&](int l, int vec) { r += exp_sum_far<T>(slots[l * kVecs + vec], b.m, halves(b.c).x); });
+        return r;
+    }
     Pair s[4] = {0, 0, 0, 0};
     sweep<T>(table, slots, whole, 0, n, [&](int, int, uint4 v) { s[0] = exp_sum<T>(s[0], v, b); },
              [&](int, const auto& v) {
@@ -389,17 +409,8 @@ template <class T> __device__ __forceinline__ float exp_sums(const Layer* table,
     const float2 h = halves(add2(add2(s[0], s[1]), add2(s[2], s[3])));
     return (h.x + h.y) * b.right;
 }
-template <class T> __device__ __noinline__ float exp_sum_inf(uint4 v) {
-    float f[kPerVec<T>], r = 0.f;
-    unpack<T>(v, f);
-    for (int j = 0; j < kPerVec<T>; ++j) r += f[j] == INFINITY ? 1.f : f[j] == f[j] ? 0.f : f[j];
-    return r;
-}
 
 // Two such sums joined, the same whichever comes first (no product is contracted into the sum).
-__device__ __forceinline__ float scale_to(float m, float to, float c) {
-    return m == to ? 1.f : exp2_approx((m - to) * c);
-}
 __device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
     const float m = fmaxf(a.x, b.x);
     return make_float2(m, __fadd_rn(__fmul_rn(a.y, scale_to(a.x, m, c)), __fmul_rn(b.y, scale_to(b.x, m, c))));
@@ -414,9 +425,15 @@ __device__ __forceinline__ float log_sum(float m, float scaled_m, float sum) {
 struct Place {
     int rank, layer, position;
 };
+// token / cols: tokens and columns are below 2^24, so that the product's rounding is off by one at most
+__device__ __forceinline__ int shard_of(const LogitsCut& in, int token) {
+    if (in.tp == 1) return 0;
+    const int s = (int)((float)token * in.per_col), r = token - s * in.cols;
+    return r < 0 ? s - 1 : r >= in.cols ? s + 1 : s;
+}
 template <class T>
 __device__ __forceinline__ Place place_of(const LogitsCut& in, const Deal& d, int64_t row, int token) {
-    const int s = in.tp == 1 ? 0 : token / in.cols;
+    const int s = shard_of(in, token);
     int       q = token - s * in.cols;
     if (!d.aligned) q += (int)((uintptr_t)row_of<T>(in, s, row) & 15) / (int)sizeof(T);
     const int l = s * d.per_shard + q / kPerLayer<T>;
@@ -426,49 +443,99 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 
 // ---- penalties, biases, masks --------------------------------------------------------------------------------
 //
-// A sweep over the row with everything that is sparse prepared in shared memory: one counter per column of the block's
-// share (the history is read once per block and lands there with shared-memory atomics: sums of whole numbers, so that
-// no order shows), and a hash table of the bias entries with one flag per column that has one.  The elements go from
-// memory through registers to memory; the running (maximum, its id, sum of exponentials) stays on the thread.
+// A sweep over the row, vectors from memory through registers to memory, the next four on their way while four are worked
+// on, mask bits from shared memory.  What changes a logit by its token is sparse: the history's tokens and the biases.  One
+// counter per column of the block's share is kept in shared memory (the history lands there with shared-memory atomics:
+// sums of whole numbers, so that no order shows), and a hash table of the bias entries.  The sweep hands the columns that
+// have either over to a queue of its warp, together with the element, and does not write them; the warp takes 32 of them at
+// a time through penalties, bias and mask.  The running (maximum, where it is, sum of exponentials) of both stays on the
+// thread.
+// A long history is read once per row, each block of the cluster taking its part and counting into the share of whichever
+// block holds the token; a short one by every block for itself, which saves two cluster barriers.
 
-constexpr int kHash = 2048;               // slots of the bias table, over twice NEREUS_BIAS_MAX
+constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
+constexpr int kSpread = 2048;             // tokens from which on the cluster's blocks share the reading of the history
 
-// Counter of a column: the top bit "in the history", the others "generated so often".
-template <class Count> constexpr uint32_t kSeen = 1u << (sizeof(Count) * 8 - 1);
+// Counter of a column, 0 for a token that is not in the history: the top bit "in the prompt", the others "generated so
+// often".
+template <class Count> constexpr uint32_t kPrompt = 1u << (sizeof(Count) * 8 - 1);
 
 template <class Count> __device__ __forceinline__ void count_token(uint32_t* words, int column, bool generated) {
-    if (sizeof(Count) == 4) {
-        atomicOr(&words[column], kSeen<Count>);
-        if (generated) atomicAdd(&words[column], 1u);
-    } else {
-        const int shift = (column & 1) * 16;
-        atomicOr(&words[column >> 1], kSeen<Count> << shift);
-        if (generated) atomicAdd(&words[column >> 1], 1u << shift);
+    const int shift = sizeof(Count) == 4 ? 0 : (column & 1) * 16;
+    uint32_t* word = words + (sizeof(Count) == 4 ? column : column >> 1);
+    if (generated) atomicAdd(word, 1u << shift);
+    else atomicOr(word, kPrompt<Count> << shift);
+}
+template <class Count> __device__ __forceinline__ void count_token_at(int rank, uint32_t* words, int column, bool generated) {
+    const int      shift = sizeof(Count) == 4 ? 0 : (column & 1) * 16;
+    const uint32_t word = peer_address(words + (sizeof(Count) == 4 ? column : column >> 1), rank);
+    if (generated) asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(word), "r"(1u << shift) : "memory");
+    else asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(word), "r"(kPrompt<Count> << shift) : "memory");
+}
+template <class Count> __device__ __forceinline__ uint32_t counter_of(const uint32_t* words, int column) {
+    return reinterpret_cast<const Count*>(words)[column];
+}
+// Bit j: counter `column` + j is set.  `column` is a vector's first.
+template <class Count, int E> __device__ __forceinline__ uint32_t counted(const uint32_t* words, int column) {
+    constexpr int N = E * (int)sizeof(Count) / 4;          // words of a vector
+    const uint32_t* from = words + column * (int)sizeof(Count) / 4;
+    uint32_t w[N], r = 0;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) *reinterpret_cast<uint2*>(w + i) = *reinterpret_cast<const uint2*>(from + i);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const uint32_t c = sizeof(Count) == 4 ? w[j * N / E] : w[j * N / E] & 0xffffu << (j % 2 * 16);
+        r |= (c ? 1u : 0u) << j;
     }
+    return r;
+}
+
+// Elements a .. b - 1 of E as bits, where these may lie outside.
+__device__ __forceinline__ uint32_t bits_between(int a, int b, int E) {
+    const uint32_t below = (1u << min(max(b, 0), E)) - 1;
+    return below & ~((1u << min(max(a, 0), E)) - 1);
+}
+// A vector of a layer that the row fills in part; what is not the row's is -inf.
+template <class T> __device__ __noinline__ uint4 edge_vector(const Layer& l, int vec) {
+    constexpr int E = kPerVec<T>;
+    const int a = l.lo - vec * E, b = l.hi - vec * E;
+    if (a <= 0 && b >= E) return __ldcs(reinterpret_cast<const uint4*>(l.in) + vec);
+    T e[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) e[j] = j >= a && j < b ? reinterpret_cast<const T*>(l.in)[vec * E + j] : from_float<T>(-INFINITY);
+    return *reinterpret_cast<const uint4*>(e);
+}
+template <int E> __device__ __forceinline__ float far_sum(const float (&x)[E], float base) {
+    float r = 0.f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) r += scale_to(x[j], base, kLog2e);
+    return r;
 }
 
 template <class TI, class TO, class Count>
-__global__ void __launch_bounds__(kThreads, 4) process_kernel(const __grid_constant__ LogitsCut in,
-                                                           const __grid_constant__ LogitsCut out, Deal deal,
-                                                           const __grid_constant__ nereus_penalties_t how, int32_t* token,
-                                                           float* lse) {
+__global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_constant__ LogitsCut in,
+                                                              const __grid_constant__ LogitsCut out, Deal deal,
+                                                              const __grid_constant__ nereus_penalties_t how, int32_t* token,
+                                                              float* lse) {
     constexpr int E = kPerVec<TI>;
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ float2 scratch[kWarps], from_peers[kMaxCtas];
     __shared__ int    id_scratch[kWarps], id_peers[kMaxCtas];
+    __shared__ uint2  masks;
     const int     tid = threadIdx.x, rank = blockIdx.x & ((1 << deal.log_c) - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
-    if (deal.log_c) cluster_arrive();
-
-    Layer*    table = reinterpret_cast<Layer*>(dynamic);
-    uint32_t* flags = reinterpret_cast<uint32_t*>(table + deal.mine);
-    uint32_t* hash = flags + (how.bias_ids ? deal.mine * kVecs / 4 : 0);   // flags: a bit per element, a byte per vector
-    uint32_t* counters = hash + (how.bias_ids ? 2 * kHash : 0);
-    int32_t*  hash_id = reinterpret_cast<int32_t*>(hash);
-    int32_t*  hash_entry = hash_id + kHash;
+    constexpr int kMaskWords = kPerLayer<TI> / 32 + 1;       // of a layer, which may begin anywhere in a word
+    Layer*     table = reinterpret_cast<Layer*>(dynamic);
+    uint32_t*  words = reinterpret_cast<uint32_t*>(table + deal.mine);                       // mask words
+    uint32_t*  biased = words + (how.mask ? (deal.mine * kMaskWords + 3) / 4 * 4 : 0);        // a byte per vector
+    int32_t*   hash_id = reinterpret_cast<int32_t*>(biased + (how.bias_ids ? deal.mine * kVecs / 4 : 0));
+    int32_t*   hash_entry = hash_id + kHash;                  // the last entry of the id, then its value
+    uint32_t*  counters = reinterpret_cast<uint32_t*>(hash_id + (how.bias_ids ? 2 * kHash : 0));
+    __shared__ float    queued[kWarps][64 * E + 32];
+    __shared__ uint16_t queued_column[kWarps][64 * E + 32];
 
     const float rho = how.repetition ? how.repetition[row] : 1.f;
-    const float pres = how.presence ? how.presence[row] : 0.f, freq = how.frequency ? how.frequency[row] : 0.f;
+    const float presence = how.presence ? how.presence[row] : 0.f, frequency = how.frequency ? how.frequency[row] : 0.f;
     int total = 0, prompt = 0;
     if (how.history) {
         total = how.total_len ? max(0, min((int)how.history_len, how.total_len[row])) : (int)how.history_len;
@@ -480,174 +547,327 @@ __global__ void __launch_bounds__(kThreads, 4) process_kernel(const __grid_const
     const int      mask_last = (in.vocab - 1) >> 5;
 
     const int n_all = layers_of(deal, rank);
-    float m = -INFINITY, sum = 0.f;
-    int   at = 0x7fffffff;
-    for (int first = 0; first < n_all; first += deal.mine) {       // one round unless the counters do not fit
+    // The largest value of the sweep and the first vector that has it; the largest of the gathered and its id.  The sum is
+    // kept from a base that follows the maximum only when it has fallen 40 behind: its terms stay below 2^58, and most
+    // vectors leave it alone.
+    float m = -INFINITY, base = -INFINITY, base_c = 0.f, right = 1.f, sum = 0.f;
+    const char* m_vector = nullptr;
+    int         m_token = 0;
+    uint32_t    m_held = 0;                                  // elements of the vector that are the sweep's
+    float       m_one = -INFINITY;
+    int         m_one_token = 0x7fffffff;
+    auto rebase = [&](float top) {
+        sum *= scale_to(base, top, kLog2e);
+        base = top;
+        base_c = top * kLog2e;
+        right = exp2_approx(fmaf(-top, kLog2e, base_c));
+    };
+    const bool  sparse = total > 0 || how.bias_ids;
+    const bool  rounds = deal.mine << deal.log_c < deal.layers;      // the counters do not fit at once
+    const bool  spread = deal.log_c && !rounds && total >= kSpread;
+    for (int first = 0; first < n_all || first == 0; first += deal.mine) {
         const int n = min(deal.mine, n_all - first);
         __syncthreads();
-        if (tid < n) table[tid] = layer_of<TI, TO>(in, out, deal, row, rank, first + tid);
+        const uint32_t whole = fill_table<TI, TO>(table, &masks, in, out, deal, row, rank, first, n).x;
+        // this thread's two vectors of the next layer, on their way
+        auto fetch = [&](int l, uint4 (&v)[2]) {
+            if (l >= n) return;
+            if (whole >> l & 1u) {
+                const uint4* from = reinterpret_cast<const uint4*>(table[l].in) + tid;
+                v[0] = __ldcs(from);
+                v[1] = __ldcs(from + kThreads);
+            } else {
+#pragma unroll 1
+                for (int i = 0; i < 2; ++i) {
+                    const uint4 e = edge_vector<TI>(table[l], tid + i * kThreads);
+                    if (i == 0) v[0] = e; else v[1] = e;
+                }
+            }
+        };
+        uint4 next[2] = {};
+        fetch(0, next);
         if (total > 0)
             for (int i = tid; i < n * kPerLayer<TI> * (int)sizeof(Count) / 16; i += kThreads)
                 reinterpret_cast<uint4*>(counters)[i] = make_uint4(0, 0, 0, 0);
-        if (how.bias_ids) {
-            for (int i = tid; i < n * kVecs / 4; i += kThreads) flags[i] = 0;
-            for (int i = tid; i < 2 * kHash; i += kThreads) hash_id[i] = -1;
-        }
-        __syncthreads();
-        for (int i = tid; i < total; i += kThreads) {
-            const int id = hist[i];
-            if ((uint32_t)id >= (uint32_t)in.vocab) continue;
-            const Place p = place_of<TI>(in, deal, row, id);
-            const int   l = p.layer - first;
-            if (p.rank == rank && (uint32_t)l < (uint32_t)n) count_token<Count>(counters, l * kPerLayer<TI> + p.position, i >= prompt);
-        }
         if (how.bias_ids)
-            for (int i = tid; i < how.bias_count; i += kThreads) {
-                const int id = how.bias_ids[row * how.bias_count + i];
-                if ((uint32_t)id >= (uint32_t)in.vocab) continue;
+            for (int i = tid; i < 2 * kHash / 4; i += kThreads) reinterpret_cast<int4*>(hash_id)[i] = make_int4(-1, -1, -1, -1);
+        if (how.bias_ids)
+            for (int i = tid; i < n * kVecs / 4; i += kThreads) biased[i] = 0;
+        if (mask) {
+#pragma unroll 4
+            for (int i = tid; i < n * kMaskWords; i += kThreads) {
+                const int w = (table[i / kMaskWords].token >> 5) + i % kMaskWords;
+                words[i] = w >= 0 && w <= mask_last ? (uint32_t)mask[w] : 0u;
+            }
+        }
+        if (deal.log_c && first == 0) cluster_arrive();      // this block runs, and its counters are zero
+        __syncthreads();
+        if (spread) {
+            cluster_wait();
+            const int part = (total + (1 << deal.log_c) - 1) >> deal.log_c, end = min(total, (rank + 1) * part);
+            auto count = [&](int i, int id) {
+                if ((uint32_t)id >= (uint32_t)in.vocab) return;
+                const Place p = place_of<TI>(in, deal, row, id);
+                count_token_at<Count>(p.rank, counters, p.layer * kPerLayer<TI> + p.position, i >= prompt);
+            };
+            int i = rank * part + tid;
+            for (; i + 3 * kThreads < end; i += 4 * kThreads) {
+                int id[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) id[j] = hist[i + j * kThreads];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) count(i + j * kThreads, id[j]);
+            }
+            for (; i < end; i += kThreads) count(i, hist[i]);
+        } else {
+            auto count = [&](int i, int id) {
+                if ((uint32_t)id >= (uint32_t)in.vocab) return;
                 const Place p = place_of<TI>(in, deal, row, id);
                 const int   l = p.layer - first;
-                if (p.rank != rank || (uint32_t)l >= (uint32_t)n) continue;
-                const int byte = l * kVecs + p.position / E;
-                atomicOr(&flags[byte >> 2], 1u << ((byte & 3) * 8 + p.position % E));
+                if (p.rank == rank && (uint32_t)l < (uint32_t)n) count_token<Count>(counters, l * kPerLayer<TI> + p.position, i >= prompt);
+            };
+            int i = tid;
+            for (; i + 7 * kThreads < total; i += 8 * kThreads) {
+                int id[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) id[j] = hist[i + j * kThreads];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) count(i + j * kThreads, id[j]);
+            }
+#pragma unroll 4
+            for (; i < total; i += kThreads) count(i, hist[i]);
+        }
+        if (how.bias_ids) {
+            // slot of the id in the hash table, or -1 where another block holds the token
+            auto slot_of = [&](int i) {
+                const int id = how.bias_ids[row * how.bias_count + i];
+                if ((uint32_t)id >= (uint32_t)in.vocab) return -1;
+                const Place p = place_of<TI>(in, deal, row, id);
+                const int   l = p.layer - first;
+                if (p.rank != rank || (uint32_t)l >= (uint32_t)n) return -1;
+                const int vec = l * kVecs + p.position / E;
+                atomicOr(biased + vec / 4, 1u << (vec % 4 * 8 + p.position % E));
                 uint32_t h = (uint32_t)id * 2654435761u % kHash;
                 for (int probe = 0; probe < kHash; ++probe, h = (h + 1) % kHash) {
                     const int was = atomicCAS(&hash_id[h], -1, id);
-                    if (was == -1 || was == id) { atomicMax(&hash_entry[h], i); break; }
+                    if (was == -1 || was == id) break;
                 }
+                return (int)h;
+            };
+            // of the entries of one id the last counts; then its value takes the entry's place in the table
+            constexpr int kMost = (NEREUS_BIAS_MAX + kThreads - 1) / kThreads;
+            int slot[kMost];
+#pragma unroll
+            for (int j = 0; j < kMost; ++j) {
+                const int i = tid + j * kThreads;
+                slot[j] = i < how.bias_count ? slot_of(i) : -1;
+                if (slot[j] >= 0) atomicMax(&hash_entry[slot[j]], i);
             }
+            __syncthreads();
+            bool last[kMost];
+#pragma unroll
+            for (int j = 0; j < kMost; ++j) last[j] = slot[j] >= 0 && hash_entry[slot[j]] == tid + j * kThreads;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < kMost; ++j)
+                if (last[j]) hash_entry[slot[j]] = __float_as_int(how.bias_values[row * how.bias_count + tid + j * kThreads]);
+        }
+        if (spread) {
+            cluster_arrive();
+            cluster_wait();
+            cluster_arrive();                  // what the exchange at the end waits for
+        }
         __syncthreads();
-        auto work = [&](int l, int vec) {
+
+        // bit j: element j of the vector is allowed
+        auto allowed = [&](int l, int vec) {
+            const uint32_t* w = words + l * kMaskWords;
+            const int       bit = (table[l].token & 31) + vec * E;
+            return __funnelshift_r(w[bit >> 5], w[min((bit >> 5) + 1, kMaskWords - 1)], bit & 31);
+        };
+        // a queued column, x its element
+        float* const    queue = queued[tid >> 5];
+        uint16_t* const queue_column = queued_column[tid >> 5];
+        int             waiting = 0;
+        auto change = [&](int at) {
+            float        x = queue[at];
+            const int    column = queue_column[at], l = column / kPerLayer<TI>, p = column % kPerLayer<TI>;
             const Layer& L = table[l];
-            const int    p0 = vec * E;
-            const bool   whole = p0 >= L.lo && p0 + E <= L.hi;
-            float x[E];
-            if (whole) {
-                unpack<TI>(__ldcs(reinterpret_cast<const uint4*>(L.in + vec * 16)), x);
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j)
-                    x[j] = p0 + j >= L.lo && p0 + j < L.hi ? to_float(reinterpret_cast<const TI*>(L.in)[p0 + j]) : -INFINITY;
-            }
-            const int v0 = L.token + p0;
             if (total > 0) {
-                uint32_t c[E];
-                uint32_t any = 0;
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    c[j] = reinterpret_cast<const Count*>(counters)[l * kPerLayer<TI> + p0 + j];
-                    any |= c[j];
-                }
-                if (any) {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        if (!c[j]) continue;
-                        x[j] = x[j] > 0.f ? __fdiv_rn(x[j], rho) : __fmul_rn(x[j], rho);
-                        if (const uint32_t k = c[j] & (kSeen<Count> - 1))
-                            x[j] = __fsub_rn(__fsub_rn(x[j], __fmul_rn(freq, (float)k)), pres);
-                    }
+                if (const uint32_t c = counter_of<Count>(counters, column)) {
+                    x = x > 0.f ? __fdiv_rn(x, rho) : __fmul_rn(x, rho);
+                    if (const uint32_t made = c & (kPrompt<Count> - 1))
+                        x = __fsub_rn(__fsub_rn(x, __fmul_rn(frequency, (float)made)), presence);
                 }
             }
             if (how.bias_ids) {
-                if (const uint32_t f = reinterpret_cast<const uint8_t*>(flags)[l * kVecs + vec]) {
+                // the table is never full: an empty slot ends the search for a token without a bias
+                uint32_t h = (uint32_t)(L.token + p) * 2654435761u % kHash;
+                while (hash_id[h] != L.token + p && hash_id[h] != -1) h = (h + 1) % kHash;
+                if (hash_id[h] != -1) x = __fadd_rn(x, __int_as_float(hash_entry[h]));
+            }
+            if (mask && !(allowed(l, p / E) >> (p % E) & 1u)) x = -INFINITY;
+            const TO y = from_float<TO>(x);
+            reinterpret_cast<TO*>(L.out)[p] = y;
+            x = to_float(y);
+            if (x > m_one || (x == m_one && x > -INFINITY && L.token + p < m_one_token)) { m_one = x; m_one_token = L.token + p; }
+            if (x > base + 40.f) rebase(x);
+            sum += is_far(base_c) ? scale_to(x, base, kLog2e) : exp2_approx(fmaf(x, kLog2e, -base_c)) * right;
+        };
+
+        // One layer at a time, a thread's two vectors together; after the last the rest of the queue.
+#pragma unroll 1
+        for (int l = 0; l <= n; ++l) {
+            if (l < n) {
+                const uint4 v[2] = {next[0], next[1]};
+                fetch(l + 1, next);
+                const Layer& L = table[l];
+                float    x[2][E], top[2];
+                uint32_t held[2], other[2] = {0, 0};      // elements that the sweep writes; that the queue takes
+                const bool edge = !(whole >> l & 1u);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        if (!(f >> j & 1)) continue;
-                        uint32_t h = (uint32_t)(v0 + j) * 2654435761u % kHash;
-                        for (int probe = 0; probe < kHash && hash_id[h] != v0 + j; ++probe) h = (h + 1) % kHash;
-                        x[j] = __fadd_rn(x[j], how.bias_values[row * how.bias_count + hash_entry[h]]);
+                for (int i = 0; i < 2; ++i) {
+                    const int vec = tid + i * kThreads;
+                    unpack<TI>(v[i], x[i]);
+                    held[i] = (1u << E) - 1;
+                    if (edge) held[i] = bits_between(L.lo - vec * E, L.hi - vec * E, E);
+                    if (sparse) {
+                        if (how.bias_ids) other[i] = reinterpret_cast<const uint8_t*>(biased)[l * kVecs + vec];
+                        if (total > 0) other[i] |= counted<Count, E>(counters, l * kPerLayer<TI> + vec * E);
+                        held[i] &= ~other[i];
                     }
                 }
-            }
-            if (mask) {
-                const int      w = max(v0, 0) >> 5;
-                const uint32_t low = (uint32_t)mask[w], high = (uint32_t)mask[min(w + 1, mask_last)];
+                if (sparse && __any_sync(0xffffffffu, other[0] | other[1])) {
+                    // into the queue by lane and element, always in the same order: so that the sums come out alike
+                    int upto = __popc(other[0]) + __popc(other[1]), at = waiting - upto;
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const int v = v0 + j;
-                    const uint32_t word = v >> 5 == w ? low : high;
-                    if (!(word >> (v & 31) & 1u)) x[j] = -INFINITY;
+                    for (int o = 1; o < 32; o *= 2) {
+                        const int below = __shfl_up_sync(0xffffffffu, upto, o);
+                        if ((tid & 31) >= o) upto += below;
+                    }
+                    at += upto;
+                    waiting += __shfl_sync(0xffffffffu, upto, 31);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+                        if (other[i]) {
+#pragma unroll
+                            for (int j = 0; j < E; ++j)
+                                if (other[i] >> j & 1u) {
+                                    queue[at] = x[i][j];
+                                    queue_column[at++] = (uint16_t)(l * kPerLayer<TI> + (tid + i * kThreads) * E + j);
+                                }
+                        }
+                    __syncwarp();
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int vec = tid + i * kThreads;
+                    if (mask) {
+                        const uint32_t f = allowed(l, vec);
+#pragma unroll
+                        for (int j = 0; j < E; ++j) x[i][j] = f >> j & 1u ? x[i][j] : -INFINITY;
+                    }
+                    // written, and from here on what was written
+                    TO y[E];
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        y[j] = from_float<TO>(x[i][j]);
+                        x[i][j] = to_float(y[j]);
+                    }
+                    char* const o = L.out + vec * E * (int)sizeof(TO);
+                    if (L.vec_out && held[i] == (1u << E) - 1) {
+                        const uint4* w = reinterpret_cast<const uint4*>(y);
+#pragma unroll
+                        for (int j = 0; j < E * (int)sizeof(TO) / 16; ++j) __stcs(reinterpret_cast<uint4*>(o) + j, w[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < E; ++j) {
+                            if (held[i] >> j & 1u) reinterpret_cast<TO*>(o)[j] = y[j];
+                            else x[i][j] = -INFINITY;
+                        }
+                    }
+                    top[i] = x[i][0];
+#pragma unroll
+                    for (int j = 1; j < E; ++j) top[i] = fmaxf(top[i], x[i][j]);
+                }
+                const float most = fmaxf(top[0], top[1]);
+                if (most > m) {
+                    m = most;
+                    const int vec = top[0] == most ? tid : tid + kThreads;
+                    m_vector = L.out + vec * E * (int)sizeof(TO);
+                    m_token = L.token + vec * E;
+                    m_held = top[0] == most ? held[0] : held[1];
+                }
+                if (most > base + 40.f) rebase(most);
+                if (is_far(base_c)) {
+                    sum += far_sum(x[0], base) + far_sum(x[1], base);
+                } else {
+                    Pair part[2] = {0, 0};
+                    const Pair c = pair(kLog2e, kLog2e), minus = pair(-base_c, -base_c);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < E; j += 2) part[i] = add2(part[i], exp2_pair(fma2(pair(x[i][j], x[i][j + 1]), c, minus)));
+                    const float2 h = halves(add2(part[0], part[1]));
+                    sum = fmaf(h.x + h.y, right, sum);
                 }
             }
-            // written, and from here on what was written
-            TO y[E];
-            float top = -INFINITY;
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                y[j] = from_float<TO>(x[j]);
-                x[j] = to_float(y[j]);
-                top = fmaxf(top, x[j]);
-            }
-            if (whole && L.vec_out) {
-                const uint4* w = reinterpret_cast<const uint4*>(y);
-                uint4*       o = reinterpret_cast<uint4*>(L.out + p0 * (int)sizeof(TO));
-#pragma unroll
-                for (int j = 0; j < E * (int)sizeof(TO) / 16; ++j) __stcs(o + j, w[j]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    if (p0 + j >= L.lo && p0 + j < L.hi) reinterpret_cast<TO*>(L.out)[p0 + j] = y[j];
-                    else x[j] = -INFINITY;
-                }
-            }
-            if (top > m) {
-                sum *= scale_to(m, top, kLog2e);
-                m = top;
-#pragma unroll
-                for (int j = E - 1; j >= 0; --j)
-                    if (x[j] == top) at = v0 + j;
-            }
-            if (m == INFINITY) {
-                for (int j = 0; j < E; ++j) sum += x[j] == INFINITY ? 1.f : x[j] == x[j] ? 0.f : x[j];
-            } else {
-                const float base = m == -INFINITY ? 0.f : m;
-                float       part = 0.f;
-#pragma unroll
-                for (int j = 0; j < E; ++j) part += exp2_approx((x[j] - base) * kLog2e);
-                sum += part;
-            }
-        };
 #pragma unroll 1
-        for (int l = 0; l < n; ++l) for_edges<TI>(table, l, work);
+            for (const int least = l < n ? 32 : 1; waiting >= least;) {
+                const int now = min(waiting, 32);
+                waiting -= now;
+                if ((tid & 31) < now) change(waiting + (tid & 31));
+            }
+            __syncwarp();
+        }
     }
+    const float m_sweep = m;
+    m = fmaxf(m, m_one);
+    sum *= scale_to(base, m, kLog2e);
 
-    // the block's result, and the cluster's on its first block
-    const float mine = m;
-    float2 v = make_float2(m, sum);
-#pragma unroll
-    for (int o = 16; o; o >>= 1)
-        v = join(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)), kLog2e);
-    const int warp_at = (int)__reduce_min_sync(0xffffffffu, mine == v.x ? (uint32_t)at : 0x7fffffffu);
-    if ((tid & 31) == 0) { scratch[tid >> 5] = v; id_scratch[tid >> 5] = warp_at; }
+    // the warp's result, the block's on its first warp, and the cluster's on its first block
+    auto warp_join = [&](float2 v) {
+        const float top = warp_max(v.x);
+        return make_float2(top, warp_sum(v.y * scale_to(v.x, top, kLog2e)));
+    };
+    float2 v = warp_join(make_float2(m, sum));
+    // the lowest id of the maximum: only the threads that have it read their vector back
+    int at = m_one == v.x ? m_one_token : 0x7fffffff;
+    if (m_sweep == v.x && m_vector) {
+#pragma unroll 1
+        for (int j = E - 1; j >= 0; --j)
+            if ((m_held >> j & 1u) && to_float(reinterpret_cast<const TO*>(m_vector)[j]) == v.x) at = min(at, m_token + j);
+    }
+    at = (int)__reduce_min_sync(0xffffffffu, (uint32_t)at);
+    const int lane = tid & 31;
+    if (lane == 0) { scratch[tid >> 5] = v; id_scratch[tid >> 5] = at; }
     __syncthreads();
     if (deal.log_c) cluster_wait();
-    if (tid == 0) {
-        v = scratch[0];
-        int id = id_scratch[0];
-        for (int i = 1; i < kWarps; ++i) {
-            if (scratch[i].x > v.x) id = id_scratch[i];
-            else if (scratch[i].x == v.x) id = min(id, id_scratch[i]);
-            v = join(v, scratch[i], kLog2e);
-        }
-        if (deal.log_c) {
+    if (tid < 32) {
+        const float2 mine = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
+        v = warp_join(mine);
+        at = (int)__reduce_min_sync(0xffffffffu, lane < kWarps && mine.x == v.x ? (uint32_t)id_scratch[lane] : 0x7fffffffu);
+        if (lane == 0) {
             peer_store(peer_address(&from_peers[rank], 0), v.x, v.y);
-            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&id_peers[rank], 0)), "r"(id) : "memory");
-        } else {
-            from_peers[0] = v;
-            id_peers[0] = id;
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&id_peers[rank], 0)), "r"(at) : "memory");
         }
     }
-    if (deal.log_c) { __syncwarp(); cluster_arrive(); cluster_wait(); }
-    if (rank == 0 && tid == 0) {
-        v = from_peers[0];
-        int id = id_peers[0];
-        for (int i = 1; i < 1 << deal.log_c; ++i) {
-            if (from_peers[i].x > v.x) id = id_peers[i];
-            else if (from_peers[i].x == v.x) id = min(id, id_peers[i]);
-            v = join(v, from_peers[i], kLog2e);
+    if (deal.log_c) {
+        __syncwarp();
+        cluster_arrive();
+        if (rank) return;
+        cluster_wait();
+    }
+    if (tid < 32) {
+        __syncwarp();
+        const int    ctas = 1 << deal.log_c;
+        const float2 mine = lane < ctas ? from_peers[lane] : make_float2(-INFINITY, 0.f);
+        v = warp_join(mine);
+        at = (int)__reduce_min_sync(0xffffffffu, lane < ctas && mine.x == v.x ? (uint32_t)id_peers[lane] : 0x7fffffffu);
+        if (lane == 0) {
+            if (token) token[row] = v.x > -INFINITY ? at : -1;
+            if (lse) lse[row] = log_sum(v.x, v.x, v.y);
         }
-        if (token) token[row] = v.x > -INFINITY ? id : -1;
-        if (lse) lse[row] = log_sum(v.x, v.x, v.y);
     }
 }
 
@@ -704,7 +924,7 @@ __global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant_
     __shared__ uint2 masks;
     if (tid == 0) n_found = 0;
     if (tid < k) best[tid] = 0;
-    const uint32_t whole = fill_table<T, T>(table, &masks, in, LogitsCut(), deal, row, rank, n).x;
+    const uint32_t whole = fill_table<T, T>(table, &masks, in, LogitsCut(), deal, row, rank, 0, n).x;
     load_share<T>(table, slots, whole, n, quarter);
 
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;
@@ -718,13 +938,7 @@ __global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant_
                       }
                   });
     const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1), m = fmaxf(f0, f1), m_warp = warp_max(m);
-    float sum = 0.f;
-    if (m_warp == INFINITY) {
-        for (int i = 0; i < n; ++i) for_edges<T>(table, i, [&](int l, int vec) { sum += exp_sum_inf<T>(slots[l * kVecs + vec]); });
-    } else {
-        const Base b = base_of(m_warp, c);
-        sum = exp_sums<T>(table, slots, whole, n, b);
-    }
+    float sum = exp_sums<T>(table, slots, whole, n, base_of(m_warp, c));
     sum = warp_sum(sum);
     if ((tid & 31) == 0) scratch[tid >> 5] = make_float2(m_warp, sum);
 
@@ -900,7 +1114,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
     __shared__ uint2 masks;
     int id = -1;                                  // entry `tid`
     if (tid < k) id = how.ids[row * k + tid];
-    const uint2 whole = fill_table<T, T>(table, &masks, in, grad, deal, row, rank, n);
+    const uint2 whole = fill_table<T, T>(table, &masks, in, grad, deal, row, rank, 0, n);
     if (weight == 0.f) {
         if (rank == 0 && tid == 0 && kPass != kBackward) loss[row] = 0.f;
         if (rank == 0 && tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
@@ -920,7 +1134,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
         if (id >= 0) {
             y = how.values[row * k + tid];
             const Place at = place_of<T>(in, deal, row, id);
-            const int   s = in.tp == 1 ? 0 : id / in.cols;
+            const int   s = shard_of(in, id);
             x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
             if (at.rank == rank) { place = at.layer; place_at = at.position; }
         }
@@ -1044,7 +1258,7 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
     __syncthreads();
     {
         const Base  b = base_of(m, c);
-        const float scale = rest_scale_of_row * b.right;
+        const float scale = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
         const Pair  s = pair(scale, scale);
         auto gradient = [&](uint4 v) {
             Pair e[Vec<T>::kPairs];
@@ -1053,6 +1267,18 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
             for (int j = 0; j < Vec<T>::kPairs; ++j) e[j] = mul2(exp2_pair(fma2(e[j], b.c, b.minus_mc)), s);
             return Vec<T>::pack(e);
         };
+        auto gradient_far = [&](uint4 v) {
+            float e[kPerVec<T>];
+            unpack<T>(v, e);
+            Pair p[Vec<T>::kPairs];
+#pragma unroll
+            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(pair(scale_to(e[2 * j], b.m, c), scale_to(e[2 * j + 1], b.m, c)), s);
+            return Vec<T>::pack(p);
+        };
+        if (b.far)
+            for (int i = 0; i < n; ++i)
+                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, gradient_far(slots[l * kVecs + vec])); });
+        else
         sweep<T>(table, slots, whole.y, 0, n, [&](int l, int vec, uint4 v) { store_vector<T>(table[l], vec, gradient(v)); },
                  [&](int l, const auto& v) {
                      uint4 o[v.n];
@@ -1133,6 +1359,7 @@ LogitsCut cut_of(const nereus_logits_t& v) {
     LogitsCut c;
     for (int s = 0; s < NEREUS_VOCAB_MAX_TP; ++s) c.shard[s] = s < v.tp ? (char*)v.shard[s] : nullptr;
     c.row_bytes = v.row_stride * size_of(v.dtype);
+    c.per_col = 1.f / (float)v.shard_cols;
     c.tp = v.tp; c.cols = (int32_t)v.shard_cols; c.vocab = (int32_t)v.vocab;
     return c;
 }
@@ -1187,15 +1414,15 @@ int device_of(Device* d) {
     if (!d->smem) {
         int most = 0;
         NEREUS_CUDA(cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, d->id));
-        d->smem = most - 16384;                                   // 16 KiB: the kernels' static part
+        d->smem = most - 28672;                                   // 28 KiB: the kernels' static part
         smem[d->id].store(d->smem);
     }
     return NEREUS_OK;
 }
 
-// Deals a row out over the fewest blocks whose share takes at most kSmemShare bytes at `per_layer` a layer and `fixed`
-// once.  The number of rows has no part in it: a row's sums come out the same in any batch.
-Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed) {
+// Deals a row out over the fewest blocks whose share has at most `most` layers and takes at most kSmemShare bytes, at
+// `per_layer` a layer and `fixed` once.  The number of rows has no part in it: a row's sums come out the same in any batch.
+Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int most) {
     Deal d;
     const int64_t e = 16 / size_of(v.dtype), w = held_cols(v, 0), bytes = v.row_stride * size_of(v.dtype);
     d.aligned = v.rows < 2 || bytes % 16 == 0;
@@ -1207,7 +1434,7 @@ Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed) {
     d.layers = (int)(d.per_shard * used);
     d.log_c = 0;
     auto share = [&] { return (int64_t)(d.layers + (1 << d.log_c) - 1) >> d.log_c; };
-    while (d.log_c < 3 && share() * per_layer + fixed > kSmemShare) ++d.log_c;
+    while (d.log_c < 3 && (share() > most || share() * per_layer + fixed > kSmemShare)) ++d.log_c;
     d.mine = (int)share();
     return d;
 }
@@ -1245,7 +1472,7 @@ int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + kVecs * 16;
-    const Deal    d = deal_of(in, per_layer, 0);
+    const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
     return launch(distill_kernel<T, kPass>, opted, in.rows, d, d.mine * per_layer, dev, stream,
                   cut_of(in), kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
 }
@@ -1271,11 +1498,12 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
     static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) + (how.bias_ids ? kVecs : 0);
-    const int64_t fixed = how.bias_ids ? 2 * kHash * 4 : 0;
-    Deal d = deal_of(in, per_layer, fixed);
+    const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
+                              (how.bias_ids ? kVecs : 0) + (how.mask ? (kPerLayer<TI> / 32 + 1) * 4 : 0);
+    const int64_t fixed = (how.bias_ids ? 2 * kHash * 4 : 0) + 16;
+    Deal d = deal_of(in, per_layer, fixed, 4);
     // what does not fit is done in rounds
-    while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > kThreads)) d.mine = (d.mine + 1) / 2;
+    while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
     return launch(process_kernel<TI, TO, Count>, opted, in.rows, d, d.mine * per_layer + fixed, dev, stream,
                   cut_of(in), cut_of(out), d, how, token, lse);
 }
@@ -1286,7 +1514,7 @@ int top_launch(const nereus_logits_t& in, int k, float temperature, float* value
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + kVecs * 16;
-    const Deal    d = deal_of(in, per_layer, 0);
+    const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
     // the slots also take the lists of all blocks of the cluster
     const int64_t lists = d.log_c ? ((int64_t)k << d.log_c) * 8 + d.mine * (int64_t)sizeof(Layer) : 0;
     return launch(top_kernel<T>, opted, in.rows, d, std::max(d.mine * per_layer, lists), dev, stream, cut_of(in),
