@@ -443,18 +443,16 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 
 // ---- penalties, biases, masks --------------------------------------------------------------------------------
 //
-// A sweep over the row, vectors from memory through registers to memory, the next four on their way while four are worked
-// on, mask bits from shared memory.  What changes a logit by its token is sparse: the history's tokens and the biases.  One
-// counter per column of the block's share is kept in shared memory (the history lands there with shared-memory atomics:
-// sums of whole numbers, so that no order shows), and a hash table of the bias entries.  The sweep hands the columns that
-// have either over to a queue of its warp, together with the element, and does not write them; the warp takes 32 of them at
-// a time through penalties, bias and mask.  The running (maximum, where it is, sum of exponentials) of both stays on the
-// thread.
-// A long history is read once per row, each block of the cluster taking its part and counting into the share of whichever
-// block holds the token; a short one by every block for itself, which saves two cluster barriers.
+// A sweep over the row, elements through a ring of three layers in shared memory to registers and from there to memory.
+// Everything else waits in shared memory: mask bits, one counter per column of the block's share (the history lands there
+// with shared-memory atomics: sums of whole numbers, so that no order shows), a hash table of the bias entries with a flag
+// per column.  The running (maximum, where it is, sum of exponentials) stays on the thread.
+// Every block reads the whole history (from L2) and keeps what falls into its share: reading it once per cluster and
+// counting into the peers' shared memory was no faster (256 rows of up to 16384 tokens: 166 against 170 us) and takes two
+// cluster barriers.
 
+constexpr int kRing   = 3;                // layers on their way to a block
 constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
-constexpr int kSpread = 2048;             // tokens from which on the cluster's blocks share the reading of the history
 
 // Counter of a column, 0 for a token that is not in the history: the top bit "in the prompt", the others "generated so
 // often".
@@ -466,28 +464,52 @@ template <class Count> __device__ __forceinline__ void count_token(uint32_t* wor
     if (generated) atomicAdd(word, 1u << shift);
     else atomicOr(word, kPrompt<Count> << shift);
 }
-template <class Count> __device__ __forceinline__ void count_token_at(int rank, uint32_t* words, int column, bool generated) {
-    const int      shift = sizeof(Count) == 4 ? 0 : (column & 1) * 16;
-    const uint32_t word = peer_address(words + (sizeof(Count) == 4 ? column : column >> 1), rank);
-    if (generated) asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;" ::"r"(word), "r"(1u << shift) : "memory");
-    else asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(word), "r"(kPrompt<Count> << shift) : "memory");
-}
-template <class Count> __device__ __forceinline__ uint32_t counter_of(const uint32_t* words, int column) {
-    return reinterpret_cast<const Count*>(words)[column];
-}
-// Bit j: counter `column` + j is set.  `column` is a vector's first.
-template <class Count, int E> __device__ __forceinline__ uint32_t counted(const uint32_t* words, int column) {
+// The counters of a vector, `column` its first; returns whether one is set.
+template <class Count, int E> __device__ __forceinline__ bool counts_of(const uint32_t* words, int column, uint32_t (&c)[E]) {
     constexpr int N = E * (int)sizeof(Count) / 4;          // words of a vector
     const uint32_t* from = words + column * (int)sizeof(Count) / 4;
-    uint32_t w[N], r = 0;
+    uint32_t w[N], any = 0;
 #pragma unroll
     for (int i = 0; i < N; i += 2) *reinterpret_cast<uint2*>(w + i) = *reinterpret_cast<const uint2*>(from + i);
 #pragma unroll
+    for (int i = 0; i < N; ++i) any |= w[i];
+#pragma unroll
+    for (int j = 0; j < E; ++j) c[j] = sizeof(Count) == 4 ? w[j * N / E] : w[j * N / E] >> (j % 2 * 16) & 0xffffu;
+    return any != 0;
+}
+
+// Penalties of a vector whose counters are c.  A quotient x / rho has to come out as IEEE division rounds it, for many x
+// that share rho: with y = the rounded 1 / rho, q = x y and the remainder r = x - q rho, exact by fma, q + r y by fma is
+// the correctly rounded quotient (Markstein, Computation of elementary functions on the IBM RISC System/6000 processor,
+// 1990) as long as nothing on the way over- or underflows; a vector or row where that could be is divided.
+struct Penalty {
+    float rho, inverse, frequency, presence;
+    bool  plain;               // rho lies in 2^-60 .. 2^60, as x has to
+};
+__device__ __forceinline__ Penalty penalty_of(float rho, float frequency, float presence) {
+    return {rho, __frcp_rn(rho), frequency, presence, rho >= 0x1p-60f && rho <= 0x1p60f};
+}
+template <class Count, int E> __device__ __forceinline__ void penalise(float (&x)[E], const uint32_t (&c)[E], const Penalty& p) {
+    float q[E];
+    bool  odd = !p.plain;
+#pragma unroll
     for (int j = 0; j < E; ++j) {
-        const uint32_t c = sizeof(Count) == 4 ? w[j * N / E] : w[j * N / E] & 0xffffu << (j % 2 * 16);
-        r |= (c ? 1u : 0u) << j;
+        constexpr uint32_t least = 0x21800000u, most = 0x5d800000u;      // 2^-60, 2^60
+        odd |= x[j] > 0.f && __float_as_uint(x[j]) - least > most - least;
+        q[j] = x[j] * p.inverse;
+        q[j] = fmaf(fmaf(-q[j], p.rho, x[j]), p.inverse, q[j]);
     }
-    return r;
+    if (odd) {
+#pragma unroll
+        for (int j = 0; j < E; ++j) q[j] = __fdiv_rn(x[j], p.rho);
+    }
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        const float    y = x[j] > 0.f ? q[j] : __fmul_rn(x[j], p.rho);
+        const uint32_t made = c[j] & (kPrompt<Count> - 1);
+        const float    z = __fsub_rn(__fsub_rn(y, __fmul_rn(p.frequency, (float)made)), p.presence);
+        x[j] = !c[j] ? x[j] : made ? z : y;
+    }
 }
 
 // Elements a .. b - 1 of E as bits, where these may lie outside.
@@ -504,6 +526,12 @@ template <class T> __device__ __noinline__ uint4 edge_vector(const Layer& l, int
 #pragma unroll
     for (int j = 0; j < E; ++j) e[j] = j >= a && j < b ? reinterpret_cast<const T*>(l.in)[vec * E + j] : from_float<T>(-INFINITY);
     return *reinterpret_cast<const uint4*>(e);
+}
+// The bias of a token that has one.
+__device__ __noinline__ float bias_of(const int32_t* ids, const int32_t* values, int token) {
+    uint32_t h = (uint32_t)token * 2654435761u % kHash;
+    while (ids[h] != token && ids[h] != -1) h = (h + 1) % kHash;     // the table is never full
+    return __int_as_float(values[h]);
 }
 template <int E> __device__ __forceinline__ float far_sum(const float (&x)[E], float base) {
     float r = 0.f;
@@ -524,18 +552,18 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     __shared__ uint2  masks;
     const int     tid = threadIdx.x, rank = blockIdx.x & ((1 << deal.log_c) - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
+    if (deal.log_c) cluster_arrive();              // this block runs: its shared memory may be written
     constexpr int kMaskWords = kPerLayer<TI> / 32 + 1;       // of a layer, which may begin anywhere in a word
     Layer*     table = reinterpret_cast<Layer*>(dynamic);
-    uint32_t*  words = reinterpret_cast<uint32_t*>(table + deal.mine);                       // mask words
+    uint4*     ring = reinterpret_cast<uint4*>(table + deal.mine);
+    uint32_t*  words = reinterpret_cast<uint32_t*>(ring + kRing * kVecs);                    // mask words
     uint32_t*  biased = words + (how.mask ? (deal.mine * kMaskWords + 3) / 4 * 4 : 0);        // a byte per vector
     int32_t*   hash_id = reinterpret_cast<int32_t*>(biased + (how.bias_ids ? deal.mine * kVecs / 4 : 0));
     int32_t*   hash_entry = hash_id + kHash;                  // the last entry of the id, then its value
     uint32_t*  counters = reinterpret_cast<uint32_t*>(hash_id + (how.bias_ids ? 2 * kHash : 0));
-    __shared__ float    queued[kWarps][64 * E + 32];
-    __shared__ uint16_t queued_column[kWarps][64 * E + 32];
 
-    const float rho = how.repetition ? how.repetition[row] : 1.f;
-    const float presence = how.presence ? how.presence[row] : 0.f, frequency = how.frequency ? how.frequency[row] : 0.f;
+    const Penalty penalty = penalty_of(how.repetition ? how.repetition[row] : 1.f, how.frequency ? how.frequency[row] : 0.f,
+                                       how.presence ? how.presence[row] : 0.f);
     int total = 0, prompt = 0;
     if (how.history) {
         total = how.total_len ? max(0, min((int)how.history_len, how.total_len[row])) : (int)how.history_len;
@@ -547,45 +575,39 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     const int      mask_last = (in.vocab - 1) >> 5;
 
     const int n_all = layers_of(deal, rank);
-    // The largest value of the sweep and the first vector that has it; the largest of the gathered and its id.  The sum is
-    // kept from a base that follows the maximum only when it has fallen 40 behind: its terms stay below 2^58, and most
-    // vectors leave it alone.
+    // The largest value and the first vector that has it.  The sum is kept from a base that follows the maximum only when
+    // it has fallen 40 behind: its terms stay below 2^58, and most vectors leave it alone.
     float m = -INFINITY, base = -INFINITY, base_c = 0.f, right = 1.f, sum = 0.f;
     const char* m_vector = nullptr;
     int         m_token = 0;
-    uint32_t    m_held = 0;                                  // elements of the vector that are the sweep's
-    float       m_one = -INFINITY;
-    int         m_one_token = 0x7fffffff;
+    uint32_t    m_held = 0;                                  // elements of the vector that are the row's
     auto rebase = [&](float top) {
         sum *= scale_to(base, top, kLog2e);
         base = top;
         base_c = top * kLog2e;
         right = exp2_approx(fmaf(-top, kLog2e, base_c));
     };
-    const bool  sparse = total > 0 || how.bias_ids;
-    const bool  rounds = deal.mine << deal.log_c < deal.layers;      // the counters do not fit at once
-    const bool  spread = deal.log_c && !rounds && total >= kSpread;
-    for (int first = 0; first < n_all || first == 0; first += deal.mine) {
+    for (int first = 0; first < n_all; first += deal.mine) {      // one round unless the counters do not fit
         const int n = min(deal.mine, n_all - first);
         __syncthreads();
         const uint32_t whole = fill_table<TI, TO>(table, &masks, in, out, deal, row, rank, first, n).x;
-        // this thread's two vectors of the next layer, on their way
-        auto fetch = [&](int l, uint4 (&v)[2]) {
-            if (l >= n) return;
-            if (whole >> l & 1u) {
-                const uint4* from = reinterpret_cast<const uint4*>(table[l].in) + tid;
-                v[0] = __ldcs(from);
-                v[1] = __ldcs(from + kThreads);
-            } else {
-#pragma unroll 1
-                for (int i = 0; i < 2; ++i) {
-                    const uint4 e = edge_vector<TI>(table[l], tid + i * kThreads);
-                    if (i == 0) v[0] = e; else v[1] = e;
+        // this thread's two vectors of layer l into their places in the ring
+        auto fetch = [&](int l) {
+            if (l < n) {
+                uint4* const to = ring + l % kRing * kVecs + tid;
+                if (whole >> l & 1u) {
+                    const char* from = table[l].in + tid * 16;
+                    copy_async(smem_address(to), from);
+                    copy_async(smem_address(to + kThreads), from + kThreads * 16);
+                } else {
+                    to[0] = edge_vector<TI>(table[l], tid);
+                    to[kThreads] = edge_vector<TI>(table[l], tid + kThreads);
                 }
             }
+            copy_commit();
         };
-        uint4 next[2] = {};
-        fetch(0, next);
+#pragma unroll 1
+        for (int l = 0; l < kRing; ++l) fetch(l);
         if (total > 0)
             for (int i = tid; i < n * kPerLayer<TI> * (int)sizeof(Count) / 16; i += kThreads)
                 reinterpret_cast<uint4*>(counters)[i] = make_uint4(0, 0, 0, 0);
@@ -600,26 +622,8 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
                 words[i] = w >= 0 && w <= mask_last ? (uint32_t)mask[w] : 0u;
             }
         }
-        if (deal.log_c && first == 0) cluster_arrive();      // this block runs, and its counters are zero
         __syncthreads();
-        if (spread) {
-            cluster_wait();
-            const int part = (total + (1 << deal.log_c) - 1) >> deal.log_c, end = min(total, (rank + 1) * part);
-            auto count = [&](int i, int id) {
-                if ((uint32_t)id >= (uint32_t)in.vocab) return;
-                const Place p = place_of<TI>(in, deal, row, id);
-                count_token_at<Count>(p.rank, counters, p.layer * kPerLayer<TI> + p.position, i >= prompt);
-            };
-            int i = rank * part + tid;
-            for (; i + 3 * kThreads < end; i += 4 * kThreads) {
-                int id[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) id[j] = hist[i + j * kThreads];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) count(i + j * kThreads, id[j]);
-            }
-            for (; i < end; i += kThreads) count(i, hist[i]);
-        } else {
+        {
             auto count = [&](int i, int id) {
                 if ((uint32_t)id >= (uint32_t)in.vocab) return;
                 const Place p = place_of<TI>(in, deal, row, id);
@@ -672,11 +676,6 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
             for (int j = 0; j < kMost; ++j)
                 if (last[j]) hash_entry[slot[j]] = __float_as_int(how.bias_values[row * how.bias_count + tid + j * kThreads]);
         }
-        if (spread) {
-            cluster_arrive();
-            cluster_wait();
-            cluster_arrive();                  // what the exchange at the end waits for
-        }
         __syncthreads();
 
         // bit j: element j of the vector is allowed
@@ -685,144 +684,95 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
             const int       bit = (table[l].token & 31) + vec * E;
             return __funnelshift_r(w[bit >> 5], w[min((bit >> 5) + 1, kMaskWords - 1)], bit & 31);
         };
-        // a queued column, x its element
-        float* const    queue = queued[tid >> 5];
-        uint16_t* const queue_column = queued_column[tid >> 5];
-        int             waiting = 0;
-        auto change = [&](int at) {
-            float        x = queue[at];
-            const int    column = queue_column[at], l = column / kPerLayer<TI>, p = column % kPerLayer<TI>;
+        // One layer at a time, a thread's two vectors together.
+#pragma unroll 1
+        for (int l = 0; l < n; ++l) {
+            copy_wait<kRing - 1>();
             const Layer& L = table[l];
+            float    x[2][E], top[2];
+            uint32_t held[2] = {(1u << E) - 1, (1u << E) - 1};     // elements that are the row's
+            unpack<TI>(ring[l % kRing * kVecs + tid], x[0]);
+            unpack<TI>(ring[l % kRing * kVecs + tid + kThreads], x[1]);
+            fetch(l + kRing);
+            if (!(whole >> l & 1u)) {
+                held[0] = bits_between(L.lo - tid * E, L.hi - tid * E, E);
+                held[1] = bits_between(L.lo - (tid + kThreads) * E, L.hi - (tid + kThreads) * E, E);
+            }
             if (total > 0) {
-                if (const uint32_t c = counter_of<Count>(counters, column)) {
-                    x = x > 0.f ? __fdiv_rn(x, rho) : __fmul_rn(x, rho);
-                    if (const uint32_t made = c & (kPrompt<Count> - 1))
-                        x = __fsub_rn(__fsub_rn(x, __fmul_rn(frequency, (float)made)), presence);
+                uint32_t   c0[E], c1[E];
+                const bool a = counts_of<Count>(counters, l * kPerLayer<TI> + tid * E, c0);
+                const bool b = counts_of<Count>(counters, l * kPerLayer<TI> + (tid + kThreads) * E, c1);
+                if (a || b) {
+                    penalise<Count>(x[0], c0, penalty);
+                    penalise<Count>(x[1], c1, penalty);
                 }
             }
             if (how.bias_ids) {
-                // the table is never full: an empty slot ends the search for a token without a bias
-                uint32_t h = (uint32_t)(L.token + p) * 2654435761u % kHash;
-                while (hash_id[h] != L.token + p && hash_id[h] != -1) h = (h + 1) % kHash;
-                if (hash_id[h] != -1) x = __fadd_rn(x, __int_as_float(hash_entry[h]));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int      vec = tid + i * kThreads;
+                    const uint32_t f = reinterpret_cast<const uint8_t*>(biased)[l * kVecs + vec];
+                    if (f) {
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+                            if (f >> j & 1u) x[i][j] = __fadd_rn(x[i][j], bias_of(hash_id, hash_entry, L.token + vec * E + j));
+                    }
+                }
             }
-            if (mask && !(allowed(l, p / E) >> (p % E) & 1u)) x = -INFINITY;
-            const TO y = from_float<TO>(x);
-            reinterpret_cast<TO*>(L.out)[p] = y;
-            x = to_float(y);
-            if (x > m_one || (x == m_one && x > -INFINITY && L.token + p < m_one_token)) { m_one = x; m_one_token = L.token + p; }
-            if (x > base + 40.f) rebase(x);
-            sum += is_far(base_c) ? scale_to(x, base, kLog2e) : exp2_approx(fmaf(x, kLog2e, -base_c)) * right;
-        };
-
-        // One layer at a time, a thread's two vectors together; after the last the rest of the queue.
-#pragma unroll 1
-        for (int l = 0; l <= n; ++l) {
-            if (l < n) {
-                const uint4 v[2] = {next[0], next[1]};
-                fetch(l + 1, next);
-                const Layer& L = table[l];
-                float    x[2][E], top[2];
-                uint32_t held[2], other[2] = {0, 0};      // elements that the sweep writes; that the queue takes
-                const bool edge = !(whole >> l & 1u);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int vec = tid + i * kThreads;
-                    unpack<TI>(v[i], x[i]);
-                    held[i] = (1u << E) - 1;
-                    if (edge) held[i] = bits_between(L.lo - vec * E, L.hi - vec * E, E);
-                    if (sparse) {
-                        if (how.bias_ids) other[i] = reinterpret_cast<const uint8_t*>(biased)[l * kVecs + vec];
-                        if (total > 0) other[i] |= counted<Count, E>(counters, l * kPerLayer<TI> + vec * E);
-                        held[i] &= ~other[i];
-                    }
+            for (int i = 0; i < 2; ++i) {
+                const int vec = tid + i * kThreads;
+                if (mask) {
+                    const uint32_t f = allowed(l, vec);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) x[i][j] = f >> j & 1u ? x[i][j] : -INFINITY;
                 }
-                if (sparse && __any_sync(0xffffffffu, other[0] | other[1])) {
-                    // into the queue by lane and element, always in the same order: so that the sums come out alike
-                    int upto = __popc(other[0]) + __popc(other[1]), at = waiting - upto;
+                // written, and from here on what was written
+                TO y[E];
 #pragma unroll
-                    for (int o = 1; o < 32; o *= 2) {
-                        const int below = __shfl_up_sync(0xffffffffu, upto, o);
-                        if ((tid & 31) >= o) upto += below;
-                    }
-                    at += upto;
-                    waiting += __shfl_sync(0xffffffffu, upto, 31);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (other[i]) {
-#pragma unroll
-                            for (int j = 0; j < E; ++j)
-                                if (other[i] >> j & 1u) {
-                                    queue[at] = x[i][j];
-                                    queue_column[at++] = (uint16_t)(l * kPerLayer<TI> + (tid + i * kThreads) * E + j);
-                                }
-                        }
-                    __syncwarp();
+                for (int j = 0; j < E; ++j) {
+                    y[j] = from_float<TO>(x[i][j]);
+                    x[i][j] = to_float(y[j]);
                 }
+                char* const o = L.out + vec * E * (int)sizeof(TO);
+                if (L.vec_out && held[i] == (1u << E) - 1) {
+                    const uint4* w = reinterpret_cast<const uint4*>(y);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int vec = tid + i * kThreads;
-                    if (mask) {
-                        const uint32_t f = allowed(l, vec);
-#pragma unroll
-                        for (int j = 0; j < E; ++j) x[i][j] = f >> j & 1u ? x[i][j] : -INFINITY;
-                    }
-                    // written, and from here on what was written
-                    TO y[E];
+                    for (int j = 0; j < E * (int)sizeof(TO) / 16; ++j) __stcs(reinterpret_cast<uint4*>(o) + j, w[j]);
+                } else {
 #pragma unroll
                     for (int j = 0; j < E; ++j) {
-                        y[j] = from_float<TO>(x[i][j]);
-                        x[i][j] = to_float(y[j]);
+                        if (held[i] >> j & 1u) reinterpret_cast<TO*>(o)[j] = y[j];
+                        else x[i][j] = -INFINITY;
                     }
-                    char* const o = L.out + vec * E * (int)sizeof(TO);
-                    if (L.vec_out && held[i] == (1u << E) - 1) {
-                        const uint4* w = reinterpret_cast<const uint4*>(y);
-#pragma unroll
-                        for (int j = 0; j < E * (int)sizeof(TO) / 16; ++j) __stcs(reinterpret_cast<uint4*>(o) + j, w[j]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < E; ++j) {
-                            if (held[i] >> j & 1u) reinterpret_cast<TO*>(o)[j] = y[j];
-                            else x[i][j] = -INFINITY;
-                        }
-                    }
-                    top[i] = x[i][0];
-#pragma unroll
-                    for (int j = 1; j < E; ++j) top[i] = fmaxf(top[i], x[i][j]);
                 }
-                const float most = fmaxf(top[0], top[1]);
-                if (most > m) {
-                    m = most;
-                    const int vec = top[0] == most ? tid : tid + kThreads;
-                    m_vector = L.out + vec * E * (int)sizeof(TO);
-                    m_token = L.token + vec * E;
-                    m_held = top[0] == most ? held[0] : held[1];
-                }
-                if (most > base + 40.f) rebase(most);
-                if (is_far(base_c)) {
-                    sum += far_sum(x[0], base) + far_sum(x[1], base);
-                } else {
-                    Pair part[2] = {0, 0};
-                    const Pair c = pair(kLog2e, kLog2e), minus = pair(-base_c, -base_c);
+                top[i] = x[i][0];
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < E; j += 2) part[i] = add2(part[i], exp2_pair(fma2(pair(x[i][j], x[i][j + 1]), c, minus)));
-                    const float2 h = halves(add2(part[0], part[1]));
-                    sum = fmaf(h.x + h.y, right, sum);
-                }
+                for (int j = 1; j < E; ++j) top[i] = fmaxf(top[i], x[i][j]);
             }
-#pragma unroll 1
-            for (const int least = l < n ? 32 : 1; waiting >= least;) {
-                const int now = min(waiting, 32);
-                waiting -= now;
-                if ((tid & 31) < now) change(waiting + (tid & 31));
+            const float most = fmaxf(top[0], top[1]);
+            if (most > m) {
+                m = most;
+                const int vec = top[0] == most ? tid : tid + kThreads;
+                m_vector = L.out + vec * E * (int)sizeof(TO);
+                m_token = L.token + vec * E;
+                m_held = top[0] == most ? held[0] : held[1];
             }
-            __syncwarp();
+            if (most > base + 40.f) rebase(most);
+            if (is_far(base_c)) {
+                sum += far_sum(x[0], base) + far_sum(x[1], base);
+            } else {
+                Pair part[2] = {0, 0};
+                const Pair c = pair(kLog2e, kLog2e), minus = pair(-base_c, -base_c);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < E; j += 2) part[i] = add2(part[i], exp2_pair(fma2(pair(x[i][j], x[i][j + 1]), c, minus)));
+                const float2 h = halves(add2(part[0], part[1]));
+                sum = fmaf(h.x + h.y, right, sum);
+            }
         }
     }
-    const float m_sweep = m;
-    m = fmaxf(m, m_one);
     sum *= scale_to(base, m, kLog2e);
 
     // the warp's result, the block's on its first warp, and the cluster's on its first block
@@ -832,11 +782,11 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     };
     float2 v = warp_join(make_float2(m, sum));
     // the lowest id of the maximum: only the threads that have it read their vector back
-    int at = m_one == v.x ? m_one_token : 0x7fffffff;
-    if (m_sweep == v.x && m_vector) {
+    int at = 0x7fffffff;
+    if (m == v.x && m_vector) {
 #pragma unroll 1
         for (int j = E - 1; j >= 0; --j)
-            if ((m_held >> j & 1u) && to_float(reinterpret_cast<const TO*>(m_vector)[j]) == v.x) at = min(at, m_token + j);
+            if ((m_held >> j & 1u) && to_float(reinterpret_cast<const TO*>(m_vector)[j]) == v.x) at = m_token + j;
     }
     at = (int)__reduce_min_sync(0xffffffffu, (uint32_t)at);
     const int lane = tid & 31;
@@ -1414,7 +1364,7 @@ int device_of(Device* d) {
     if (!d->smem) {
         int most = 0;
         NEREUS_CUDA(cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, d->id));
-        d->smem = most - 28672;                                   // 28 KiB: the kernels' static part
+        d->smem = most - 16384;                                   // 16 KiB: the kernels' static part
         smem[d->id].store(d->smem);
     }
     return NEREUS_OK;
@@ -1500,7 +1450,7 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
                               (how.bias_ids ? kVecs : 0) + (how.mask ? (kPerLayer<TI> / 32 + 1) * 4 : 0);
-    const int64_t fixed = (how.bias_ids ? 2 * kHash * 4 : 0) + 16;
+    const int64_t fixed = (how.bias_ids ? 2 * kHash * 4 : 0) + 16 + kRing * kVecs * 16;
     Deal d = deal_of(in, per_layer, fixed, 4);
     // what does not fit is done in rounds
     while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
