@@ -823,14 +823,12 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
 
 // ---- a teacher's top logits ----------------------------------------------------------------------------------
 //
-// Every thread knows the largest of its own elements after the pass that also sums the exponentials.  The k-th largest
-// of a block's 512 such maxima bounds the block's k-th largest element from below, whatever the order of the row, and
-// few elements reach it (those of the k threads, and what else of theirs does); only the threads whose maximum reaches
-// it look through their elements again, in shared memory.  What they find is ranked by counting, (value, lower id)
-// as one 64-bit key, and the blocks' lists are joined by binary search.  Rows with so many equal values that the list
-// would overflow take an exact search for the k-th key and the id to cut at.
-
-constexpr int kCandidates = 1024;
+// Every thread knows the largest of its own elements when the row has arrived.  If each of W warps takes the j-th largest
+// of its 32 such maxima, j = k / W rounded up, at least k elements reach the least of these W values, whatever the order of
+// the row: it bounds the row's k-th largest from below, and for most rows some 1.5 k elements reach it.  The threads whose
+// maximum does look through their elements in shared memory once more, what they find goes to the cluster's first block,
+// as one 64-bit key of (value, lower id), and is ranked there by counting.  A block that finds more than it may send (rows
+// of few distinct values) searches its share for its k-th key and the id to cut at, exactly.
 
 // orders as the values do, -0 as +0; NaN below everything
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -842,6 +840,7 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 constexpr uint32_t kKeyMinusInf = 0x007fffffu;
+__host__ __device__ constexpr int list_of(int log_c) { return log_c < 2 ? 512 : 256; }     // keys a block may send
 
 __device__ __forceinline__ int block_count(int v, int* scratch) {
     v = __reduce_add_sync(0xffffffffu, v);
@@ -854,169 +853,184 @@ __device__ __forceinline__ int block_count(int v, int* scratch) {
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, float inv_t,
-                                                       float* values, int32_t* ids, float* lse) {
+__global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, int j,
+                                                          float inv_t, float* values, int32_t* ids, float* lse) {
     constexpr int E = kPerVec<T>;
+    typedef unsigned long long Key;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2 scratch[kWarps];
-    __shared__ int    count_scratch[kWarps];
-    __shared__ unsigned long long found[kCandidates];
-    __shared__ unsigned long long best[NEREUS_TOP_MAX_K];          // the block's own, falling, 0 where there are fewer
-    __shared__ float2 stats;                                       // (maximum, sum) of the block
-    __shared__ int    n_found;
-    const int     tid = threadIdx.x, ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
+    __shared__ float2   scratch[kWarps], from_peers[kMaxCtas];
+    __shared__ uint32_t least[kWarps], least_of_peers[kMaxCtas];
+    __shared__ int      count_scratch[kWarps], counts[kMaxCtas], n_found;
+    __shared__ uint2    masks;
+    const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
-    const int     n = layers_of(deal, rank), quarter = (n + 3) / 4;
+    const int     n = layers_of(deal, rank), quarter = (n + 3) / 4, most = list_of(deal.log_c);
     const float   c = inv_t * kLog2e;
+    if (deal.log_c) cluster_arrive();              // this block runs: its shared memory may be written
 
     Layer* table = reinterpret_cast<Layer*>(dynamic);
     uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    __shared__ uint2 masks;
+    Key*   lists = reinterpret_cast<Key*>(slots + deal.mine * kVecs);     // the first block's: `most` keys of each block
     if (tid == 0) n_found = 0;
-    if (tid < k) best[tid] = 0;
     const uint32_t whole = fill_table<T, T>(table, &masks, in, LogitsCut(), deal, row, rank, 0, n).x;
     load_share<T>(table, slots, whole, n, quarter);
 
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;
+    bool has0 = false, has1 = false;
     on_arrival<T>(table, slots, whole, n, quarter,
-                  [&](int, int vec, uint4 v) { if (vec < kThreads) m0 = Vec<T>::max(m0, v); else m1 = Vec<T>::max(m1, v); },
+                  [&](int, int vec, uint4 v) {
+                      if (vec < kThreads) { m0 = Vec<T>::max(m0, v); has0 = true; }
+                      else { m1 = Vec<T>::max(m1, v); has1 = true; }
+                  },
                   [&](int, const auto& v) {
+                      has0 = has1 = true;
 #pragma unroll
-                      for (int j = 0; j < v.n; j += 2) {
-                          m0 = Vec<T>::max(m0, v.v[j]);
-                          m1 = Vec<T>::max(m1, v.v[j + 1]);
+                      for (int i = 0; i < v.n; i += 2) {
+                          m0 = Vec<T>::max(m0, v.v[i]);
+                          m1 = Vec<T>::max(m1, v.v[i + 1]);
                       }
                   });
     const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1), m = fmaxf(f0, f1), m_warp = warp_max(m);
-    float sum = exp_sums<T>(table, slots, whole, n, base_of(m_warp, c));
-    sum = warp_sum(sum);
-    if ((tid & 31) == 0) scratch[tid >> 5] = make_float2(m_warp, sum);
 
-    // the k-th largest of the threads' maxima (of both halves of each for a large k), to 16 bits from below
-    const bool     two = k > 96;
-    const uint32_t key0 = key_of(two ? f0 : m), key1 = key_of(f1);
-    uint32_t       t = 0;
+    // the warp's j-th largest maximum (of both halves of each thread's elements where j is large), to 16 bits from below;
+    // a warp in which a lane has no element does not take part
+    {
+        const bool     full = __all_sync(0xffffffffu, has0 || has1), two = j > 8 && __all_sync(0xffffffffu, has0 && has1);
+        const uint32_t key0 = key_of(two ? f0 : m), key1 = two ? key_of(f1) : 0;
+        uint32_t       t = 0;
 #pragma unroll 1
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t u = t | 1u << bit;
-        int reach = __syncthreads_count(key0 >= u);
-        if (two) reach += __syncthreads_count(key1 >= u);
-        if (reach >= k) t = u;
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t u = t | 1u << bit;
+            int reach = __popc(__ballot_sync(0xffffffffu, key0 >= u));
+            if (two) reach += __popc(__ballot_sync(0xffffffffu, key1 >= u));
+            if (reach >= j) t = u;
+        }
+        if (lane == 0) least[warp] = full ? max(t, kKeyMinusInf) : 0xffffffffu;
     }
-    t = max(t, kKeyMinusInf);
-    const float bound = value_of(t);
-    // every element of this thread's share that reaches `least` (so is not NaN): f(key, token)
-    auto each = [&](float least, auto f) {
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-            const Layer& L = table[i];
-#pragma unroll 1
-            for (int vec = tid; vec < kVecs; vec += kThreads) {
-                const int p0 = vec * E;
-                if (p0 >= L.hi || p0 + E <= L.lo) continue;
-                const uint4 v = slots[i * kVecs + vec];
-                if (!(Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), v)) >= least)) continue;
-                float x[E];
-                unpack<T>(v, x);
+    const float sum = warp_sum(exp_sums<T>(table, slots, whole, n, base_of(m_warp, c)));
+    if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
+    __syncthreads();
+
+    // the least over the cluster for everyone, the joined sums for the first block
+    if (deal.log_c) cluster_wait();
+    if (warp == 0) {
+        const float2   mine = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
+        const uint32_t low = __reduce_min_sync(0xffffffffu, lane < kWarps ? least[lane] : 0xffffffffu);
+        const float    top = warp_max(mine.x), all = warp_sum(mine.y * scale_to(mine.x, top, c));
+        if (lane < ctas) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&least_of_peers[rank], lane)), "r"(low) : "memory");
+        if (lane == 0) peer_store(peer_address(&from_peers[rank], 0), top, all);
+    }
+    if (deal.log_c) {
+        __syncwarp();
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    uint32_t low = least_of_peers[0];
+    for (int i = 1; i < ctas; ++i) low = min(low, least_of_peers[i]);
+    // no warp is full in rows of less than 32 vectors: everything is sent
+    const float bound = low == 0xffffffffu || j > 64 ? -INFINITY : value_of(low);
+
+    // every element of a vector of this thread that reaches `bar` (so is not NaN): f(key, token)
+    auto look = [&](int i, int vec, float bar, auto f) {
+        const Layer& L = table[i];
+        const int    a = L.lo - vec * E, b = L.hi - vec * E;
+        if (b <= 0 || a >= E) return;
+        float x[E];
+        unpack<T>(slots[i * kVecs + vec], x);
+        uint32_t hits = 0;
 #pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (x[j] >= least && p0 + j >= L.lo && p0 + j < L.hi) f(key_of(x[j]), L.token + p0 + j);
-            }
+        for (int e = 0; e < E; ++e) hits |= (x[e] >= bar && e >= a && e < b ? 1u : 0u) << e;
+        for (; hits; hits &= hits - 1) {
+            const int e = __ffs(hits) - 1;
+            f(key_of(to_float(reinterpret_cast<const T*>(slots + i * kVecs + vec)[e])), L.token + vec * E + e);
         }
     };
-    auto push = [&](uint32_t kk, int v) {
+    const uint32_t list = peer_address(lists + rank * most, 0);
+    auto push = [&](uint32_t key, int v) {
         const int i = atomicAdd(&n_found, 1);
-        if (i < kCandidates) found[i] = (unsigned long long)kk << 32 | (0xffffffffu - (uint32_t)v);
+        if (i < most)
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + i * 8), "l"((Key)key << 32 | (0xffffffffu - (uint32_t)v)) : "memory");
     };
-    if (m >= bound) each(bound, push);
-    __syncthreads();
-    float2 v;
-    if (tid == 0) {
-        v = scratch[0];
-        for (int i = 1; i < kWarps; ++i) v = join(v, scratch[i], c);
-        stats = v;
+    if (m >= bound) {
+        uint32_t hits[2] = {0, 0};               // bit i: the thread's first / second vector of layer i
+        for (int i = 0; i < n; ++i) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                hits[h] |= (Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), slots[i * kVecs + tid + h * kThreads])) >= bound ? 1u : 0u) << i;
+        }
+#pragma unroll 1
+        while (hits[0] | hits[1]) {
+            const int h = hits[0] ? 0 : 1, i = __ffs(h ? hits[1] : hits[0]) - 1;
+            if (h) hits[1] &= hits[1] - 1; else hits[0] &= hits[0] - 1;
+            look(i, tid + h * kThreads, bound, push);
+        }
     }
-    if (n_found > kCandidates) {
+    __syncthreads();
+    if (n_found > most) {
+        auto each = [&](auto f) {
+#pragma unroll 1
+            for (int i = 0; i < n; ++i)
+#pragma unroll 1
+                for (int vec = tid; vec < kVecs; vec += kThreads) look(i, vec, -INFINITY, f);
+        };
         uint32_t kth = 0;                      // the largest key that k elements reach, 0 if there are fewer
 #pragma unroll 1
         for (int bit = 31; bit >= 0; --bit) {
             int reach = 0;
-            each(-INFINITY, [&](uint32_t kk, int) { reach += kk >= (kth | 1u << bit); });
+            each([&](uint32_t key, int) { reach += key >= (kth | 1u << bit); });
             if (block_count(reach, count_scratch) >= k) kth |= 1u << bit;
         }
         int above = 0;
-        each(-INFINITY, [&](uint32_t kk, int) { above += kk > kth; });
+        each([&](uint32_t key, int) { above += key > kth; });
         above = block_count(above, count_scratch);
         int before = -1;                       // the largest id up to which fewer than k are taken
 #pragma unroll 1
         for (int bit = 23; bit >= 0; --bit) {
             int reach = 0;
-            each(-INFINITY, [&](uint32_t kk, int id) { reach += kk == kth && id <= before + (1 << bit); });
+            each([&](uint32_t key, int id) { reach += key == kth && id <= before + (1 << bit); });
             if (above + block_count(reach, count_scratch) < k) before += 1 << bit;
         }
         if (tid == 0) n_found = 0;
         __syncthreads();
-        each(-INFINITY, [&](uint32_t kk, int id) { if (kk > kth || (kk == kth && id <= before + 1)) push(kk, id); });
+        each([&](uint32_t key, int id) { if (key > kth || (key == kth && id <= before + 1)) push(key, id); });
         __syncthreads();
     }
-    const int n_list = n_found;
-    for (int i = tid; i < n_list; i += kThreads) {
-        const unsigned long long mine = found[i];
-        int place = 0;
-        for (int j = 0; j < n_list; ++j) place += found[j] > mine;
-        if (place < k) best[place] = mine;
-    }
-    __syncthreads();
-
-    unsigned long long mine = tid < k ? best[tid] : 0;
-    int  place = tid;
+    if (tid == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&counts[rank], 0)), "r"(n_found) : "memory");
     if (deal.log_c) {
-        // the lists of all blocks, side by side where the row was: nothing reads its elements any more
-        unsigned long long* lists = reinterpret_cast<unsigned long long*>(slots);
+        __syncwarp();
         cluster_arrive();
+        if (rank) return;
         cluster_wait();
-        for (int i = tid; i < ctas * k; i += kThreads) lists[i] = peer_load64(peer_address(&best[i % k], i / k));
-        if (tid < ctas) {
-            const unsigned long long w = peer_load64(peer_address(&stats, tid));
-            scratch[tid] = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
-        }
-        cluster_arrive();
+    } else {
         __syncthreads();
-        if (mine)
-            for (int r = 0; r < ctas; ++r) {
-                if (r == rank) continue;
-                int lo = 0, hi = k;            // how many of list r are larger
-                while (lo < hi) {
-                    const int mid = (lo + hi) / 2;
-                    if (lists[r * k + mid] > mine) lo = mid + 1; else hi = mid;
-                }
-                place += lo;
-            }
     }
-    if (mine && place < k) {
-        values[row * k + place] = value_of((uint32_t)(mine >> 32));
-        ids[row * k + place] = (int32_t)(0xffffffffu - (uint32_t)mine);
-    }
-    if (rank == 0) {
-        // places that no element takes
-        int have = mine != 0;
-        if (deal.log_c) {
-            have = 0;
-            const unsigned long long* lists = reinterpret_cast<const unsigned long long*>(slots);
-            for (int i = tid; i < ctas * k; i += kThreads) have += lists[i] != 0;
+
+    int total = 0;
+    for (int i = 0; i < ctas; ++i) total += counts[i];
+    for (int e = tid; e < total; e += kThreads) {
+        int from = 0, at = e;
+        while (at >= counts[from]) at -= counts[from++];
+        const Key mine = lists[from * most + at];
+        int place = 0;
+        for (int i = 0; i < ctas; ++i) {
+            const Key* of = lists + i * most;
+            const int  count = counts[i];
+#pragma unroll 4
+            for (int q = 0; q < count; ++q) place += of[q] > mine;
         }
-        have = block_count(have, count_scratch);
-        if (tid >= have && tid < k) { values[row * k + tid] = -INFINITY; ids[row * k + tid] = -1; }
-        if (tid == 0) {
-            v = stats;
-            if (deal.log_c) {
-                v = scratch[0];
-                for (int i = 1; i < ctas; ++i) v = join(v, scratch[i], c);
-            }
-            lse[row] = log_sum(v.x, v.x * inv_t, v.y);
+        if (place < k) {
+            values[row * k + place] = value_of((uint32_t)(mine >> 32));
+            ids[row * k + place] = (int32_t)(0xffffffffu - (uint32_t)mine);
         }
     }
-    if (deal.log_c) cluster_wait();            // the peers have read this block's list
+    if (tid >= total && tid < k) { values[row * k + tid] = -INFINITY; ids[row * k + tid] = -1; }      // no element is left
+    if (warp == 0) {
+        const float2 mine = lane < ctas ? from_peers[lane] : make_float2(-INFINITY, 0.f);
+        const float  top = warp_max(mine.x), all = warp_sum(mine.y * scale_to(mine.x, top, c));
+        if (lane == 0) lse[row] = log_sum(top, top * inv_t, all);
+    }
 }
 
 // ---- distillation --------------------------------------------------------------------------------------------
@@ -1465,10 +1479,21 @@ int top_launch(const nereus_logits_t& in, int k, float temperature, float* value
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + kVecs * 16;
     const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
-    // the slots also take the lists of all blocks of the cluster
-    const int64_t lists = d.log_c ? ((int64_t)k << d.log_c) * 8 + d.mine * (int64_t)sizeof(Layer) : 0;
-    return launch(top_kernel<T>, opted, in.rows, d, std::max(d.mine * per_layer, lists), dev, stream, cut_of(in),
-                  d, k, 1.f / temperature, values, ids, lse);
+    // warps of which every lane has a vector, at least: how many of the k largest each has to vouch for
+    const int64_t w = held_cols(in, 0), e = kPerVec<T>, last = (in.vocab - 1) / in.shard_cols;
+    int full = 0;
+    for (int rank = 0; rank < 1 << d.log_c; ++rank) {
+        int64_t lanes = 0;
+        for (int l = rank; l < d.layers; l += 1 << d.log_c) {
+            const int64_t cols = l / d.per_shard == last ? in.vocab - last * in.shard_cols : w;
+            lanes = std::max(lanes, (cols + e - 1) / e - (int64_t)(l % d.per_shard) * kVecs);
+        }
+        full += (int)std::min<int64_t>(std::max<int64_t>(lanes, 0) / 32, kWarps);
+    }
+    const int     j = full ? (k + full - 1) / full : 1;
+    const int64_t lists = ((int64_t)list_of(d.log_c) << d.log_c) * 8;
+    return launch(top_kernel<T>, opted, in.rows, d, d.mine * per_layer + lists, dev, stream, cut_of(in), d, k, j,
+                  1.f / temperature, values, ids, lse);
 }
 
 }  // namespace
