@@ -222,11 +222,6 @@ __device__ __forceinline__ uint32_t peer_address(const void* p, int rank) {
 __device__ __forceinline__ void peer_store(uint32_t at, float a, float b) {
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(a), "f"(b) : "memory");
 }
-__device__ __forceinline__ unsigned long long peer_load64(uint32_t at) {
-    unsigned long long v;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
-    return v;
-}
 __device__ __forceinline__ float warp_max(float v) {                 // NaN is passed over
     float r;
     asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -288,35 +283,33 @@ __device__ __forceinline__ void sweep(const Layer* table, const uint4* slots, ui
         ++i;
     }
 }
-// Starts the copies of the block's share into its slots, in four commit groups of `quarter` layers.
+// Starts the copies of layers [a, b) of the block's share into its slots, one commit group.  Every thread copies what it
+// reads back itself, so that it may do this as soon as it has no more use for the slots' old contents.
 template <class T>
-__device__ __forceinline__ void load_share(const Layer* table, uint4* slots, uint32_t whole, int n, int quarter) {
+__device__ __forceinline__ void load_layers(const Layer* table, uint4* slots, uint32_t whole, int a, int b) {
     const int      t = threadIdx.x;
     const uint32_t to = smem_address(slots + t);
     bool           part = false;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
 #pragma unroll 2
-        for (int i = g * quarter; i < min(n, (g + 1) * quarter); ++i) {
-            const char* from = table[i].in + t * 16;
-            if (whole >> i & 1u) {
-                copy_async(to + i * (kVecs * 16), from);
-                copy_async(to + i * (kVecs * 16) + kThreads * 16, from + kThreads * 16);
-            } else {
-                const int lo = table[i].lo, hi = table[i].hi;
+    for (int i = a; i < b; ++i) {
+        const char* from = table[i].in + t * 16;
+        if (whole >> i & 1u) {
+            copy_async(to + i * (kVecs * 16), from);
+            copy_async(to + i * (kVecs * 16) + kThreads * 16, from + kThreads * 16);
+        } else {
+            const int lo = table[i].lo, hi = table[i].hi;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int p = (t + h * kThreads) * kPerVec<T>;
-                    if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + i * (kVecs * 16) + h * kThreads * 16, from + h * kThreads * 16);
-                    else part |= p < hi && p + kPerVec<T> > lo;
-                }
+            for (int h = 0; h < 2; ++h) {
+                const int p = (t + h * kThreads) * kPerVec<T>;
+                if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + i * (kVecs * 16) + h * kThreads * 16, from + h * kThreads * 16);
+                else part |= p < hi && p + kPerVec<T> > lo;
             }
         }
-        copy_commit();
     }
+    copy_commit();
     if (part) {                               // vectors that the row fills in part: its ends
 #pragma unroll 1
-        for (int i = 0; i < n; ++i) {
+        for (int i = a; i < b; ++i) {
             if (whole >> i & 1u) continue;
             for_edges<T>(table, i, [&](int, int v) {
                 const int lo = table[i].lo, hi = table[i].hi, p = v * kPerVec<T>;
@@ -331,6 +324,12 @@ __device__ __forceinline__ void load_share(const Layer* table, uint4* slots, uin
         }
     }
 }
+// ... the whole share, in four commit groups of `quarter` layers
+template <class T>
+__device__ __forceinline__ void load_share(const Layer* table, uint4* slots, uint32_t whole, int n, int quarter) {
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) load_layers<T>(table, slots, whole, min(n, q * quarter), min(n, (q + 1) * quarter));
+}
 
 // sweep over the block's share, in the order of arrival.
 template <class T, class F, class G>
@@ -341,7 +340,7 @@ __device__ __forceinline__ void on_arrival(const Layer* table, const uint4* slot
         else if (q == 1) copy_wait<2>();
         else if (q == 2) copy_wait<1>();
         else copy_wait<0>();
-        sweep<T>(table, slots, whole, q * quarter, min(n, (q + 1) * quarter), f, g);
+        sweep<T>(table, slots, whole, min(n, q * quarter), min(n, (q + 1) * quarter), f, g);
     }
 }
 
@@ -821,14 +820,83 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     }
 }
 
+// ---- rows that are read once ---------------------------------------------------------------------------------
+//
+// Where nothing is written per element the row need not stay on the chip: one block takes a whole row, its layers through
+// a ring in shared memory, several blocks on an SM.
+
+constexpr int kStreamRing = 3;            // layers on their way to a block
+
+// Fills a table of any number of layers.  Ends in a barrier.
+template <class T>
+__device__ __forceinline__ void fill_long_table(Layer* table, const LogitsCut& in, const Deal& d, int64_t row) {
+    for (int i = threadIdx.x; i < d.layers; i += kThreads) table[i] = layer_of<T, T>(in, LogitsCut(), d, row, 0, i);
+    __syncthreads();
+}
+// Starts the copies of this thread's two vectors of layer l, one commit group; nothing but the group past the last layer.
+template <class T>
+__device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int l, int n) {
+    if (l < n) {
+        uint4* const to = ring + l % kStreamRing * kVecs + threadIdx.x;
+        const Layer& L = table[l];
+        if (L.hi - L.lo == kPerLayer<T>) {
+            const char* from = L.in + threadIdx.x * 16;
+            copy_async(smem_address(to), from);
+            copy_async(smem_address(to + kThreads), from + kThreads * 16);
+        } else {
+            to[0] = edge_vector<T>(L, threadIdx.x);
+            to[kThreads] = edge_vector<T>(L, threadIdx.x + kThreads);
+        }
+    }
+    copy_commit();
+}
+
+// A running sum of exponentials: (base, sum of 2^((x - base) c)) whose base follows the maximum only when that has gone
+// 2^40 ahead: terms stay below 2^41 and most vectors leave it alone.  c = log2(e) / T; see Base for the arithmetic.
+struct Running {
+    float base, base_c, right, ahead, sum;
+    Pair  c, minus;
+    __device__ __forceinline__ explicit Running(float scale) {
+        c = pair(scale, scale);
+        base = -INFINITY;
+        ahead = -INFINITY;
+        base_c = sum = 0.f;
+        right = 1.f;
+        minus = pair(-0.f, -0.f);
+    }
+    // before the elements whose maximum is `top` are added
+    __device__ __forceinline__ void see(float top) {
+        if (top > ahead) {
+            const float scale = halves(c).x;
+            sum *= scale_to(base, top, scale);
+            base = top;
+            base_c = top * scale;
+            right = exp2_approx(fmaf(-top, scale, base_c));
+            minus = pair(-base_c, -base_c);
+            ahead = top + 40.f / scale;
+        }
+    }
+    template <class T> __device__ __forceinline__ void add(uint4 a, uint4 b) {
+        if (is_far(base_c)) {
+            sum += exp_sum_far<T>(a, base, halves(c).x) + exp_sum_far<T>(b, base, halves(c).x);
+        } else {
+            const Base  at = {c, minus, base, right, false};
+            const float2 h = halves(add2(exp_sum<T>(0, a, at), exp_sum<T>(0, b, at)));
+            sum = fmaf(h.x + h.y, right, sum);
+        }
+    }
+};
+
 // ---- a teacher's top logits ----------------------------------------------------------------------------------
 //
-// Every thread knows the largest of its own elements when the row has arrived.  If each of W warps takes the j-th largest
-// of its 32 such maxima, j = k / W rounded up, at least k elements reach the least of these W values, whatever the order of
-// the row: it bounds the row's k-th largest from below, and for most rows some 1.5 k elements reach it.  The threads whose
-// maximum does look through their elements in shared memory once more, what they find goes to the cluster's first block,
-// as one 64-bit key of (value, lower id), and is ranked there by counting.  A block that finds more than it may send (rows
-// of few distinct values) searches its share for its k-th key and the id to cut at, exactly.
+// One pass over the row sums the exponentials and notes the largest of every 16 (fp32: 8) elements, a thread's two vectors
+// of a layer, in two bytes (fp32 rounded up).  If each of the 8 warps takes the j-th largest of its threads' maxima, j =
+// k / 8 rounded up, at least k elements reach the least of these 8 values, whatever the order of the row: it bounds the
+// row's k-th largest from below, and for most rows some 1.4 k elements reach it.  Only the vectors whose note does are read
+// again, and what is found in them is ranked by counting, as one 64-bit key of (value, lower id).  Rows of so few distinct
+// values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly.
+
+constexpr int kCandidates = 1024;
 
 // orders as the values do, -0 as +0; NaN below everything
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -840,7 +908,13 @@ __device__ __forceinline__ float value_of(uint32_t key) {
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 constexpr uint32_t kKeyMinusInf = 0x007fffffu;
-__host__ __device__ constexpr int list_of(int log_c) { return log_c < 2 ? 512 : 256; }     // keys a block may send
+
+// A note: the upper half of a float that is not below x, ordered by its value as a float.
+__device__ __forceinline__ uint16_t note_of(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return (uint16_t)((u >> 16) + ((u & 0xffffu) && !(u >> 31) ? 1u : 0u));       // a negative one is cut towards 0: up
+}
+__device__ __forceinline__ float value_of_note(uint16_t n) { return __uint_as_float((uint32_t)n << 16); }
 
 __device__ __forceinline__ int block_count(int v, int* scratch) {
     v = __reduce_add_sync(0xffffffffu, v);
@@ -853,47 +927,50 @@ __device__ __forceinline__ int block_count(int v, int* scratch) {
 }
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, int j,
+__global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant__ LogitsCut in, Deal deal, int k, int j,
                                                           float inv_t, float* values, int32_t* ids, float* lse) {
     constexpr int E = kPerVec<T>;
     typedef unsigned long long Key;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2   scratch[kWarps], from_peers[kMaxCtas];
-    __shared__ uint32_t least[kWarps], least_of_peers[kMaxCtas];
-    __shared__ int      count_scratch[kWarps], counts[kMaxCtas], n_found;
-    __shared__ uint2    masks;
-    const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
-    const int64_t row = blockIdx.x >> deal.log_c;
-    const int     n = layers_of(deal, rank), quarter = (n + 3) / 4, most = list_of(deal.log_c);
+    __shared__ float2   scratch[kWarps];
+    __shared__ uint32_t least[kWarps];
+    __shared__ int      count_scratch[kWarps], n_found, n_pairs;
+    __shared__ __align__(16) Key found[kCandidates];
+    const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers;
+    const int64_t row = blockIdx.x;
     const float   c = inv_t * kLog2e;
-    if (deal.log_c) cluster_arrive();              // this block runs: its shared memory may be written
 
-    Layer* table = reinterpret_cast<Layer*>(dynamic);
-    uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    Key*   lists = reinterpret_cast<Key*>(slots + deal.mine * kVecs);     // the first block's: `most` keys of each block
-    if (tid == 0) n_found = 0;
-    const uint32_t whole = fill_table<T, T>(table, &masks, in, LogitsCut(), deal, row, rank, 0, n).x;
-    load_share<T>(table, slots, whole, n, quarter);
+    uint4*    ring = reinterpret_cast<uint4*>(dynamic);
+    Layer*    table = reinterpret_cast<Layer*>(ring + kStreamRing * kVecs);
+    uint16_t* notes = reinterpret_cast<uint16_t*>(table + n) + tid;          // of this thread, layer by layer
+    if (tid == 0) n_found = n_pairs = 0;
+    fill_long_table<T>(table, in, deal, row);
+#pragma unroll 1
+    for (int l = 0; l < kStreamRing; ++l) load_layer<T>(table, ring, l, n);
 
-    typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;
-    bool has0 = false, has1 = false;
-    on_arrival<T>(table, slots, whole, n, quarter,
-                  [&](int, int vec, uint4 v) {
-                      if (vec < kThreads) { m0 = Vec<T>::max(m0, v); has0 = true; }
-                      else { m1 = Vec<T>::max(m1, v); has1 = true; }
-                  },
-                  [&](int, const auto& v) {
-                      has0 = has1 = true;
-#pragma unroll
-                      for (int i = 0; i < v.n; i += 2) {
-                          m0 = Vec<T>::max(m0, v.v[i]);
-                          m1 = Vec<T>::max(m1, v.v[i + 1]);
-                      }
-                  });
-    const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1), m = fmaxf(f0, f1), m_warp = warp_max(m);
+    Running running(c);
+    float   f0 = -INFINITY, f1 = -INFINITY;      // the largest of the thread's first and second vectors
+    bool    has0 = false, has1 = false;
+#pragma unroll 1
+    for (int l = 0; l < n; ++l) {
+        copy_wait<kStreamRing - 1>();
+        const uint4 a = ring[l % kStreamRing * kVecs + tid], b = ring[l % kStreamRing * kVecs + tid + kThreads];
+        load_layer<T>(table, ring, l + kStreamRing, n);
+        const float ma = Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), a)), mb = Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), b));
+        const float m = fmaxf(ma, mb);
+        f0 = fmaxf(f0, ma);
+        f1 = fmaxf(f1, mb);
+        const int lo = table[l].lo, hi = table[l].hi;
+        has0 |= tid * E < hi && (tid + 1) * E > lo;
+        has1 |= (tid + kThreads) * E < hi && (tid + kThreads + 1) * E > lo;
+        notes[l * kThreads] = sizeof(T) == 2 ? (uint16_t)(__float_as_uint(m) >> 16) : note_of(m);
+        running.see(m);
+        running.template add<T>(a, b);
+    }
 
-    // the warp's j-th largest maximum (of both halves of each thread's elements where j is large), to 16 bits from below;
-    // a warp in which a lane has no element does not take part
+    // the warp's j-th largest maximum (of both vectors' where j is large), to 16 bits from below; a warp in which a lane
+    // has no element does not take part
+    const float m = fmaxf(f0, f1);
     {
         const bool     full = __all_sync(0xffffffffu, has0 || has1), two = j > 8 && __all_sync(0xffffffffu, has0 && has1);
         const uint32_t key0 = key_of(two ? f0 : m), key1 = two ? key_of(f1) : 0;
@@ -905,75 +982,66 @@ __global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant_
             if (two) reach += __popc(__ballot_sync(0xffffffffu, key1 >= u));
             if (reach >= j) t = u;
         }
-        if (lane == 0) least[warp] = full ? max(t, kKeyMinusInf) : 0xffffffffu;
+        const float top = warp_max(m), sum = warp_sum(running.sum * scale_to(running.base, top, c));
+        if (lane == 0) {
+            least[warp] = full ? max(t, kKeyMinusInf) : 0xffffffffu;
+            scratch[warp] = make_float2(top, sum);
+        }
     }
-    const float sum = warp_sum(exp_sums<T>(table, slots, whole, n, base_of(m_warp, c)));
-    if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
     __syncthreads();
-
-    // the least over the cluster for everyone, the joined sums for the first block
-    if (deal.log_c) cluster_wait();
-    if (warp == 0) {
-        const float2   mine = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
-        const uint32_t low = __reduce_min_sync(0xffffffffu, lane < kWarps ? least[lane] : 0xffffffffu);
-        const float    top = warp_max(mine.x), all = warp_sum(mine.y * scale_to(mine.x, top, c));
-        if (lane < ctas) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&least_of_peers[rank], lane)), "r"(low) : "memory");
-        if (lane == 0) peer_store(peer_address(&from_peers[rank], 0), top, all);
-    }
-    if (deal.log_c) {
-        __syncwarp();
-        cluster_arrive();
-        cluster_wait();
-    } else {
-        __syncthreads();
-    }
-    uint32_t low = least_of_peers[0];
-    for (int i = 1; i < ctas; ++i) low = min(low, least_of_peers[i]);
-    // no warp is full in rows of less than 32 vectors: everything is sent
+    uint32_t low = least[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) low = min(low, least[i]);
+    // no warp is full in rows of less than 32 vectors: everything is a candidate
     const float bound = low == 0xffffffffu || j > 64 ? -INFINITY : value_of(low);
 
-    // every element of a vector of this thread that reaches `bar` (so is not NaN): f(key, token)
-    auto look = [&](int i, int vec, float bar, auto f) {
-        const Layer& L = table[i];
-        const int    a = L.lo - vec * E, b = L.hi - vec * E;
-        if (b <= 0 || a >= E) return;
-        float x[E];
-        unpack<T>(slots[i * kVecs + vec], x);
-        uint32_t hits = 0;
+    // every element of this thread's vectors of layer l that is not NaN: f(key, token)
+    auto look = [&](int l, auto f) {
+        const Layer& L = table[l];
+#pragma unroll 1
+        for (int vec = tid; vec < kVecs; vec += kThreads) {
+            const int a = L.lo - vec * E, b = L.hi - vec * E;
+            if (b <= 0 || a >= E) continue;
+            float x[E];
+            unpack<T>(edge_vector<T>(L, vec), x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) hits |= (x[e] >= bar && e >= a && e < b ? 1u : 0u) << e;
-        for (; hits; hits &= hits - 1) {
-            const int e = __ffs(hits) - 1;
-            f(key_of(to_float(reinterpret_cast<const T*>(slots + i * kVecs + vec)[e])), L.token + vec * E + e);
+            for (int e = 0; e < E; ++e)
+                if (x[e] == x[e] && e >= a && e < b) f(key_of(x[e]), L.token + vec * E + e);
         }
     };
-    const uint32_t list = peer_address(lists + rank * most, 0);
     auto push = [&](uint32_t key, int v) {
         const int i = atomicAdd(&n_found, 1);
-        if (i < most)
-            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(list + i * 8), "l"((Key)key << 32 | (0xffffffffu - (uint32_t)v)) : "memory");
+        if (i < kCandidates) found[i] = (Key)key << 32 | (0xffffffffu - (uint32_t)v);
     };
+    // the noted pairs of vectors into a list where the ring was, then each of their elements on a thread of its own
+    constexpr int kPairs = kStreamRing * kVecs * 4;
+    uint32_t*     pairs = reinterpret_cast<uint32_t*>(ring);
     if (m >= bound) {
-        uint32_t hits[2] = {0, 0};               // bit i: the thread's first / second vector of layer i
-        for (int i = 0; i < n; ++i) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                hits[h] |= (Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), slots[i * kVecs + tid + h * kThreads])) >= bound ? 1u : 0u) << i;
-        }
-#pragma unroll 1
-        while (hits[0] | hits[1]) {
-            const int h = hits[0] ? 0 : 1, i = __ffs(h ? hits[1] : hits[0]) - 1;
-            if (h) hits[1] &= hits[1] - 1; else hits[0] &= hits[0] - 1;
-            look(i, tid + h * kThreads, bound, push);
+#pragma unroll 4
+        for (int l = 0; l < n; ++l)
+            if (value_of_note(notes[l * kThreads]) >= bound) {
+                const int i = atomicAdd(&n_pairs, 1);
+                if (i < kPairs) pairs[i] = (uint32_t)l * kThreads + tid;
+            }
+    }
+    __syncthreads();
+    const bool crowded = n_pairs > kPairs;
+    if (!crowded) {
+        const int elements = n_pairs * 2 * E;
+#pragma unroll 4
+        for (int i = tid; i < elements; i += kThreads) {
+            const uint32_t pair = pairs[i / (2 * E)];
+            const int      l = pair / kThreads, p = (pair % kThreads + i / E % 2 * kThreads) * E + i % E;
+            const Layer&   L = table[l];
+            const float    x = p >= L.lo && p < L.hi ? to_float(reinterpret_cast<const T*>(L.in)[p]) : NAN;
+            if (x >= bound) push(key_of(x), L.token + p);
         }
     }
     __syncthreads();
-    if (n_found > most) {
+    if (crowded || n_found > kCandidates) {
         auto each = [&](auto f) {
 #pragma unroll 1
-            for (int i = 0; i < n; ++i)
-#pragma unroll 1
-                for (int vec = tid; vec < kVecs; vec += kThreads) look(i, vec, -INFINITY, f);
+            for (int l = 0; l < n; ++l) look(l, f);
         };
         uint32_t kth = 0;                      // the largest key that k elements reach, 0 if there are fewer
 #pragma unroll 1
@@ -997,37 +1065,28 @@ __global__ void __launch_bounds__(kThreads, 3) top_kernel(const __grid_constant_
         each([&](uint32_t key, int id) { if (key > kth || (key == kth && id <= before + 1)) push(key, id); });
         __syncthreads();
     }
-    if (tid == 0) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(peer_address(&counts[rank], 0)), "r"(n_found) : "memory");
-    if (deal.log_c) {
-        __syncwarp();
-        cluster_arrive();
-        if (rank) return;
-        cluster_wait();
-    } else {
-        __syncthreads();
-    }
-
-    int total = 0;
-    for (int i = 0; i < ctas; ++i) total += counts[i];
-    for (int e = tid; e < total; e += kThreads) {
-        int from = 0, at = e;
-        while (at >= counts[from]) at -= counts[from++];
-        const Key mine = lists[from * most + at];
+    const int total = n_found, groups = (total + 3) / 4;         // the list is read four keys at a time
+    if (tid < 4 * groups - total) found[total + tid] = 0;
+    __syncthreads();
+    // a key on `team` neighbouring threads that share the comparing
+    const int team = total <= 32 ? 8 : total <= 64 ? 4 : total <= 128 ? 2 : 1, part = tid & (team - 1);
+    for (int at = tid / team; at < (total + 31) / 32 * 32; at += kThreads / team) {
+        const Key mine = at < total ? found[at] : 0;
         int place = 0;
-        for (int i = 0; i < ctas; ++i) {
-            const Key* of = lists + i * most;
-            const int  count = counts[i];
 #pragma unroll 4
-            for (int q = 0; q < count; ++q) place += of[q] > mine;
+        for (int q = part; q < groups; q += team) {
+            const ulonglong2 a = reinterpret_cast<const ulonglong2*>(found)[2 * q], b = reinterpret_cast<const ulonglong2*>(found)[2 * q + 1];
+            place += (a.x > mine) + (a.y > mine) + (b.x > mine) + (b.y > mine);
         }
-        if (place < k) {
+        for (int o = 1; o < team; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
+        if (mine && part == 0 && place < k) {
             values[row * k + place] = value_of((uint32_t)(mine >> 32));
             ids[row * k + place] = (int32_t)(0xffffffffu - (uint32_t)mine);
         }
     }
     if (tid >= total && tid < k) { values[row * k + tid] = -INFINITY; ids[row * k + tid] = -1; }      // no element is left
     if (warp == 0) {
-        const float2 mine = lane < ctas ? from_peers[lane] : make_float2(-INFINITY, 0.f);
+        const float2 mine = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
         const float  top = warp_max(mine.x), all = warp_sum(mine.y * scale_to(mine.x, top, c));
         if (lane == 0) lse[row] = log_sum(top, top * inv_t, all);
     }
@@ -1403,28 +1462,46 @@ Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int mos
     return d;
 }
 
-// Launches a kernel with a cluster of blocks per row.
+// What is kept of a kernel's launches on a device.
+struct Kept {
+    std::atomic<bool>     opted{false};
+    std::atomic<uint64_t> clusters[4];            // for each cluster size: shared memory << 20 | clusters that fit at once
+};
+// Launches a kernel with a cluster of blocks for each row, or, where the kernel goes from row to row, for as many rows as
+// fit on the device at once (and no more than give every cluster the same number of rows, or one less).
 template <class... P, class... A>
-int launch(void (*kernel)(P...), std::atomic<bool>* opted, int64_t rows, const Deal& d, int64_t smem, const Device& dev,
+int launch(void (*kernel)(P...), Kept* kept, int64_t rows, bool loops, const Deal& d, int64_t smem, const Device& dev,
            cudaStream_t stream, A... args) {
     if (smem > dev.smem) return NEREUS_ERR_TOO_LARGE;
-    if (!opted[dev.id].load()) {
+    Kept& of = kept[dev.id];
+    if (!of.opted.load()) {
         NEREUS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem));
-        opted[dev.id].store(true);
+        of.opted.store(true);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows << d.log_c));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr = {};
-    if (d.log_c) {
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = 1u << d.log_c;
-        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1u << d.log_c;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (loops) {
+        uint64_t fit = of.clusters[d.log_c].load();
+        if ((int64_t)(fit >> 20) != smem) {
+            int n = 0;
+            cfg.gridDim = dim3(1u << d.log_c);
+            NEREUS_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
+            fit = (uint64_t)smem << 20 | (uint64_t)std::max(1, n);
+            of.clusters[d.log_c].store(fit);
+        }
+        const int64_t most = (int64_t)(fit & 0xfffff), each = (rows + most - 1) / most;
+        rows = (rows + each - 1) / each;
     }
+    cfg.gridDim = dim3((unsigned)(rows << d.log_c));
+    if (!d.log_c) cfg.numAttrs = 0;
     NEREUS_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
     return NEREUS_OK;
 }
@@ -1432,12 +1509,12 @@ int launch(void (*kernel)(P...), std::atomic<bool>* opted, int64_t rows, const D
 template <class T, int kPass>
 int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
                    const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
-    static std::atomic<bool> opted[kMaxDevices];
+    static Kept kept[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + kVecs * 16;
     const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
-    return launch(distill_kernel<T, kPass>, opted, in.rows, d, d.mine * per_layer, dev, stream,
+    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, d.mine * per_layer, dev, stream,
                   cut_of(in), kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
 }
 
@@ -1459,7 +1536,7 @@ int distill(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
 template <class TI, class TO, class Count>
 int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const nereus_penalties_t& how, int32_t* token,
                    float* lse, cudaStream_t stream) {
-    static std::atomic<bool> opted[kMaxDevices];
+    static Kept kept[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
@@ -1468,32 +1545,21 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
     Deal d = deal_of(in, per_layer, fixed, 4);
     // what does not fit is done in rounds
     while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
-    return launch(process_kernel<TI, TO, Count>, opted, in.rows, d, d.mine * per_layer + fixed, dev, stream,
+    return launch(process_kernel<TI, TO, Count>, kept, in.rows, false, d, d.mine * per_layer + fixed, dev, stream,
                   cut_of(in), cut_of(out), d, how, token, lse);
 }
 
 template <class T>
 int top_launch(const nereus_logits_t& in, int k, float temperature, float* values, int32_t* ids, float* lse, cudaStream_t stream) {
-    static std::atomic<bool> opted[kMaxDevices];
+    static Kept kept[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    const int64_t per_layer = sizeof(Layer) + kVecs * 16;
-    const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
+    Deal d = deal_of(in, 0, 0, 1 << 30);
     // warps of which every lane has a vector, at least: how many of the k largest each has to vouch for
-    const int64_t w = held_cols(in, 0), e = kPerVec<T>, last = (in.vocab - 1) / in.shard_cols;
-    int full = 0;
-    for (int rank = 0; rank < 1 << d.log_c; ++rank) {
-        int64_t lanes = 0;
-        for (int l = rank; l < d.layers; l += 1 << d.log_c) {
-            const int64_t cols = l / d.per_shard == last ? in.vocab - last * in.shard_cols : w;
-            lanes = std::max(lanes, (cols + e - 1) / e - (int64_t)(l % d.per_shard) * kVecs);
-        }
-        full += (int)std::min<int64_t>(std::max<int64_t>(lanes, 0) / 32, kWarps);
-    }
-    const int     j = full ? (k + full - 1) / full : 1;
-    const int64_t lists = ((int64_t)list_of(d.log_c) << d.log_c) * 8;
-    return launch(top_kernel<T>, opted, in.rows, d, d.mine * per_layer + lists, dev, stream, cut_of(in), d, k, j,
-                  1.f / temperature, values, ids, lse);
+    const int64_t w = held_cols(in, 0), vecs = (w + kPerVec<T> - 1) / kPerVec<T>;
+    const int     full = (int)std::min<int64_t>(vecs / 32, kWarps), j = full ? (k + full - 1) / full : 1;
+    const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + kThreads * 2);
+    return launch(top_kernel<T>, kept, in.rows, false, d, smem, dev, stream, cut_of(in), d, k, j, 1.f / temperature, values, ids, lse);
 }
 
 }  // namespace
