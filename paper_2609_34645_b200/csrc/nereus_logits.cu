@@ -889,14 +889,15 @@ struct Running {
 
 // ---- a teacher's top logits ----------------------------------------------------------------------------------
 //
-// One pass over the row sums the exponentials and notes the largest of every 16 (fp32: 8) elements, a thread's two vectors
-// of a layer, in two bytes (fp32 rounded up).  If each of the 8 warps takes the j-th largest of its threads' maxima, j =
+// One pass over the row sums the exponentials and notes the largest of every 16 elements, a thread's vectors of one layer
+// (fp32: of two), in two bytes (fp32 rounded up).  If each of the 8 warps takes the j-th largest of its threads' maxima, j =
 // k / 8 rounded up, at least k elements reach the least of these 8 values, whatever the order of the row: it bounds the
 // row's k-th largest from below, and for most rows some 1.4 k elements reach it.  Only the vectors whose note does are read
 // again, and what is found in them is ranked by counting, as one 64-bit key of (value, lower id).  Rows of so few distinct
 // values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly.
 
 constexpr int kCandidates = 1024;
+template <class T> constexpr int kNote = (int)sizeof(T) / 2;          // layers of a note
 
 // orders as the values do, -0 as +0; NaN below everything
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -934,16 +935,19 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ float2   scratch[kWarps];
     __shared__ uint32_t least[kWarps];
-    __shared__ int      count_scratch[kWarps], n_found, n_pairs;
-    __shared__ __align__(16) Key found[kCandidates];
+    __shared__ int      count_scratch[kWarps], n_found, n_noted;
     const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers;
     const int64_t row = blockIdx.x;
     const float   c = inv_t * kLog2e;
 
     uint4*    ring = reinterpret_cast<uint4*>(dynamic);
     Layer*    table = reinterpret_cast<Layer*>(ring + kStreamRing * kVecs);
-    uint16_t* notes = reinterpret_cast<uint16_t*>(table + n) + tid;          // of this thread, layer by layer
-    if (tid == 0) n_found = n_pairs = 0;
+    uint16_t* notes = reinterpret_cast<uint16_t*>(table + n) + tid;          // of this thread
+    // once the row has gone through, the ring takes the lists of what is found
+    Key*      found = reinterpret_cast<Key*>(ring);
+    uint32_t* noted_list = reinterpret_cast<uint32_t*>(found + kCandidates);
+    constexpr int kNoted = (kStreamRing * kVecs * 16 - kCandidates * 8) / 4;
+    if (tid == 0) n_found = n_noted = 0;
     fill_long_table<T>(table, in, deal, row);
 #pragma unroll 1
     for (int l = 0; l < kStreamRing; ++l) load_layer<T>(table, ring, l, n);
@@ -951,6 +955,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     Running running(c);
     float   f0 = -INFINITY, f1 = -INFINITY;      // the largest of the thread's first and second vectors
     bool    has0 = false, has1 = false;
+    float   to_note = -INFINITY;
 #pragma unroll 1
     for (int l = 0; l < n; ++l) {
         copy_wait<kStreamRing - 1>();
@@ -963,7 +968,8 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
         const int lo = table[l].lo, hi = table[l].hi;
         has0 |= tid * E < hi && (tid + 1) * E > lo;
         has1 |= (tid + kThreads) * E < hi && (tid + kThreads + 1) * E > lo;
-        notes[l * kThreads] = sizeof(T) == 2 ? (uint16_t)(__float_as_uint(m) >> 16) : note_of(m);
+        to_note = l % kNote<T> ? fmaxf(to_note, m) : m;
+        notes[l / kNote<T> * kThreads] = sizeof(T) == 2 ? (uint16_t)(__float_as_uint(to_note) >> 16) : note_of(to_note);
         running.see(m);
         running.template add<T>(a, b);
     }
@@ -1013,28 +1019,42 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
         const int i = atomicAdd(&n_found, 1);
         if (i < kCandidates) found[i] = (Key)key << 32 | (0xffffffffu - (uint32_t)v);
     };
-    // the noted pairs of vectors into a list where the ring was, then each of their elements on a thread of its own
-    constexpr int kPairs = kStreamRing * kVecs * 4;
-    uint32_t*     pairs = reinterpret_cast<uint32_t*>(ring);
+    // the notes that reach it into a list, then each of their vectors on a thread of its own
     if (m >= bound) {
-#pragma unroll 4
-        for (int l = 0; l < n; ++l)
-            if (value_of_note(notes[l * kThreads]) >= bound) {
-                const int i = atomicAdd(&n_pairs, 1);
-                if (i < kPairs) pairs[i] = (uint32_t)l * kThreads + tid;
+        const int notes_of = (n + kNote<T> - 1) / kNote<T>;
+#pragma unroll 1
+        for (int q0 = 0; q0 < notes_of; q0 += 32) {
+            uint32_t  reach = 0;
+            const int count = min(32, notes_of - q0);
+#pragma unroll 8
+            for (int q = 0; q < count; ++q) reach |= (value_of_note(notes[(q0 + q) * kThreads]) >= bound ? 1u : 0u) << q;
+            for (; reach; reach &= reach - 1) {
+                const int i = atomicAdd(&n_noted, 1);
+                if (i < kNoted) noted_list[i] = (uint32_t)(q0 + __ffs(reach) - 1) * kThreads + tid;
             }
+        }
     }
     __syncthreads();
-    const bool crowded = n_pairs > kPairs;
+    const bool crowded = n_noted > kNoted;
     if (!crowded) {
-        const int elements = n_pairs * 2 * E;
-#pragma unroll 4
-        for (int i = tid; i < elements; i += kThreads) {
-            const uint32_t pair = pairs[i / (2 * E)];
-            const int      l = pair / kThreads, p = (pair % kThreads + i / E % 2 * kThreads) * E + i % E;
-            const Layer&   L = table[l];
-            const float    x = p >= L.lo && p < L.hi ? to_float(reinterpret_cast<const T*>(L.in)[p]) : NAN;
-            if (x >= bound) push(key_of(x), L.token + p);
+        const int vecs = n_noted * 2 * kNote<T>;
+#pragma unroll 1
+        for (int i = tid; i < vecs; i += kThreads) {
+            const uint32_t note = noted_list[i / (2 * kNote<T>)];
+            const int      vec = note % kThreads + i % 2 * kThreads, l = note / kThreads * kNote<T> + i / 2 % kNote<T>;
+            if (l >= n) continue;
+            const Layer& L = table[l];
+            const int    a = L.lo - vec * E, b = L.hi - vec * E;
+            if (b <= 0 || a >= E) continue;
+            float x[E];
+            unpack<T>(edge_vector<T>(L, vec), x);
+            uint32_t hits = 0;
+#pragma unroll
+            for (int e = 0; e < E; ++e) hits |= (x[e] >= bound ? 1u : 0u) << e;
+            hits &= bits_between(a, b, E);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (hits >> e & 1u) push(key_of(x[e]), L.token + vec * E + e);
         }
     }
     __syncthreads();
@@ -1558,7 +1578,8 @@ int top_launch(const nereus_logits_t& in, int k, float temperature, float* value
     // warps of which every lane has a vector, at least: how many of the k largest each has to vouch for
     const int64_t w = held_cols(in, 0), vecs = (w + kPerVec<T> - 1) / kPerVec<T>;
     const int     full = (int)std::min<int64_t>(vecs / 32, kWarps), j = full ? (k + full - 1) / full : 1;
-    const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + kThreads * 2);
+    const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)sizeof(Layer) +
+                         (d.layers + kNote<T> - 1) / kNote<T> * (int64_t)kThreads * 2;
     return launch(top_kernel<T>, kept, in.rows, false, d, smem, dev, stream, cut_of(in), d, k, j, 1.f / temperature, values, ids, lse);
 }
 
