@@ -165,6 +165,9 @@ template <> struct Vec<float> {
         return fmaxf(m, fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))));
     }
     static __device__ __forceinline__ Max join(Max a, Max b) { return fmaxf(a, b); }
+    static __device__ __forceinline__ Max max(uint4 v) {
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
     static __device__ __forceinline__ float value(Max m) { return m; }
 };
 template <> struct Vec<__nv_bfloat16> {
@@ -189,7 +192,8 @@ template <> struct Vec<__nv_bfloat16> {
         asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
-    static __device__ __forceinline__ Max max(Max m, uint4 v) { return join(m, join(join(v.x, v.y), join(v.z, v.w))); }
+    static __device__ __forceinline__ Max max(uint4 v) { return join(join(v.x, v.y), join(v.z, v.w)); }
+    static __device__ __forceinline__ Max max(Max m, uint4 v) { return join(m, max(v)); }
     static __device__ __forceinline__ float value(Max m) {
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
@@ -833,11 +837,12 @@ __device__ __forceinline__ void fill_long_table(Layer* table, const LogitsCut& i
     for (int i = threadIdx.x; i < d.layers; i += kThreads) table[i] = layer_of<T, T>(in, LogitsCut(), d, row, 0, i);
     __syncthreads();
 }
-// Starts the copies of this thread's two vectors of layer l, one commit group; nothing but the group past the last layer.
+// Starts the copies of this thread's two vectors of layer l into place `slot` of the ring, one commit group; nothing but the
+// group past the last layer.
 template <class T>
-__device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int l, int n) {
+__device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int slot, int l, int n) {
     if (l < n) {
-        uint4* const to = ring + l % kStreamRing * kVecs + threadIdx.x;
+        uint4* const to = ring + slot * kVecs + threadIdx.x;
         const Layer& L = table[l];
         if (L.hi - L.lo == kPerLayer<T>) {
             const char* from = L.in + threadIdx.x * 16;
@@ -849,6 +854,22 @@ __device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int 
         }
     }
     copy_commit();
+}
+// f(layer, first vector, second vector) for this thread's vectors of all layers of the row, in order.
+template <class T, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
+#pragma unroll
+    for (int l = 0; l < kStreamRing; ++l) load_layer<T>(table, ring, l, l, n);
+    const uint4* mine = ring + threadIdx.x;
+#pragma unroll 1
+    for (int l = 0; l < n; l += kStreamRing)
+#pragma unroll
+        for (int slot = 0; slot < kStreamRing; ++slot) {
+            if (l + slot >= n) break;
+            copy_wait<kStreamRing - 1>();
+            const uint4 a = mine[slot * kVecs], b = mine[slot * kVecs + kThreads];
+            load_layer<T>(table, ring, slot, l + slot + kStreamRing, n);
+            f(l + slot, a, b);
+        }
 }
 
 // A running sum of exponentials: (base, sum of 2^((x - base) c)) whose base follows the maximum only when that has gone
@@ -949,29 +970,27 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     constexpr int kNoted = (kStreamRing * kVecs * 16 - kCandidates * 8) / 4;
     if (tid == 0) n_found = n_noted = 0;
     fill_long_table<T>(table, in, deal, row);
-#pragma unroll 1
-    for (int l = 0; l < kStreamRing; ++l) load_layer<T>(table, ring, l, n);
 
     Running running(c);
-    float   f0 = -INFINITY, f1 = -INFINITY;      // the largest of the thread's first and second vectors
-    bool    has0 = false, has1 = false;
-    float   to_note = -INFINITY;
-#pragma unroll 1
-    for (int l = 0; l < n; ++l) {
-        copy_wait<kStreamRing - 1>();
-        const uint4 a = ring[l % kStreamRing * kVecs + tid], b = ring[l % kStreamRing * kVecs + tid + kThreads];
-        load_layer<T>(table, ring, l + kStreamRing, n);
-        const float ma = Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), a)), mb = Vec<T>::value(Vec<T>::max(Vec<T>::lowest(), b));
-        const float m = fmaxf(ma, mb);
-        f0 = fmaxf(f0, ma);
-        f1 = fmaxf(f1, mb);
-        const int lo = table[l].lo, hi = table[l].hi;
-        has0 |= tid * E < hi && (tid + 1) * E > lo;
-        has1 |= (tid + kThreads) * E < hi && (tid + kThreads + 1) * E > lo;
+    typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;         // of the thread's first and second vectors
+    float to_note = -INFINITY;
+    stream<T>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+        const typename Vec<T>::Max ma = Vec<T>::max(a), mb = Vec<T>::max(b);
+        const float m = Vec<T>::value(Vec<T>::join(ma, mb));
+        m0 = Vec<T>::join(m0, ma);
+        m1 = Vec<T>::join(m1, mb);
         to_note = l % kNote<T> ? fmaxf(to_note, m) : m;
         notes[l / kNote<T> * kThreads] = sizeof(T) == 2 ? (uint16_t)(__float_as_uint(to_note) >> 16) : note_of(to_note);
         running.see(m);
         running.template add<T>(a, b);
+    });
+    const float f0 = Vec<T>::value(m0), f1 = Vec<T>::value(m1);
+    bool has0 = false, has1 = false;
+    for (int l = 0; l < n; ++l) {
+        const int lo = table[l].lo, hi = table[l].hi;
+        has0 |= tid * E < hi && (tid + 1) * E > lo;
+        has1 |= (tid + kThreads) * E < hi && (tid + kThreads + 1) * E > lo;
+        if (hi - lo == kPerLayer<T>) break;
     }
 
     // the warp's j-th largest maximum (of both vectors' where j is large), to 16 bits from below; a warp in which a lane
