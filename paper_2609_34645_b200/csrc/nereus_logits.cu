@@ -908,6 +908,18 @@ struct Running {
     }
 };
 
+// A vector with -inf in the elements of `bits`.
+template <class T> __device__ __forceinline__ uint4 without(uint4 v, uint32_t bits) {
+    Pair p[Vec<T>::kPairs];
+    Vec<T>::unpack(v, p);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kPairs; ++i) {
+        const float2 h = halves(p[i]);
+        p[i] = pair(bits >> 2 * i & 1u ? -INFINITY : h.x, bits >> (2 * i + 1) & 1u ? -INFINITY : h.y);
+    }
+    return Vec<T>::pack(p);
+}
+
 // ---- a teacher's top logits ----------------------------------------------------------------------------------
 //
 // One pass over the row sums the exponentials and notes the largest of every 16 elements, a thread's vectors of one layer
@@ -1133,11 +1145,10 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
 
 // ---- distillation --------------------------------------------------------------------------------------------
 //
-// The sum over the rest is taken on its own, with -inf put in the entries' places in shared memory: as the difference
-// of the whole sum and the entries' it would lose its digits where the entries hold nearly all of the mass.  The
-// gradient of a token of the rest is exp((x - m) / T) times one number per row.  The entries, k <= 256, are worked out
-// by one thread each on the block's first k / 32 warps (every block of the cluster works out all of them rather than
-// wait for another exchange), and their gradients are stored after the others.
+// The sum over the rest is taken on its own, with the entries left out: as the difference of the whole sum and the
+// entries' it would lose its digits where the entries hold nearly all of the mass.  The gradient of a token of the rest is
+// exp((x - m) / T) times one number per row.  The entries, k <= 256, are worked out by one thread each on the block's first
+// k / 32 warps.
 
 enum Pass { kForward, kBackward, kStep };
 
@@ -1157,14 +1168,158 @@ __device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2*
     return r;
 }
 
+// Entry `threadIdx.x` of a row: the teacher's logit, its probability, the student's logit; id -1 where there is none.
+// p_rest and mass (the sum of all P) are the row's.
+struct Entry {
+    int   id;
+    float y, x, lse, log_p, p, p_rest, mass;
+};
+template <class T>
+__device__ __forceinline__ void fetch_entry(Entry& e, int id, const LogitsCut& in, const nereus_distill_t& how, int64_t row) {
+    e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
+    if (how.lse) e.lse = how.lse[row];
+    if ((uint32_t)id >= (uint32_t)in.vocab) return;
+    e.id = id;
+    e.y = how.values[row * how.k + threadIdx.x];
+    const int s = shard_of(in, id);
+    e.x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
+}
+__device__ __forceinline__ void teacher_side(Entry& e, int vocab, const nereus_distill_t& how, int warps, float2* scratch) {
+    const float t = how.temperature;
+    if (how.lse) {
+        e.log_p = e.y / t - e.lse;
+        e.p = e.id >= 0 ? expf(e.log_p) : 0.f;
+        const float2 s = entry_sum(e.p, e.id >= 0 ? 1.f : 0.f, warps, scratch);
+        e.p_rest = (int)s.y < vocab ? fmaxf(0.f, 1.f - s.x) : 0.f;
+        return;
+    }
+    float top = warp_max(e.id >= 0 ? e.y : -INFINITY);
+    if (warps > 1) {
+        asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].x = top;
+        asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+        for (int i = 0; i < warps; ++i) top = fmaxf(top, scratch[i].x);
+    }
+    const float  v = e.id >= 0 ? expf((e.y - top) / t) : 0.f;
+    const float2 s = entry_sum(v, e.id >= 0 ? 1.f : 0.f, warps, scratch);
+    e.log_p = (e.y - top) / t - logf(s.x);
+    e.p = s.y > 0.f ? v / s.x : 0.f;
+    if (s.y == 0.f) e.mass = 0.f;
+}
+
+// The divergence's terms of the entry and of the rest, Q f of both, and f (the derivative after Q; of the forward KL only
+// its products with Q are used, which stay finite where Q is 0).
+struct Groups {
+    float q, q_rest, term, term_rest, qf, qf_rest, f, f_rest;
+};
+__device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill_t& how, float m, float total, float rest) {
+    Groups g = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float log_total = logf(total), log_q = (e.x - m) / how.temperature - log_total, log_q_rest = logf(rest) - log_total;
+    const bool  is = e.id >= 0;
+    g.q = is ? expf(log_q) : 0.f;
+    g.q_rest = rest / total;
+    float p_rest = e.p_rest;
+    if (how.divergence == NEREUS_FORWARD_KL) {
+        if (e.p > 0.f) g.term = e.p * (e.log_p - log_q);
+        if (p_rest > 0.f) g.term_rest = p_rest * (logf(p_rest) - log_q_rest);
+    } else if (how.divergence == NEREUS_REVERSE_KL) {
+        p_rest = fmaxf(p_rest, 5.9604644775390625e-8f);
+        if (g.q > 0.f) { g.f = log_q - e.log_p; g.term = g.qf = g.q * g.f; }
+        if (g.q_rest > 0.f) { g.f_rest = log_q_rest - logf(p_rest); g.term_rest = g.qf_rest = g.q_rest * g.f_rest; }
+    } else {
+        const float a = how.beta, b = 1.f - how.beta;
+        if (is) {
+            const float log_m = logf(a * e.p + b * g.q);
+            if (g.q > 0.f) { g.f = b * (log_q - log_m); g.qf = g.q * g.f; }
+            g.term = g.qf + (e.p > 0.f ? a * e.p * (e.log_p - log_m) : 0.f);
+        }
+        const float log_m = logf(a * p_rest + b * g.q_rest);
+        if (g.q_rest > 0.f) { g.f_rest = b * (log_q_rest - log_m); g.qf_rest = g.q_rest * g.f_rest; }
+        g.term_rest = g.qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
+    }
+    return g;
+}
+
+// The loss alone.  The row goes by once (see above: rows that are read once); which elements are entries stands in shared
+// memory, two bytes (fp32: one) for a thread's two vectors of a layer.
+template <class T>
+__global__ void __launch_bounds__(kThreads, 4) distill_forward_kernel(const __grid_constant__ LogitsCut in, Deal deal,
+                                                                      const __grid_constant__ nereus_distill_t how,
+                                                                      float* loss, float* saved) {
+    constexpr int E = kPerVec<T>;
+    typedef std::conditional_t<E == 8, uint16_t, uint8_t> Flags;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    __shared__ float2 scratch[kWarps], entry_scratch[kWarps];
+    const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers, entry_warps = (how.k + 31) >> 5;
+    const int64_t row = blockIdx.x;
+    const float   weight = how.weight ? how.weight[row] : 1.f, t = how.temperature, c = kLog2e / t;
+    int           id = -1;
+    if (tid < how.k) id = how.ids[row * how.k + tid];
+    if (weight == 0.f) {
+        if (tid == 0) loss[row] = 0.f;
+        if (tid < 4) saved[row * 4 + tid] = 0.f;
+        return;
+    }
+    uint4*    ring = reinterpret_cast<uint4*>(dynamic);
+    Layer*    table = reinterpret_cast<Layer*>(ring + kStreamRing * kVecs);
+    uint32_t* flags = reinterpret_cast<uint32_t*>(table + n);
+    for (int i = tid; i < n * kThreads * (int)sizeof(Flags) / 4; i += kThreads) flags[i] = 0;
+    fill_long_table<T>(table, in, deal, row);
+
+    Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
+    if (warp < entry_warps) {
+        fetch_entry<T>(e, id, in, how, row);
+        if (e.id >= 0) {
+            const Place at = place_of<T>(in, deal, row, e.id);
+            const int   vec = at.position / E, slot = at.layer * kThreads + vec % kThreads;
+            const int   bit = slot * 2 * E + vec / kThreads * E + at.position % E;
+            atomicOr(&flags[bit >> 5], 1u << (bit & 31));
+        }
+    }
+    __syncthreads();
+    const Flags* mine = reinterpret_cast<const Flags*>(flags) + tid;
+    Running running(c);
+    typename Vec<T>::Max top = Vec<T>::lowest();
+    stream<T>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+        const typename Vec<T>::Max m = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
+        top = Vec<T>::join(top, m);
+        running.see(Vec<T>::value(m));
+        if (const uint32_t f = mine[l * kThreads]) {
+            a = without<T>(a, f);
+            b = without<T>(b, f >> E);
+        }
+        running.template add<T>(a, b);
+    });
+    if (warp < entry_warps) teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
+
+    const float m_warp = warp_max(Vec<T>::value(top)), sum = warp_sum(running.sum * scale_to(running.base, m_warp, c));
+    if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
+    __syncthreads();
+    if (warp >= entry_warps) return;
+    const float2 part = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
+    const float  m = warp_max(part.x), rest = warp_sum(part.y * scale_to(part.x, m, c));
+    const float  total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+    const Groups g = groups_of(e, how, m, total, rest);
+    const float  d = entry_sum(g.term, 0.f, entry_warps, entry_scratch).x + g.term_rest;
+    if (tid == 0) {
+        loss[row] = weight * d;
+        float* const o = saved + row * 4;
+        o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
+    }
+}
+
+// The gradient, from saved sums or together with the loss.  -inf is put in the entries' places in shared memory before the
+// sum, and their gradients are stored after the others'.  Every block of the cluster works out all entries rather than
+// wait for another exchange.
 template <class T, int kPass>
 __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_constant__ LogitsCut in,
-                                                           const __grid_constant__ LogitsCut grad, Deal deal,
-                                                           const __grid_constant__ nereus_distill_t how, float* loss,
-                                                           float* saved, const float* grad_loss) {
+                                                              const __grid_constant__ LogitsCut grad, Deal deal,
+                                                              const __grid_constant__ nereus_distill_t how, float* loss,
+                                                              const float* saved, const float* grad_loss) {
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ float2 scratch[kWarps], entry_scratch[kWarps], from_peers[kMaxCtas];
     __shared__ float  rest_scale_of_row;
+    __shared__ uint2  masks;
     const int     k = how.k, tid = threadIdx.x, warp = tid >> 5, entry_warps = (k + 31) >> 5;
     const int     ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
@@ -1173,60 +1328,31 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
 
     Layer* table = reinterpret_cast<Layer*>(dynamic);
     uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    __shared__ uint2 masks;
-    int id = -1;                                  // entry `tid`
+    int    id = -1;
     if (tid < k) id = how.ids[row * k + tid];
     const uint2 whole = fill_table<T, T>(table, &masks, in, grad, deal, row, rank, 0, n);
     if (weight == 0.f) {
-        if (rank == 0 && tid == 0 && kPass != kBackward) loss[row] = 0.f;
-        if (rank == 0 && tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
-        if (kPass != kForward)
-            for (int i = 0; i < n; ++i)
-                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
+        if (rank == 0 && tid == 0 && kPass == kStep) loss[row] = 0.f;
+        for (int i = 0; i < n; ++i)
+            for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
         return;
     }
-    if (kPass != kBackward && deal.log_c) cluster_arrive();       // the peers run: their shared memory may be written
-    // the teacher's side of the entry, the student's logit, and its place if the block holds it
-    const float t = how.temperature, c = kLog2e / t;
-    int   entries = 0, place = -1, place_at = 0;  // layer, position
-    float x = 0.f, y = 0.f, teacher_lse = 0.f, log_p = 0.f, p = 0.f, p_rest = 0.f, mass = 1.f;
-    if ((uint32_t)id >= (uint32_t)in.vocab) id = -1;
+    if (kPass == kStep && deal.log_c) cluster_arrive();           // the peers run: their shared memory may be written
+    Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
+    int   place = -1, place_at = 0;               // layer and position, if the block holds it
     if (warp < entry_warps) {
-        if (how.lse) teacher_lse = how.lse[row];
-        if (id >= 0) {
-            y = how.values[row * k + tid];
-            const Place at = place_of<T>(in, deal, row, id);
-            const int   s = shard_of(in, id);
-            x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
+        fetch_entry<T>(e, id, in, how, row);
+        if (e.id >= 0) {
+            const Place at = place_of<T>(in, deal, row, e.id);
             if (at.rank == rank) { place = at.layer; place_at = at.position; }
         }
     }
     load_share<T>(table, slots, whole.x, n, quarter);
-    if (warp < entry_warps) {
-        if (how.lse) {
-            log_p = y / t - teacher_lse;
-            p = id >= 0 ? expf(log_p) : 0.f;
-            const float2 s = entry_sum(p, id >= 0 ? 1.f : 0.f, entry_warps, entry_scratch);
-            entries = (int)s.y;
-            p_rest = entries < in.vocab ? fmaxf(0.f, 1.f - s.x) : 0.f;
-        } else {
-            float top = warp_max(id >= 0 ? y : -INFINITY);
-            if (entry_warps > 1) {
-                if ((tid & 31) == 0) scratch[warp].x = top;
-                asm volatile("bar.sync 1, %0;" ::"r"(entry_warps * 32) : "memory");
-                for (int i = 0; i < entry_warps; ++i) top = fmaxf(top, scratch[i].x);
-            }
-            const float  e = id >= 0 ? expf((y - top) / t) : 0.f;
-            const float2 s = entry_sum(e, id >= 0 ? 1.f : 0.f, entry_warps, entry_scratch);
-            entries = (int)s.y;
-            log_p = (y - top) / t - logf(s.x);
-            p = entries ? e / s.x : 0.f;
-            if (!entries) mass = 0.f;
-        }
-    }
-    // a block may overwrite the logits once all blocks have read the entries' (the exchange orders the other passes)
+    if (warp < entry_warps) teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
+    // a block may overwrite the logits once all blocks have read the entries' (the exchange orders the step)
     if (kPass == kBackward && deal.log_c) cluster_arrive();
 
+    const float t = how.temperature, c = kLog2e / t;
     float m, total = 0.f, rest;
     if (kPass == kBackward) {
         m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
@@ -1262,60 +1388,28 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
             m = all.x;
             rest = all.y;
         }
-        if (kPass == kForward && rank) return;
     }
 
-    // the groups: an entry on its thread, the rest on all of them
     float g = 0.f, divergence = 0.f, divergence_rest = 0.f;
     if (warp < entry_warps) {
-        if (kPass != kBackward) total = rest + entry_sum(id >= 0 ? expf((x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
-        const float log_total = logf(total);
-        const float log_q = (x - m) / t - log_total, q = expf(log_q);
-        const float log_q_rest = logf(rest) - log_total, q_rest = rest / total;
-        float term = 0.f, qf = 0.f, slope = 0.f, term_rest = 0.f, qf_rest = 0.f, slope_rest = 0.f;
-        if (how.divergence == NEREUS_FORWARD_KL) {
-            if (p > 0.f) term = p * (log_p - log_q);
-            if (p_rest > 0.f) term_rest = p_rest * (logf(p_rest) - log_q_rest);
-        } else if (how.divergence == NEREUS_REVERSE_KL) {
-            p_rest = fmaxf(p_rest, 5.9604644775390625e-8f);
-            if (q > 0.f && id >= 0) { slope = log_q - log_p; term = qf = q * slope; }
-            if (q_rest > 0.f) { slope_rest = log_q_rest - logf(p_rest); term_rest = qf_rest = q_rest * slope_rest; }
-        } else {
-            const float a = how.beta, b = 1.f - how.beta;
-            if (id >= 0) {
-                const float log_m = logf(a * p + b * q);
-                if (q > 0.f) { slope = b * (log_q - log_m); qf = q * slope; }
-                term = qf + (p > 0.f ? a * p * (log_p - log_m) : 0.f);
-            }
-            const float log_m = logf(a * p_rest + b * q_rest);
-            if (q_rest > 0.f) { slope_rest = b * (log_q_rest - log_m); qf_rest = q_rest * slope_rest; }
-            term_rest = qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
-        }
-        // of the forward KL the gradient takes Q f and Q sum Q f, which stay finite where Q is 0 and need no sum: its
-        // loss is summed after the gradient has gone out
-        const bool early = how.divergence == NEREUS_FORWARD_KL && kPass != kForward;
-        float2 sums = make_float2(0.f, 0.f);
-        if (!early) sums = entry_sum(id >= 0 ? term : 0.f, qf, entry_warps, entry_scratch);
-        divergence = early ? (id >= 0 ? term : 0.f) : sums.x;
-        divergence_rest = term_rest;
-        if (kPass == kForward && tid == 0) {
-            const float d = divergence + divergence_rest;
-            loss[row] = weight * d;
-            float* const o = saved + row * 4;
-            o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
-        }
-        const float scale = (kPass == kBackward && grad_loss ? weight * grad_loss[row] : weight) / t, mean = sums.y + qf_rest;
+        if (kPass == kStep) total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+        const Groups v = groups_of(e, how, m, total, rest);
+        // the forward KL's gradient needs no sum over the groups: its loss is summed after the gradient has gone out
+        float2 sums = make_float2(v.term, 0.f);
+        if (how.divergence != NEREUS_FORWARD_KL) sums = entry_sum(v.term, v.qf, entry_warps, entry_scratch);
+        divergence = sums.x;
+        divergence_rest = v.term_rest;
+        const float scale = (kPass == kBackward && grad_loss ? weight * grad_loss[row] : weight) / t, mean = sums.y + v.qf_rest;
         float rest_scale;
         if (how.divergence == NEREUS_FORWARD_KL) {
-            g = (mass * q - p) * scale;
-            rest_scale = (mass - (p_rest > 0.f && rest > 0.f ? p_rest / q_rest : 0.f)) * scale / total;
+            g = (e.mass * v.q - e.p) * scale;
+            rest_scale = (e.mass - (e.p_rest > 0.f && rest > 0.f ? e.p_rest / v.q_rest : 0.f)) * scale / total;
         } else {
-            g = q > 0.f ? q * (slope - mean) * scale : 0.f;
-            rest_scale = (slope_rest - mean) * scale / total;
+            g = v.q > 0.f ? v.q * (v.f - mean) * scale : 0.f;
+            rest_scale = (v.f_rest - mean) * scale / total;
         }
         if (tid == 0) rest_scale_of_row = rest_scale;
     }
-    if (kPass == kForward) return;
     if (kPass == kBackward && deal.log_c) cluster_wait();
     __syncthreads();
     {
@@ -1323,36 +1417,37 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
         const float scale = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
         const Pair  s = pair(scale, scale);
         auto gradient = [&](uint4 v) {
-            Pair e[Vec<T>::kPairs];
-            Vec<T>::unpack(v, e);
-#pragma unroll
-            for (int j = 0; j < Vec<T>::kPairs; ++j) e[j] = mul2(exp2_pair(fma2(e[j], b.c, b.minus_mc)), s);
-            return Vec<T>::pack(e);
-        };
-        auto gradient_far = [&](uint4 v) {
-            float e[kPerVec<T>];
-            unpack<T>(v, e);
             Pair p[Vec<T>::kPairs];
+            Vec<T>::unpack(v, p);
 #pragma unroll
-            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(pair(scale_to(e[2 * j], b.m, c), scale_to(e[2 * j + 1], b.m, c)), s);
+            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(exp2_pair(fma2(p[j], b.c, b.minus_mc)), s);
             return Vec<T>::pack(p);
         };
-        if (b.far)
+        auto gradient_far = [&](uint4 v) {
+            float x[kPerVec<T>];
+            unpack<T>(v, x);
+            Pair p[Vec<T>::kPairs];
+#pragma unroll
+            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(pair(scale_to(x[2 * j], b.m, c), scale_to(x[2 * j + 1], b.m, c)), s);
+            return Vec<T>::pack(p);
+        };
+        if (b.far) {
             for (int i = 0; i < n; ++i)
                 for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, gradient_far(slots[l * kVecs + vec])); });
-        else
-        sweep<T>(table, slots, whole.y, 0, n, [&](int l, int vec, uint4 v) { store_vector<T>(table[l], vec, gradient(v)); },
-                 [&](int l, const auto& v) {
-                     uint4 o[v.n];
+        } else {
+            sweep<T>(table, slots, whole.y, 0, n, [&](int l, int vec, uint4 v) { store_vector<T>(table[l], vec, gradient(v)); },
+                     [&](int l, const auto& v) {
+                         uint4 o[v.n];
 #pragma unroll
-                     for (int j = 0; j < v.n; ++j) o[j] = gradient(v.v[j]);
+                         for (int j = 0; j < v.n; ++j) o[j] = gradient(v.v[j]);
 #pragma unroll
-                     for (int j = 0; j < v.n; j += 2) {
-                         uint4* const to = reinterpret_cast<uint4*>(table[l + j / 2].out) + tid;
-                         __stcs(to, o[j]);
-                         __stcs(to + kThreads, o[j + 1]);
-                     }
-                 });
+                         for (int j = 0; j < v.n; j += 2) {
+                             uint4* const to = reinterpret_cast<uint4*>(table[l + j / 2].out) + tid;
+                             __stcs(to, o[j]);
+                             __stcs(to + kThreads, o[j + 1]);
+                         }
+                     });
+        }
     }
     __syncthreads();                                  // the entries' places have been written as of the rest
     if (place >= 0) reinterpret_cast<T*>(table[place].out)[place_at] = from_float<T>(g);
@@ -1545,16 +1640,26 @@ int launch(void (*kernel)(P...), Kept* kept, int64_t rows, bool loops, const Dea
     return NEREUS_OK;
 }
 
+template <class T>
+int forward_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved, cudaStream_t stream) {
+    static Kept kept[kMaxDevices];
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    const Deal    d = deal_of(in, 0, 0, 1 << 30);
+    const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + kThreads * kPerVec<T> / 4);
+    return launch(distill_forward_kernel<T>, kept, in.rows, false, d, smem, dev, stream, cut_of(in), d, how, loss, saved);
+}
+
 template <class T, int kPass>
-int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
-                   const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
+int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, const float* saved,
+                   const float* grad_loss, const nereus_logits_t& grad, cudaStream_t stream) {
     static Kept kept[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + kVecs * 16;
     const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
-    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, d.mine * per_layer, dev, stream,
-                  cut_of(in), kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
+    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, d.mine * per_layer, dev, stream, cut_of(in), cut_of(grad),
+                  d, how, loss, saved, grad_loss);
 }
 
 template <int kPass>
@@ -1568,8 +1673,13 @@ int distill(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
     }
     if (in->rows == 0) return NEREUS_OK;
     if ((kPass != kBackward && !loss) || (kPass != kStep && !saved)) return NEREUS_ERR_ARG;
-    auto go = in->dtype == NEREUS_BF16 ? distill_launch<__nv_bfloat16, kPass> : distill_launch<float, kPass>;
-    return go(*in, *how, loss, saved, grad_loss, grad, (cudaStream_t)stream);
+    const bool   half = in->dtype == NEREUS_BF16;
+    cudaStream_t st = (cudaStream_t)stream;
+    if constexpr (kPass == kForward)
+        return half ? forward_launch<__nv_bfloat16>(*in, *how, loss, saved, st) : forward_launch<float>(*in, *how, loss, saved, st);
+    else
+        return half ? distill_launch<__nv_bfloat16, kPass>(*in, *how, loss, saved, grad_loss, *grad, st)
+                    : distill_launch<float, kPass>(*in, *how, loss, saved, grad_loss, *grad, st);
 }
 
 template <class TI, class TO, class Count>
