@@ -260,94 +260,6 @@ template <class T, class F> __device__ __forceinline__ void for_edges(const Laye
     for (int v = threadIdx.x; v < kVecs; v += kThreads)
         if (v * kPerVec<T> < hi && (v + 1) * kPerVec<T> > lo) f(i, v);
 }
-template <int N> struct Batch {
-    enum { n = N };
-    uint4 v[N];
-};
-// The block's share from shared memory, layers [a, b): f(layer, vector, value) one at a time where the row fills a layer
-// in part; otherwise g(layer, batch) with the thread's four values of two layers, so that four independent vectors are
-// in work at a time, or its two of one layer where the next is not whole.
-template <class T, class F, class G>
-__device__ __forceinline__ void sweep(const Layer* table, const uint4* slots, uint32_t whole, int a, int b, F f, G g) {
-    const uint4* mine = slots + threadIdx.x;
-    for (int i = a; i < b;) {
-        const uint4* s = mine + i * kVecs;
-        if (i + 1 < b && (whole >> i & 3u) == 3u) {
-            const Batch<4> v = {{s[0], s[kThreads], s[kVecs], s[kVecs + kThreads]}};
-            g(i, v);
-            i += 2;
-            continue;
-        }
-        if (whole >> i & 1u) {
-            const Batch<2> v = {{s[0], s[kThreads]}};
-            g(i, v);
-        } else {
-            for_edges<T>(table, i, [&](int l, int vec) { f(l, vec, slots[l * kVecs + vec]); });
-        }
-        ++i;
-    }
-}
-// Starts the copies of layers [a, b) of the block's share into its slots, one commit group.  Every thread copies what it
-// reads back itself, so that it may do this as soon as it has no more use for the slots' old contents.
-template <class T>
-__device__ __forceinline__ void load_layers(const Layer* table, uint4* slots, uint32_t whole, int a, int b) {
-    const int      t = threadIdx.x;
-    const uint32_t to = smem_address(slots + t);
-    bool           part = false;
-#pragma unroll 2
-    for (int i = a; i < b; ++i) {
-        const char* from = table[i].in + t * 16;
-        if (whole >> i & 1u) {
-            copy_async(to + i * (kVecs * 16), from);
-            copy_async(to + i * (kVecs * 16) + kThreads * 16, from + kThreads * 16);
-        } else {
-            const int lo = table[i].lo, hi = table[i].hi;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int p = (t + h * kThreads) * kPerVec<T>;
-                if (p >= lo && p + kPerVec<T> <= hi) copy_async(to + i * (kVecs * 16) + h * kThreads * 16, from + h * kThreads * 16);
-                else part |= p < hi && p + kPerVec<T> > lo;
-            }
-        }
-    }
-    copy_commit();
-    if (part) {                               // vectors that the row fills in part: its ends
-#pragma unroll 1
-        for (int i = a; i < b; ++i) {
-            if (whole >> i & 1u) continue;
-            for_edges<T>(table, i, [&](int, int v) {
-                const int lo = table[i].lo, hi = table[i].hi, p = v * kPerVec<T>;
-                if (p >= lo && p + kPerVec<T> <= hi) return;
-                T e[kPerVec<T>];
-#pragma unroll
-                for (int j = 0; j < kPerVec<T>; ++j)
-                    e[j] = p + j >= lo && p + j < hi ? reinterpret_cast<const T*>(table[i].in)[p + j] : from_float<T>(-INFINITY);
-#pragma unroll
-                for (int j = 0; j < kPerVec<T>; ++j) reinterpret_cast<T*>(&slots[i * kVecs + v])[j] = e[j];
-            });
-        }
-    }
-}
-// ... the whole share, in four commit groups of `quarter` layers
-template <class T>
-__device__ __forceinline__ void load_share(const Layer* table, uint4* slots, uint32_t whole, int n, int quarter) {
-#pragma unroll 1
-    for (int q = 0; q < 4; ++q) load_layers<T>(table, slots, whole, min(n, q * quarter), min(n, (q + 1) * quarter));
-}
-
-// sweep over the block's share, in the order of arrival.
-template <class T, class F, class G>
-__device__ __forceinline__ void on_arrival(const Layer* table, const uint4* slots, uint32_t whole, int n, int quarter, F f, G g) {
-#pragma unroll 1
-    for (int q = 0; q < 4; ++q) {
-        if (q == 0) copy_wait<3>();
-        else if (q == 1) copy_wait<2>();
-        else if (q == 2) copy_wait<1>();
-        else copy_wait<0>();
-        sweep<T>(table, slots, whole, min(n, q * quarter), min(n, (q + 1) * quarter), f, g);
-    }
-}
-
 template <class T>
 __device__ __forceinline__ void store_vector(const Layer& l, int vec, uint4 v) {
     const int p = vec * kPerVec<T>;
@@ -394,29 +306,6 @@ template <class T> __device__ __noinline__ float exp_sum_far(uint4 v, float m, f
     unpack<T>(v, f);
     for (int j = 0; j < kPerVec<T>; ++j) r += scale_to(f[j], m, c);
     return r;
-}
-// ... over the thread's part of the block's share
-template <class T> __device__ __forceinline__ float exp_sums(const Layer* table, const uint4* slots, uint32_t whole, int n, const Base& b) {
-    if (b.far) {
-        float r = 0.f;
-        for (int i = 0; i < n; ++i)
-            for_edges<T>(table, i, [&](int l, int vec) { r += exp_sum_far<T>(slots[l * kVecs + vec], b.m, halves(b.c).x); });
-        return r;
-    }
-    Pair s[4] = {0, 0, 0, 0};
-    sweep<T>(table, slots, whole, 0, n, [&](int, int, uint4 v) { s[0] = exp_sum<T>(s[0], v, b); },
-             [&](int, const auto& v) {
-#pragma unroll
-                 for (int j = 0; j < v.n; ++j) s[j] = exp_sum<T>(s[j], v.v[j], b);
-             });
-    const float2 h = halves(add2(add2(s[0], s[1]), add2(s[2], s[3])));
-    return (h.x + h.y) * b.right;
-}
-
-// Two such sums joined, the same whichever comes first (no product is contracted into the sum).
-__device__ __forceinline__ float2 join(float2 a, float2 b, float c) {
-    const float m = fmaxf(a.x, b.x);
-    return make_float2(m, __fadd_rn(__fmul_rn(a.y, scale_to(a.x, m, c)), __fmul_rn(b.y, scale_to(b.x, m, c))));
 }
 // log of a sum of exponentials from its maximum, the scaled maximum and the sum of exp(x - max)
 __device__ __forceinline__ float log_sum(float m, float scaled_m, float sum) {
@@ -829,12 +718,13 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
 // Where nothing is written per element the row need not stay on the chip: one block takes a whole row, its layers through
 // a ring in shared memory, several blocks on an SM.
 
-constexpr int kStreamRing = 3;            // layers on their way to a block
+constexpr int kStreamRing = 3;            // layers on their way to a block that needs the row once
+constexpr int kStepRing   = 4;            // ... and twice
 
 // Fills a table of any number of layers.  Ends in a barrier.
 template <class T>
-__device__ __forceinline__ void fill_long_table(Layer* table, const LogitsCut& in, const Deal& d, int64_t row) {
-    for (int i = threadIdx.x; i < d.layers; i += kThreads) table[i] = layer_of<T, T>(in, LogitsCut(), d, row, 0, i);
+__device__ __forceinline__ void fill_long_table(Layer* table, const LogitsCut& in, const LogitsCut& out, const Deal& d, int64_t row) {
+    for (int i = threadIdx.x; i < d.layers; i += kThreads) table[i] = layer_of<T, T>(in, out, d, row, 0, i);
     __syncthreads();
 }
 // Starts the copies of this thread's two vectors of layer l into place `slot` of the ring, one commit group; nothing but the
@@ -855,21 +745,38 @@ __device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int 
     }
     copy_commit();
 }
-// f(layer, first vector, second vector) for this thread's vectors of all layers of the row, in order.
-template <class T, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
+// f(layer, first vector, second vector) for this thread's vectors of all layers of the row, in order, through a ring of R
+// layers.
+template <class T, int R, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
 #pragma unroll
-    for (int l = 0; l < kStreamRing; ++l) load_layer<T>(table, ring, l, l, n);
+    for (int l = 0; l < R; ++l) load_layer<T>(table, ring, l, l, n);
     const uint4* mine = ring + threadIdx.x;
 #pragma unroll 1
-    for (int l = 0; l < n; l += kStreamRing)
+    for (int l = 0; l < n; l += R)
 #pragma unroll
-        for (int slot = 0; slot < kStreamRing; ++slot) {
+        for (int slot = 0; slot < R; ++slot) {
             if (l + slot >= n) break;
-            copy_wait<kStreamRing - 1>();
+            copy_wait<R - 1>();
             const uint4 a = mine[slot * kVecs], b = mine[slot * kVecs + kThreads];
-            load_layer<T>(table, ring, slot, l + slot + kStreamRing, n);
+            if (l + slot + R < n) load_layer<T>(table, ring, slot, l + slot + R, n);      // the last R layers stay
+            else copy_commit();
             f(l + slot, a, b);
         }
+}
+// The same backwards, after stream: the last R layers are still in the ring, and of the others those come first that L2 has
+// seen last.
+template <class T, int R, class F> __device__ __forceinline__ void stream_back(const Layer* table, uint4* ring, int n, F f) {
+    const uint4* mine = ring + threadIdx.x;
+    int slot = (n - 1) % R;
+#pragma unroll 1
+    for (int l = n - 1; l >= 0; --l) {
+        copy_wait<R - 1>();
+        const uint4 a = mine[slot * kVecs], b = mine[slot * kVecs + kThreads];
+        if (l >= R) load_layer<T>(table, ring, slot, l - R, n);
+        else copy_commit();
+        f(l, a, b);
+        slot = slot ? slot - 1 : R - 1;
+    }
 }
 
 // A running sum of exponentials: (base, sum of 2^((x - base) c)) whose base follows the maximum only when that has gone
@@ -981,12 +888,12 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     uint32_t* noted_list = reinterpret_cast<uint32_t*>(found + kCandidates);
     constexpr int kNoted = (kStreamRing * kVecs * 16 - kCandidates * 8) / 4;
     if (tid == 0) n_found = n_noted = 0;
-    fill_long_table<T>(table, in, deal, row);
+    fill_long_table<T>(table, in, LogitsCut(), deal, row);
 
     Running running(c);
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;         // of the thread's first and second vectors
     float to_note = -INFINITY;
-    stream<T>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+    stream<T, kStreamRing>(table, ring, n, [&](int l, uint4 a, uint4 b) {
         const typename Vec<T>::Max ma = Vec<T>::max(a), mb = Vec<T>::max(b);
         const float m = Vec<T>::value(Vec<T>::join(ma, mb));
         m0 = Vec<T>::join(m0, ma);
@@ -1151,6 +1058,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
 // k / 32 warps.
 
 enum Pass { kForward, kBackward, kStep };
+constexpr int kStepBlocks = 4;
 
 // Sum of two values over the first `warps` warps, the only ones to call it; the same on every thread.
 __device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2* scratch) {
@@ -1240,36 +1148,45 @@ __device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill
     return g;
 }
 
-// The loss alone.  The row goes by once (see above: rows that are read once); which elements are entries stands in shared
-// memory, two bytes (fp32: one) for a thread's two vectors of a layer.
-template <class T>
-__global__ void __launch_bounds__(kThreads, 4) distill_forward_kernel(const __grid_constant__ LogitsCut in, Deal deal,
-                                                                      const __grid_constant__ nereus_distill_t how,
-                                                                      float* loss, float* saved) {
-    constexpr int E = kPerVec<T>;
+// A row goes by once for its sums (see above: rows that are read once); which elements are entries stands in shared memory,
+// two bytes (fp32: one) for a thread's two vectors of a layer.  The step lets it go by a second time for the gradient,
+// backwards: the layers read last are in the ring, and the ones before them in L2.  The gradients of the entries are stored after
+// the others'.
+template <class T, int kPass>
+__global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
+    distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
+                   const __grid_constant__ nereus_distill_t how, float* loss, float* saved, const float* grad_loss) {
+    constexpr int E = kPerVec<T>, R = kPass == kStep ? kStepRing : kStreamRing;
     typedef std::conditional_t<E == 8, uint16_t, uint8_t> Flags;
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ float2 scratch[kWarps], entry_scratch[kWarps];
+    __shared__ float  rest_scale_of_row, m_of_row;
     const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers, entry_warps = (how.k + 31) >> 5;
     const int64_t row = blockIdx.x;
     const float   weight = how.weight ? how.weight[row] : 1.f, t = how.temperature, c = kLog2e / t;
     int           id = -1;
     if (tid < how.k) id = how.ids[row * how.k + tid];
+    uint4*    ring = reinterpret_cast<uint4*>(dynamic);
+    Layer*    table = reinterpret_cast<Layer*>(ring + R * kVecs);
+    uint32_t* flags = reinterpret_cast<uint32_t*>(table + n);
     if (weight == 0.f) {
-        if (tid == 0) loss[row] = 0.f;
-        if (tid < 4) saved[row * 4 + tid] = 0.f;
+        if (tid == 0 && kPass != kBackward) loss[row] = 0.f;
+        if (tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
+        if (kPass != kForward) {
+            fill_long_table<T>(table, in, grad, deal, row);
+            for (int i = 0; i < n; ++i)
+                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
+        }
         return;
     }
-    uint4*    ring = reinterpret_cast<uint4*>(dynamic);
-    Layer*    table = reinterpret_cast<Layer*>(ring + kStreamRing * kVecs);
-    uint32_t* flags = reinterpret_cast<uint32_t*>(table + n);
-    for (int i = tid; i < n * kThreads * (int)sizeof(Flags) / 4; i += kThreads) flags[i] = 0;
-    fill_long_table<T>(table, in, deal, row);
+    if (kPass != kBackward)
+        for (int i = tid; i < n * kThreads * (int)sizeof(Flags) / 4; i += kThreads) flags[i] = 0;
+    fill_long_table<T>(table, in, kPass == kForward ? LogitsCut() : grad, deal, row);
 
     Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
     if (warp < entry_warps) {
         fetch_entry<T>(e, id, in, how, row);
-        if (e.id >= 0) {
+        if (kPass != kBackward && e.id >= 0) {
             const Place at = place_of<T>(in, deal, row, e.id);
             const int   vec = at.position / E, slot = at.layer * kThreads + vec % kThreads;
             const int   bit = slot * 2 * E + vec / kThreads * E + at.position % E;
@@ -1277,128 +1194,49 @@ __global__ void __launch_bounds__(kThreads, 4) distill_forward_kernel(const __gr
         }
     }
     __syncthreads();
-    const Flags* mine = reinterpret_cast<const Flags*>(flags) + tid;
-    Running running(c);
-    typename Vec<T>::Max top = Vec<T>::lowest();
-    stream<T>(table, ring, n, [&](int l, uint4 a, uint4 b) {
-        const typename Vec<T>::Max m = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
-        top = Vec<T>::join(top, m);
-        running.see(Vec<T>::value(m));
-        if (const uint32_t f = mine[l * kThreads]) {
-            a = without<T>(a, f);
-            b = without<T>(b, f >> E);
-        }
-        running.template add<T>(a, b);
-    });
-    if (warp < entry_warps) teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
 
-    const float m_warp = warp_max(Vec<T>::value(top)), sum = warp_sum(running.sum * scale_to(running.base, m_warp, c));
-    if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
-    __syncthreads();
-    if (warp >= entry_warps) return;
-    const float2 part = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
-    const float  m = warp_max(part.x), rest = warp_sum(part.y * scale_to(part.x, m, c));
-    const float  total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
-    const Groups g = groups_of(e, how, m, total, rest);
-    const float  d = entry_sum(g.term, 0.f, entry_warps, entry_scratch).x + g.term_rest;
-    if (tid == 0) {
-        loss[row] = weight * d;
-        float* const o = saved + row * 4;
-        o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
-    }
-}
-
-// The gradient, from saved sums or together with the loss.  -inf is put in the entries' places in shared memory before the
-// sum, and their gradients are stored after the others'.  Every block of the cluster works out all entries rather than
-// wait for another exchange.
-template <class T, int kPass>
-__global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_constant__ LogitsCut in,
-                                                              const __grid_constant__ LogitsCut grad, Deal deal,
-                                                              const __grid_constant__ nereus_distill_t how, float* loss,
-                                                              const float* saved, const float* grad_loss) {
-    extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2 scratch[kWarps], entry_scratch[kWarps], from_peers[kMaxCtas];
-    __shared__ float  rest_scale_of_row;
-    __shared__ uint2  masks;
-    const int     k = how.k, tid = threadIdx.x, warp = tid >> 5, entry_warps = (k + 31) >> 5;
-    const int     ctas = 1 << deal.log_c, rank = blockIdx.x & (ctas - 1);
-    const int64_t row = blockIdx.x >> deal.log_c;
-    const int     n = layers_of(deal, rank), quarter = (n + 3) / 4;
-    float         weight = how.weight ? how.weight[row] : 1.f;
-
-    Layer* table = reinterpret_cast<Layer*>(dynamic);
-    uint4* slots = reinterpret_cast<uint4*>(table + deal.mine);
-    int    id = -1;
-    if (tid < k) id = how.ids[row * k + tid];
-    const uint2 whole = fill_table<T, T>(table, &masks, in, grad, deal, row, rank, 0, n);
-    if (weight == 0.f) {
-        if (rank == 0 && tid == 0 && kPass == kStep) loss[row] = 0.f;
-        for (int i = 0; i < n; ++i)
-            for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
-        return;
-    }
-    if (kPass == kStep && deal.log_c) cluster_arrive();           // the peers run: their shared memory may be written
-    Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
-    int   place = -1, place_at = 0;               // layer and position, if the block holds it
-    if (warp < entry_warps) {
-        fetch_entry<T>(e, id, in, how, row);
-        if (e.id >= 0) {
-            const Place at = place_of<T>(in, deal, row, e.id);
-            if (at.rank == rank) { place = at.layer; place_at = at.position; }
-        }
-    }
-    load_share<T>(table, slots, whole.x, n, quarter);
-    if (warp < entry_warps) teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
-    // a block may overwrite the logits once all blocks have read the entries' (the exchange orders the step)
-    if (kPass == kBackward && deal.log_c) cluster_arrive();
-
-    const float t = how.temperature, c = kLog2e / t;
-    float m, total = 0.f, rest;
-    if (kPass == kBackward) {
-        m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
-        copy_wait<0>();
-    } else {
+    float m = 0.f, total = 0.f, rest = 0.f;
+    if (kPass != kBackward) {
+        const Flags* mine = reinterpret_cast<const Flags*>(flags) + tid;
+        Running running(c);
         typename Vec<T>::Max top = Vec<T>::lowest();
-        on_arrival<T>(table, slots, whole.x, n, quarter, [&](int, int, uint4 v) { top = Vec<T>::max(top, v); },
-                      [&](int, const auto& v) {
-#pragma unroll
-                          for (int j = 0; j < v.n; ++j) top = Vec<T>::max(top, v.v[j]);
-                      });
-        m = warp_max(Vec<T>::value(top));
-        __syncthreads();                          // the elements are there; scratch is free
-        if ((tid & 31) == 0) scratch[warp].x = m;
-        if (place >= 0) reinterpret_cast<T*>(slots + place * kVecs)[place_at] = from_float<T>(-INFINITY);
+        stream<T, R>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+            const typename Vec<T>::Max v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
+            top = Vec<T>::join(top, v);
+            running.see(Vec<T>::value(v));
+            if (const uint32_t f = mine[l * kThreads]) {
+                a = without<T>(a, f);
+                b = without<T>(b, f >> E);
+            }
+            running.template add<T>(a, b);
+        });
+        const float m_warp = warp_max(Vec<T>::value(top)), sum = warp_sum(running.sum * scale_to(running.base, m_warp, c));
+        if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kWarps; ++i) m = fmaxf(m, scratch[i].x);
-        const Base b = base_of(m, c);
-        const float sum = warp_sum(exp_sums<T>(table, slots, whole.x, n, b));
-        if ((tid & 31) == 0) scratch[warp].y = sum;
-        __syncthreads();
-        rest = scratch[0].y;
-#pragma unroll
-        for (int i = 1; i < kWarps; ++i) rest += scratch[i].y;
-        if (deal.log_c) {
-            cluster_wait();
-            if (tid < ctas) peer_store(peer_address(&from_peers[rank], tid), m, rest);
-            cluster_arrive();
-            cluster_wait();
-            float2 all = from_peers[0];
-            for (int i = 1; i < ctas; ++i) all = join(all, from_peers[i], c);
-            m = all.x;
-            rest = all.y;
-        }
     }
-
     float g = 0.f, divergence = 0.f, divergence_rest = 0.f;
     if (warp < entry_warps) {
-        if (kPass == kStep) total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+        teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
+        if (kPass == kBackward) {
+            m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
+        } else {
+            const float2 part = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
+            m = warp_max(part.x);
+            rest = warp_sum(part.y * scale_to(part.x, m, c));
+            total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+        }
         const Groups v = groups_of(e, how, m, total, rest);
-        // the forward KL's gradient needs no sum over the groups: its loss is summed after the gradient has gone out
+        // the forward KL's gradient needs no sum over the groups: a step sums its loss after the gradient has gone out
         float2 sums = make_float2(v.term, 0.f);
-        if (how.divergence != NEREUS_FORWARD_KL) sums = entry_sum(v.term, v.qf, entry_warps, entry_scratch);
+        if (how.divergence != NEREUS_FORWARD_KL || kPass == kForward) sums = entry_sum(v.term, v.qf, entry_warps, entry_scratch);
         divergence = sums.x;
         divergence_rest = v.term_rest;
+        if (kPass == kForward && tid == 0) {
+            const float d = divergence + divergence_rest;
+            loss[row] = weight * d;
+            float* const o = saved + row * 4;
+            o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
+        }
         const float scale = (kPass == kBackward && grad_loss ? weight * grad_loss[row] : weight) / t, mean = sums.y + v.qf_rest;
         float rest_scale;
         if (how.divergence == NEREUS_FORWARD_KL) {
@@ -1408,50 +1246,50 @@ __global__ void __launch_bounds__(kThreads, 3) distill_kernel(const __grid_const
             g = v.q > 0.f ? v.q * (v.f - mean) * scale : 0.f;
             rest_scale = (v.f_rest - mean) * scale / total;
         }
-        if (tid == 0) rest_scale_of_row = rest_scale;
+        if (tid == 0) { rest_scale_of_row = rest_scale; m_of_row = m; }
     }
-    if (kPass == kBackward && deal.log_c) cluster_wait();
+    if (kPass == kForward) return;
     __syncthreads();
     {
-        const Base  b = base_of(m, c);
+        const Base  b = base_of(m_of_row, c);
         const float scale = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
         const Pair  s = pair(scale, scale);
         auto gradient = [&](uint4 v) {
             Pair p[Vec<T>::kPairs];
             Vec<T>::unpack(v, p);
+            if (b.far) {
 #pragma unroll
-            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(exp2_pair(fma2(p[j], b.c, b.minus_mc)), s);
+                for (int j = 0; j < Vec<T>::kPairs; ++j) {
+                    const float2 x = halves(p[j]);
+                    p[j] = mul2(pair(scale_to(x.x, b.m, c), scale_to(x.y, b.m, c)), s);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(exp2_pair(fma2(p[j], b.c, b.minus_mc)), s);
+            }
             return Vec<T>::pack(p);
         };
-        auto gradient_far = [&](uint4 v) {
-            float x[kPerVec<T>];
-            unpack<T>(v, x);
-            Pair p[Vec<T>::kPairs];
-#pragma unroll
-            for (int j = 0; j < Vec<T>::kPairs; ++j) p[j] = mul2(pair(scale_to(x[2 * j], b.m, c), scale_to(x[2 * j + 1], b.m, c)), s);
-            return Vec<T>::pack(p);
+        auto write = [&](int l, uint4 a, uint4 b) {
+            const Layer& L = table[l];
+            const uint4  ga = gradient(a), gb = gradient(b);
+            if (L.vec_out && L.hi - L.lo == kPerLayer<T>) {
+                uint4* const to = reinterpret_cast<uint4*>(L.out) + tid;
+                __stcs(to, ga);
+                __stcs(to + kThreads, gb);
+            } else {
+                store_vector<T>(L, tid, ga);
+                store_vector<T>(L, tid + kThreads, gb);
+            }
         };
-        if (b.far) {
-            for (int i = 0; i < n; ++i)
-                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, gradient_far(slots[l * kVecs + vec])); });
-        } else {
-            sweep<T>(table, slots, whole.y, 0, n, [&](int l, int vec, uint4 v) { store_vector<T>(table[l], vec, gradient(v)); },
-                     [&](int l, const auto& v) {
-                         uint4 o[v.n];
-#pragma unroll
-                         for (int j = 0; j < v.n; ++j) o[j] = gradient(v.v[j]);
-#pragma unroll
-                         for (int j = 0; j < v.n; j += 2) {
-                             uint4* const to = reinterpret_cast<uint4*>(table[l + j / 2].out) + tid;
-                             __stcs(to, o[j]);
-                             __stcs(to + kThreads, o[j + 1]);
-                         }
-                     });
-        }
+        if constexpr (kPass == kStep) stream_back<T, R>(table, ring, n, write);
+        else stream<T, R>(table, ring, n, write);
     }
     __syncthreads();                                  // the entries' places have been written as of the rest
-    if (place >= 0) reinterpret_cast<T*>(table[place].out)[place_at] = from_float<T>(g);
-    if (kPass == kStep && rank == 0 && warp < entry_warps) {
+    if (e.id >= 0) {
+        const int s = shard_of(in, e.id);
+        row_of<T>(grad, s, row)[e.id - s * in.cols] = from_float<T>(g);
+    }
+    if (kPass == kStep && warp < entry_warps) {
         if (how.divergence == NEREUS_FORWARD_KL) divergence = entry_sum(divergence, 0.f, entry_warps, entry_scratch).x;
         if (tid == 0) loss[row] = weight * (divergence + divergence_rest);
     }
@@ -1640,26 +1478,16 @@ int launch(void (*kernel)(P...), Kept* kept, int64_t rows, bool loops, const Dea
     return NEREUS_OK;
 }
 
-template <class T>
-int forward_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved, cudaStream_t stream) {
+template <class T, int kPass>
+int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
+                   const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
     static Kept kept[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const Deal    d = deal_of(in, 0, 0, 1 << 30);
-    const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + kThreads * kPerVec<T> / 4);
-    return launch(distill_forward_kernel<T>, kept, in.rows, false, d, smem, dev, stream, cut_of(in), d, how, loss, saved);
-}
-
-template <class T, int kPass>
-int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, const float* saved,
-                   const float* grad_loss, const nereus_logits_t& grad, cudaStream_t stream) {
-    static Kept kept[kMaxDevices];
-    Device dev;
-    if (int rc = device_of(&dev)) return rc;
-    const int64_t per_layer = sizeof(Layer) + kVecs * 16;
-    const Deal    d = deal_of(in, per_layer, 0, 1 << 20);
-    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, d.mine * per_layer, dev, stream, cut_of(in), cut_of(grad),
-                  d, how, loss, saved, grad_loss);
+    const int64_t smem = (kPass == kStep ? kStepRing : kStreamRing) * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + (kPass == kBackward ? 0 : kThreads * kPerVec<T> / 4));
+    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, smem, dev, stream, cut_of(in),
+                  kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
 }
 
 template <int kPass>
@@ -1673,13 +1501,8 @@ int distill(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
     }
     if (in->rows == 0) return NEREUS_OK;
     if ((kPass != kBackward && !loss) || (kPass != kStep && !saved)) return NEREUS_ERR_ARG;
-    const bool   half = in->dtype == NEREUS_BF16;
-    cudaStream_t st = (cudaStream_t)stream;
-    if constexpr (kPass == kForward)
-        return half ? forward_launch<__nv_bfloat16>(*in, *how, loss, saved, st) : forward_launch<float>(*in, *how, loss, saved, st);
-    else
-        return half ? distill_launch<__nv_bfloat16, kPass>(*in, *how, loss, saved, grad_loss, *grad, st)
-                    : distill_launch<float, kPass>(*in, *how, loss, saved, grad_loss, *grad, st);
+    auto go = in->dtype == NEREUS_BF16 ? distill_launch<__nv_bfloat16, kPass> : distill_launch<float, kPass>;
+    return go(*in, *how, loss, saved, grad_loss, grad, (cudaStream_t)stream);
 }
 
 template <class TI, class TO, class Count>
