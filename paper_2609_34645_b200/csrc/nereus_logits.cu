@@ -54,7 +54,8 @@ struct Deal {
 };
 
 constexpr int kThreads  = 256;
-constexpr int kVecs     = 2 * kThreads;           // vectors of a layer
+constexpr int kWide     = 512;                    // ... of the blocks that write a gradient
+constexpr int kVecs     = 2 * kThreads;           // vectors of a layer: two a thread, in wide blocks too
 constexpr int kWarps    = kThreads / 32;
 constexpr int kMaxCtas  = 8;                      // portable cluster size
 constexpr float kLog2e  = 1.4426950408889634f;
@@ -70,7 +71,7 @@ struct __align__(16) Layer {
 static_assert(sizeof(Layer) == 32, "Layer is read as two 16-byte words");
 
 template <class T> constexpr int kPerVec = 16 / (int)sizeof(T);
-template <class T> constexpr int kPerLayer = kVecs * kPerVec<T>;
+template <class T, int TH = kThreads> constexpr int kPerLayer = 2 * TH * kPerVec<T>;
 
 template <class T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
@@ -88,19 +89,19 @@ __device__ __forceinline__ int width_of(const LogitsCut& c, int s) {
 }
 
 // Block `rank`'s i-th layer of a row; hi = 0 where it has none.
-template <class TI, class TO>
+template <class TI, class TO, int TH = kThreads>
 __device__ __forceinline__ Layer layer_of(const LogitsCut& in, const LogitsCut& out, const Deal& d, int64_t row, int rank, int i) {
     Layer r = {nullptr, nullptr, 0, 0, 0, 0};
     const int l = (i << d.log_c) + rank;
     if (l >= d.layers) return r;
-    const int s = l / d.per_shard, first = (l - s * d.per_shard) * kPerLayer<TI>;
+    const int s = l / d.per_shard, first = (l - s * d.per_shard) * kPerLayer<TI, TH>;
     const int w = width_of(in, s);
     if (!w) return r;
     const uintptr_t a = (uintptr_t)row_of<TI>(in, s, row);
     const int       phase = (int)(a & 15) / (int)sizeof(TI);       // the row starts at this position of its first vector
     r.in = (const char*)(a & ~(uintptr_t)15) + (int64_t)first * (int)sizeof(TI);
     r.lo = max(0, phase - first);
-    r.hi = max(0, min(kPerLayer<TI>, phase + w - first));
+    r.hi = max(0, min(kPerLayer<TI, TH>, phase + w - first));
     r.token = s * in.cols + first - phase;
     if (out.tp) {
         r.out = (char*)row_of<TO>(out, s, row) + (int64_t)(first - phase) * (int)sizeof(TO);
@@ -153,6 +154,7 @@ template <> struct Vec<float> {
     static constexpr int kPairs = 2;
     typedef float Max;
     static __device__ __forceinline__ Max lowest() { return -INFINITY; }
+    static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     static __device__ __forceinline__ void unpack(uint4 v, Pair (&p)[2]) {
         p[0] = pair(__uint_as_float(v.x), __uint_as_float(v.y));
         p[1] = pair(__uint_as_float(v.z), __uint_as_float(v.w));
@@ -174,6 +176,7 @@ template <> struct Vec<__nv_bfloat16> {
     static constexpr int kPairs = 4;
     typedef uint32_t Max;
     static __device__ __forceinline__ Max lowest() { return 0xff80ff80u; }
+    static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     static __device__ __forceinline__ Pair open(uint32_t w) { return pair(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
     static __device__ __forceinline__ uint32_t close(Pair p) {
         const float2 f = halves(p);
@@ -254,10 +257,10 @@ __device__ __forceinline__ uint2 fill_table(Layer* table, uint2* masks, const Lo
 }
 
 // f(layer, vector of the layer) for every vector of this thread in a layer that the row fills in part.
-template <class T, class F> __device__ __forceinline__ void for_edges(const Layer* table, int i, F f) {
+template <class T, int TH = kThreads, class F> __device__ __forceinline__ void for_edges(const Layer* table, int i, F f) {
     const int lo = table[i].lo, hi = table[i].hi;
 #pragma unroll 1
-    for (int v = threadIdx.x; v < kVecs; v += kThreads)
+    for (int v = threadIdx.x; v < 2 * TH; v += TH)
         if (v * kPerVec<T> < hi && (v + 1) * kPerVec<T> > lo) f(i, v);
 }
 template <class T>
@@ -323,13 +326,13 @@ __device__ __forceinline__ int shard_of(const LogitsCut& in, int token) {
     const int s = (int)((float)token * in.per_col), r = token - s * in.cols;
     return r < 0 ? s - 1 : r >= in.cols ? s + 1 : s;
 }
-template <class T>
+template <class T, int TH = kThreads>
 __device__ __forceinline__ Place place_of(const LogitsCut& in, const Deal& d, int64_t row, int token) {
     const int s = shard_of(in, token);
     int       q = token - s * in.cols;
     if (!d.aligned) q += (int)((uintptr_t)row_of<T>(in, s, row) & 15) / (int)sizeof(T);
-    const int l = s * d.per_shard + q / kPerLayer<T>;
-    return {l & ((1 << d.log_c) - 1), l >> d.log_c, q % kPerLayer<T>};
+    const int l = s * d.per_shard + q / kPerLayer<T, TH>;
+    return {l & ((1 << d.log_c) - 1), l >> d.log_c, q % kPerLayer<T, TH>};
 }
 __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0, (d.layers - rank + (1 << d.log_c) - 1) >> d.log_c); }
 
@@ -414,6 +417,7 @@ template <class T> __device__ __noinline__ uint4 edge_vector(const Layer& l, int
     constexpr int E = kPerVec<T>;
     const int a = l.lo - vec * E, b = l.hi - vec * E;
     if (a <= 0 && b >= E) return __ldcs(reinterpret_cast<const uint4*>(l.in) + vec);
+    if (b <= 0 || a >= E) return Vec<T>::none();
     T e[E];
 #pragma unroll
     for (int j = 0; j < E; ++j) e[j] = j >= a && j < b ? reinterpret_cast<const T*>(l.in)[vec * E + j] : from_float<T>(-INFINITY);
@@ -719,37 +723,41 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
 // a ring in shared memory, several blocks on an SM.
 
 constexpr int kStreamRing = 3;            // layers on their way to a block that needs the row once
-constexpr int kStepRing   = 4;            // ... and twice
+constexpr int kStepRing   = 5;            // ... and twice
 
 // Fills a table of any number of layers.  Ends in a barrier.
-template <class T>
+template <class T, int TH = kThreads>
 __device__ __forceinline__ void fill_long_table(Layer* table, const LogitsCut& in, const LogitsCut& out, const Deal& d, int64_t row) {
-    for (int i = threadIdx.x; i < d.layers; i += kThreads) table[i] = layer_of<T, T>(in, out, d, row, 0, i);
+    for (int i = threadIdx.x; i < d.layers; i += TH) table[i] = layer_of<T, T, TH>(in, out, d, row, 0, i);
     __syncthreads();
 }
 // Starts the copies of this thread's two vectors of layer l into place `slot` of the ring, one commit group; nothing but the
 // group past the last layer.
-template <class T>
+template <class T, int TH>
 __device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int slot, int l, int n) {
     if (l < n) {
-        uint4* const to = ring + slot * kVecs + threadIdx.x;
+        uint4* const to = ring + slot * 2 * TH + threadIdx.x;
         const Layer& L = table[l];
-        if (L.hi - L.lo == kPerLayer<T>) {
-            const char* from = L.in + threadIdx.x * 16;
+        const char* from = L.in + threadIdx.x * 16;
+        if (L.hi - L.lo == kPerLayer<T, TH>) {
             copy_async(smem_address(to), from);
-            copy_async(smem_address(to + kThreads), from + kThreads * 16);
+            copy_async(smem_address(to + TH), from + TH * 16);
         } else {
-            to[0] = edge_vector<T>(L, threadIdx.x);
-            to[kThreads] = edge_vector<T>(L, threadIdx.x + kThreads);
+#pragma unroll 1
+            for (int v = 0; v < 2 * TH; v += TH) {
+                const int at = ((int)threadIdx.x + v) * kPerVec<T>;
+                if (at >= L.lo && at + kPerVec<T> <= L.hi) copy_async(smem_address(to + v), from + v * 16);
+                else to[v] = edge_vector<T>(L, threadIdx.x + v);
+            }
         }
     }
     copy_commit();
 }
 // f(layer, first vector, second vector) for this thread's vectors of all layers of the row, in order, through a ring of R
 // layers.
-template <class T, int R, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
+template <class T, int TH, int R, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
 #pragma unroll
-    for (int l = 0; l < R; ++l) load_layer<T>(table, ring, l, l, n);
+    for (int l = 0; l < R; ++l) load_layer<T, TH>(table, ring, l, l, n);
     const uint4* mine = ring + threadIdx.x;
 #pragma unroll 1
     for (int l = 0; l < n; l += R)
@@ -757,22 +765,22 @@ template <class T, int R, class F> __device__ __forceinline__ void stream(const 
         for (int slot = 0; slot < R; ++slot) {
             if (l + slot >= n) break;
             copy_wait<R - 1>();
-            const uint4 a = mine[slot * kVecs], b = mine[slot * kVecs + kThreads];
-            if (l + slot + R < n) load_layer<T>(table, ring, slot, l + slot + R, n);      // the last R layers stay
+            const uint4 a = mine[slot * 2 * TH], b = mine[slot * 2 * TH + TH];
+            if (l + slot + R < n) load_layer<T, TH>(table, ring, slot, l + slot + R, n);      // the last R layers stay
             else copy_commit();
             f(l + slot, a, b);
         }
 }
 // The same backwards, after stream: the last R layers are still in the ring, and of the others those come first that L2 has
 // seen last.
-template <class T, int R, class F> __device__ __forceinline__ void stream_back(const Layer* table, uint4* ring, int n, F f) {
+template <class T, int TH, int R, class F> __device__ __forceinline__ void stream_back(const Layer* table, uint4* ring, int n, F f) {
     const uint4* mine = ring + threadIdx.x;
     int slot = (n - 1) % R;
 #pragma unroll 1
     for (int l = n - 1; l >= 0; --l) {
         copy_wait<R - 1>();
-        const uint4 a = mine[slot * kVecs], b = mine[slot * kVecs + kThreads];
-        if (l >= R) load_layer<T>(table, ring, slot, l - R, n);
+        const uint4 a = mine[slot * 2 * TH], b = mine[slot * 2 * TH + TH];
+        if (l >= R) load_layer<T, TH>(table, ring, slot, l - R, n);
         else copy_commit();
         f(l, a, b);
         slot = slot ? slot - 1 : R - 1;
@@ -893,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     Running running(c);
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;         // of the thread's first and second vectors
     float to_note = -INFINITY;
-    stream<T, kStreamRing>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+    stream<T, kThreads, kStreamRing>(table, ring, n, [&](int l, uint4 a, uint4 b) {
         const typename Vec<T>::Max ma = Vec<T>::max(a), mb = Vec<T>::max(b);
         const float m = Vec<T>::value(Vec<T>::join(ma, mb));
         m0 = Vec<T>::join(m0, ma);
@@ -1058,7 +1066,10 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
 // k / 32 warps.
 
 enum Pass { kForward, kBackward, kStep };
-constexpr int kStepBlocks = 4;
+// Threads of a block.  A wide block has half as many rows in work for the same warps on an SM: the step's second reading
+// finds more of them in L2 (8192 x 128256 bf16: 796 against 828 us), and a row alone takes less long (131 x 50257: 15.2
+// against 18.4 us); the forward pass reads once and is better off with smaller layers (102 against 109 us).
+__host__ __device__ constexpr int threads_of(int pass) { return pass == kForward ? kThreads : kWide; }
 
 // Sum of two values over the first `warps` warps, the only ones to call it; the same on every thread.
 __device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2* scratch) {
@@ -1153,13 +1164,14 @@ __device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill
 // backwards: the layers read last are in the ring, and the ones before them in L2.  The gradients of the entries are stored after
 // the others'.
 template <class T, int kPass>
-__global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
+__global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
                    const __grid_constant__ nereus_distill_t how, float* loss, float* saved, const float* grad_loss) {
     constexpr int E = kPerVec<T>, R = kPass == kStep ? kStepRing : kStreamRing;
+    constexpr int TH = threads_of(kPass), W = TH / 32;
     typedef std::conditional_t<E == 8, uint16_t, uint8_t> Flags;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2 scratch[kWarps], entry_scratch[kWarps];
+    __shared__ float2 scratch[W], entry_scratch[W];
     __shared__ float  rest_scale_of_row, m_of_row;
     const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers, entry_warps = (how.k + 31) >> 5;
     const int64_t row = blockIdx.x;
@@ -1167,29 +1179,29 @@ __global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
     int           id = -1;
     if (tid < how.k) id = how.ids[row * how.k + tid];
     uint4*    ring = reinterpret_cast<uint4*>(dynamic);
-    Layer*    table = reinterpret_cast<Layer*>(ring + R * kVecs);
+    Layer*    table = reinterpret_cast<Layer*>(ring + R * 2 * TH);
     uint32_t* flags = reinterpret_cast<uint32_t*>(table + n);
     if (weight == 0.f) {
         if (tid == 0 && kPass != kBackward) loss[row] = 0.f;
         if (tid < 4 && kPass == kForward) saved[row * 4 + tid] = 0.f;
         if (kPass != kForward) {
-            fill_long_table<T>(table, in, grad, deal, row);
+            fill_long_table<T, TH>(table, in, grad, deal, row);
             for (int i = 0; i < n; ++i)
-                for_edges<T>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
+                for_edges<T, TH>(table, i, [&](int l, int vec) { store_vector<T>(table[l], vec, make_uint4(0, 0, 0, 0)); });
         }
         return;
     }
     if (kPass != kBackward)
-        for (int i = tid; i < n * kThreads * (int)sizeof(Flags) / 4; i += kThreads) flags[i] = 0;
-    fill_long_table<T>(table, in, kPass == kForward ? LogitsCut() : grad, deal, row);
+        for (int i = tid; i < n * TH * (int)sizeof(Flags) / 4; i += TH) flags[i] = 0;
+    fill_long_table<T, TH>(table, in, kPass == kForward ? LogitsCut() : grad, deal, row);
 
     Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
     if (warp < entry_warps) {
         fetch_entry<T>(e, id, in, how, row);
         if (kPass != kBackward && e.id >= 0) {
-            const Place at = place_of<T>(in, deal, row, e.id);
-            const int   vec = at.position / E, slot = at.layer * kThreads + vec % kThreads;
-            const int   bit = slot * 2 * E + vec / kThreads * E + at.position % E;
+            const Place at = place_of<T, TH>(in, deal, row, e.id);
+            const int   vec = at.position / E, slot = at.layer * TH + vec % TH;
+            const int   bit = slot * 2 * E + vec / TH * E + at.position % E;
             atomicOr(&flags[bit >> 5], 1u << (bit & 31));
         }
     }
@@ -1200,11 +1212,11 @@ __global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
         const Flags* mine = reinterpret_cast<const Flags*>(flags) + tid;
         Running running(c);
         typename Vec<T>::Max top = Vec<T>::lowest();
-        stream<T, R>(table, ring, n, [&](int l, uint4 a, uint4 b) {
+        stream<T, TH, R>(table, ring, n, [&](int l, uint4 a, uint4 b) {
             const typename Vec<T>::Max v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
             top = Vec<T>::join(top, v);
             running.see(Vec<T>::value(v));
-            if (const uint32_t f = mine[l * kThreads]) {
+            if (const uint32_t f = mine[l * TH]) {
                 a = without<T>(a, f);
                 b = without<T>(b, f >> E);
             }
@@ -1220,7 +1232,7 @@ __global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
         if (kPass == kBackward) {
             m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
         } else {
-            const float2 part = lane < kWarps ? scratch[lane] : make_float2(-INFINITY, 0.f);
+            const float2 part = lane < W ? scratch[lane] : make_float2(-INFINITY, 0.f);
             m = warp_max(part.x);
             rest = warp_sum(part.y * scale_to(part.x, m, c));
             total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
@@ -1272,17 +1284,17 @@ __global__ void __launch_bounds__(kThreads, kPass == kStep ? kStepBlocks : 4)
         auto write = [&](int l, uint4 a, uint4 b) {
             const Layer& L = table[l];
             const uint4  ga = gradient(a), gb = gradient(b);
-            if (L.vec_out && L.hi - L.lo == kPerLayer<T>) {
+            if (L.vec_out && L.hi - L.lo == kPerLayer<T, TH>) {
                 uint4* const to = reinterpret_cast<uint4*>(L.out) + tid;
                 __stcs(to, ga);
-                __stcs(to + kThreads, gb);
+                __stcs(to + TH, gb);
             } else {
                 store_vector<T>(L, tid, ga);
-                store_vector<T>(L, tid + kThreads, gb);
+                store_vector<T>(L, tid + TH, gb);
             }
         };
-        if constexpr (kPass == kStep) stream_back<T, R>(table, ring, n, write);
-        else stream<T, R>(table, ring, n, write);
+        if constexpr (kPass == kStep) stream_back<T, TH, R>(table, ring, n, write);
+        else stream<T, TH, R>(table, ring, n, write);
     }
     __syncthreads();                                  // the entries' places have been written as of the rest
     if (e.id >= 0) {
@@ -1417,7 +1429,7 @@ int device_of(Device* d) {
 
 // Deals a row out over the fewest blocks whose share has at most `most` layers and takes at most kSmemShare bytes, at
 // `per_layer` a layer and `fixed` once.  The number of rows has no part in it: a row's sums come out the same in any batch.
-Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int most) {
+Deal deal_of(const nereus_logits_t& v, int threads, int64_t per_layer, int64_t fixed, int most) {
     Deal d;
     const int64_t e = 16 / size_of(v.dtype), w = held_cols(v, 0), bytes = v.row_stride * size_of(v.dtype);
     d.aligned = v.rows < 2 || bytes % 16 == 0;
@@ -1425,7 +1437,7 @@ Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int mos
         if (held_cols(v, s) && (uintptr_t)v.shard[s] % 16) d.aligned = 0;
     const int64_t vecs = d.aligned ? (w + e - 1) / e : (w + 2 * e - 2) / e;
     const int64_t used = (v.vocab + v.shard_cols - 1) / v.shard_cols;
-    d.per_shard = (int)((vecs + kVecs - 1) / kVecs);
+    d.per_shard = (int)((vecs + 2 * threads - 1) / (2 * threads));
     d.layers = (int)(d.per_shard * used);
     d.log_c = 0;
     auto share = [&] { return (int64_t)(d.layers + (1 << d.log_c) - 1) >> d.log_c; };
@@ -1434,46 +1446,29 @@ Deal deal_of(const nereus_logits_t& v, int64_t per_layer, int64_t fixed, int mos
     return d;
 }
 
-// What is kept of a kernel's launches on a device.
-struct Kept {
-    std::atomic<bool>     opted{false};
-    std::atomic<uint64_t> clusters[4];            // for each cluster size: shared memory << 20 | clusters that fit at once
-};
-// Launches a kernel with a cluster of blocks for each row, or, where the kernel goes from row to row, for as many rows as
-// fit on the device at once (and no more than give every cluster the same number of rows, or one less).
+// Launches a kernel with a cluster of blocks for each row.  `opted`: whether the kernel has been given its shared memory,
+// per device.
 template <class... P, class... A>
-int launch(void (*kernel)(P...), Kept* kept, int64_t rows, bool loops, const Deal& d, int64_t smem, const Device& dev,
-           cudaStream_t stream, A... args) {
+int launch(void (*kernel)(P...), std::atomic<bool>* opted, int threads, int64_t rows, const Deal& d, int64_t smem,
+           const Device& dev, cudaStream_t stream, A... args) {
     if (smem > dev.smem) return NEREUS_ERR_TOO_LARGE;
-    Kept& of = kept[dev.id];
-    if (!of.opted.load()) {
+    if (!opted[dev.id].load()) {
         NEREUS_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem));
-        of.opted.store(true);
+        opted[dev.id].store(true);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((unsigned)(rows << d.log_c));
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr = {};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1u << d.log_c;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (loops) {
-        uint64_t fit = of.clusters[d.log_c].load();
-        if ((int64_t)(fit >> 20) != smem) {
-            int n = 0;
-            cfg.gridDim = dim3(1u << d.log_c);
-            NEREUS_CUDA(cudaOccupancyMaxActiveClusters(&n, kernel, &cfg));
-            fit = (uint64_t)smem << 20 | (uint64_t)std::max(1, n);
-            of.clusters[d.log_c].store(fit);
-        }
-        const int64_t most = (int64_t)(fit & 0xfffff), each = (rows + most - 1) / most;
-        rows = (rows + each - 1) / each;
+    if (d.log_c) {
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 1u << d.log_c;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
     }
-    cfg.gridDim = dim3((unsigned)(rows << d.log_c));
-    if (!d.log_c) cfg.numAttrs = 0;
     NEREUS_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
     return NEREUS_OK;
 }
@@ -1481,12 +1476,13 @@ int launch(void (*kernel)(P...), Kept* kept, int64_t rows, bool loops, const Dea
 template <class T, int kPass>
 int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
                    const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
-    static Kept kept[kMaxDevices];
+    constexpr int TH = threads_of(kPass);
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    const Deal    d = deal_of(in, 0, 0, 1 << 30);
-    const int64_t smem = (kPass == kStep ? kStepRing : kStreamRing) * kVecs * 16 + d.layers * (int64_t)(sizeof(Layer) + (kPass == kBackward ? 0 : kThreads * kPerVec<T> / 4));
-    return launch(distill_kernel<T, kPass>, kept, in.rows, false, d, smem, dev, stream, cut_of(in),
+    const Deal    d = deal_of(in, TH, 0, 0, 1 << 30);
+    const int64_t smem = (kPass == kStep ? kStepRing : kStreamRing) * 2 * TH * 16 + d.layers * (int64_t)(sizeof(Layer) + (kPass == kBackward ? 0 : TH * kPerVec<T> / 4));
+    return launch(distill_kernel<T, kPass>, opted, TH, in.rows, d, smem, dev, stream, cut_of(in),
                   kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
 }
 
@@ -1508,31 +1504,31 @@ int distill(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
 template <class TI, class TO, class Count>
 int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const nereus_penalties_t& how, int32_t* token,
                    float* lse, cudaStream_t stream) {
-    static Kept kept[kMaxDevices];
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
                               (how.bias_ids ? kVecs : 0) + (how.mask ? (kPerLayer<TI> / 32 + 1) * 4 : 0);
     const int64_t fixed = (how.bias_ids ? 2 * kHash * 4 : 0) + 16 + kRing * kVecs * 16;
-    Deal d = deal_of(in, per_layer, fixed, 4);
+    Deal d = deal_of(in, kThreads, per_layer, fixed, 4);
     // what does not fit is done in rounds
     while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
-    return launch(process_kernel<TI, TO, Count>, kept, in.rows, false, d, d.mine * per_layer + fixed, dev, stream,
+    return launch(process_kernel<TI, TO, Count>, opted, kThreads, in.rows, d, d.mine * per_layer + fixed, dev, stream,
                   cut_of(in), cut_of(out), d, how, token, lse);
 }
 
 template <class T>
 int top_launch(const nereus_logits_t& in, int k, float temperature, float* values, int32_t* ids, float* lse, cudaStream_t stream) {
-    static Kept kept[kMaxDevices];
+    static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    Deal d = deal_of(in, 0, 0, 1 << 30);
+    Deal d = deal_of(in, kThreads, 0, 0, 1 << 30);
     // warps of which every lane has a vector, at least: how many of the k largest each has to vouch for
     const int64_t w = held_cols(in, 0), vecs = (w + kPerVec<T> - 1) / kPerVec<T>;
     const int     full = (int)std::min<int64_t>(vecs / 32, kWarps), j = full ? (k + full - 1) / full : 1;
     const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)sizeof(Layer) +
                          (d.layers + kNote<T> - 1) / kNote<T> * (int64_t)kThreads * 2;
-    return launch(top_kernel<T>, kept, in.rows, false, d, smem, dev, stream, cut_of(in), d, k, j, 1.f / temperature, values, ids, lse);
+    return launch(top_kernel<T>, opted, kThreads, in.rows, d, smem, dev, stream, cut_of(in), d, k, j, 1.f / temperature, values, ids, lse);
 }
 
 }  // namespace
