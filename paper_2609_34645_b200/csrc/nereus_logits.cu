@@ -346,8 +346,8 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 // counting into the peers' shared memory was no faster (256 rows of up to 16384 tokens: 166 against 170 us) and takes two
 // cluster barriers.
 
-constexpr int kRing   = 3;                // layers on their way to a block
 constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
+constexpr int kRing   = 3;                // layers on their way to a block
 
 // Counter of a column, 0 for a token that is not in the history: the top bit "in the prompt", the others "generated so
 // often".
@@ -424,10 +424,11 @@ template <class T> __device__ __noinline__ uint4 edge_vector(const Layer& l, int
     return *reinterpret_cast<const uint4*>(e);
 }
 // The bias of a token that has one.
-__device__ __noinline__ float bias_of(const int32_t* ids, const int32_t* values, int token) {
-    uint32_t h = (uint32_t)token * 2654435761u % kHash;
+__device__ __forceinline__ uint32_t hash_of(int token) { return (uint32_t)token * 2654435761u >> 16 & (kHash - 1); }
+__device__ __noinline__ float bias_of(const int32_t* ids, const float* values, int token) {
+    uint32_t h = hash_of(token);
     while (ids[h] != token && ids[h] != -1) h = (h + 1) % kHash;     // the table is never full
-    return __int_as_float(values[h]);
+    return values[h];
 }
 template <int E> __device__ __forceinline__ float far_sum(const float (&x)[E], float base) {
     float r = 0.f;
@@ -455,8 +456,9 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     uint32_t*  words = reinterpret_cast<uint32_t*>(ring + kRing * kVecs);                    // mask words
     uint32_t*  biased = words + (how.mask ? (deal.mine * kMaskWords + 3) / 4 * 4 : 0);        // a byte per vector
     int32_t*   hash_id = reinterpret_cast<int32_t*>(biased + (how.bias_ids ? deal.mine * kVecs / 4 : 0));
-    int32_t*   hash_entry = hash_id + kHash;                  // the last entry of the id, then its value
-    uint32_t*  counters = reinterpret_cast<uint32_t*>(hash_id + (how.bias_ids ? 2 * kHash : 0));
+    int32_t*   hash_entry = hash_id + kHash;                  // the last entry of the id
+    float*     hash_value = reinterpret_cast<float*>(hash_entry + kHash);
+    uint32_t*  counters = reinterpret_cast<uint32_t*>(hash_id + (how.bias_ids ? 3 * kHash : 0));
 
     const Penalty penalty = penalty_of(how.repetition ? how.repetition[row] : 1.f, how.frequency ? how.frequency[row] : 0.f,
                                        how.presence ? how.presence[row] : 0.f);
@@ -485,6 +487,24 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     };
     for (int first = 0; first < n_all; first += deal.mine) {      // one round unless the counters do not fit
         const int n = min(deal.mine, n_all - first);
+        // what is a memory latency away and needed soon: the first tokens of the history, and the biases
+        constexpr int kAhead = 4, kMost = (NEREUS_BIAS_MAX + kThreads - 1) / kThreads;
+        int   ahead[kAhead], bias_id[kMost];
+        float bias_value[kMost];
+        if (how.history) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+                ahead[j] = tid + j * kThreads < how.history_len ? how.history[row * how.history_stride + tid + j * kThreads] : -1;
+        }
+        if (how.bias_ids) {
+#pragma unroll
+            for (int j = 0; j < kMost; ++j) {
+                const bool    is = tid + j * kThreads < how.bias_count;
+                const int64_t at = row * how.bias_count + tid + j * kThreads;
+                bias_id[j] = is ? how.bias_ids[at] : -1;
+                bias_value[j] = is ? how.bias_values[at] : 0.f;
+            }
+        }
         __syncthreads();
         const uint32_t whole = fill_table<TI, TO>(table, &masks, in, out, deal, row, rank, first, n).x;
         // this thread's two vectors of layer l into their places in the ring
@@ -496,8 +516,12 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
                     copy_async(smem_address(to), from);
                     copy_async(smem_address(to + kThreads), from + kThreads * 16);
                 } else {
-                    to[0] = edge_vector<TI>(table[l], tid);
-                    to[kThreads] = edge_vector<TI>(table[l], tid + kThreads);
+#pragma unroll 1
+                    for (int v = 0; v < kVecs; v += kThreads) {
+                        const int p = (tid + v) * E;
+                        if (p >= table[l].lo && p + E <= table[l].hi) copy_async(smem_address(to + v), table[l].in + (tid + v) * 16);
+                        else to[v] = edge_vector<TI>(table[l], tid + v);
+                    }
                 }
             }
             copy_commit();
@@ -526,51 +550,47 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
                 const int   l = p.layer - first;
                 if (p.rank == rank && (uint32_t)l < (uint32_t)n) count_token<Count>(counters, l * kPerLayer<TI> + p.position, i >= prompt);
             };
-            int i = tid;
-            for (; i + 7 * kThreads < total; i += 8 * kThreads) {
-                int id[8];
+            // four tokens a thread at a time, the next four on their way
+            for (int i = tid; i - tid < total; i += kAhead * kThreads) {
+                int id[kAhead];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) id[j] = hist[i + j * kThreads];
+                for (int j = 0; j < kAhead; ++j) {
+                    const int next = i + (j + kAhead) * kThreads;
+                    id[j] = ahead[j];
+                    ahead[j] = next < total ? hist[next] : -1;
+                }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) count(i + j * kThreads, id[j]);
+                for (int j = 0; j < kAhead; ++j)
+                    if (i + j * kThreads < total) count(i + j * kThreads, id[j]);
             }
-#pragma unroll 4
-            for (; i < total; i += kThreads) count(i, hist[i]);
         }
         if (how.bias_ids) {
-            // slot of the id in the hash table, or -1 where another block holds the token
-            auto slot_of = [&](int i) {
-                const int id = how.bias_ids[row * how.bias_count + i];
-                if ((uint32_t)id >= (uint32_t)in.vocab) return -1;
-                const Place p = place_of<TI>(in, deal, row, id);
-                const int   l = p.layer - first;
-                if (p.rank != rank || (uint32_t)l >= (uint32_t)n) return -1;
-                const int vec = l * kVecs + p.position / E;
-                atomicOr(biased + vec / 4, 1u << (vec % 4 * 8 + p.position % E));
-                uint32_t h = (uint32_t)id * 2654435761u % kHash;
-                for (int probe = 0; probe < kHash; ++probe, h = (h + 1) % kHash) {
-                    const int was = atomicCAS(&hash_id[h], -1, id);
-                    if (was == -1 || was == id) break;
-                }
-                return (int)h;
-            };
-            // of the entries of one id the last counts; then its value takes the entry's place in the table
-            constexpr int kMost = (NEREUS_BIAS_MAX + kThreads - 1) / kThreads;
+            // an entry's slot in the hash table, or -1 where another block holds the token
             int slot[kMost];
 #pragma unroll
             for (int j = 0; j < kMost; ++j) {
-                const int i = tid + j * kThreads;
-                slot[j] = i < how.bias_count ? slot_of(i) : -1;
-                if (slot[j] >= 0) atomicMax(&hash_entry[slot[j]], i);
+                const int id = bias_id[j];
+                slot[j] = -1;
+                if (j * kThreads >= how.bias_count) continue;
+                if ((uint32_t)id >= (uint32_t)in.vocab) continue;
+                const Place p = place_of<TI>(in, deal, row, id);
+                const int   l = p.layer - first;
+                if (p.rank != rank || (uint32_t)l >= (uint32_t)n) continue;
+                const int vec = l * kVecs + p.position / E;
+                atomicOr(biased + vec / 4, 1u << (vec % 4 * 8 + p.position % E));
+                uint32_t h = hash_of(id);
+                for (;; h = (h + 1) % kHash) {             // over twice as many slots as entries: one is free
+                    const int was = atomicCAS(&hash_id[h], -1, id);
+                    if (was == -1 || was == id) break;
+                }
+                slot[j] = (int)h;
+                atomicMax(&hash_entry[h], tid + j * kThreads);
             }
             __syncthreads();
-            bool last[kMost];
-#pragma unroll
-            for (int j = 0; j < kMost; ++j) last[j] = slot[j] >= 0 && hash_entry[slot[j]] == tid + j * kThreads;
-            __syncthreads();
+            // of the entries of one id the last counts
 #pragma unroll
             for (int j = 0; j < kMost; ++j)
-                if (last[j]) hash_entry[slot[j]] = __float_as_int(how.bias_values[row * how.bias_count + tid + j * kThreads]);
+                if (slot[j] >= 0 && hash_entry[slot[j]] == tid + j * kThreads) hash_value[slot[j]] = bias_value[j];
         }
         __syncthreads();
 
@@ -611,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
                     if (f) {
 #pragma unroll
                         for (int j = 0; j < E; ++j)
-                            if (f >> j & 1u) x[i][j] = __fadd_rn(x[i][j], bias_of(hash_id, hash_entry, L.token + vec * E + j));
+                            if (f >> j & 1u) x[i][j] = __fadd_rn(x[i][j], bias_of(hash_id, hash_value, L.token + vec * E + j));
                     }
                 }
             }
@@ -1509,7 +1529,7 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
     if (int rc = device_of(&dev)) return rc;
     const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
                               (how.bias_ids ? kVecs : 0) + (how.mask ? (kPerLayer<TI> / 32 + 1) * 4 : 0);
-    const int64_t fixed = (how.bias_ids ? 2 * kHash * 4 : 0) + 16 + kRing * kVecs * 16;
+    const int64_t fixed = (how.bias_ids ? 12 * kHash : 0) + 16 + kRing * kVecs * 16;
     Deal d = deal_of(in, kThreads, per_layer, fixed, 4);
     // what does not fit is done in rounds
     while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
