@@ -441,11 +441,12 @@ int nereus_static_status(int* device_status);
  * modulo 16 bytes on the read and the written side are moved in 16-byte vectors.
  * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and
  * may be captured into a CUDA graph.  rows = 0 is a call that does nothing.  A row's results are the same, bit for
- * bit, whatever other rows the call has and wherever the row stands among them.
+ * bit, whatever other rows the call has and wherever the row stands among them, as long as its shards start alike modulo
+ * 16 bytes.
  * Common errors: ARG (null pointer, non-positive size, a shard or stride too small for its columns), UNSUPPORTED
  * (dtype), ALIGN (a pointer that is not aligned to its element), MISMATCH (the written view has other rows,
  * vocabulary or cut than the read one), ALIAS (a written view overlaps a read one without being it, or itself),
- * TOO_LARGE (limits named with each call), CUDA. */
+ * TOO_LARGE (limits named with each call; rows > 2^24), CUDA.  The buffers are on the current device. */
 #define NEREUS_VOCAB_MAX_TP 64
 typedef struct {
     int32_t dtype;                 /* NEREUS_BF16 or NEREUS_FP32 */
@@ -494,7 +495,8 @@ int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out,
 /* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
  * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of
  * exp(x / temperature).  NaN is never taken; a row with fewer than k other logits ends in (-inf, -1).
- * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite), TOO_LARGE (vocab). */
+ * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite), TOO_LARGE (a row
+ * whose records do not fit shared memory; vocab <= 2^18 always does). */
 #define NEREUS_TOP_MAX_K 256
 int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, float* values, int32_t* ids, float* lse,
                        void* cuda_stream);
@@ -533,10 +535,11 @@ int nereus_distill_forward(const nereus_logits_t* in, const nereus_distill_t* ho
  * in->dtype).  grad_loss (device, [rows]) or NULL = 1.  grad == in is allowed. */
 int nereus_distill_backward(const nereus_logits_t* in, const nereus_distill_t* how, const float* saved,
                             const float* grad_loss, const nereus_logits_t* grad, void* cuda_stream);
-/* Both in one launch, the row kept on the chip between its sums and its gradient: loss, and grad = weight[r] * dD/dx,
- * the gradient of the sum of the losses.  grad == in is allowed.
+/* Both in one launch: loss, and grad = weight[r] * dD/dx, the gradient of the sum of the losses.  The row goes through the
+ * chip for its sums and once more for the gradient, the second time as far as it can out of shared memory and L2.
+ * grad == in is allowed.
  * Errors of the three: common, ARG (k, divergence, beta, temperature), UNSUPPORTED (lse == NULL with another divergence
- * than the forward KL; grad->dtype), TOO_LARGE (vocab). */
+ * than the forward KL; grad->dtype), TOO_LARGE (a row whose records do not fit shared memory; vocab <= 2^18 always does). */
 int nereus_distill_step(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
                         const nereus_logits_t* grad, void* cuda_stream);
 

@@ -4,18 +4,17 @@
 //
 // Logits come cut by vocabulary into column shards, one device buffer each.  All three walk rows of some 100,000
 // elements with a handful of operations on each, so their floor is HBM bandwidth: every logit read once, every written
-// one stored once.  The common frame:
-//   * A row belongs to one thread-block cluster of C = 1, 2, 4 or 8 blocks of 256 threads; its 16-byte vectors are dealt
-//     out in layers of 512 (8 KiB, two vectors a thread), layer l to block l % C.  A layer lies inside one shard, so that everything about it
-//     but the thread's own vector is the same for the block: one 32-byte record per layer in shared memory.
-//   * A block's share of the row stays in shared memory (cp.async, every thread reads back only the vectors that it
-//     copied itself, so arrival needs no barrier and no wait that could hang), because the result needs the row's sums
-//     before the first element can be written.  C is the smallest for which three blocks fit on an SM, so that one
-//     block loads while another reduces and a third stores.  The number of rows has no part in it, so that a row's
-//     result is the same, bit for bit, in any batch.
-//   * The blocks of a cluster exchange a few numbers through distributed shared memory and one cluster barrier.
+// one stored once; 2 exponentials an element (16 a clock and SM) come next.  What the kernels share:
+//   * A row's 16-byte vectors are dealt out in layers of two vectors a thread.  A layer lies inside one shard, so that
+//     everything about it but the thread's own vectors is the same for the block: one 32-byte record in shared memory.
+//   * Elements come through a ring of layers in shared memory by cp.async.  Every thread reads back only what it copied
+//     itself, so that an arrival needs no barrier, and no wait that could hang: nothing here spins on a flag.
 //   * Rows of any alignment: vectors that a row fills only in part (its ends, where it does not start on a 16-byte
 //     boundary) are read and written element by element; what lies outside the row is -inf in shared memory.
+//   * The number of rows decides nothing but the grid: a row's result is the same, bit for bit, in any batch in which its
+//     shards start alike modulo 16 bytes.
+//   * One block takes a whole row where that leaves it little to keep (teacher_top, distillation), a cluster of 1 to 8
+//     blocks where every column needs a counter (process).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -240,23 +239,22 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
-// Fills the block's table with its layers first .. first + n - 1, n <= 32.  Returned through `masks`: which layers lie
-// wholly inside the row, and which of these can also be written in 16-byte vectors.  Ends in a barrier.
+// Fills the block's table with its layers first .. first + n - 1, n <= 32; bit i of the answer: layer i lies wholly inside
+// the row.  Ends in a barrier.
 template <class TI, class TO>
-__device__ __forceinline__ uint2 fill_table(Layer* table, uint2* masks, const LogitsCut& in, const LogitsCut& out, const Deal& d,
+__device__ __forceinline__ uint32_t fill_table(Layer* table, uint32_t* mask, const LogitsCut& in, const LogitsCut& out, const Deal& d,
                                             int64_t row, int rank, int first, int n) {
     if (threadIdx.x < 32) {
         Layer l = {nullptr, nullptr, 0, 0, 0, 0};
         if ((int)threadIdx.x < n) table[threadIdx.x] = l = layer_of<TI, TO>(in, out, d, row, rank, first + (int)threadIdx.x);
-        const bool     whole = l.hi - l.lo == kPerLayer<TI>;
-        const uint32_t a = __ballot_sync(0xffffffffu, whole), b = __ballot_sync(0xffffffffu, whole && l.vec_out);
-        if (threadIdx.x == 0) *masks = make_uint2(a, b);
+        const uint32_t whole = __ballot_sync(0xffffffffu, l.hi - l.lo == kPerLayer<TI>);
+        if (threadIdx.x == 0) *mask = whole;
     }
     __syncthreads();
-    return *masks;
+    return *mask;
 }
 
-// f(layer, vector of the layer) for every vector of this thread in a layer that the row fills in part.
+// f(layer, vector of the layer) for every vector of this thread in layer i that holds elements of the row.
 template <class T, int TH = kThreads, class F> __device__ __forceinline__ void for_edges(const Layer* table, int i, F f) {
     const int lo = table[i].lo, hi = table[i].hi;
 #pragma unroll 1
@@ -344,7 +342,10 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 // per column.  The running (maximum, where it is, sum of exponentials) stays on the thread.
 // Every block reads the whole history (from L2) and keeps what falls into its share: reading it once per cluster and
 // counting into the peers' shared memory was no faster (256 rows of up to 16384 tokens: 166 against 170 us) and takes two
-// cluster barriers.
+// cluster barriers.  A share is at most four layers where counters allow, for as many blocks as a small batch can use.
+// Bound by instruction issue (penalties and history) and, below a hundred rows, by the chain of phases within a block, not
+// by HBM: 256 x 152064 fp32 with histories up to 16384 takes 165 us, 2.0 TB/s; 64 x 128256 bf16 to fp32 30 us; one row of
+// 128256 9 us.
 
 constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
 constexpr int kRing   = 3;                // layers on their way to a block
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ float2 scratch[kWarps], from_peers[kMaxCtas];
     __shared__ int    id_scratch[kWarps], id_peers[kMaxCtas];
-    __shared__ uint2  masks;
+    __shared__ uint32_t whole_layers;
     const int     tid = threadIdx.x, rank = blockIdx.x & ((1 << deal.log_c) - 1);
     const int64_t row = blockIdx.x >> deal.log_c;
     if (deal.log_c) cluster_arrive();              // this block runs: its shared memory may be written
@@ -506,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
             }
         }
         __syncthreads();
-        const uint32_t whole = fill_table<TI, TO>(table, &masks, in, out, deal, row, rank, first, n).x;
+        const uint32_t whole = fill_table<TI, TO>(table, &whole_layers, in, out, deal, row, rank, first, n);
         // this thread's two vectors of layer l into their places in the ring
         auto fetch = [&](int l) {
             if (l < n) {
@@ -863,6 +864,8 @@ template <class T> __device__ __forceinline__ uint4 without(uint4 v, uint32_t bi
 // row's k-th largest from below, and for most rows some 1.4 k elements reach it.  Only the vectors whose note does are read
 // again, and what is found in them is ranked by counting, as one 64-bit key of (value, lower id).  Rows of so few distinct
 // values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly.
+// 4096 x 128256 bf16, k = 64: 233-243 us, 4.3-4.5 TB/s read, the exponentials at 60% of their rate and four blocks an SM
+// short of hiding the selection (a quarter of a row's time); 512 x 152064 fp32, k = 128: 76 us, 4.1 TB/s.
 
 constexpr int kCandidates = 1024;
 template <class T> constexpr int kNote = (int)sizeof(T) / 2;          // layers of a note
@@ -1183,6 +1186,10 @@ __device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill
 // two bytes (fp32: one) for a thread's two vectors of a layer.  The step lets it go by a second time for the gradient,
 // backwards: the layers read last are in the ring, and the ones before them in L2.  The gradients of the entries are stored after
 // the others'.
+// Forward, 1024 x 152064 fp32: 102-106 us, 5.9-6.1 TB/s, HBM.  Backward, 2048 x 128256 bf16: 190 us, 5.5 TB/s, HBM with as
+// many bytes written as read.  Step, 8192 x 128256 bf16, a quarter of the rows without weight: 800-830 us, 4.4-4.6 TB/s of
+// the bytes that have to move; about half of the second reading misses L2, which 300 rows in work fill, and HBM then
+// carries 5.4 TB/s.  (Holding the row in a cluster's shared memory instead took 930 us: the cluster's exchange left HBM idle.)
 template <class T, int kPass>
 __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
