@@ -345,7 +345,7 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 // cluster barriers.  A share is at most four layers where counters allow, for as many blocks as a small batch can use.
 // Bound by instruction issue (penalties and history) and, below a hundred rows, by the chain of phases within a block, not
 // by HBM: 256 x 152064 fp32 with histories up to 16384 takes 165 us, 2.0 TB/s; 64 x 128256 bf16 to fp32 30 us; one row of
-// 128256 9 us.
+// 128256 9 us of GPU time.
 
 constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
 constexpr int kRing   = 3;                // layers on their way to a block
@@ -864,8 +864,8 @@ template <class T> __device__ __forceinline__ uint4 without(uint4 v, uint32_t bi
 // row's k-th largest from below, and for most rows some 1.4 k elements reach it.  Only the vectors whose note does are read
 // again, and what is found in them is ranked by counting, as one 64-bit key of (value, lower id).  Rows of so few distinct
 // values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly.
-// 4096 x 128256 bf16, k = 64: 233-243 us, 4.3-4.5 TB/s read, the exponentials at 60% of their rate and four blocks an SM
-// short of hiding the selection (a quarter of a row's time); 512 x 152064 fp32, k = 128: 76 us, 4.1 TB/s.
+// 4096 x 128256 bf16, k = 64: 233-244 us, 4.3-4.5 TB/s read, the exponentials at 60% of their rate and four blocks an SM
+// short of hiding the selection (a quarter of a row's time); 512 x 152064 fp32, k = 128: 76-80 us, 3.9-4.1 TB/s.
 
 constexpr int kCandidates = 1024;
 template <class T> constexpr int kNote = (int)sizeof(T) / 2;          // layers of a note
@@ -1184,12 +1184,12 @@ __device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill
 
 // A row goes by once for its sums (see above: rows that are read once); which elements are entries stands in shared memory,
 // two bytes (fp32: one) for a thread's two vectors of a layer.  The step lets it go by a second time for the gradient,
-// backwards: the layers read last are in the ring, and the ones before them in L2.  The gradients of the entries are stored after
-// the others'.
-// Forward, 1024 x 152064 fp32: 102-106 us, 5.9-6.1 TB/s, HBM.  Backward, 2048 x 128256 bf16: 190 us, 5.5 TB/s, HBM with as
+// backwards: the layers read last are in the ring, and some of the ones before them in L2.  The gradients of the entries are
+// stored after the others'.
+// Forward, 1024 x 152064 fp32: 102-106 us, 5.9-6.1 TB/s, HBM.  Backward, 2048 x 128256 bf16: 190-194 us, 5.4-5.5 TB/s, HBM with as
 // many bytes written as read.  Step, 8192 x 128256 bf16, a quarter of the rows without weight: 800-830 us, 4.4-4.6 TB/s of
-// the bytes that have to move; about half of the second reading misses L2, which 300 rows in work fill, and HBM then
-// carries 5.4 TB/s.  (Holding the row in a cluster's shared memory instead took 930 us: the cluster's exchange left HBM idle.)
+// the bytes that have to move; about two thirds of the second reading come from HBM (2368 rows, 455 MB of them live: 750 MB
+// read, 556 written), which at that traffic per row carries 5.4 TB/s.  (Holding the row in a cluster's shared memory instead took 930 us: the cluster's exchange left HBM idle.)
 template <class T, int kPass>
 __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
