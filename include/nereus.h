@@ -495,10 +495,10 @@ int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out,
 /* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
  * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of
  * exp(x / temperature).  NaN is never taken; a row with fewer than k other logits ends in (-inf, -1).
- * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite), TOO_LARGE (a row
+ * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite in fp32), TOO_LARGE (a row
  * whose records do not fit shared memory; vocab <= 2^18 always does). */
 #define NEREUS_TOP_MAX_K 256
-int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, float* values, int32_t* ids, float* lse,
+int nereus_teacher_top(const nereus_logits_t* in, int k, double temperature, float* values, int32_t* ids, float* lse,
                        void* cuda_stream);
 
 /* TRAINING: distillation from a teacher's top logits.  A row's tokens fall into the groups of its entries, one token
@@ -511,7 +511,9 @@ int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, floa
  *   NEREUS_REVERSE_KL   D = sum_g Q_g log(Q_g / P_g), P_rest at least 2^-24 (the resolution of its sum)
  *   NEREUS_JENSEN       D = beta KL(P || M) + (1 - beta) KL(Q || M), M = beta P + (1 - beta) Q, 0 < beta < 1
  * Its gradient is dD/dx_v = Q_v (f_g(v) - sum_g Q_g f_g) / T with f = -P/Q, log(Q/P), (1 - beta) log(Q/M).
- * loss[r] = weight[r] * D.  A row of weight 0 is not read: its loss, saved sums and gradient are 0, whatever it holds.
+ * What a row has once per entry is worked out in 64 bits from the values as they are given: D and the gradient keep their
+ * digits where the student is near the teacher or the teacher leaves next to nothing to the rest.  The sum over the rest is
+ * fp32, 1e-7 off.  loss[r] = weight[r] * D.  A row of weight 0 is not read: its loss, saved sums and gradient are 0, whatever it holds.
  * Entries of one row have distinct ids; ids outside [0, vocab) are unused entries; a row without entries has no loss.
  * A student that gives an entry no mass at all where the teacher does has loss +inf in the forward KL (and a finite
  * gradient); a teacher that gives an entry none where the student does, in the reverse KL, loss +inf and gradient NaN. */
@@ -521,8 +523,8 @@ int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, floa
 typedef struct {
     int32_t k;                     /* entries per row, 1..NEREUS_TOP_MAX_K */
     int32_t divergence;
-    float   beta;                  /* NEREUS_JENSEN only */
-    float   temperature;
+    double  beta;                  /* NEREUS_JENSEN only */
+    double  temperature;           /* above 0 and finite in fp32 too */
     const float*   values;         /* device [rows, k]: the teacher's logits, as nereus_teacher_top leaves them */
     const int32_t* ids;            /* device [rows, k] */
     const float*   lse;            /* device [rows]: the teacher's log-sum-exp of logit / T, or NULL */

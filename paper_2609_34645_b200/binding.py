@@ -112,8 +112,8 @@ class Penalties(ctypes.Structure):
 
 class Distill(ctypes.Structure):
     """nereus_distill_t."""
-    _fields_ = [("k", ctypes.c_int32), ("divergence", ctypes.c_int32), ("beta", ctypes.c_float),
-                ("temperature", ctypes.c_float), ("values", ctypes.c_void_p), ("ids", ctypes.c_void_p),
+    _fields_ = [("k", ctypes.c_int32), ("divergence", ctypes.c_int32), ("beta", ctypes.c_double),
+                ("temperature", ctypes.c_double), ("values", ctypes.c_void_p), ("ids", ctypes.c_void_p),
                 ("lse", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
 
 
@@ -171,7 +171,7 @@ _SIGS = {
     "nereus_transition_validate": [_vp],
     "nereus_debug_set_rect": [_vp, _i, _P(Rect)],
     "nereus_logits_process": [_P(Logits), _P(Logits), _P(Penalties), _vp, _vp, _vp],
-    "nereus_teacher_top": [_P(Logits), _i, ctypes.c_float, _vp, _vp, _vp, _vp],
+    "nereus_teacher_top": [_P(Logits), _i, ctypes.c_double, _vp, _vp, _vp, _vp],
     "nereus_distill_forward": [_P(Logits), _P(Distill), _vp, _vp, _vp],
     "nereus_distill_backward": [_P(Logits), _P(Distill), _vp, _vp, _P(Logits), _vp],
     "nereus_distill_step": [_P(Logits), _P(Distill), _vp, _P(Logits), _vp],

@@ -295,11 +295,23 @@ __device__ __forceinline__ Base base_of(float m, float c) {
 __device__ __forceinline__ float scale_to(float m, float to, float c) {
     return m == to ? 1.f : exp2_approx((m - to) * c);
 }
-template <class T> __device__ __forceinline__ Pair exp_sum(Pair sum, uint4 v, const Base& b) {
-    Pair p[Vec<T>::kPairs];
+// The same without the roundings of the exponent, c in 64 bits.
+__device__ __forceinline__ float scale_finely(float m, float to, double c) {
+    if (m == to) return 1.f;
+    const double z = ((double)m - (double)to) * c;
+    const float  t = (float)z;
+    return t > -150.f ? exp2_approx(t) * fmaf((float)(z - (double)t), 0.693147182f, 1.f) : 0.f;
+}
+// Sums of 2^(x c - mc), with kFine of 2^(x (c + low) - mc).
+template <class T, bool kFine> __device__ __forceinline__ Pair exp_sum(uint4 v, Pair c, Pair low, Pair minus_mc) {
+    Pair p[Vec<T>::kPairs], sum = 0;
     Vec<T>::unpack(v, p);
 #pragma unroll
-    for (int i = 0; i < Vec<T>::kPairs; ++i) sum = add2(sum, exp2_pair(fma2(p[i], b.c, b.minus_mc)));
+    for (int i = 0; i < Vec<T>::kPairs; ++i) {
+        Pair z = fma2(p[i], c, minus_mc);
+        if (kFine) z = fma2(p[i], low, z);
+        sum = add2(sum, exp2_pair(z));
+    }
     return sum;
 }
 template <class T> __device__ __noinline__ float exp_sum_far(uint4 v, float m, float c) {
@@ -775,10 +787,12 @@ __device__ __forceinline__ void load_layer(const Layer* table, uint4* ring, int 
     copy_commit();
 }
 // f(layer, first vector, second vector) for this thread's vectors of all layers of the row, in order, through a ring of R
-// layers.
-template <class T, int TH, int R, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
+// layers, after start_stream.
+template <class T, int TH, int R> __device__ __forceinline__ void start_stream(const Layer* table, uint4* ring, int n) {
 #pragma unroll
     for (int l = 0; l < R; ++l) load_layer<T, TH>(table, ring, l, l, n);
+}
+template <class T, int TH, int R, class F> __device__ __forceinline__ void stream(const Layer* table, uint4* ring, int n, F f) {
     const uint4* mine = ring + threadIdx.x;
 #pragma unroll 1
     for (int l = 0; l < n; l += R)
@@ -808,13 +822,25 @@ template <class T, int TH, int R, class F> __device__ __forceinline__ void strea
     }
 }
 
+// 1 / T, and log2(e) / T: rounded, and as the sum of two fp32.  The first of these is cut, not rounded, and the second at
+// least 2^-126, so that -inf times either is -inf.
+struct Scale {
+    double inv_t;
+    float  c, high, low;
+};
+
 // A running sum of exponentials: (base, sum of 2^((x - base) c)) whose base follows the maximum only when that has gone
 // 2^40 ahead: terms stay below 2^41 and most vectors leave it alone.  c = log2(e) / T; see Base for the arithmetic.
-struct Running {
-    float base, base_c, right, ahead, sum;
+// kFine, for sums that a difference of near numbers is made of: c has its second part (alone, the first shifts the whole
+// sum by up to 4e-8 |x - base| / T), and the base follows 2^8 behind, since an element ahead of it carries half a unit in
+// the last place of the distance in its exponent.  What is left is 1e-7, half of it ex2.approx's.
+template <bool kFine> struct Running {
+    static constexpr float kAhead = kFine ? 8.f : 40.f;
+    float base, base_c, right, ahead, sum, low;
     Pair  c, minus;
-    __device__ __forceinline__ explicit Running(float scale) {
+    __device__ __forceinline__ explicit Running(float scale, float scale_low = 0.f) {
         c = pair(scale, scale);
+        low = scale_low;
         base = -INFINITY;
         ahead = -INFINITY;
         base_c = sum = 0.f;
@@ -828,17 +854,17 @@ struct Running {
             sum *= scale_to(base, top, scale);
             base = top;
             base_c = top * scale;
-            right = exp2_approx(fmaf(-top, scale, base_c));
+            right = exp2_approx(fmaf(-top, scale, base_c) - (kFine ? top * low : 0.f));
             minus = pair(-base_c, -base_c);
-            ahead = top + 40.f / scale;
+            ahead = top + kAhead / scale;
         }
     }
     template <class T> __device__ __forceinline__ void add(uint4 a, uint4 b) {
         if (is_far(base_c)) {
             sum += exp_sum_far<T>(a, base, halves(c).x) + exp_sum_far<T>(b, base, halves(c).x);
         } else {
-            const Base  at = {c, minus, base, right, false};
-            const float2 h = halves(add2(exp_sum<T>(0, a, at), exp_sum<T>(0, b, at)));
+            const Pair   d = pair(low, low);
+            const float2 h = halves(add2(exp_sum<T, kFine>(a, c, d, minus), exp_sum<T, kFine>(b, c, d, minus)));
             sum = fmaf(h.x + h.y, right, sum);
         }
     }
@@ -921,9 +947,10 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
     if (tid == 0) n_found = n_noted = 0;
     fill_long_table<T>(table, in, LogitsCut(), deal, row);
 
-    Running running(c);
+    Running<false> running(c);
     typename Vec<T>::Max m0 = Vec<T>::lowest(), m1 = m0;         // of the thread's first and second vectors
     float to_note = -INFINITY;
+    start_stream<T, kThreads, kStreamRing>(table, ring, n);
     stream<T, kThreads, kStreamRing>(table, ring, n, [&](int l, uint4 a, uint4 b) {
         const typename Vec<T>::Max ma = Vec<T>::max(a), mb = Vec<T>::max(b);
         const float m = Vec<T>::value(Vec<T>::join(ma, mb));
@@ -1094,31 +1121,37 @@ enum Pass { kForward, kBackward, kStep };
 // against 18.4 us); the forward pass reads once and is better off with smaller layers (102 against 109 us).
 __host__ __device__ constexpr int threads_of(int pass) { return pass == kForward ? kThreads : kWide; }
 
+// The divergence is a small difference of large terms where the student is near its teacher (terms of order P d, their sum
+// of order P d^2), and the teacher's rest a small difference of 1 and a sum near it: in 32 bits neither keeps a digit there.
+// So all that is done once per entry is done in 64 bits, from the logits, the teacher's and the sum over the rest on: an
+// exponential of the teacher's and one of the student's, and logarithms for the loss.  Q sums to one as exactly, because S is
+// the sum over the rest and these exponentials; only the rest's own relative error, 1e-7, is left, and it moves a
+// divergence by Q_rest - P_rest times that.
+
 // Sum of two values over the first `warps` warps, the only ones to call it; the same on every thread.
-__device__ __forceinline__ float2 entry_sum(float a, float b, int warps, float2* scratch) {
+__device__ __forceinline__ double2 entry_sum(double a, double b, int warps, double2* scratch) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         a += __shfl_xor_sync(0xffffffffu, a, o);
         b += __shfl_xor_sync(0xffffffffu, b, o);
     }
-    if (warps == 1) return make_float2(a, b);
+    if (warps == 1) return make_double2(a, b);
     asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
-    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_float2(a, b);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_double2(a, b);
     asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
-    float2 r = scratch[0];
+    double2 r = scratch[0];
     for (int i = 1; i < warps; ++i) { r.x += scratch[i].x; r.y += scratch[i].y; }
     return r;
 }
 
-// Entry `threadIdx.x` of a row: the teacher's logit, its probability, the student's logit; id -1 where there is none.
-// p_rest and mass (the sum of all P) are the row's.
+// Entry `threadIdx.x` of a row: the teacher's and the student's logit; id -1 where there is none.
 struct Entry {
     int   id;
-    float y, x, lse, log_p, p, p_rest, mass;
+    float y, x, lse;
 };
 template <class T>
 __device__ __forceinline__ void fetch_entry(Entry& e, int id, const LogitsCut& in, const nereus_distill_t& how, int64_t row) {
-    e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
+    e = {-1, 0.f, 0.f, 0.f};
     if (how.lse) e.lse = how.lse[row];
     if ((uint32_t)id >= (uint32_t)in.vocab) return;
     e.id = id;
@@ -1126,59 +1159,72 @@ __device__ __forceinline__ void fetch_entry(Entry& e, int id, const LogitsCut& i
     const int s = shard_of(in, id);
     e.x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
 }
-__device__ __forceinline__ void teacher_side(Entry& e, int vocab, const nereus_distill_t& how, int warps, float2* scratch) {
-    const float t = how.temperature;
+
+// The entry's probability; P_rest and the sum of all P are the row's.
+struct Teacher {
+    double log_p, p, p_rest, mass;
+};
+__device__ __forceinline__ Teacher teacher_of(const Entry& e, int vocab, const nereus_distill_t& how, double inv_t, int warps,
+                                              double2* scratch) {
+    Teacher r;
     if (how.lse) {
-        e.log_p = e.y / t - e.lse;
-        e.p = e.id >= 0 ? expf(e.log_p) : 0.f;
-        const float2 s = entry_sum(e.p, e.id >= 0 ? 1.f : 0.f, warps, scratch);
-        e.p_rest = (int)s.y < vocab ? fmaxf(0.f, 1.f - s.x) : 0.f;
-        return;
+        r.log_p = (double)e.y * inv_t - (double)e.lse;
+        r.p = e.id >= 0 ? exp(r.log_p) : 0.0;
+        const double2 s = entry_sum(r.p, e.id >= 0 ? 1.0 : 0.0, warps, scratch);
+        r.p_rest = (int)s.y < vocab ? fmax(0.0, 1.0 - s.x) : 0.0;
+        r.mass = 1.0;
+        return r;
     }
     float top = warp_max(e.id >= 0 ? e.y : -INFINITY);
     if (warps > 1) {
         asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
         if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5].x = top;
         asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
-        for (int i = 0; i < warps; ++i) top = fmaxf(top, scratch[i].x);
+        for (int i = 0; i < warps; ++i) top = fmaxf(top, (float)scratch[i].x);
     }
-    const float  v = e.id >= 0 ? expf((e.y - top) / t) : 0.f;
-    const float2 s = entry_sum(v, e.id >= 0 ? 1.f : 0.f, warps, scratch);
-    e.log_p = (e.y - top) / t - logf(s.x);
-    e.p = s.y > 0.f ? v / s.x : 0.f;
-    if (s.y == 0.f) e.mass = 0.f;
+    const double  z = ((double)e.y - (double)top) * inv_t, v = e.id >= 0 ? exp(z) : 0.0;
+    const double2 s = entry_sum(v, e.id >= 0 ? 1.0 : 0.0, warps, scratch);
+    r.log_p = z - log(s.x);
+    r.p = s.y > 0.0 ? v / s.x : 0.0;
+    r.p_rest = 0.0;
+    r.mass = s.y > 0.0 ? 1.0 : 0.0;
+    return r;
 }
 
-// The divergence's terms of the entry and of the rest, Q f of both, and f (the derivative after Q; of the forward KL only
-// its products with Q are used, which stay finite where Q is 0).
-struct Groups {
-    float q, q_rest, term, term_rest, qf, qf_rest, f, f_rest;
+// The student's entry: (x - m) / T, its probability, and the rest's; sums in units of exp(m / T).
+struct Student {
+    double z, q, q_rest, total, rest;
 };
-__device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill_t& how, float m, float total, float rest) {
-    Groups g = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const float log_total = logf(total), log_q = (e.x - m) / how.temperature - log_total, log_q_rest = logf(rest) - log_total;
-    const bool  is = e.id >= 0;
-    g.q = is ? expf(log_q) : 0.f;
-    g.q_rest = rest / total;
-    float p_rest = e.p_rest;
-    if (how.divergence == NEREUS_FORWARD_KL) {
-        if (e.p > 0.f) g.term = e.p * (e.log_p - log_q);
-        if (p_rest > 0.f) g.term_rest = p_rest * (logf(p_rest) - log_q_rest);
-    } else if (how.divergence == NEREUS_REVERSE_KL) {
-        p_rest = fmaxf(p_rest, 5.9604644775390625e-8f);
-        if (g.q > 0.f) { g.f = log_q - e.log_p; g.term = g.qf = g.q * g.f; }
-        if (g.q_rest > 0.f) { g.f_rest = log_q_rest - logf(p_rest); g.term_rest = g.qf_rest = g.q_rest * g.f_rest; }
-    } else {
-        const float a = how.beta, b = 1.f - how.beta;
-        if (is) {
-            const float log_m = logf(a * e.p + b * g.q);
-            if (g.q > 0.f) { g.f = b * (log_q - log_m); g.qf = g.q * g.f; }
-            g.term = g.qf + (e.p > 0.f ? a * e.p * (e.log_p - log_m) : 0.f);
+// P log(P / Q) of the entry and of the rest.
+__device__ __forceinline__ double2 forward_terms(const Teacher& p, const Student& q) {
+    const double log_total = log(q.total);
+    return make_double2(p.p > 0.0 ? p.p * (p.log_p - (q.z - log_total)) : 0.0,
+                        p.p_rest > 0.0 ? p.p_rest * (log(p.p_rest) - (log(q.rest) - log_total)) : 0.0);
+}
+// The divergence's terms of the entry and of the rest, f (its derivative after Q) and Q f of both: reverse KL, Jensen.
+struct Groups {
+    double term, term_rest, qf, qf_rest, f, f_rest;
+};
+__device__ __forceinline__ Groups groups_of(bool is, const Teacher& p, const Student& q, const nereus_distill_t& how) {
+    Groups g = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
+    const double log_total = log(q.total), log_q = q.z - log_total, log_q_rest = log(q.rest) - log_total;
+    if (how.divergence == NEREUS_REVERSE_KL) {
+        if (q.q > 0.0) { g.f = log_q - p.log_p; g.term = g.qf = q.q * g.f; }
+        if (q.q_rest > 0.0) {
+            g.f_rest = log_q_rest - log(fmax(p.p_rest, 5.9604644775390625e-8));
+            g.term_rest = g.qf_rest = q.q_rest * g.f_rest;
         }
-        const float log_m = logf(a * p_rest + b * g.q_rest);
-        if (g.q_rest > 0.f) { g.f_rest = b * (log_q_rest - log_m); g.qf_rest = g.q_rest * g.f_rest; }
-        g.term_rest = g.qf_rest + (p_rest > 0.f ? a * p_rest * (logf(p_rest) - log_m) : 0.f);
+        return g;
     }
+    const double a = how.beta, b = 1.0 - a;
+    if (is) {
+        const double log_m = log(a * p.p + b * q.q);
+        if (q.q > 0.0) { g.f = b * (log_q - log_m); g.qf = q.q * g.f; }
+        g.term = g.qf + (p.p > 0.0 ? a * p.p * (p.log_p - log_m) : 0.0);
+    }
+    const double log_m = log(a * p.p_rest + b * q.q_rest);
+    if (q.q_rest > 0.0) { g.f_rest = b * (log_q_rest - log_m); g.qf_rest = q.q_rest * g.f_rest; }
+    g.term_rest = g.qf_rest + (p.p_rest > 0.0 ? a * p.p_rest * (log(p.p_rest) - log_m) : 0.0);
     return g;
 }
 
@@ -1193,16 +1239,17 @@ __device__ __forceinline__ Groups groups_of(const Entry& e, const nereus_distill
 template <class T, int kPass>
 __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
-                   const __grid_constant__ nereus_distill_t how, float* loss, float* saved, const float* grad_loss) {
+                   const __grid_constant__ nereus_distill_t how, Scale scale, float* loss, float* saved, const float* grad_loss) {
     constexpr int E = kPerVec<T>, R = kPass == kStep ? kStepRing : kStreamRing;
     constexpr int TH = threads_of(kPass), W = TH / 32;
     typedef std::conditional_t<E == 8, uint16_t, uint8_t> Flags;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2 scratch[W], entry_scratch[W];
-    __shared__ float  rest_scale_of_row, m_of_row;
+    __shared__ double2 entry_scratch[W];
+    __shared__ float2  scratch[W];
+    __shared__ float   rest_scale_of_row, m_of_row;
     const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers, entry_warps = (how.k + 31) >> 5;
     const int64_t row = blockIdx.x;
-    const float   weight = how.weight ? how.weight[row] : 1.f, t = how.temperature, c = kLog2e / t;
+    const float   weight = how.weight ? how.weight[row] : 1.f, c = scale.c;
     int           id = -1;
     if (tid < how.k) id = how.ids[row * how.k + tid];
     uint4*    ring = reinterpret_cast<uint4*>(dynamic);
@@ -1221,8 +1268,9 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     if (kPass != kBackward)
         for (int i = tid; i < n * TH * (int)sizeof(Flags) / 4; i += TH) flags[i] = 0;
     fill_long_table<T, TH>(table, in, kPass == kForward ? LogitsCut() : grad, deal, row);
+    start_stream<T, TH, R>(table, ring, n);
 
-    Entry e = {-1, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 1.f};
+    Entry e = {-1, 0.f, 0.f, 0.f};
     if (warp < entry_warps) {
         fetch_entry<T>(e, id, in, how, row);
         if (kPass != kBackward && e.id >= 0) {
@@ -1234,10 +1282,9 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     }
     __syncthreads();
 
-    float m = 0.f, total = 0.f, rest = 0.f;
     if (kPass != kBackward) {
         const Flags* mine = reinterpret_cast<const Flags*>(flags) + tid;
-        Running running(c);
+        Running<true> running(scale.high, scale.low);
         typename Vec<T>::Max top = Vec<T>::lowest();
         stream<T, TH, R>(table, ring, n, [&](int l, uint4 a, uint4 b) {
             const typename Vec<T>::Max v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
@@ -1249,50 +1296,68 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
             }
             running.template add<T>(a, b);
         });
-        const float m_warp = warp_max(Vec<T>::value(top)), sum = warp_sum(running.sum * scale_to(running.base, m_warp, c));
+        const float m_warp = warp_max(Vec<T>::value(top));
+        const float sum = warp_sum(running.sum * scale_finely(running.base, m_warp, (double)scale.high + (double)scale.low));
         if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
         __syncthreads();
     }
-    float g = 0.f, divergence = 0.f, divergence_rest = 0.f;
+    Teacher teacher;
+    Student student;
+    double  divergence = 0.0, divergence_rest = 0.0;
+    float   g = 0.f;
     if (warp < entry_warps) {
-        teacher_side(e, in.vocab, how, entry_warps, entry_scratch);
+        teacher = teacher_of(e, in.vocab, how, scale.inv_t, entry_warps, entry_scratch);
+        float m;
         if (kPass == kBackward) {
-            m = saved[row * 4]; total = saved[row * 4 + 1]; rest = saved[row * 4 + 2];
+            m = saved[row * 4]; student.rest = saved[row * 4 + 2];
         } else {
             const float2 part = lane < W ? scratch[lane] : make_float2(-INFINITY, 0.f);
             m = warp_max(part.x);
-            rest = warp_sum(part.y * scale_to(part.x, m, c));
-            total = rest + entry_sum(e.id >= 0 ? expf((e.x - m) / t) : 0.f, 0.f, entry_warps, entry_scratch).x;
+            student.rest = (double)part.y * (double)scale_finely(part.x, m, (double)scale.high + (double)scale.low);
+#pragma unroll
+            for (int o = 16; o; o >>= 1) student.rest += __shfl_xor_sync(0xffffffffu, student.rest, o);
         }
-        const Groups v = groups_of(e, how, m, total, rest);
-        // the forward KL's gradient needs no sum over the groups: a step sums its loss after the gradient has gone out
-        float2 sums = make_float2(v.term, 0.f);
-        if (how.divergence != NEREUS_FORWARD_KL || kPass == kForward) sums = entry_sum(v.term, v.qf, entry_warps, entry_scratch);
-        divergence = sums.x;
-        divergence_rest = v.term_rest;
-        if (kPass == kForward && tid == 0) {
-            const float d = divergence + divergence_rest;
-            loss[row] = weight * d;
-            float* const o = saved + row * 4;
-            o[0] = m; o[1] = total; o[2] = rest; o[3] = d;
-        }
-        const float scale = (kPass == kBackward && grad_loss ? weight * grad_loss[row] : weight) / t, mean = sums.y + v.qf_rest;
-        float rest_scale;
+        student.z = ((double)e.x - (double)m) * scale.inv_t;
+        const double mine = e.id >= 0 ? exp(student.z) : 0.0;
+        student.total = student.rest + entry_sum(mine, 0.0, entry_warps, entry_scratch).x;
+        student.q = mine / student.total;
+        student.q_rest = student.rest / student.total;
+
+        const double to_grad = (double)weight * (kPass == kBackward && grad_loss ? (double)grad_loss[row] : 1.0) * scale.inv_t;
+        double       rest_scale;
         if (how.divergence == NEREUS_FORWARD_KL) {
-            g = (e.mass * v.q - e.p) * scale;
-            rest_scale = (e.mass - (e.p_rest > 0.f && rest > 0.f ? e.p_rest / v.q_rest : 0.f)) * scale / total;
+            // Q f, not f, which need not be finite; a step works out its loss after the gradient has gone out
+            g = (float)((teacher.mass * student.q - teacher.p) * to_grad);
+            rest_scale = (teacher.mass * student.q_rest - teacher.p_rest) * to_grad / student.rest;
+            if (!(student.rest > 0.0)) rest_scale = teacher.mass * to_grad / student.total;
+            if (kPass == kForward) {
+                const double2 d = forward_terms(teacher, student);
+                divergence = entry_sum(d.x, 0.0, entry_warps, entry_scratch).x;
+                divergence_rest = d.y;
+            }
         } else {
-            g = v.q > 0.f ? v.q * (v.f - mean) * scale : 0.f;
-            rest_scale = (v.f_rest - mean) * scale / total;
+            const Groups  v = groups_of(e.id >= 0, teacher, student, how);
+            const double2 sums = entry_sum(v.term, v.qf, entry_warps, entry_scratch);
+            const double  mean = sums.y + v.qf_rest;
+            divergence = sums.x;
+            divergence_rest = v.term_rest;
+            g = student.q > 0.0 ? (float)(student.q * (v.f - mean) * to_grad) : 0.f;
+            rest_scale = (v.f_rest - mean) * to_grad / student.total;
         }
-        if (tid == 0) { rest_scale_of_row = rest_scale; m_of_row = m; }
+        if (kPass == kForward && tid == 0) {
+            const double d = divergence + divergence_rest;
+            loss[row] = (float)((double)weight * d);
+            float* const o = saved + row * 4;
+            o[0] = m; o[1] = (float)student.total; o[2] = (float)student.rest; o[3] = (float)d;
+        }
+        if (tid == 0) { rest_scale_of_row = (float)rest_scale; m_of_row = m; }
     }
     if (kPass == kForward) return;
     __syncthreads();
     {
         const Base  b = base_of(m_of_row, c);
-        const float scale = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
-        const Pair  s = pair(scale, scale);
+        const float to_rest = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
+        const Pair  s = pair(to_rest, to_rest);
         auto gradient = [&](uint4 v) {
             Pair p[Vec<T>::kPairs];
             Vec<T>::unpack(v, p);
@@ -1329,8 +1394,12 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
         row_of<T>(grad, s, row)[e.id - s * in.cols] = from_float<T>(g);
     }
     if (kPass == kStep && warp < entry_warps) {
-        if (how.divergence == NEREUS_FORWARD_KL) divergence = entry_sum(divergence, 0.f, entry_warps, entry_scratch).x;
-        if (tid == 0) loss[row] = weight * (divergence + divergence_rest);
+        if (how.divergence == NEREUS_FORWARD_KL) {
+            const double2 d = forward_terms(teacher, student);
+            divergence = entry_sum(d.x, 0.0, entry_warps, entry_scratch).x;
+            divergence_rest = d.y;
+        }
+        if (tid == 0) loss[row] = (float)((double)weight * (divergence + divergence_rest));
     }
 }
 
@@ -1399,6 +1468,7 @@ LogitsCut cut_of(const nereus_logits_t& v) {
 }
 
 bool misaligned(const void* p) { return (uintptr_t)p & 3; }
+bool is_temperature(double t) { return (float)t > 0.f && std::isfinite((float)t); }
 
 int check_penalties(const nereus_logits_t& in, const nereus_penalties_t& h) {
     if (h.history) {
@@ -1426,8 +1496,8 @@ int check_distill(const nereus_logits_t* in, const nereus_distill_t* h) {
     if (int rc = check_view(in)) return rc;
     if (!h || h->k < 1 || h->k > NEREUS_TOP_MAX_K || !h->values || !h->ids) return NEREUS_ERR_ARG;
     if (h->divergence < NEREUS_FORWARD_KL || h->divergence > NEREUS_JENSEN) return NEREUS_ERR_ARG;
-    if (h->divergence == NEREUS_JENSEN && !(h->beta > 0.f && h->beta < 1.f)) return NEREUS_ERR_ARG;
-    if (!(h->temperature > 0.f) || !std::isfinite(h->temperature)) return NEREUS_ERR_ARG;
+    if (h->divergence == NEREUS_JENSEN && !(h->beta > 0.0 && h->beta < 1.0)) return NEREUS_ERR_ARG;
+    if (!is_temperature(h->temperature)) return NEREUS_ERR_ARG;
     if (!h->lse && h->divergence != NEREUS_FORWARD_KL) return NEREUS_ERR_UNSUPPORTED;
     if (misaligned(h->values) || misaligned(h->ids) || misaligned(h->lse) || misaligned(h->weight)) return NEREUS_ERR_ALIGN;
     return NEREUS_OK;
@@ -1500,6 +1570,16 @@ int launch(void (*kernel)(P...), std::atomic<bool>* opted, int threads, int64_t 
     return NEREUS_OK;
 }
 
+Scale scale_of(double temperature) {
+    Scale r;
+    r.inv_t = 1.0 / temperature;
+    const double c = 1.4426950408889634 * r.inv_t;
+    r.c = r.high = (float)c;
+    if ((double)r.high > c) r.high = std::nextafter(r.high, 0.f);
+    r.low = c < 0x1p127 ? std::max((float)(c - (double)r.high), 0x1p-126f) : 0x1p-126f;
+    return r;
+}
+
 template <class T, int kPass>
 int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float* loss, float* saved,
                    const float* grad_loss, const nereus_logits_t* grad, cudaStream_t stream) {
@@ -1508,9 +1588,10 @@ int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const Deal    d = deal_of(in, TH, 0, 0, 1 << 30);
+    const Scale   scale = scale_of(how.temperature);
     const int64_t smem = (kPass == kStep ? kStepRing : kStreamRing) * 2 * TH * 16 + d.layers * (int64_t)(sizeof(Layer) + (kPass == kBackward ? 0 : TH * kPerVec<T> / 4));
     return launch(distill_kernel<T, kPass>, opted, TH, in.rows, d, smem, dev, stream, cut_of(in),
-                  kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, loss, saved, grad_loss);
+                  kPass == kForward ? LogitsCut() : cut_of(*grad), d, how, scale, loss, saved, grad_loss);
 }
 
 template <int kPass>
@@ -1545,7 +1626,7 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
 }
 
 template <class T>
-int top_launch(const nereus_logits_t& in, int k, float temperature, float* values, int32_t* ids, float* lse, cudaStream_t stream) {
+int top_launch(const nereus_logits_t& in, int k, double temperature, float* values, int32_t* ids, float* lse, cudaStream_t stream) {
     static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
@@ -1555,7 +1636,7 @@ int top_launch(const nereus_logits_t& in, int k, float temperature, float* value
     const int     full = (int)std::min<int64_t>(vecs / 32, kWarps), j = full ? (k + full - 1) / full : 1;
     const int64_t smem = kStreamRing * kVecs * 16 + d.layers * (int64_t)sizeof(Layer) +
                          (d.layers + kNote<T> - 1) / kNote<T> * (int64_t)kThreads * 2;
-    return launch(top_kernel<T>, opted, kThreads, in.rows, d, smem, dev, stream, cut_of(in), d, k, j, 1.f / temperature, values, ids, lse);
+    return launch(top_kernel<T>, opted, kThreads, in.rows, d, smem, dev, stream, cut_of(in), d, k, j, (float)(1.0 / temperature), values, ids, lse);
 }
 
 }  // namespace
@@ -1582,11 +1663,11 @@ int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out,
     return go(*in, *out, *how, token, lse, (cudaStream_t)cuda_stream);
 }
 
-int nereus_teacher_top(const nereus_logits_t* in, int k, float temperature, float* values, int32_t* ids, float* lse,
+int nereus_teacher_top(const nereus_logits_t* in, int k, double temperature, float* values, int32_t* ids, float* lse,
                        void* cuda_stream) {
     if (int rc = check_view(in)) return rc;
     if (k < 1 || k > NEREUS_TOP_MAX_K || k > in->vocab) return NEREUS_ERR_ARG;
-    if (!(temperature > 0.f) || !std::isfinite(temperature)) return NEREUS_ERR_ARG;
+    if (!is_temperature(temperature)) return NEREUS_ERR_ARG;
     if (misaligned(values) || misaligned(ids) || misaligned(lse)) return NEREUS_ERR_ALIGN;
     if (in->rows == 0) return NEREUS_OK;
     if (!values || !ids || !lse) return NEREUS_ERR_ARG;

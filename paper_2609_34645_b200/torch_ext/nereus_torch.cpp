@@ -124,10 +124,10 @@ bool failed(int rc, const char* what) {
     return true;
 }
 
-float float_of(PyObject* o) {
+double double_of(PyObject* o) {
     const double d = PyFloat_AsDouble(o);
     if (d == -1.0 && PyErr_Occurred()) throw python_error();
-    return (float)d;
+    return d;
 }
 
 bool counted(Py_ssize_t got, Py_ssize_t want) {
@@ -208,7 +208,7 @@ PyObject* teacher_top(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (k == -1 && PyErr_Occurred()) throw python_error();
     const int64_t room = k < 1 || k > NEREUS_TOP_MAX_K ? 1 : k;             // out of range: refused by the library
     at::Tensor values = empty({x.v.rows, room}, at::kFloat, x), ids = empty({x.v.rows, room}, at::kInt, x), lse = empty({x.v.rows}, at::kFloat, x);
-    if (failed(nereus_teacher_top(&x.v, room == k ? (int)k : 0, float_of(a[3]), (float*)values.data_ptr(), (int32_t*)ids.data_ptr(),
+    if (failed(nereus_teacher_top(&x.v, room == k ? (int)k : 0, double_of(a[3]), (float*)values.data_ptr(), (int32_t*)ids.data_ptr(),
                                   (float*)lse.data_ptr(), stream_of(x)), "nereus_teacher_top"))
         return nullptr;
     THPObjectPtr v(THPVariable_Wrap(std::move(values))), i(THPVariable_Wrap(std::move(ids))), l(THPVariable_Wrap(std::move(lse)));
@@ -229,8 +229,8 @@ nereus_distill_t distill_of(PyObject* const* a, const View& x) {
     how.weight = (const float*)arg_of(a[3], at::kFloat, rows, -1, x, "weight");
     how.divergence = (int32_t)PyLong_AsLong(a[4]);
     if (how.divergence == -1 && PyErr_Occurred()) throw python_error();
-    how.temperature = float_of(a[5]);
-    how.beta = float_of(a[6]);
+    how.temperature = double_of(a[5]);
+    how.beta = double_of(a[6]);
     return how;
 }
 
