@@ -495,8 +495,8 @@ int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out,
 /* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
  * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of
  * exp(x / temperature).  NaN is never taken; a row with fewer than k other logits ends in (-inf, -1).
- * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k, temperature not > 0 and finite in fp32), TOO_LARGE (a row
- * whose records do not fit shared memory; vocab <= 2^18 always does). */
+ * 1 <= k <= min(vocab, NEREUS_TOP_MAX_K).  Errors: common, ARG (k; temperature, which has to be a positive normal number
+ * in fp32 too), TOO_LARGE (a row whose records do not fit shared memory; vocab <= 2^18 always does). */
 #define NEREUS_TOP_MAX_K 256
 int nereus_teacher_top(const nereus_logits_t* in, int k, double temperature, float* values, int32_t* ids, float* lse,
                        void* cuda_stream);
@@ -524,7 +524,7 @@ typedef struct {
     int32_t k;                     /* entries per row, 1..NEREUS_TOP_MAX_K */
     int32_t divergence;
     double  beta;                  /* NEREUS_JENSEN only */
-    double  temperature;           /* above 0 and finite in fp32 too */
+    double  temperature;           /* a positive normal number in fp32 too */
     const float*   values;         /* device [rows, k]: the teacher's logits, as nereus_teacher_top leaves them */
     const int32_t* ids;            /* device [rows, k] */
     const float*   lse;            /* device [rows]: the teacher's log-sum-exp of logit / T, or NULL */

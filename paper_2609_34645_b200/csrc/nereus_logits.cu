@@ -280,14 +280,17 @@ __device__ __forceinline__ void store_vector(const Layer& l, int vec, uint4 v) {
 
 // Sums of exponentials are kept as (m, sum of 2^((x - m) c)), c = log2(e) / T.  An element costs one fma: with
 // mc = round(m c), 2^(x c - mc) has no rounding but the fma's own, and the sum of these is put right once by 2^(mc - m c).
-// Where m c is too large for that (a row of the type's lowest value, an infinity) the elements' differences are taken.
+// mc - m c is up to half a unit in the last place of mc: from |mc| = 2^31 on these two powers leave the range of fp32 in
+// opposite directions, and their product is NaN.  From there on (a mask's -1e10, the type's lowest value, an infinity, a low
+// temperature) the elements' differences are taken instead; where neighbouring floats are that far apart they are as exact.
+// What counts is the maximum that a thread has seen so far, not the row's: its first vectors may be masked ones.
 // A maximum of -inf goes with a sum of 0 (or NaN), one of +inf with the number of such elements.
 struct Base {
     Pair  c, minus_mc;
     float m, right;
     bool  far;
 };
-__device__ __forceinline__ bool is_far(float mc) { return !(fabsf(mc) < 0x1p100f); }
+__device__ __forceinline__ bool is_far(float mc, float from = 0x1p31f) { return !(fabsf(mc) < from); }
 __device__ __forceinline__ Base base_of(float m, float c) {
     const float b = m == -INFINITY ? 0.f : m, mc = b * c;
     return {pair(c, c), pair(-mc, -mc), b, exp2_approx(fmaf(-b, c, mc)), is_far(mc)};
@@ -314,11 +317,22 @@ template <class T, bool kFine> __device__ __forceinline__ Pair exp_sum(uint4 v, 
     }
     return sum;
 }
-template <class T> __device__ __noinline__ float exp_sum_far(uint4 v, float m, float c) {
-    float f[kPerVec<T>], r = 0.f;
-    unpack<T>(v, f);
-    for (int j = 0; j < kPerVec<T>; ++j) r += scale_to(f[j], m, c);
-    return r;
+// 2^((x - m) c) of elements where m is far.  Beside a maximum of +inf only such elements count.
+__device__ __forceinline__ Pair exp_far(Pair x, float m, Pair c) {
+    if (m == INFINITY) {
+        const float2 f = halves(x);
+        return pair(f.x == m ? 1.f : f.x != f.x ? f.x : 0.f, f.y == m ? 1.f : f.y != f.y ? f.y : 0.f);
+    }
+    return exp2_pair(mul2(add2(x, pair(-m, -m)), c));
+}
+template <class T> __device__ __noinline__ float exp_sum_far(uint4 a, uint4 b, float m, Pair c) {
+    Pair p[Vec<T>::kPairs], q[Vec<T>::kPairs], sum = 0;
+    Vec<T>::unpack(a, p);
+    Vec<T>::unpack(b, q);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kPairs; ++i) sum = add2(add2(sum, exp_far(p[i], m, c)), exp_far(q[i], m, c));
+    const float2 h = halves(sum);
+    return h.x + h.y;
 }
 // log of a sum of exponentials from its maximum, the scaled maximum and the sum of exp(x - max)
 __device__ __forceinline__ float log_sum(float m, float scaled_m, float sum) {
@@ -444,10 +458,11 @@ __device__ __noinline__ float bias_of(const int32_t* ids, const float* values, i
     return values[h];
 }
 template <int E> __device__ __forceinline__ float far_sum(const float (&x)[E], float base) {
-    float r = 0.f;
+    Pair sum = 0;
 #pragma unroll
-    for (int j = 0; j < E; ++j) r += scale_to(x[j], base, kLog2e);
-    return r;
+    for (int j = 0; j < E; j += 2) sum = add2(sum, exp_far(pair(x[j], x[j + 1]), base, pair(kLog2e, kLog2e)));
+    const float2 h = halves(sum);
+    return h.x + h.y;
 }
 
 template <class TI, class TO, class Count>
@@ -688,8 +703,9 @@ __global__ void __launch_bounds__(kThreads, 3) process_kernel(const __grid_const
                 m_held = top[0] == most ? held[0] : held[1];
             }
             if (most > base + 40.f) rebase(most);
-            if (is_far(base_c)) {
-                sum += far_sum(x[0], base) + far_sum(x[1], base);
+            if (__any_sync(0xffffffffu, is_far(base_c))) {       // seldom, and then for the whole warp
+                const float from = base == -INFINITY ? 0.f : base;
+                sum += far_sum(x[0], from) + far_sum(x[1], from);
             } else {
                 Pair part[2] = {0, 0};
                 const Pair c = pair(kLog2e, kLog2e), minus = pair(-base_c, -base_c);
@@ -836,6 +852,7 @@ struct Scale {
 // the last place of the distance in its exponent.  What is left is 1e-7, half of it ex2.approx's.
 template <bool kFine> struct Running {
     static constexpr float kAhead = kFine ? 8.f : 40.f;
+    static constexpr float kFar = kFine ? 0x1p27f : 0x1p31f;      // the second part of c adds 2^-23 of mc to the exponent
     float base, base_c, right, ahead, sum, low;
     Pair  c, minus;
     __device__ __forceinline__ explicit Running(float scale, float scale_low = 0.f) {
@@ -860,8 +877,8 @@ template <bool kFine> struct Running {
         }
     }
     template <class T> __device__ __forceinline__ void add(uint4 a, uint4 b) {
-        if (is_far(base_c)) {
-            sum += exp_sum_far<T>(a, base, halves(c).x) + exp_sum_far<T>(b, base, halves(c).x);
+        if (__any_sync(0xffffffffu, is_far(base_c, kFar))) {     // seldom, and then for the whole warp
+            sum += exp_sum_far<T>(a, b, base == -INFINITY ? 0.f : base, c);
         } else {
             const Pair   d = pair(low, low);
             const float2 h = halves(add2(exp_sum<T, kFine>(a, c, d, minus), exp_sum<T, kFine>(b, c, d, minus)));
@@ -1468,7 +1485,7 @@ LogitsCut cut_of(const nereus_logits_t& v) {
 }
 
 bool misaligned(const void* p) { return (uintptr_t)p & 3; }
-bool is_temperature(double t) { return (float)t > 0.f && std::isfinite((float)t); }
+bool is_temperature(double t) { return (float)t >= 0x1p-126f && std::isfinite((float)t); }
 
 int check_penalties(const nereus_logits_t& in, const nereus_penalties_t& h) {
     if (h.history) {
