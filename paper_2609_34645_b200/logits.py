@@ -4,7 +4,8 @@
 
 Logits are one tensor [rows, vocab] or, where the head is cut over tensor-parallel ranks, the list of its column shards
 [rows, shard_cols] in rank order; ``vocab`` says how many of the columns count when the vocabulary was padded before
-the cut.  Shards are bf16 or fp32, contiguous along the vocabulary, all with the same stride between rows.
+the cut, or the last shard is narrower than the others.  Shards are bf16 or fp32, contiguous along the vocabulary, all with
+the same stride between rows (a narrower last one, as ``x.split(w, dim=1)`` gives it, is a slice of the same tensor).
 
 Everything runs in the CUDA library on torch's current stream and synchronises nothing; what is returned was allocated
 on that stream unless the caller passed it in.  Wrong types, devices or shapes raise ValueError, everything the library
@@ -90,10 +91,11 @@ class _DistillLoss(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
         ids, values, saved, *shards = ctx.saved_tensors
+        grad = _t.empty_like(shards)
         # columns past the vocabulary take no part in the loss
-        padded = ctx.how["vocab"] is not None and ctx.how["vocab"] < sum(s.shape[1] for s in shards)
-        new = torch.zeros if padded else torch.empty
-        grad = [new(s.shape, dtype=s.dtype, device=s.device) for s in shards]
+        if ctx.how["vocab"] is not None and ctx.how["vocab"] < sum(s.shape[1] for s in shards):
+            for g in grad:
+                g.zero_()
         x = shards[0] if ctx.n == 1 else shards
         distill_backward(x, ids, values, saved, grad_loss=grad_loss.contiguous(), grad=grad[0] if ctx.n == 1 else grad,
                          **ctx.how)

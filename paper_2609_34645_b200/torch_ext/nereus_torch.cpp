@@ -94,20 +94,28 @@ void* arg_of(PyObject* o, at::ScalarType type, int64_t d0, int64_t d1, const Vie
     return t.data_ptr();
 }
 
-// New logits of x's shape, in x's type or another.
+// New logits of x's shape, in x's type or another.  Shards are tensors of their own, unless the last is narrower than the
+// others: then, as all shards have one stride between rows, they are column slices of one tensor.
 PyObject* empty_like(PyObject* x, PyObject* dtype) {
-    auto make = [&](PyObject* o) {
-        const at::Tensor& t = THPVariable_Unpack(o);
-        return THPVariable_Wrap(at::empty(t.sizes(), t.options().dtype(dtype == Py_None ? t.scalar_type() : reinterpret_cast<THPDtype*>(dtype)->scalar_type)));
-    };
     if (dtype != Py_None && !THPDtype_Check(dtype)) throw Wrong{"out_dtype: expected a torch.dtype"};
-    if (THPVariable_Check(x)) return make(x);
+    auto make = [&](const at::Tensor& t, c10::IntArrayRef shape) {
+        return at::empty(shape, t.options().dtype(dtype == Py_None ? t.scalar_type() : reinterpret_cast<THPDtype*>(dtype)->scalar_type));
+    };
+    if (THPVariable_Check(x)) return THPVariable_Wrap(make(THPVariable_Unpack(x), THPVariable_Unpack(x).sizes()));
     THPObjectPtr items(PySequence_Fast(x, "logits"));
     if (!items) throw python_error();
     const Py_ssize_t n = PySequence_Fast_GET_SIZE(items.get());
+    if (n < 1) throw Wrong{"logits: expected a tensor or a sequence of shards"};          // an iterator, gone through already
+    auto shard = [&](Py_ssize_t i) -> const at::Tensor& { return tensor_of(PySequence_Fast_GET_ITEM(items.get(), i), "logits"); };
     THPObjectPtr list(PyList_New(n));
     if (!list) throw python_error();
-    for (Py_ssize_t i = 0; i < n; ++i) PyList_SET_ITEM(list.get(), i, make(PySequence_Fast_GET_ITEM(items.get(), i)));
+    const int64_t rows = shard(0).size(0), cols = shard(0).size(1), last = shard(n - 1).size(1);
+    const at::Tensor whole = cols == last ? at::Tensor() : make(shard(0), {rows, (n - 1) * cols + last});
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject* o = THPVariable_Wrap(whole.defined() ? whole.narrow(1, i * cols, i + 1 < n ? cols : last) : make(shard(i), shard(i).sizes()));
+        if (!o) throw python_error();
+        PyList_SET_ITEM(list.get(), i, o);
+    }
     return list.release();
 }
 
@@ -285,6 +293,14 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NEREUS_END
 }
 
+// x -> uninitialised logits like x
+PyObject* empty_like_of(PyObject*, PyObject* x) {
+    NEREUS_BEGIN
+    view_of(x, 1, nullptr);
+    return empty_like(x, Py_None);
+    NEREUS_END
+}
+
 PyObject* set_error(PyObject*, PyObject* cls) {
     Py_INCREF(cls);
     Py_XSETREF(g_error, cls);
@@ -293,7 +309,8 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define NEREUS_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {NEREUS_FAST(process),         NEREUS_FAST(teacher_top),  NEREUS_FAST(distill_forward),
-                           NEREUS_FAST(distill_backward), NEREUS_FAST(distill_step), {"set_error", set_error, METH_O, nullptr},
+                           NEREUS_FAST(distill_backward), NEREUS_FAST(distill_step), {"empty_like", empty_like_of, METH_O, nullptr},
+                           {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nereus_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
