@@ -442,7 +442,7 @@ int nereus_static_status(int* device_status);
  * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and
  * may be captured into a CUDA graph.  rows = 0 is a call that does nothing.  A row's results are the same, bit for
  * bit, whatever other rows the call has and wherever the row stands among them, as long as its shards start alike modulo
- * 16 bytes.
+ * 16 bytes (nereus_logits_process: in calls with the same parts NULL and the same side of 32768 of history_len, too).
  * Common errors: ARG (null pointer, non-positive size, a shard or stride too small for its columns), UNSUPPORTED
  * (dtype), ALIGN (a pointer that is not aligned to its element), MISMATCH (the written view has other rows,
  * vocabulary or cut than the read one), ALIAS (a written view overlaps a read one without being it, or itself),

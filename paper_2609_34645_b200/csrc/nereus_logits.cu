@@ -1541,22 +1541,37 @@ int device_of(Device* d) {
     return NEREUS_OK;
 }
 
-// Deals a row out over the fewest blocks whose share has at most `most` layers and takes at most kSmemShare bytes, at
-// `per_layer` a layer and `fixed` once.  The number of rows has no part in it: a row's sums come out the same in any batch.
-Deal deal_of(const nereus_logits_t& v, int threads, int64_t per_layer, int64_t fixed, int most) {
+// Layers of a shard of w columns whose rows start on 16-byte boundaries, and of one whose rows start anywhere: a vector more.
+int layers_aligned(int64_t w, int64_t e, int threads) { return (int)(((w + e - 1) / e + 2 * threads - 1) / (2 * threads)); }
+int layers_anywhere(int64_t w, int64_t e, int threads) { return (int)(((w + 2 * e - 2) / e + 2 * threads - 1) / (2 * threads)); }
+
+// A row for each block.
+Deal deal_of(const nereus_logits_t& v, int threads) {
     Deal d;
     const int64_t e = 16 / size_of(v.dtype), w = held_cols(v, 0), bytes = v.row_stride * size_of(v.dtype);
     d.aligned = v.rows < 2 || bytes % 16 == 0;
     for (int s = 0; s < v.tp; ++s)
         if (held_cols(v, s) && (uintptr_t)v.shard[s] % 16) d.aligned = 0;
-    const int64_t vecs = d.aligned ? (w + e - 1) / e : (w + 2 * e - 2) / e;
-    const int64_t used = (v.vocab + v.shard_cols - 1) / v.shard_cols;
-    d.per_shard = (int)((vecs + 2 * threads - 1) / (2 * threads));
-    d.layers = (int)(d.per_shard * used);
+    d.per_shard = d.aligned ? layers_aligned(w, e, threads) : layers_anywhere(w, e, threads);
+    d.layers = d.mine = d.per_shard * (int)((v.vocab + v.shard_cols - 1) / v.shard_cols);
     d.log_c = 0;
-    auto share = [&] { return (int64_t)(d.layers + (1 << d.log_c) - 1) >> d.log_c; };
-    while (d.log_c < 3 && (share() > most || share() * per_layer + fixed > kSmemShare)) ++d.log_c;
-    d.mine = (int)share();
+    return d;
+}
+
+// Deals a row out over the fewest blocks whose share has at most `most` layers and takes at most kSmemShare bytes, at
+// `per_layer` a layer and `fixed` once.  Which layer goes to which block, and with it the order of a row's sums, must not
+// depend on the other rows: neither their number nor where they start has a part in it.  So a shard has its layers for rows
+// that start anywhere, always (one more, and for aligned rows an empty one, only where its vectors fill layers exactly), and
+// the number of blocks goes by those of aligned rows.  The last shard's empty one shifts no other and is left out.
+Deal spread_of(const nereus_logits_t& v, int threads, int64_t per_layer, int64_t fixed, int most) {
+    Deal d = deal_of(v, threads);
+    const int64_t e = 16 / size_of(v.dtype), w = held_cols(v, 0);
+    const int     used = (int)((v.vocab + v.shard_cols - 1) / v.shard_cols), least = layers_aligned(w, e, threads), main = least * used;
+    d.per_shard = layers_anywhere(w, e, threads);
+    d.layers = d.per_shard * used - (d.aligned ? d.per_shard - least : 0);
+    auto share = [&](int layers) { return (int64_t)(layers + (1 << d.log_c) - 1) >> d.log_c; };
+    while (d.log_c < 3 && (share(main) > most || share(main) * per_layer + fixed > kSmemShare)) ++d.log_c;
+    d.mine = (int)share(d.layers);
     return d;
 }
 
@@ -1604,7 +1619,7 @@ int distill_launch(const nereus_logits_t& in, const nereus_distill_t& how, float
     static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    const Deal    d = deal_of(in, TH, 0, 0, 1 << 30);
+    const Deal    d = deal_of(in, TH);
     const Scale   scale = scale_of(how.temperature);
     const int64_t smem = (kPass == kStep ? kStepRing : kStreamRing) * 2 * TH * 16 + d.layers * (int64_t)(sizeof(Layer) + (kPass == kBackward ? 0 : TH * kPerVec<T> / 4));
     return launch(distill_kernel<T, kPass>, opted, TH, in.rows, d, smem, dev, stream, cut_of(in),
@@ -1635,7 +1650,7 @@ int process_launch(const nereus_logits_t& in, const nereus_logits_t& out, const 
     const int64_t per_layer = sizeof(Layer) + (how.history ? kPerLayer<TI> * sizeof(Count) : 0) +
                               (how.bias_ids ? kVecs : 0) + (how.mask ? (kPerLayer<TI> / 32 + 1) * 4 : 0);
     const int64_t fixed = (how.bias_ids ? 12 * kHash : 0) + 16 + kRing * kVecs * 16;
-    Deal d = deal_of(in, kThreads, per_layer, fixed, 4);
+    Deal d = spread_of(in, kThreads, per_layer, fixed, 4);
     // what does not fit is done in rounds
     while (d.mine > 1 && (d.mine * per_layer + fixed > dev.smem || d.mine > 32)) d.mine = (d.mine + 1) / 2;
     return launch(process_kernel<TI, TO, Count>, opted, kThreads, in.rows, d, d.mine * per_layer + fixed, dev, stream,
@@ -1647,7 +1662,7 @@ int top_launch(const nereus_logits_t& in, int k, double temperature, float* valu
     static std::atomic<bool> opted[kMaxDevices];
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    Deal d = deal_of(in, kThreads, 0, 0, 1 << 30);
+    Deal d = deal_of(in, kThreads);
     // warps of which every lane has a vector, at least: how many of the k largest each has to vouch for
     const int64_t w = held_cols(in, 0), vecs = (w + kPerVec<T> - 1) / kPerVec<T>;
     const int     full = (int)std::min<int64_t>(vecs / 32, kWarps), j = full ? (k + full - 1) / full : 1;
