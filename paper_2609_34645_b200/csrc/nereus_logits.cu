@@ -1189,7 +1189,7 @@ __device__ __forceinline__ Teacher teacher_of(const Entry& e, int vocab, const n
         r.p = e.id >= 0 ? exp(r.log_p) : 0.0;
         const double2 s = entry_sum(r.p, e.id >= 0 ? 1.0 : 0.0, warps, scratch);
         r.p_rest = (int)s.y < vocab ? fmax(0.0, 1.0 - s.x) : 0.0;
-        r.mass = 1.0;
+        r.mass = s.x + r.p_rest;         // 1 unless the entries alone have more than that, or are all tokens
         return r;
     }
     float top = warp_max(e.id >= 0 ? e.y : -INFINITY);
