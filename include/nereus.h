@@ -530,7 +530,9 @@ typedef struct {
     const float*   lse;            /* device [rows]: the teacher's log-sum-exp of logit / T, or NULL */
     const float*   weight;         /* device [rows], or NULL = 1 */
 } nereus_distill_t;
-/* The loss alone: loss (device, [rows]) and the sums a backward pass needs, saved (device, [rows, 4]): m, S, S_rest, D. */
+/* The loss alone: loss (device, [rows]) and the sums a backward pass needs, saved (device, [rows, 4]): m, S, S_rest, D.
+ * An S_rest below 2^-126, a rest that lies 87 T below the largest logit, loses digits there, and below 2^-149 is 0: the
+ * backward pass then leaves the rest without a gradient.  Loss and step have no such limit. */
 int nereus_distill_forward(const nereus_logits_t* in, const nereus_distill_t* how, float* loss, float* saved,
                            void* cuda_stream);
 /* The gradient from the saved sums: grad = weight[r] * grad_loss[r] * dD/dx, in the logits' type (grad->dtype ==

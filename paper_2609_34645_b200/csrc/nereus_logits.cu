@@ -1177,15 +1177,16 @@ __device__ __forceinline__ void fetch_entry(Entry& e, int id, const LogitsCut& i
     e.x = to_float(row_of<T>(in, s, row)[id - s * in.cols]);
 }
 
-// The entry's probability; P_rest and the sum of all P are the row's.
+// The entry's probability, log P = y / T - norm; norm, P_rest and the sum of all P are the row's.
 struct Teacher {
-    double log_p, p, p_rest, mass;
+    double log_p, p, norm, p_rest, mass;
 };
 __device__ __forceinline__ Teacher teacher_of(const Entry& e, int vocab, const nereus_distill_t& how, double inv_t, int warps,
                                               double2* scratch) {
     Teacher r;
     if (how.lse) {
-        r.log_p = (double)e.y * inv_t - (double)e.lse;
+        r.norm = (double)e.lse;
+        r.log_p = (double)e.y * inv_t - r.norm;
         r.p = e.id >= 0 ? exp(r.log_p) : 0.0;
         const double2 s = entry_sum(r.p, e.id >= 0 ? 1.0 : 0.0, warps, scratch);
         r.p_rest = (int)s.y < vocab ? fmax(0.0, 1.0 - s.x) : 0.0;
@@ -1201,22 +1202,28 @@ __device__ __forceinline__ Teacher teacher_of(const Entry& e, int vocab, const n
     }
     const double  z = ((double)e.y - (double)top) * inv_t, v = e.id >= 0 ? exp(z) : 0.0;
     const double2 s = entry_sum(v, e.id >= 0 ? 1.0 : 0.0, warps, scratch);
-    r.log_p = z - log(s.x);
+    r.norm = (double)top * inv_t + log(s.x);
+    r.log_p = (double)e.y * inv_t - r.norm;
     r.p = s.y > 0.0 ? v / s.x : 0.0;
     r.p_rest = 0.0;
     r.mass = s.y > 0.0 ? 1.0 : 0.0;
     return r;
 }
 
-// The student's entry: (x - m) / T, its probability, and the rest's; sums in units of exp(m / T).
+// The student's entry: (x - m) / T, its probability, and the rest's; total and rest in units of exp(m / T).
 struct Student {
     double z, q, q_rest, total, rest;
 };
+// What the forward KL's loss needs of a row.
+struct Sums {
+    double norm, p_rest, total, rest;
+    float  m;
+};
 // P log(P / Q) of the entry and of the rest.
-__device__ __forceinline__ double2 forward_terms(const Teacher& p, const Student& q) {
-    const double log_total = log(q.total);
-    return make_double2(p.p > 0.0 ? p.p * (p.log_p - (q.z - log_total)) : 0.0,
-                        p.p_rest > 0.0 ? p.p_rest * (log(p.p_rest) - (log(q.rest) - log_total)) : 0.0);
+__device__ __forceinline__ double2 forward_terms(const Entry& e, const Sums& r, double inv_t) {
+    const double log_p = (double)e.y * inv_t - r.norm, p = e.id >= 0 ? exp(log_p) : 0.0, log_total = log(r.total);
+    return make_double2(p > 0.0 ? p * (log_p - (((double)e.x - (double)r.m) * inv_t - log_total)) : 0.0,
+                        r.p_rest > 0.0 ? r.p_rest * (log(r.p_rest) - (log(r.rest) - log_total)) : 0.0);
 }
 // The divergence's terms of the entry and of the rest, f (its derivative after Q) and Q f of both: reverse KL, Jensen.
 struct Groups {
@@ -1261,9 +1268,10 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     constexpr int TH = threads_of(kPass), W = TH / 32;
     typedef std::conditional_t<E == 8, uint16_t, uint8_t> Flags;
     extern __shared__ __align__(16) unsigned char dynamic[];
+    __shared__ Sums    sums_of_row;
     __shared__ double2 entry_scratch[W];
     __shared__ float2  scratch[W];
-    __shared__ float   rest_scale_of_row, m_of_row;
+    __shared__ float   m_scratch[W], rest_scale_of_row, near_of_row;
     const int     tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = deal.layers, entry_warps = (how.k + 31) >> 5;
     const int64_t row = blockIdx.x;
     const float   weight = how.weight ? how.weight[row] : 1.f, c = scale.c;
@@ -1304,35 +1312,48 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
         Running<true> running(scale.high, scale.low);
         typename Vec<T>::Max top = Vec<T>::lowest();
         stream<T, TH, R>(table, ring, n, [&](int l, uint4 a, uint4 b) {
-            const typename Vec<T>::Max v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
+            typename Vec<T>::Max v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
             top = Vec<T>::join(top, v);
-            running.see(Vec<T>::value(v));
             if (const uint32_t f = mine[l * TH]) {
                 a = without<T>(a, f);
                 b = without<T>(b, f >> E);
+                v = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
             }
+            running.see(Vec<T>::value(v));
             running.template add<T>(a, b);
         });
-        const float m_warp = warp_max(Vec<T>::value(top));
-        const float sum = warp_sum(running.sum * scale_finely(running.base, m_warp, (double)scale.high + (double)scale.low));
-        if (lane == 0) scratch[warp] = make_float2(m_warp, sum);
+        const float m_warp = warp_max(Vec<T>::value(top)), base = warp_max(running.base);
+        const float sum = warp_sum(running.sum * scale_finely(running.base, base, (double)scale.high + (double)scale.low));
+        if (lane == 0) {
+            scratch[warp] = make_float2(base, sum);
+            m_scratch[warp] = m_warp;
+        }
         __syncthreads();
     }
-    Teacher teacher;
-    Student student;
     double  divergence = 0.0, divergence_rest = 0.0;
     float   g = 0.f;
     if (warp < entry_warps) {
-        teacher = teacher_of(e, in.vocab, how, scale.inv_t, entry_warps, entry_scratch);
-        float m;
+        Student student;
+        const Teacher teacher = teacher_of(e, in.vocab, how, scale.inv_t, entry_warps, entry_scratch);
+        // the row's largest logit, one near the rest's largest, and the sum over the rest in units of exp(near / T): the rest
+        // may lie so far below the entries that in units of exp(m / T) it is no fp32, nor the gradient's factor
+        float  m, near;
+        double sum;
         if (kPass == kBackward) {
-            m = saved[row * 4]; student.rest = saved[row * 4 + 2];
+            m = near = saved[row * 4];
+            student.rest = sum = saved[row * 4 + 2];
+            if (sum > 0.0 && sum < 1.0) {
+                near = (float)((double)m + log(sum) / scale.inv_t);
+                sum *= exp(((double)m - (double)near) * scale.inv_t);
+            }
         } else {
             const float2 part = lane < W ? scratch[lane] : make_float2(-INFINITY, 0.f);
-            m = warp_max(part.x);
-            student.rest = (double)part.y * (double)scale_finely(part.x, m, (double)scale.high + (double)scale.low);
+            m = warp_max(lane < W ? m_scratch[lane] : -INFINITY);
+            near = warp_max(part.x);
+            sum = (double)part.y * (double)scale_finely(part.x, near, (double)scale.high + (double)scale.low);
 #pragma unroll
-            for (int o = 16; o; o >>= 1) student.rest += __shfl_xor_sync(0xffffffffu, student.rest, o);
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            student.rest = near == m ? sum : sum * exp(((double)near - (double)m) * scale.inv_t);
         }
         student.z = ((double)e.x - (double)m) * scale.inv_t;
         const double mine = e.id >= 0 ? exp(student.z) : 0.0;
@@ -1341,14 +1362,15 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
         student.q_rest = student.rest / student.total;
 
         const double to_grad = (double)weight * (kPass == kBackward && grad_loss ? (double)grad_loss[row] : 1.0) * scale.inv_t;
-        double       rest_scale;
+        double       to_rest;              // the gradient of the whole rest
         if (how.divergence == NEREUS_FORWARD_KL) {
             // Q f, not f, which need not be finite; a step works out its loss after the gradient has gone out
             g = (float)((teacher.mass * student.q - teacher.p) * to_grad);
-            rest_scale = (teacher.mass * student.q_rest - teacher.p_rest) * to_grad / student.rest;
-            if (!(student.rest > 0.0)) rest_scale = teacher.mass * to_grad / student.total;
+            to_rest = (teacher.mass * student.q_rest - teacher.p_rest) * to_grad;
+            const Sums sums = {teacher.norm, teacher.p_rest, student.total, student.rest, m};
+            if (kPass == kStep && tid == 0) sums_of_row = sums;
             if (kPass == kForward) {
-                const double2 d = forward_terms(teacher, student);
+                const double2 d = forward_terms(e, sums, scale.inv_t);
                 divergence = entry_sum(d.x, 0.0, entry_warps, entry_scratch).x;
                 divergence_rest = d.y;
             }
@@ -1359,7 +1381,7 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
             divergence = sums.x;
             divergence_rest = v.term_rest;
             g = student.q > 0.0 ? (float)(student.q * (v.f - mean) * to_grad) : 0.f;
-            rest_scale = (v.f_rest - mean) * to_grad / student.total;
+            to_rest = student.q_rest * (v.f_rest - mean) * to_grad;
         }
         if (kPass == kForward && tid == 0) {
             const double d = divergence + divergence_rest;
@@ -1367,12 +1389,12 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
             float* const o = saved + row * 4;
             o[0] = m; o[1] = (float)student.total; o[2] = (float)student.rest; o[3] = (float)d;
         }
-        if (tid == 0) { rest_scale_of_row = (float)rest_scale; m_of_row = m; }
+        if (tid == 0) { rest_scale_of_row = sum == 0.0 ? 0.f : (float)(to_rest / sum); near_of_row = near; }
     }
     if (kPass == kForward) return;
     __syncthreads();
     {
-        const Base  b = base_of(m_of_row, c);
+        const Base  b = base_of(near_of_row, c);
         const float to_rest = b.far ? rest_scale_of_row : rest_scale_of_row * b.right;
         const Pair  s = pair(to_rest, to_rest);
         auto gradient = [&](uint4 v) {
@@ -1412,7 +1434,7 @@ __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     }
     if (kPass == kStep && warp < entry_warps) {
         if (how.divergence == NEREUS_FORWARD_KL) {
-            const double2 d = forward_terms(teacher, student);
+            const double2 d = forward_terms(e, sums_of_row, scale.inv_t);
             divergence = entry_sum(d.x, 0.0, entry_warps, entry_scratch).x;
             divergence_rest = d.y;
         }
