@@ -9,7 +9,8 @@ the same stride between rows (a narrower last one, as ``x.split(w, dim=1)`` give
 
 Everything runs in the CUDA library on torch's current stream and synchronises nothing; what is returned was allocated
 on that stream unless the caller passed it in.  Wrong types, devices or shapes raise ValueError, everything the library
-refuses raises NereusError.  The arguments are marshalled by ``_nereus_torch.so`` (``python -m
+refuses raises NereusError.  Under autograd only ``distill_loss`` is differentiable; what the other calls return carries no
+gradient, whatever the logits require.  The arguments are marshalled by ``_nereus_torch.so`` (``python -m
 paper_2609_34645_b200.build``); importing this module without it raises.
 """
 from __future__ import annotations
@@ -80,17 +81,17 @@ def distill_step(x, ids, values, *, grad=None, vocab=None, lse=None, weight=None
 
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, ids, values, how, *shards):
+    def forward(ctx, ids, values, lse, weight, how, *shards):
         x = shards[0] if len(shards) == 1 else list(shards)
-        loss, saved = distill_forward(x, ids, values, **how)
-        ctx.save_for_backward(ids, values, saved, *shards)
+        loss, saved = distill_forward(x, ids, values, lse=lse, weight=weight, **how)
+        ctx.save_for_backward(ids, values, lse, weight, saved, *shards)
         ctx.how, ctx.n = how, len(shards)
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
-        ids, values, saved, *shards = ctx.saved_tensors
+        ids, values, lse, weight, saved, *shards = ctx.saved_tensors
         grad = _t.empty_like(shards)
         # columns past the vocabulary take no part in the loss
         if ctx.how["vocab"] is not None and ctx.how["vocab"] < sum(s.shape[1] for s in shards):
@@ -98,12 +99,16 @@ class _DistillLoss(torch.autograd.Function):
                 g.zero_()
         x = shards[0] if ctx.n == 1 else shards
         distill_backward(x, ids, values, saved, grad_loss=grad_loss.contiguous(), grad=grad[0] if ctx.n == 1 else grad,
-                         **ctx.how)
-        return (None, None, None, *grad)
+                         lse=lse, weight=weight, **ctx.how)
+        return (None, None, None, None, None, *grad)
 
 
 def distill_loss(x, ids, values, *, vocab=None, lse=None, weight=None, divergence="forward_kl", temperature=1.0,
                  beta=0.5):
-    """distill_forward's loss [rows], differentiable with respect to x (a tensor or its shards)."""
-    how = {"vocab": vocab, "lse": lse, "weight": weight, "divergence": divergence, "temperature": temperature, "beta": beta}
-    return _DistillLoss.apply(ids, values, how, *((x,) if isinstance(x, torch.Tensor) else x))
+    """distill_forward's loss [rows], differentiable with respect to x (a tensor or its shards) and to nothing else: the
+    teacher's side and the weights may not require a gradient."""
+    for name, t in (("values", values), ("lse", lse), ("weight", weight)):
+        if isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{name}: distill_loss has no gradient with respect to it; detach it")
+    how = {"vocab": vocab, "divergence": divergence, "temperature": temperature, "beta": beta}
+    return _DistillLoss.apply(ids, values, lse, weight, how, *((x,) if isinstance(x, torch.Tensor) else x))

@@ -119,6 +119,18 @@ PyObject* empty_like(PyObject* x, PyObject* dtype) {
     return list.release();
 }
 
+// The caller's tensors that a call has written: autograd has to notice where it had saved one of them.
+void written(PyObject* x) {
+    auto bump = [](PyObject* o) {
+        const at::Tensor& t = tensor_of(o, "logits");
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    };
+    if (THPVariable_Check(x)) return bump(x);
+    THPObjectPtr items(PySequence_Fast(x, "logits"));
+    if (!items) throw python_error();
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(items.get()); ++i) bump(PySequence_Fast_GET_ITEM(items.get(), i));
+}
+
 at::Tensor empty(c10::IntArrayRef shape, at::ScalarType type, const View& like) {
     return at::empty(shape, at::TensorOptions().dtype(type).device(like.device));
 }
@@ -201,6 +213,7 @@ PyObject* process(PyObject*, PyObject* const* a, Py_ssize_t n) {
     at::Tensor token = empty({rows}, at::kInt, x), lse = empty({rows}, at::kFloat, x);
     if (failed(nereus_logits_process(&x.v, &y.v, &how, (int32_t*)token.data_ptr(), (float*)lse.data_ptr(), stream_of(x)), "nereus_logits_process"))
         return nullptr;
+    if (a[2] != Py_None) written(a[2]);
     THPObjectPtr t(THPVariable_Wrap(std::move(token))), l(THPVariable_Wrap(std::move(lse)));
     return PyTuple_Pack(3, out.get(), t.get(), l.get());
     NEREUS_END
@@ -271,6 +284,7 @@ PyObject* distill_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float* saved = (const float*)arg_of(a[9], at::kFloat, x.v.rows, 4, x, "saved");
     const float* up = (const float*)arg_of(a[10], at::kFloat, x.v.rows, -1, x, "grad_loss");
     if (failed(nereus_distill_backward(&x.v, &how, saved, up, &y.v, stream_of(x)), "nereus_distill_backward")) return nullptr;
+    if (a[11] != Py_None) written(a[11]);
     return grad.release();
     NEREUS_END
 }
@@ -288,6 +302,7 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const View y = view_of(grad.get(), x.v.vocab, &x);
     at::Tensor loss = empty({x.v.rows}, at::kFloat, x);
     if (failed(nereus_distill_step(&x.v, &how, (float*)loss.data_ptr(), &y.v, stream_of(x)), "nereus_distill_step")) return nullptr;
+    if (a[9] != Py_None) written(a[9]);
     THPObjectPtr l(THPVariable_Wrap(std::move(loss)));
     return PyTuple_Pack(2, l.get(), grad.get());
     NEREUS_END
