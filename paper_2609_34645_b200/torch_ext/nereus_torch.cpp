@@ -198,6 +198,8 @@ PyObject* process(PyObject*, PyObject* const* a, Py_ssize_t n) {
         how.bias_count = tensor_of(a[10], "bias_ids").size(-1);
         how.bias_ids = (const int32_t*)arg_of(a[10], at::kInt, rows, how.bias_count, x, "bias_ids");
         how.bias_values = (const float*)arg_of(a[11], at::kFloat, rows, how.bias_count, x, "bias_values");
+    } else if (a[11] != Py_None && tensor_of(a[11], "bias_values").numel()) {
+        throw Wrong{"bias_values belong to bias_ids"};
     }
     if (a[12] != Py_None) {
         const at::Tensor& m = tensor_of(a[12], "mask");

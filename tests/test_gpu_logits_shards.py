@@ -58,3 +58,11 @@ def test_shards_that_can_be_gone_through_once_are_refused():
     x = torch.randn(2, 8, device="cuda")
     with pytest.raises(ValueError):
         L.process(iter([x, x]))
+
+
+def test_bias_values_without_ids_are_refused():
+    x = torch.randn(2, 8, device="cuda")
+    with pytest.raises(ValueError, match="bias_ids"):
+        L.process(x, bias_values=torch.ones(2, 3, device="cuda"))
+    none = torch.empty(2, 0, device="cuda")
+    assert torch.equal(L.process(x, bias_ids=none.int(), bias_values=none)[0], x)
