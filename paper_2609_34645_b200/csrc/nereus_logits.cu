@@ -162,9 +162,6 @@ template <> struct Vec<float> {
         const float2 a = halves(p[0]), b = halves(p[1]);
         return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
-    static __device__ __forceinline__ Max max(Max m, uint4 v) {
-        return fmaxf(m, fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))));
-    }
     static __device__ __forceinline__ Max join(Max a, Max b) { return fmaxf(a, b); }
     static __device__ __forceinline__ Max max(uint4 v) {
         return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
@@ -195,7 +192,6 @@ template <> struct Vec<__nv_bfloat16> {
         return r;
     }
     static __device__ __forceinline__ Max max(uint4 v) { return join(join(v.x, v.y), join(v.z, v.w)); }
-    static __device__ __forceinline__ Max max(Max m, uint4 v) { return join(m, max(v)); }
     static __device__ __forceinline__ float value(Max m) {
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
