@@ -365,9 +365,10 @@ __device__ __forceinline__ int layers_of(const Deal& d, int rank) { return max(0
 // Every block reads the whole history (from L2) and keeps what falls into its share: reading it once per cluster and
 // counting into the peers' shared memory was no faster (256 rows of up to 16384 tokens: 166 against 170 us) and takes two
 // cluster barriers.  A share is at most four layers where counters allow, for as many blocks as a small batch can use.
-// Bound by instruction issue (penalties and history) and, below a hundred rows, by the chain of phases within a block, not
-// by HBM: 256 x 152064 fp32 with histories up to 16384 takes 165 us, 2.0 TB/s; 64 x 128256 bf16 to fp32 30 us; one row of
-// 128256 9 us of GPU time.
+// Not bound by HBM, which is at 20% for 256 rows of 152064 fp32 with histories up to 16384 (167 us, 1.9-2.0 TB/s): issue slots
+// are 63% busy there, and three blocks, 24 warps, an SM (74 registers, 68 KB) are too few to cover one another's phases in
+// the rest.  64 x 128256 bf16 to fp32, with 16 biases, 33 us: 86 KB a block, of which the bias table takes 24, leave two
+// blocks an SM, and 512 blocks are two waves.  One row of 128256: 9 us of GPU time, a chain of phases on 8 SMs.
 
 constexpr int kHash   = 2048;             // slots of the bias table, over twice NEREUS_BIAS_MAX
 constexpr int kRing   = 3;                // layers on their way to a block
@@ -902,7 +903,8 @@ template <class T> __device__ __forceinline__ uint4 without(uint4 v, uint32_t bi
 // k / 8 rounded up, at least k elements reach the least of these 8 values, whatever the order of the row: it bounds the
 // row's k-th largest from below, and for most rows some 1.4 k elements reach it.  Only the vectors whose note does are read
 // again, and what is found in them is ranked by counting, as one 64-bit key of (value, lower id).  Rows of so few distinct
-// values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly.
+// values that more is found than the list holds are searched for the k-th key and the id to cut at, exactly: some 57 more
+// passes over the row, 28 ms for 4096 rows of 128256 that a mask left 20 tokens each, of which the 64 largest were asked.
 // 4096 x 128256 bf16, k = 64: 233-244 us, 4.3-4.5 TB/s read, the exponentials at 60% of their rate and four blocks an SM
 // short of hiding the selection (a quarter of a row's time); 512 x 152064 fp32, k = 128: 76-80 us, 3.9-4.1 TB/s.
 
@@ -1130,8 +1132,8 @@ __global__ void __launch_bounds__(kThreads, 4) top_kernel(const __grid_constant_
 
 enum Pass { kForward, kBackward, kStep };
 // Threads of a block.  A wide block has half as many rows in work for the same warps on an SM: the step's second reading
-// finds more of them in L2 (8192 x 128256 bf16: 796 against 828 us), and a row alone takes less long (131 x 50257: 15.2
-// against 18.4 us); the forward pass reads once and is better off with smaller layers (102 against 109 us).
+// finds more of them in L2 (8192 x 128256 bf16: 809-816 against 826-828 us), and a row alone takes less long (131 x 50257:
+// 16.4 against 18.4 us); the forward pass reads once and is better off with smaller layers (111 against 117 us).
 __host__ __device__ constexpr int threads_of(int pass) { return pass == kForward ? kThreads : kWide; }
 
 // The divergence is a small difference of large terms where the student is near its teacher (terms of order P d, their sum
@@ -1252,10 +1254,12 @@ __device__ __forceinline__ Groups groups_of(bool is, const Teacher& p, const Stu
 // two bytes (fp32: one) for a thread's two vectors of a layer.  The step lets it go by a second time for the gradient,
 // backwards: the layers read last are in the ring, and some of the ones before them in L2.  The gradients of the entries are
 // stored after the others'.
-// Forward, 1024 x 152064 fp32: 102-106 us, 5.9-6.1 TB/s, HBM.  Backward, 2048 x 128256 bf16: 190-194 us, 5.4-5.5 TB/s, HBM with as
-// many bytes written as read.  Step, 8192 x 128256 bf16, a quarter of the rows without weight: 800-830 us, 4.4-4.6 TB/s of
-// the bytes that have to move; about two thirds of the second reading come from HBM (2368 rows, 455 MB of them live: 750 MB
-// read, 556 written), which at that traffic per row carries 5.4 TB/s.  (Holding the row in a cluster's shared memory instead took 930 us: the cluster's exchange left HBM idle.)
+// Forward, 1024 x 152064 fp32: 106-112 us, 5.6-5.9 TB/s, HBM; the second part of log2(e) / T takes 2% of it, the entries'
+// 64 bits 3% (102-106 us without either).  Backward, 2048 x 128256 bf16: 180-186 us, 5.7-5.8 TB/s, HBM with as many bytes
+// written as read.  Step, 8192 x 128256 bf16, a quarter of the rows without weight: 806-828 us, 4.5-4.6 TB/s of the bytes that
+// have to move; 37% of the second reading come from HBM (2368 rows, 455 MB of them live: 623 MB read, 560 written, 239 us),
+// and HBM idles where a block's warps wait for the few that work on the entries.  (Holding the row in a cluster's shared
+// memory instead took 930 us: the cluster's exchange left HBM idle.)
 template <class T, int kPass>
 __global__ void __launch_bounds__(threads_of(kPass), kPass == kForward ? 4 : 2)
     distill_kernel(const __grid_constant__ LogitsCut in, const __grid_constant__ LogitsCut grad, Deal deal,
