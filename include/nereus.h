@@ -492,6 +492,34 @@ typedef struct {
 int nereus_logits_process(const nereus_logits_t* in, const nereus_logits_t* out, const nereus_penalties_t* how,
                           int32_t* token, float* lse, void* cuda_stream);
 
+/* GENERATION: beam search.  The rows are requests x beams (row g * beams + b is beam b of request g).  A beam that goes on
+ * offers every token v of its row x with total(b, v) = score[b] + x[v] - log(sum over the row of exp x); a beam that has
+ * ended offers one hypothesis, its own token ended[b], at total = score[b], and its row is not read.  Of all that the
+ * beams of a request offer, the k with the largest total / norm[b] come out in falling order, equal ones by rising (b, v):
+ *   out_score[g, j] = total, rounded to fp32 once; out_parent[g, j] = the row that it goes on from; out_token[g, j] = v
+ * Totals, quotients and their order are 64 bits; the sum of a row's exponentials is fp32, 1e-7 off.  What is -inf or NaN is
+ * not offered.  A beam whose score is not finite, whose norm is not positive and finite, or whose row holds a NaN or +inf
+ * or nothing above -inf offers nothing, and in the first two cases its row is not read.  Places for which nothing is left get
+ * (-inf, -1, -1).
+ * settle = 1 (k == beams): the same k, in another order: the best that goes on from row b of the request is put at place b,
+ * the others at the places that are left, best first.  A state that is reordered by such parents (nereus_states_reorder)
+ * keeps all rows that something goes on from.  All arrays are on the device. */
+#define NEREUS_BEAM_MAX   64
+#define NEREUS_BEAM_MAX_K 128
+typedef struct {
+    int32_t beams;                 /* rows of a request, 1..NEREUS_BEAM_MAX; rows is a multiple */
+    int32_t k;                     /* 1..NEREUS_BEAM_MAX_K */
+    int32_t settle;
+    int32_t reserved;              /* 0 */
+    const float*   score;          /* [rows] */
+    const int32_t* ended;          /* [rows], or NULL: none has; outside [0, vocab): it goes on */
+    const float*   norm;           /* [rows], or NULL = 1 */
+} nereus_beams_t;
+/* out_score, out_parent, out_token: [rows / beams, k].  Errors: common, ARG (beams, k, rows, settle), TOO_LARGE (vocab above
+ * 2^24). */
+int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, float* out_score, int32_t* out_parent,
+                       int32_t* out_token, void* cuda_stream);
+
 /* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
  * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of
  * exp(x / temperature).  NaN is never taken; a row with fewer than k other logits ends in (-inf, -1).
@@ -546,6 +574,95 @@ int nereus_distill_backward(const nereus_logits_t* in, const nereus_distill_t* h
  * than the forward KL; grad->dtype), TOO_LARGE (a row whose records do not fit shared memory; vocab <= 2^18 always does). */
 int nereus_distill_step(const nereus_logits_t* in, const nereus_distill_t* how, float* loss,
                         const nereus_logits_t* grad, void* cuda_stream);
+
+/* ---- a generation stage's states and cache ------------------------------------------------------------ */
+
+/* The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and may be
+ * captured into a CUDA graph.  They move bytes: the elements' type does not matter.  Ids that come from device arrays are
+ * checked there; what is out of range is left out as said with each call and never read or written.
+ * Common errors: ARG (null pointer, negative or zero size, a stride too small), ALIGN (an int32 array that is not aligned to
+ * 4 bytes), MISMATCH (the two sides of a call do not fit), ALIAS (what a call writes overlaps what it reads), TOO_LARGE
+ * (limits named with each call), CUDA.  The buffers are on the current device. */
+
+/* States of sequences: `buffers` buffers of one geometry.  Row r of a buffer is `outer` pieces, `outer_stride` bytes apart, of
+ * `tokens` tokens of `token_bytes` contiguous bytes: [rows, tokens, heads, dim] has outer = 1, [rows, heads, tokens, dim]
+ * outer = heads; a state without tokens has tokens = 1.  Any sizes, strides and alignment work. */
+#define NEREUS_MAX_BUFFERS 256
+typedef struct {
+    int32_t buffers, rows;
+    int64_t outer, tokens, token_bytes;
+    int64_t row_stride, outer_stride;          /* bytes; outer_stride counts where outer > 1, row_stride where rows > 1 */
+    void*   buffer[NEREUS_MAX_BUFFERS];        /* device */
+} nereus_states_t;
+/* Row i of `to` becomes row parent[i] of `from`, in every buffer: its first length[parent[i]] tokens (clamped to [0, tokens];
+ * length NULL: all of them); what lies behind them stays as it was.  parent (device, [to->rows]), length (device,
+ * [from->rows]).
+ *   to != from   the two share no byte.  A parent outside [0, from->rows) leaves the row as it was.  beams = 0.
+ *   to == from   in place (the same buffers, geometry and strides): rows come in groups of `beams` (1..NEREUS_BEAM_MAX,
+ *                rows a multiple); all rows of a group are read before one is written, so that parents may cross.  A
+ *                parent outside the row's own group, or the row itself, leaves the row as it was.
+ * Errors: common, ARG (beams), MISMATCH (geometry), TOO_LARGE (rows or outer > 2^24, a buffer of more
+ * than 2^46 bytes). */
+int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to, int beams, const int32_t* parent,
+                          const int32_t* length, void* cuda_stream);
+
+/* A paged cache: `pools` pools (keys and values of every layer, of every virtual rank), all of `pages` pages; page p of pool q
+ * is page_bytes contiguous bytes at pool[q] + p * page_stride.  Any sizes and alignment work. */
+typedef struct {
+    int32_t pools, pages;          /* pools 0..NEREUS_MAX_BUFFERS; 0: the calls keep the books and move nothing */
+    int64_t page_bytes, page_stride;
+    void*   pool[NEREUS_MAX_BUFFERS];          /* device */
+} nereus_pages_t;
+/* The cache's books (device): table[r, c] = the page of tokens [c * page_size, (c + 1) * page_size) of sequence r, anything
+ * outside [0, pages) for none; length[r] = tokens of sequence r; refs[p] = how often page p is held, by rows of the table or
+ * by whatever else the caller counts (a pinned prefix); a page is free when refs[p] <= 0. */
+typedef struct {
+    int32_t rows, columns;         /* rows 0..NEREUS_CACHE_MAX_ROWS, columns 1..2^20 */
+    int64_t stride;                /* elements between two rows of the table */
+    int32_t* table;
+    int32_t* length;               /* [rows] */
+    int32_t* refs;                 /* [pages] */
+} nereus_page_table_t;
+#define NEREUS_CACHE_MAX_ROWS 8192
+#define NEREUS_CACHE_MAX_PAGES 16777216
+/* Every row i of `to` becomes a fork of row parent[i] of `from` (device, [to->rows]; outside [0, from->rows): an empty row).
+ * This is a beam search's step (parents from nereus_beam_select), a fork (a parent named twice), the freeing of a sequence (a
+ * parent named by no row: its pages lose a holder, and those that nothing else holds are free) and the making of room, at
+ * once.  With n = length[parent[i]], clamped to [0, columns * page_size], f = n / page_size:
+ *   - the lowest row that names a parent takes its table row over as it is; for every other one the first f pages are shared,
+ *     page f, where it is begun (n % page_size > 0) and there, is copied into a fresh page in all pools, and the row has no
+ *     more;
+ *   - a row has room for room_of[i] tokens (device, or NULL: `room`) behind its n: where columns f .. ceil((n + room) /
+ *     page_size) - 1 have no page they get a fresh one;
+ *   - the fresh pages are the lowest ids that are free once the rows' old holders are gone and the shared pages' new ones
+ *     counted, in the order of (row, column); length becomes n.  An empty row has length 0 and no pages (-1).
+ * `to` shares no byte with `from` (a caller keeps two sets of books and swaps them); its columns are the same.
+ * status (device, [4]): pages free after the call; pages missing; page copies made; 0.  Where pages are missing, or columns of
+ * the table (each counts as one), nothing is forked: length and refs of `to` become those of `from`, and so does the table (rows of
+ * `to` past from->rows are empty).
+ * copies (device, [to->rows, 2]): source and destination of every page copy, in the order of the rows, then -1.
+ * A page that a sequence has begun to fill is its own: where another holder has it too the copies are of what it holds when the
+ * call runs.  Errors: common, ARG (page_size, room < 0), MISMATCH (columns), TOO_LARGE (rows, columns, pages; a
+ * table of 2^31 tokens a row; a page of more than 2^30 bytes, a pool of more than 2^46). */
+int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to,
+                      const int32_t* parent, int page_size, int room, const int32_t* room_of, int32_t* copies,
+                      int32_t* status, void* cuda_stream);
+/* Moves the pages in use to the front, so that the pools can be cut to their first `keep` pages (keep < 0: to as many as
+ * are in use), e.g. to have room for a plan transition: the j-th page in use at or past `keep` goes to the j-th free page below
+ * it.  map (device, [pages]): where each page is now, -1 for free ones.  moves (device, [pages / 2, 2]): source and destination of
+ * the moves; what lies behind the last is left as it was.  `to` gets the table and refs by the new ids (entries that are no page
+ * stay as they are, entries of free pages become -1); length is neither read nor written and may be NULL.
+ * status (device, [4]): pages in use; pages in use beyond `keep`, where they are more than that: nothing is moved then; moves
+ * made; pages that hold everything now (keep, or the pools' size where nothing could be moved).
+ * Errors: common, MISMATCH (rows, columns), TOO_LARGE. */
+int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to,
+                         int64_t keep, int32_t* map, int32_t* moves, int32_t* status, void* cuda_stream);
+/* Copies page src[i] of `from` to page dst[i] of `to`, in every pool, for i < n (src, dst: device, [n]); pairs with an id out of
+ * range are left out.  `to` may be `from` (the same pools) or another cache with as many pools and pages of the same size.  A page
+ * that the call writes is neither read nor written by another of its pairs; where it is, it holds bytes of either.
+ * Errors: common, MISMATCH (pools, page_bytes). */
+int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int64_t n, const int32_t* src, const int32_t* dst,
+                      void* cuda_stream);
 
 const char* nereus_strerror(int code);
 /* cudaError_t of the last failed CUDA call made by this library on the calling thread (0 if none). */

@@ -32,6 +32,7 @@ STATIC_MAX_RECTS = 4096
 DEV_OK, DEV_BOUNDS, DEV_TIMEOUT = 0, 1, 2
 VOCAB_MAX_TP, TOP_MAX_K, BIAS_MAX, HISTORY_MAX = 64, 256, 1023, 1048576
 FORWARD_KL, REVERSE_KL, JENSEN = 0, 1, 2
+BEAM_MAX, BEAM_MAX_K, MAX_BUFFERS, CACHE_MAX_ROWS, CACHE_MAX_PAGES = 64, 128, 256, 8192, 16777216
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_34645_b200.build` "
@@ -117,6 +118,31 @@ class Distill(ctypes.Structure):
                 ("lse", ctypes.c_void_p), ("weight", ctypes.c_void_p)]
 
 
+class Beams(ctypes.Structure):
+    """nereus_beams_t."""
+    _fields_ = [("beams", ctypes.c_int32), ("k", ctypes.c_int32), ("settle", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("score", ctypes.c_void_p), ("ended", ctypes.c_void_p), ("norm", ctypes.c_void_p)]
+
+
+class States(ctypes.Structure):
+    """nereus_states_t: states of sequences, buffers of one geometry."""
+    _fields_ = [("buffers", ctypes.c_int32), ("rows", ctypes.c_int32), ("outer", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("token_bytes", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("outer_stride", ctypes.c_int64),
+                ("buffer", ctypes.c_void_p * MAX_BUFFERS)]
+
+
+class Pages(ctypes.Structure):
+    """nereus_pages_t: the pools of a paged cache."""
+    _fields_ = [("pools", ctypes.c_int32), ("pages", ctypes.c_int32), ("page_bytes", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("pool", ctypes.c_void_p * MAX_BUFFERS)]
+
+
+class PageTable(ctypes.Structure):
+    """nereus_page_table_t: page table, lengths and reference counts."""
+    _fields_ = [("rows", ctypes.c_int32), ("columns", ctypes.c_int32), ("stride", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
 _vp, _i, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
 _P = ctypes.POINTER
 _SIGS = {
@@ -175,6 +201,11 @@ _SIGS = {
     "nereus_distill_forward": [_P(Logits), _P(Distill), _vp, _vp, _vp],
     "nereus_distill_backward": [_P(Logits), _P(Distill), _vp, _vp, _P(Logits), _vp],
     "nereus_distill_step": [_P(Logits), _P(Distill), _vp, _P(Logits), _vp],
+    "nereus_beam_select": [_P(Logits), _P(Beams), _vp, _vp, _vp, _vp],
+    "nereus_states_reorder": [_P(States), _P(States), _i, _vp, _vp, _vp],
+    "nereus_cache_fork": [_P(Pages), _P(PageTable), _P(PageTable), _vp, _i, _i, _vp, _vp, _vp, _vp],
+    "nereus_cache_compact": [_P(Pages), _P(PageTable), _P(PageTable), ctypes.c_int64, _vp, _vp, _vp, _vp],
+    "nereus_cache_copy": [_P(Pages), _P(Pages), ctypes.c_int64, _vp, _vp, _vp],
 }
 for _name, _args in _SIGS.items():
     _f = getattr(_lib, _name)          # AttributeError here = the library does not export a declared symbol
@@ -526,6 +557,32 @@ def distill_backward(src: Logits, how: Distill, saved, grad_loss, grad: Logits, 
 def distill_step(src: Logits, how: Distill, loss, grad: Logits, stream=0) -> None:
     """nereus_distill_step; loss: device address."""
     _ck(_lib.nereus_distill_step(src, how, loss, grad, stream), "nereus_distill_step")
+
+
+def beam_select(src: Logits, how: Beams, score, parent, token, stream=0) -> None:
+    """nereus_beam_select; score, parent, token: device addresses."""
+    _ck(_lib.nereus_beam_select(src, how, score, parent, token, stream), "nereus_beam_select")
+
+
+def states_reorder(src: States, dst: States, beams: int, parent, length=0, stream=0) -> None:
+    """nereus_states_reorder; parent, length: device addresses, length may be 0."""
+    _ck(_lib.nereus_states_reorder(src, dst, beams, parent, length, stream), "nereus_states_reorder")
+
+
+def cache_fork(pools: Pages, src: PageTable, dst: PageTable, parent, page_size: int, room: int, room_of, copies, status,
+               stream=0) -> None:
+    """nereus_cache_fork; parent, room_of, copies, status: device addresses, room_of may be 0."""
+    _ck(_lib.nereus_cache_fork(pools, src, dst, parent, page_size, room, room_of, copies, status, stream), "nereus_cache_fork")
+
+
+def cache_compact(pools: Pages, src: PageTable, dst: PageTable, keep: int, map, moves, status, stream=0) -> None:
+    """nereus_cache_compact; map, moves, status: device addresses."""
+    _ck(_lib.nereus_cache_compact(pools, src, dst, keep, map, moves, status, stream), "nereus_cache_compact")
+
+
+def cache_copy(src: Pages, dst: Pages, n: int, src_ids, dst_ids, stream=0) -> None:
+    """nereus_cache_copy; src_ids, dst_ids: device addresses."""
+    _ck(_lib.nereus_cache_copy(src, dst, n, src_ids, dst_ids, stream), "nereus_cache_copy")
 
 
 def static_status() -> int:

@@ -1,0 +1,887 @@
+// A generation stage's states and cache for sm_100a: rows of dense states that follow the beams that go on
+// (nereus_states_reorder), and the pages of a cache: forking, freeing and making room (nereus_cache_fork), moving the pages
+// in use to the front (nereus_cache_compact), copying pages (nereus_cache_copy).
+//
+// Two kinds of work.  Bytes that move: their floor is HBM bandwidth, every byte read once and written once.  And books
+// (page table, reference counts): whole numbers, a few MB at most, where what counts is the chain of dependent steps.
+// Everything is exact, and no result depends on the order in which threads come: counts are sums of whole numbers, and free
+// pages are handed out by rank.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <climits>
+#include <cstdint>
+#include <type_traits>
+
+#include "nereus_internal.hpp"
+
+using namespace nereus;
+
+namespace nereus {
+namespace {
+
+#define NEREUS_CUDA(call)                                               \
+    do {                                                                \
+        cudaError_t e_ = (call);                                        \
+        if (e_ != cudaSuccess) { set_cuda_error((int)e_); (void)cudaGetLastError(); return NEREUS_ERR_CUDA; } \
+    } while (0)
+
+constexpr int kMaxDevices = 64;
+constexpr int64_t kMaxBytes = (int64_t)1 << 46;       // of a buffer
+constexpr int64_t kMaxPage  = (int64_t)1 << 30;
+
+// ---- copying pages -------------------------------------------------------------------------------------------
+//
+// A warp takes a tile of up to 4 KiB of one page in one pool, loads all of it and stores it.  The number of pairs may be known to the
+// device alone, so the grid is what the GPU holds and every warp goes on by the grid's size.
+
+struct Pools {
+    char*   from[NEREUS_MAX_BUFFERS];
+    char*   to[NEREUS_MAX_BUFFERS];
+    int64_t from_stride, to_stride, page_bytes;
+    int32_t pools, from_pages, to_pages, chunks;
+};
+constexpr int kCopyThreads = 256;
+constexpr int kTileVecs = 8;               // of a thread
+
+// The tiles of `n` pairs, from this warp's first on; src, dst: `step` apart.
+template <class V>
+__device__ __forceinline__ void copy_pages(const Pools& p, int64_t n, const int32_t* src, const int32_t* dst, int step, int64_t warp, int64_t warps) {
+    const int     lane = threadIdx.x & 31;
+    const int64_t per_pair = (int64_t)p.pools * p.chunks, vecs = p.page_bytes / (int64_t)sizeof(V);
+    // this warp's place as (pair, pool, chunk), and how far it goes on
+    int64_t   pair = warp / per_pair;
+    int       pool = (int)(warp - pair * per_pair) / p.chunks, chunk = (int)(warp - pair * per_pair) % p.chunks;
+    const int64_t by_pair = warps / per_pair;
+    const int by_pool = (int)(warps - by_pair * per_pair) / p.chunks, by_chunk = (int)(warps - by_pair * per_pair) % p.chunks;
+#pragma unroll 1
+    while (pair < n) {
+        const int s = src[pair * step], d = dst[pair * step];
+        if ((unsigned)s < (unsigned)p.from_pages && (unsigned)d < (unsigned)p.to_pages) {
+            const int64_t at = (int64_t)chunk * (32 * kTileVecs) + lane;
+            const V* a = reinterpret_cast<const V*>(p.from[pool] + s * p.from_stride) + at;
+            V*       b = reinterpret_cast<V*>(p.to[pool] + d * p.to_stride) + at;
+            V v[kTileVecs];
+#pragma unroll
+            for (int i = 0; i < kTileVecs; ++i)
+                if (at + 32 * i < vecs) v[i] = __ldcg(a + 32 * i);
+#pragma unroll
+            for (int i = 0; i < kTileVecs; ++i)
+                if (at + 32 * i < vecs) __stcg(b + 32 * i, v[i]);
+        }
+        chunk += by_chunk;
+        if (chunk >= p.chunks) { chunk -= p.chunks; ++pool; }
+        pool += by_pool;
+        if (pool >= p.pools) { pool -= p.pools; ++pair; }
+        pair += by_pair;
+    }
+}
+
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ Pools p, int64_t n, const int32_t* src, const int32_t* dst) {
+    copy_pages<V>(p, n, src, dst, 1, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+}
+
+// ---- what the books' kernels share -----------------------------------------------------------------------------
+//
+// The books are worked on by one cluster of `gridDim.x` blocks: its barriers cost what they cost, a microsecond or so, where
+// launches of their own would cost several.  Every block has a slice of the pages, every warp a part of the slice.
+
+constexpr int kBookThreads = 1024;
+constexpr int kBookWarps   = kBookThreads / 32;
+constexpr int kMaxCluster  = 8;
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+    cluster_arrive();
+    cluster_wait();
+}
+__device__ __forceinline__ uint32_t peer_address(const void* p, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void peer_store(uint32_t at, unsigned long long v) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
+}
+typedef unsigned long long Wide;
+
+__device__ __forceinline__ Wide warp_scan(Wide v) {                  // inclusive
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const Wide u = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+// Sum over the warps before this one of what their lanes' v is in all, and the block's total.  scratch: kBookWarps + 1.
+__device__ __forceinline__ Wide warps_before(Wide of_warp, Wide* scratch, Wide* total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __syncthreads();
+    if (lane == 0) scratch[warp] = of_warp;
+    __syncthreads();
+    if (warp == 0) {
+        const Wide mine = scratch[lane], upto = warp_scan(mine);
+        __syncwarp();
+        scratch[lane] = upto - mine;
+        if (lane == 31) scratch[kBookWarps] = upto;
+    }
+    __syncthreads();
+    *total = scratch[kBookWarps];
+    return scratch[warp];
+}
+// What the blocks before this one have, and all of them, of one number each.  Ends in no barrier: `totals` is written once.
+__device__ __forceinline__ Wide blocks_before(Wide mine, Wide* totals, int rank, int blocks, Wide* total) {
+    if (threadIdx.x < blocks) peer_store(peer_address(totals + rank, threadIdx.x), mine);
+    cluster_sync();
+    Wide before = 0, all = 0;
+    for (int b = 0; b < blocks; ++b) {
+        const Wide v = totals[b];
+        if (b < rank) before += v;
+        all += v;
+    }
+    *total = all;
+    return before;
+}
+// This warp's part [lo, hi) of the pages, by whole groups of 32.
+struct Part {
+    int lo, hi;
+};
+__device__ __forceinline__ Part part_of(int pages, int rank, int blocks) {
+    const int64_t groups = (pages + 31) / 32, parts = (int64_t)blocks * kBookWarps, i = (int64_t)rank * kBookWarps + (threadIdx.x >> 5);
+    return {(int)min((int64_t)pages, groups * i / parts * 32), (int)min((int64_t)pages, groups * (i + 1) / parts * 32)};
+}
+
+struct Books {
+    const int32_t *table, *length, *refs;
+    int64_t  stride;
+    int32_t  rows, columns, pages;
+};
+struct NewBooks {
+    int32_t *table, *length, *refs;
+    int64_t  stride;
+    int32_t  rows;
+};
+
+// ---- forking -------------------------------------------------------------------------------------------------
+
+struct Fork {
+    const int32_t *parent, *room_of;
+    int32_t *copies, *status;
+    int32_t  page_size, room;
+};
+// What becomes of a row: its parent (-1: it is empty), the tokens and full pages it starts with, and the columns until which it
+// has to have pages.
+struct Heir {
+    int     parent, n, full;
+    bool    begun;
+    int64_t until;
+};
+__device__ __forceinline__ Heir heir_of(const Books& b, const Fork& f, int row) {
+    Heir h = {f.parent[row], 0, 0, false, 0};
+    if ((unsigned)h.parent >= (unsigned)b.rows) h.parent = -1;
+    else {
+        h.n = (int)min((int64_t)max(b.length[h.parent], 0), (int64_t)b.columns * f.page_size);
+        h.full = h.n / f.page_size;
+        h.begun = h.n % f.page_size != 0;
+        const int64_t room = max(f.room_of ? f.room_of[row] : f.room, 0);
+        h.until = (h.n + room + f.page_size - 1) / f.page_size;
+    }
+    return h;
+}
+__device__ __forceinline__ bool is_page(int e, int pages) { return (unsigned)e < (unsigned)pages; }
+
+// A row's need of fresh pages, and 1 << 48 where its first is a copy.
+constexpr Wide kOneCopy = (Wide)1 << 48;
+
+// Books of a fork but for the table's plain entries.  One cluster.  first, kids: of every old row, the lowest new row that names
+// it and how many do; need: of every new row, then its sum over the rows before.
+__global__ void __launch_bounds__(kBookThreads, 1) fork_kernel(const Books from, const NewBooks to, const Fork f) {
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    __shared__ Wide scratch[kBookWarps + 1], totals[kMaxCluster];
+    __shared__ Wide lacking_columns;
+    Wide* need  = reinterpret_cast<Wide*>(dynamic);
+    int*  first = reinterpret_cast<int*>(need + to.rows);
+    int*  kids  = first + from.rows;
+    int*  changed = kids + from.rows;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = gridDim.x, rank = blockIdx.x;
+    const Part part = part_of(from.pages, rank, blocks);
+
+    cluster_arrive();                                  // this block has begun: the others may write to it
+    for (int r = tid; r < from.rows; r += kBookThreads) { first[r] = INT_MAX; kids[r] = 0; }
+    if (tid == 0) lacking_columns = 0;
+    __syncthreads();
+    for (int i = tid; i < to.rows; i += kBookThreads) {
+        const int p = f.parent[i];
+        if ((unsigned)p < (unsigned)from.rows) {
+            atomicAdd(&kids[p], 1);
+            atomicMin(&first[p], i);
+        }
+    }
+    for (int p = part.lo + lane; p < part.hi; p += 32) to.refs[p] = from.refs[p];
+    __syncthreads();
+    cluster_wait();
+    // what the rows need, a warp for each; every block gets it
+    for (int i = rank * kBookWarps + warp; i < to.rows; i += blocks * kBookWarps) {
+        const Heir h = heir_of(from, f, i);
+        Wide       w = 0;
+        if (h.parent >= 0) {
+            const int     until = (int)min(h.until, (int64_t)from.columns);
+            const int32_t* row = from.table + h.parent * from.stride;
+            if (first[h.parent] == i) {
+                for (int c = h.full + lane; c < until; c += 32) w += !is_page(row[c], from.pages);
+                w = __reduce_add_sync(0xffffffffu, (unsigned)w);
+            } else if (h.full < until) {
+                w = until - h.full;
+                if (h.begun && is_page(row[h.full], from.pages)) w += kOneCopy;
+            }
+        }
+        if (lane < blocks) peer_store(peer_address(need + i, lane), w);
+    }
+    for (int i = tid; i < to.rows; i += kBookThreads) {
+        const Heir h = heir_of(from, f, i);
+        if (h.until > from.columns) atomicAdd(&lacking_columns, (Wide)(h.until - from.columns));
+    }
+    // rows whose number of holders changes, in order: every block has the same list
+    int n_changed = 0;
+    for (int r = tid; r - tid < from.rows; r += kBookThreads) {
+        const bool     is = r < from.rows && kids[r] != 1;
+        const unsigned who = __ballot_sync(0xffffffffu, is);
+        Wide           all;
+        const int      before = (int)warps_before(__popc(who), scratch, &all);
+        if (is) changed[n_changed + before + __popc(who & ((1u << lane) - 1))] = r;
+        n_changed += (int)all;
+    }
+    cluster_sync();                                    // the new counts and the needs are there
+
+    // a thread goes down a column: beams of one request hold the same pages one above the other, whose changes are added up
+    // before they go out
+    {
+        const int64_t threads = (int64_t)blocks * kBookThreads, self = (int64_t)rank * kBookThreads + tid;
+        const int64_t lanes = min((int64_t)(from.columns + 31) / 32 * 32, threads), groups = max((int64_t)1, threads / lanes);
+        const int     group = (int)(self / lanes), n = n_changed;
+        if (group < groups)
+            for (int64_t c = self % lanes; c < from.columns; c += lanes) {
+                int page = -1, sum = 0;
+                for (int j = (int)((int64_t)n * group / groups), end = (int)((int64_t)n * (group + 1) / groups); j < end; ++j) {
+                    const int r = changed[j], k = kids[r];
+                    const int tokens = (int)min((int64_t)max(from.length[r], 0), (int64_t)from.columns * f.page_size);
+                    const bool full = c < tokens / f.page_size;
+                    if (!full && k) continue;
+                    const int e = from.table[r * from.stride + c];
+                    if (!is_page(e, from.pages)) continue;
+                    if (e != page) {
+                        if (sum) atomicAdd(&to.refs[page], sum);
+                        page = e;
+                        sum = 0;
+                    }
+                    sum += full ? k - 1 : -1;
+                }
+                if (sum) atomicAdd(&to.refs[page], sum);
+            }
+    }
+    // need: sum over the rows before
+    Wide needed = 0;
+    {
+        const int per = (to.rows + kBookThreads - 1) / kBookThreads, lo = min(tid * per, to.rows), hi = min(lo + per, to.rows);
+        Wide sum = 0;
+        for (int i = lo; i < hi; ++i) sum += need[i];
+        const Wide upto = warp_scan(sum);
+        Wide at = warps_before(__shfl_sync(0xffffffffu, upto, 31), scratch, &needed) + upto - sum;
+        for (int i = lo; i < hi; ++i) { const Wide w = need[i]; need[i] = at; at += w; }
+    }
+    const int64_t fresh = (int64_t)(needed & (kOneCopy - 1));
+    const int     n_copies = (int)(needed >> 48);
+    cluster_sync();                                    // all changes are in
+
+    // free pages, in all and before this warp
+    Wide of_warp = 0, of_block, free_pages;
+    for (int p = part.lo; p < part.hi; p += 32) of_warp += __popc(__ballot_sync(0xffffffffu, p + lane < part.hi && __ldcg(to.refs + p + lane) <= 0));
+    Wide rank_of = warps_before(of_warp, scratch, &of_block);
+    rank_of += blocks_before(of_block, totals, rank, blocks, &free_pages);
+    const int64_t missing = max((int64_t)0, fresh - (int64_t)free_pages) + (int64_t)lacking_columns;
+    const bool    fine = missing == 0;
+    if (fine) {
+        for (int p = part.lo; p < part.hi && (int64_t)rank_of < fresh; p += 32) {
+            const bool     is = p + lane < part.hi && __ldcg(to.refs + p + lane) <= 0;
+            const unsigned who = __ballot_sync(0xffffffffu, is);
+            const int64_t  j = (int64_t)rank_of + __popc(who & ((1u << lane) - 1));
+            rank_of += __popc(who);
+            if (!is || j >= fresh) continue;
+            int lo = 0, hi = to.rows;                  // the last row whose sum is not above j
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if ((int64_t)(need[mid] & (kOneCopy - 1)) <= j) lo = mid;
+                else hi = mid;
+            }
+            const Heir     h = heir_of(from, f, lo);
+            const int      until = (int)min(h.until, (int64_t)from.columns);
+            const int32_t* row = from.table + h.parent * from.stride;
+            int            k = (int)(j - (int64_t)(need[lo] & (kOneCopy - 1))), c = h.full + k;
+            const int64_t  of_row = (int64_t)((lo + 1 < to.rows ? need[lo + 1] : needed) & (kOneCopy - 1)) - (int64_t)(need[lo] & (kOneCopy - 1));
+            if (first[h.parent] == lo && of_row != until - h.full)
+                for (c = h.full; c < until; ++c)       // the row has pages between those it lacks
+                    if (!is_page(row[c], from.pages) && k-- == 0) break;
+            to.table[lo * to.stride + c] = p + lane;
+            to.refs[p + lane] = 1;
+            if (k == 0 && c == h.full && (lo + 1 < to.rows ? need[lo + 1] : needed) >> 48 != need[lo] >> 48) {
+                const int at = (int)(need[lo] >> 48);
+                f.copies[2 * at] = row[c];
+                f.copies[2 * at + 1] = p + lane;
+            }
+        }
+    } else {
+        for (int p = part.lo + lane; p < part.hi; p += 32) to.refs[p] = from.refs[p];
+    }
+    int was_free = 0;
+    if (!fine && rank == 0) {
+        for (int p = tid; p < from.pages; p += kBookThreads) was_free += from.refs[p] <= 0;
+        Wide all;
+        warps_before(__reduce_add_sync(0xffffffffu, was_free), scratch, &all);
+        was_free = (int)all;
+    }
+    const int self = rank * kBookThreads + tid;
+    for (int i = self; i < to.rows; i += blocks * kBookThreads) {
+        to.length[i] = fine ? heir_of(from, f, i).n : i < from.rows ? from.length[i] : 0;
+        if (!fine || i >= n_copies) { f.copies[2 * i] = -1; f.copies[2 * i + 1] = -1; }
+    }
+    if (self == 0) {
+        f.status[0] = fine ? (int)((int64_t)free_pages - fresh) : was_free;
+        f.status[1] = (int)min(missing, (int64_t)INT_MAX);
+        f.status[2] = fine ? n_copies : 0;
+        f.status[3] = 0;
+    }
+}
+
+// The table's plain entries, a block for a row at a time, and the copies.
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ Pools p, const Books from, const NewBooks to, const Fork f) {
+    const bool fine = f.status[1] == 0;
+    for (int i = blockIdx.x; i < to.rows; i += gridDim.x) {
+        int32_t* const out = to.table + i * to.stride;
+        if (!fine) {
+            for (int c = threadIdx.x; c < from.columns; c += kCopyThreads) out[c] = i < from.rows ? from.table[i * from.stride + c] : -1;
+            continue;
+        }
+        const Heir h = heir_of(from, f, i);
+        int        before = 0;                         // whether a row above names the same parent
+        if (h.parent >= 0)
+            for (int j = threadIdx.x; j < i; j += kCopyThreads) before |= f.parent[j] == h.parent;
+        const bool     leads = !__syncthreads_or(before);
+        const int32_t* row = from.table + max(h.parent, 0) * from.stride;
+        for (int c = threadIdx.x; c < from.columns; c += kCopyThreads) {
+            int e = -1;
+            if (h.parent >= 0 && (c < h.full || leads)) e = row[c];
+            if (c >= h.full && c < h.until && !is_page(e, from.pages)) continue;          // a fresh page, written already
+            out[c] = e;
+        }
+    }
+    const int n = f.status[2];
+    copy_pages<V>(p, n, f.copies, f.copies + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+}
+
+// ---- compacting ----------------------------------------------------------------------------------------------
+
+struct Compact {
+    int64_t  keep;
+    int32_t *map, *moves, *status;
+};
+__global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const Books from, const NewBooks to, const Compact c) {
+    __shared__ Wide scratch[kBookWarps + 1], totals[2][kMaxCluster];
+    const int  tid = threadIdx.x, lane = tid & 31, blocks = gridDim.x, rank = blockIdx.x;
+    const Part part = part_of(from.pages, rank, blocks);
+    Wide of_warp = 0, of_block, live;
+    cluster_arrive();                                  // this block has begun: the others may write to it
+    for (int p = part.lo; p < part.hi; p += 32) of_warp += __popc(__ballot_sync(0xffffffffu, p + lane < part.hi && from.refs[p + lane] > 0));
+    warps_before(of_warp, scratch, &of_block);
+    cluster_wait();
+    blocks_before(of_block, totals[0], rank, blocks, &live);
+    const int64_t missing = c.keep < 0 ? 0 : max((int64_t)0, (int64_t)live - c.keep);
+    const int     keep = missing ? from.pages : c.keep < 0 ? (int)live : (int)min(c.keep, (int64_t)from.pages);
+    // pages that go (in the upper half) and holes that take them, before this warp and in all
+    of_warp = 0;
+    for (int p = part.lo; p < part.hi; p += 32) {
+        const bool in = p + lane < part.hi, is = in && from.refs[p + lane] > 0, up = p + lane >= keep;
+        of_warp += ((Wide)__popc(__ballot_sync(0xffffffffu, is && up)) << 32) + __popc(__ballot_sync(0xffffffffu, in && !is && !up));
+    }
+    Wide all, before = warps_before(of_warp, scratch, &of_block);
+    before += blocks_before(of_block, totals[1], rank, blocks, &all);
+    const int moves = (int)(all >> 32);
+    int goes = (int)(before >> 32), hole = (int)before;
+    for (int p = part.lo; p < part.hi; p += 32) {
+        const int  page = p + lane;
+        const bool in = page < part.hi;
+        const int  r = in ? from.refs[page] : 0;
+        const bool is = r > 0, up = page >= keep;
+        const unsigned who = __ballot_sync(0xffffffffu, is && up), where = __ballot_sync(0xffffffffu, in && !is && !up), below = (1u << lane) - 1;
+        if (is && up) c.moves[2 * (goes + __popc(who & below))] = page;
+        const int h = hole + __popc(where & below);
+        const bool taken = in && !is && !up && h < moves;
+        if (taken) c.moves[2 * h + 1] = page;
+        if (in) {
+            if (!(is && up)) c.map[page] = is ? page : -1;
+            if (!taken) to.refs[page] = is && up ? 0 : r > 0 ? r : 0;
+        }
+        goes += __popc(who);
+        hole += __popc(where);
+    }
+    cluster_sync();
+    for (int j = rank * kBookThreads + tid; j < moves; j += blocks * kBookThreads) {
+        const int2 m = __ldcg(reinterpret_cast<const int2*>(c.moves) + j);
+        c.map[m.x] = m.y;
+        to.refs[m.y] = from.refs[m.x];
+    }
+    if (rank == 0 && tid == 0) {
+        c.status[0] = (int)live;
+        c.status[1] = (int)missing;
+        c.status[2] = moves;
+        c.status[3] = keep;
+    }
+}
+template <class V>
+__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ Pools p, const Books from, const NewBooks to, const Compact c) {
+    for (int i = blockIdx.x; i < to.rows; i += gridDim.x)
+        for (int j = threadIdx.x; j < from.columns; j += kCopyThreads) {
+            const int e = from.table[i * from.stride + j];
+            to.table[i * to.stride + j] = is_page(e, from.pages) ? c.map[e] : e;
+        }
+    copy_pages<V>(p, c.status[2], c.moves, c.moves + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+}
+
+// ---- reordering rows -----------------------------------------------------------------------------------------
+//
+// A thread takes one vector's place in the rows of a group: it loads what moves from every row that something goes on from,
+// then stores.  No other thread touches that place, so that parents may cross in place without a barrier.
+
+struct States {
+    char*   from[NEREUS_MAX_BUFFERS];
+    char*   to[NEREUS_MAX_BUFFERS];
+    int64_t from_row, to_row, from_outer, to_outer;        // strides
+    int64_t piece;                                         // bytes of a piece: tokens * token_bytes
+    int64_t token_bytes, tokens;
+    int32_t buffers, from_rows, to_rows, outer, group, in_place;
+    int64_t tiles, items;                                  // tiles of a piece; tiles of a group's rows in all buffers
+    int32_t blocks;                                        // of a group
+};
+constexpr int kMoveThreads = 128;
+struct Move {
+    int64_t from, to, bytes;
+};
+
+template <class V, int N>
+__global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_constant__ States s, const int32_t* parent, const int32_t* length) {
+    __shared__ Move moves[N];
+    __shared__ int  n_moves;
+    __shared__ Wide most_bytes;
+    const int group = blockIdx.x / s.blocks, block = blockIdx.x % s.blocks, tid = threadIdx.x;
+    if (tid == 0) { n_moves = 0; most_bytes = 0; }
+    __syncthreads();
+    const int row = group * s.group + tid;
+    if (tid < s.group && row < s.to_rows) {
+        const int p = parent[row];
+        if (s.in_place ? p != row && p >= group * s.group && p < (group + 1) * s.group : (unsigned)p < (unsigned)s.from_rows) {
+            const int64_t tokens = length ? min((int64_t)max(length[p], 0), s.tokens) : s.tokens;
+            if (tokens) {
+                moves[atomicAdd(&n_moves, 1)] = {p * s.from_row, row * s.to_row, tokens * s.token_bytes};
+                atomicMax(&most_bytes, (Wide)(tokens * s.token_bytes));
+            }
+        }
+    }
+    __syncthreads();
+    const int     n = n_moves;
+    const int64_t most = (int64_t)most_bytes;
+    if (!n) return;
+    constexpr int kTile = kMoveThreads * (int)sizeof(V);
+    for (int64_t item = block; item < s.items; item += s.blocks) {
+        const int64_t piece = item / s.tiles, tile = item - piece * s.tiles, at = tile * kTile + tid * (int)sizeof(V);
+        if (at >= most) continue;
+        const int   b = (int)(piece / s.outer);
+        const int64_t o = piece - (int64_t)b * s.outer;
+        const char* from = s.from[b] + o * s.from_outer + at;
+        char*       to = s.to[b] + o * s.to_outer + at;
+        V v[N];
+        bool edge = false;                                 // the last bytes of a row that are no whole vector
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n) {
+                const int64_t left = moves[i].bytes - at;
+                if (left >= (int64_t)sizeof(V)) v[i] = __ldcg(reinterpret_cast<const V*>(from + moves[i].from));
+                else edge |= left > 0;
+            }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n && moves[i].bytes - at >= (int64_t)sizeof(V)) __stcg(reinterpret_cast<V*>(to + moves[i].to), v[i]);
+        if (sizeof(V) > 1 && edge)
+            for (int k = 0; k < (int)sizeof(V); ++k) {
+                unsigned char c[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i < n && moves[i].bytes - at < (int64_t)sizeof(V) && moves[i].bytes - at > k) c[i] = from[moves[i].from + k];
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (i < n && moves[i].bytes - at < (int64_t)sizeof(V) && moves[i].bytes - at > k) to[moves[i].to + k] = c[i];
+            }
+    }
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------
+
+bool misaligned(const void* p) { return (uintptr_t)p & 3; }
+
+struct Device {
+    int id = 0, sms = 0, smem = 0;
+};
+int device_of(Device* d) {
+    static std::atomic<int> sms[kMaxDevices], smem[kMaxDevices];
+    NEREUS_CUDA(cudaGetDevice(&d->id));
+    if (d->id < 0 || d->id >= kMaxDevices) return NEREUS_ERR_UNSUPPORTED;
+    d->sms = sms[d->id].load();
+    d->smem = smem[d->id].load();
+    if (!d->sms || !d->smem) {
+        NEREUS_CUDA(cudaDeviceGetAttribute(&d->smem, cudaDevAttrMaxSharedMemoryPerBlockOptin, d->id));
+        NEREUS_CUDA(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->id));
+        smem[d->id].store(d->smem);
+        sms[d->id].store(d->sms);
+    }
+    return NEREUS_OK;
+}
+// Blocks of a kernel that an SM holds, looked up once.
+template <class K> int resident(K kernel, int threads, std::atomic<int>* known, const Device& d, int* out) {
+    int n = known[d.id].load();
+    if (!n) {
+        NEREUS_CUDA(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0));
+        if (n < 1) n = 1;
+        known[d.id].store(n);
+    }
+    *out = n;
+    return NEREUS_OK;
+}
+
+struct Range {
+    uintptr_t lo, hi;
+};
+bool meet(const Range& a, const Range& b) { return a.lo < b.hi && b.lo < a.hi; }
+Range ints(const void* p, int64_t n) { return {(uintptr_t)p, (uintptr_t)p + 4 * (uintptr_t)std::max<int64_t>(n, 0)}; }
+
+// Whether two strided sets of pieces share no byte, as far as ranges and one common stride show it.
+bool apart(uintptr_t a, int64_t na, int64_t sa, int64_t wa, uintptr_t b, int64_t nb, int64_t sb, int64_t wb) {
+    if (na < 1 || nb < 1 || wa < 1 || wb < 1) return true;
+    const uintptr_t end_a = a + (na - 1) * sa + wa, end_b = b + (nb - 1) * sb + wb;
+    if (end_a <= b || end_b <= a) return true;
+    if (sa != sb || sa < 1) return false;
+    const int64_t gap = (int64_t)((a <= b ? b - a : a - b) % (uintptr_t)sa);
+    return a <= b ? gap >= wa && gap + wb <= sa : gap >= wb && gap + wa <= sa;
+}
+// Whether no buffer of one side shares a byte with one of the other.
+struct Side {
+    void* const* base;
+    int     n;
+    int64_t count, stride, width;
+};
+bool apart(const Side& a, const Side& b) {
+    auto hull = [](const Side& s) {
+        Range r = {UINTPTR_MAX, 0};
+        for (int i = 0; i < s.n; ++i) {
+            const uintptr_t p = (uintptr_t)s.base[i];
+            r.lo = std::min(r.lo, p);
+            r.hi = std::max(r.hi, p + (s.count - 1) * s.stride + s.width);
+        }
+        return r;
+    };
+    if (!meet(hull(a), hull(b))) return true;
+    for (int i = 0; i < a.n; ++i)
+        for (int j = 0; j < b.n; ++j)
+            if (!apart((uintptr_t)a.base[i], a.count, a.stride, a.width, (uintptr_t)b.base[j], b.count, b.stride, b.width)) return false;
+    return true;
+}
+
+// The largest of 16, 4 and 1 that divides everything.
+int unit_of(uint64_t bits) { return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1; }
+
+int check_pages(const nereus_pages_t* p) {
+    if (!p || p->pools < 0 || p->pools > NEREUS_MAX_BUFFERS || p->pages < 1) return NEREUS_ERR_ARG;
+    if (p->pages > NEREUS_CACHE_MAX_PAGES) return NEREUS_ERR_TOO_LARGE;
+    if (!p->pools) return NEREUS_OK;
+    if (p->page_bytes < 1 || p->page_stride < 0 || (p->pages > 1 && p->page_stride < p->page_bytes)) return NEREUS_ERR_ARG;
+    if (p->page_bytes > kMaxPage || p->page_stride > kMaxBytes / p->pages) return NEREUS_ERR_TOO_LARGE;
+    for (int i = 0; i < p->pools; ++i)
+        if (!p->pool[i]) return NEREUS_ERR_ARG;
+    return NEREUS_OK;
+}
+int check_books(const nereus_page_table_t* t, bool length) {
+    if (!t || t->rows < 0 || t->columns < 1 || t->stride < 0 || (t->rows > 1 && t->stride < t->columns)) return NEREUS_ERR_ARG;
+    if (t->rows > NEREUS_CACHE_MAX_ROWS || t->columns > 1 << 20 || t->stride > kMaxBytes) return NEREUS_ERR_TOO_LARGE;
+    if (!t->refs || (t->rows && (!t->table || (length && !t->length)))) return NEREUS_ERR_ARG;
+    if (misaligned(t->refs) || misaligned(t->table) || (length && misaligned(t->length))) return NEREUS_ERR_ALIGN;
+    return NEREUS_OK;
+}
+// The old and new books, and arrays of a call, share no byte.
+int check_apart(const nereus_page_table_t& a, const nereus_page_table_t& b, int pages, bool length, const Range* read, int n_read, const Range* written,
+                int n_written) {
+    Range r[8], w[8];
+    int   nr = 0, nw = 0;
+    auto books = [&](const nereus_page_table_t& t, Range* x, int* n) {
+        x[(*n)++] = ints(t.refs, pages);
+        x[(*n)++] = t.rows ? ints(t.table, (t.rows - 1) * t.stride + t.columns) : Range{0, 0};
+        x[(*n)++] = t.rows && length ? ints(t.length, t.rows) : Range{0, 0};
+    };
+    books(a, r, &nr);
+    books(b, w, &nw);
+    for (int i = 0; i < n_read; ++i) r[nr++] = read[i];
+    for (int i = 0; i < n_written; ++i) w[nw++] = written[i];
+    for (int i = 0; i < nw; ++i) {
+        for (int j = 0; j < nr; ++j)
+            if (meet(w[i], r[j])) return NEREUS_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (meet(w[i], w[j])) return NEREUS_ERR_ALIAS;
+    }
+    return NEREUS_OK;
+}
+
+Pools pools_of(const nereus_pages_t& a, const nereus_pages_t& b, int* unit) {
+    Pools p;
+    uint64_t bits = (uint64_t)a.page_bytes | (a.pages > 1 ? a.page_stride : 0) | (b.pages > 1 ? b.page_stride : 0);
+    for (int i = 0; i < a.pools; ++i) {
+        p.from[i] = (char*)a.pool[i];
+        p.to[i] = (char*)b.pool[i];
+        bits |= (uintptr_t)a.pool[i] | (uintptr_t)b.pool[i];
+    }
+    *unit = a.pools ? unit_of(bits) : 16;
+    p.from_stride = a.page_stride;
+    p.to_stride = b.page_stride;
+    p.page_bytes = a.pools ? a.page_bytes : 0;
+    p.pools = a.pools;
+    p.from_pages = a.pages;
+    p.to_pages = b.pages;
+    const int64_t tile = (int64_t)*unit * 32 * kTileVecs;
+    p.chunks = a.pools ? (int32_t)((a.page_bytes + tile - 1) / tile) : 1;
+    if (!p.pools) { p.pools = 1; p.from_pages = 0; }       // no pair is in range
+    return p;
+}
+
+void book_launch(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, int64_t work, int64_t smem, cudaStream_t stream) {
+    *cfg = {};
+    // one block where the books are small: what more blocks would save is less than their barriers cost
+    const unsigned blocks = work > 16384 ? kMaxCluster : 1;
+    cfg->gridDim = dim3(blocks);
+    cfg->blockDim = dim3(kBookThreads);
+    cfg->dynamicSmemBytes = (size_t)smem;
+    cfg->stream = stream;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = blocks;
+    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
+    cfg->attrs = attr;
+    cfg->numAttrs = 1;
+}
+Books    books_of(const nereus_page_table_t& t, int pages) { return {t.table, t.length, t.refs, t.stride, t.rows, t.columns, pages}; }
+NewBooks new_books_of(const nereus_page_table_t& t) { return {t.table, t.length, t.refs, t.stride, t.rows}; }
+
+template <class V> int copy_launch(const Pools& p, int64_t n, const int32_t* src, const int32_t* dst, const Device& dev, cudaStream_t stream) {
+    static std::atomic<int> known[kMaxDevices];
+    int per_sm;
+    if (int rc = resident(copy_kernel<V>, kCopyThreads, known, dev, &per_sm)) return rc;
+    const int64_t warps = kCopyThreads / 32, tiles = n * p.pools * p.chunks;
+    const int64_t grid = std::min<int64_t>((tiles + warps - 1) / warps, (int64_t)per_sm * dev.sms);
+    copy_kernel<V><<<(unsigned)grid, kCopyThreads, 0, stream>>>(p, n, src, dst);
+    NEREUS_CUDA(cudaGetLastError());
+    return NEREUS_OK;
+}
+template <class V, class Work>
+int apply_launch(void (*kernel)(Pools, Books, NewBooks, Work), std::atomic<int>* known, const Pools& p, int64_t most_pairs, const Books& from,
+                 const NewBooks& to, const Work& w, const Device& dev, cudaStream_t stream) {
+    int per_sm;
+    if (int rc = resident(kernel, kCopyThreads, known, dev, &per_sm)) return rc;
+    const int64_t warps = kCopyThreads / 32, tiles = p.page_bytes ? most_pairs * p.pools * p.chunks : 0;
+    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>((tiles + warps - 1) / warps, to.rows), (int64_t)per_sm * dev.sms));
+    kernel<<<(unsigned)grid, kCopyThreads, 0, stream>>>(p, from, to, w);
+    NEREUS_CUDA(cudaGetLastError());
+    return NEREUS_OK;
+}
+template <class V> int fork_apply(const Pools& p, const Books& from, const NewBooks& to, const Fork& f, const Device& dev, cudaStream_t stream) {
+    static std::atomic<int> known[kMaxDevices];
+    return apply_launch<V>(fork_apply_kernel<V>, known, p, to.rows, from, to, f, dev, stream);
+}
+template <class V> int compact_apply(const Pools& p, const Books& from, const NewBooks& to, const Compact& c, const Device& dev, cudaStream_t stream) {
+    static std::atomic<int> known[kMaxDevices];
+    return apply_launch<V>(compact_apply_kernel<V>, known, p, from.pages / 2, from, to, c, dev, stream);
+}
+
+int check_states(const nereus_states_t* s) {
+    if (!s || s->buffers < 1 || s->buffers > NEREUS_MAX_BUFFERS || s->rows < 0 || s->outer < 1 || s->tokens < 0 || s->token_bytes < 1) return NEREUS_ERR_ARG;
+    if (s->rows > 1 << 24 || s->outer > 1 << 24 || s->tokens > kMaxBytes || s->token_bytes > kMaxBytes / std::max<int64_t>(s->tokens, 1)) return NEREUS_ERR_TOO_LARGE;
+    const int64_t piece = s->tokens * s->token_bytes;
+    if ((s->outer > 1 && s->outer_stride < piece) || (s->rows > 1 && s->row_stride < piece)) return NEREUS_ERR_ARG;
+    if ((s->outer > 1 && s->outer_stride > kMaxBytes / s->outer) || (s->rows > 1 && s->row_stride > kMaxBytes / s->rows)) return NEREUS_ERR_TOO_LARGE;
+    // one row's pieces lie before the next row's, or one piece of all rows before the next piece
+    if (s->outer > 1 && s->rows > 1 && s->row_stride < (s->outer - 1) * s->outer_stride + piece && s->outer_stride < (s->rows - 1) * s->row_stride + piece)
+        return NEREUS_ERR_ARG;
+    for (int i = 0; i < s->buffers; ++i)
+        if (!s->buffer[i] && s->rows && piece) return NEREUS_ERR_ARG;
+    return NEREUS_OK;
+}
+
+template <class V, int N> int reorder_launch(States& s, int64_t groups, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+    constexpr int64_t kTile = (int64_t)kMoveThreads * sizeof(V);
+    s.tiles = (s.piece + kTile - 1) / kTile;
+    s.items = s.tiles * s.outer * s.buffers;
+    // a block sees to 8 tiles or so: few enough that the last ones do not keep the GPU waiting
+    int64_t blocks = (s.items + 7) / 8;
+    const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / groups);
+    s.blocks = (int32_t)std::min<int64_t>(std::min<int64_t>(blocks, most), 1 << 20);
+    reorder_kernel<V, N><<<(unsigned)(groups * s.blocks), kMoveThreads, 0, stream>>>(s, parent, length);
+    NEREUS_CUDA(cudaGetLastError());
+    return NEREUS_OK;
+}
+template <class V> int reorder_by(States& s, int64_t groups, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+    typedef typename std::conditional<sizeof(V) == 1, unsigned char, uint32_t>::type Small;       // 64 vectors of 16 bytes are no registers
+    return s.group <= 4    ? reorder_launch<V, 4>(s, groups, parent, length, stream)
+           : s.group <= 8  ? reorder_launch<V, 8>(s, groups, parent, length, stream)
+           : s.group <= 16 ? reorder_launch<V, 16>(s, groups, parent, length, stream)
+                           : reorder_launch<Small, 64>(s, groups, parent, length, stream);
+}
+
+}  // namespace
+}  // namespace nereus
+
+extern "C" {
+
+int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to, int beams, const int32_t* parent, const int32_t* length,
+                          void* cuda_stream) {
+    if (int rc = check_states(from)) return rc;
+    if (int rc = check_states(to)) return rc;
+    if (from->buffers != to->buffers || from->outer != to->outer || from->tokens != to->tokens || from->token_bytes != to->token_bytes)
+        return NEREUS_ERR_MISMATCH;
+    if (misaligned(parent) || misaligned(length)) return NEREUS_ERR_ALIGN;
+    if (beams < 0 || beams > NEREUS_BEAM_MAX) return NEREUS_ERR_ARG;
+    if (to->rows && !parent) return NEREUS_ERR_ARG;
+    const int64_t piece = to->tokens * to->token_bytes;
+    if (!to->rows || !from->rows || !piece) return NEREUS_OK;
+    States s;
+    uint64_t bits = (from->rows > 1 ? from->row_stride : 0) | (to->rows > 1 ? to->row_stride : 0) | (to->outer > 1 ? from->outer_stride | to->outer_stride : 0);
+    bool same = true;
+    for (int i = 0; i < to->buffers; ++i) {
+        s.from[i] = (char*)from->buffer[i];
+        s.to[i] = (char*)to->buffer[i];
+        bits |= (uintptr_t)s.from[i] | (uintptr_t)s.to[i];
+        same &= s.from[i] == s.to[i];
+    }
+    if (same) {
+        if (from->rows != to->rows || (to->rows > 1 && from->row_stride != to->row_stride) || (to->outer > 1 && from->outer_stride != to->outer_stride))
+            return NEREUS_ERR_MISMATCH;
+        if (beams < 1 || to->rows % beams) return NEREUS_ERR_ARG;
+    } else {
+        if (beams) return NEREUS_ERR_ARG;
+        // rows whose pieces lie between other rows' are looked at piece by piece
+        auto side = [&](const nereus_states_t& t) {
+            const int64_t row = t.rows > 1 ? t.row_stride : 0, step = t.outer > 1 ? t.outer_stride : 0, whole = (t.outer - 1) * step + piece;
+            return row >= whole || t.rows < 2 ? Side{t.buffer, t.buffers, t.rows, row, whole} : Side{t.buffer, t.buffers, t.outer, step, (t.rows - 1) * row + piece};
+        };
+        if (!apart(side(*from), side(*to))) return NEREUS_ERR_ALIAS;
+    }
+    s.from_row = from->rows > 1 ? from->row_stride : 0;
+    s.to_row = to->rows > 1 ? to->row_stride : 0;
+    s.from_outer = to->outer > 1 ? from->outer_stride : 0;
+    s.to_outer = to->outer > 1 ? to->outer_stride : 0;
+    s.piece = piece;
+    s.token_bytes = to->token_bytes;
+    s.tokens = to->tokens;
+    s.buffers = to->buffers;
+    s.from_rows = from->rows;
+    s.to_rows = to->rows;
+    s.outer = (int32_t)to->outer;
+    s.group = same ? beams : 8;
+    s.in_place = same;
+    const int64_t groups = ((int64_t)to->rows + s.group - 1) / s.group;
+    const int unit = unit_of(bits);
+    return unit == 16  ? reorder_by<uint4>(s, groups, parent, length, (cudaStream_t)cuda_stream)
+           : unit == 4 ? reorder_by<uint32_t>(s, groups, parent, length, (cudaStream_t)cuda_stream)
+                       : reorder_by<unsigned char>(s, groups, parent, length, (cudaStream_t)cuda_stream);
+}
+
+int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int64_t n, const int32_t* src, const int32_t* dst, void* cuda_stream) {
+    if (int rc = check_pages(from)) return rc;
+    if (int rc = check_pages(to)) return rc;
+    if (n < 0) return NEREUS_ERR_ARG;
+    if (n > (int64_t)1 << 32) return NEREUS_ERR_TOO_LARGE;
+    if (from->pools != to->pools || (from->pools && from->page_bytes != to->page_bytes)) return NEREUS_ERR_MISMATCH;
+    if (misaligned(src) || misaligned(dst)) return NEREUS_ERR_ALIGN;
+    if (n && (!src || !dst)) return NEREUS_ERR_ARG;
+    bool same = from->page_stride == to->page_stride;
+    for (int i = 0; i < from->pools; ++i) same &= from->pool[i] == to->pool[i];
+    if (!same && !apart(Side{from->pool, from->pools, from->pages, from->page_stride, from->page_bytes},
+                        Side{to->pool, to->pools, to->pages, to->page_stride, to->page_bytes}))
+        return NEREUS_ERR_ALIAS;
+    if (!n || !from->pools) return NEREUS_OK;
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    int unit;
+    const Pools p = pools_of(*from, *to, &unit);
+    return unit == 16  ? copy_launch<uint4>(p, n, src, dst, dev, (cudaStream_t)cuda_stream)
+           : unit == 4 ? copy_launch<uint32_t>(p, n, src, dst, dev, (cudaStream_t)cuda_stream)
+                       : copy_launch<unsigned char>(p, n, src, dst, dev, (cudaStream_t)cuda_stream);
+}
+
+int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to, const int32_t* parent,
+                      int page_size, int room, const int32_t* room_of, int32_t* copies, int32_t* status, void* cuda_stream) {
+    if (int rc = check_pages(pools)) return rc;
+    if (int rc = check_books(from, true)) return rc;
+    if (int rc = check_books(to, true)) return rc;
+    if (from->columns != to->columns) return NEREUS_ERR_MISMATCH;
+    if (page_size < 1 || room < 0) return NEREUS_ERR_ARG;
+    if ((int64_t)page_size * from->columns > INT_MAX) return NEREUS_ERR_TOO_LARGE;
+    if (!status || (to->rows && (!parent || !copies))) return NEREUS_ERR_ARG;
+    if (misaligned(parent) || misaligned(room_of) || misaligned(copies) || misaligned(status)) return NEREUS_ERR_ALIGN;
+    const Range read[] = {ints(parent, to->rows), ints(room_of, room_of ? to->rows : 0)}, written[] = {ints(copies, 2 * (int64_t)to->rows), ints(status, 4)};
+    if (int rc = check_apart(*from, *to, pools->pages, true, read, 2, written, 2)) return rc;
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    const Books    old = books_of(*from, pools->pages);
+    const NewBooks now = new_books_of(*to);
+    const Fork     f = {parent, room_of, copies, status, page_size, room};
+    static std::atomic<bool> opted[kMaxDevices];
+    if (!opted[dev.id].load()) {
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - 2048));
+        opted[dev.id].store(true);
+    }
+    cudaLaunchConfig_t  cfg;
+    cudaLaunchAttribute attr;
+    book_launch(&cfg, &attr, pools->pages + (int64_t)from->rows * from->columns, (int64_t)to->rows * 8 + (int64_t)from->rows * 12, (cudaStream_t)cuda_stream);
+    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, fork_kernel, old, now, f));
+    int unit;
+    const Pools p = pools_of(*pools, *pools, &unit);
+    return unit == 16  ? fork_apply<uint4>(p, old, now, f, dev, (cudaStream_t)cuda_stream)
+           : unit == 4 ? fork_apply<uint32_t>(p, old, now, f, dev, (cudaStream_t)cuda_stream)
+                       : fork_apply<unsigned char>(p, old, now, f, dev, (cudaStream_t)cuda_stream);
+}
+
+int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to, int64_t keep, int32_t* map,
+                         int32_t* moves, int32_t* status, void* cuda_stream) {
+    if (int rc = check_pages(pools)) return rc;
+    if (int rc = check_books(from, false)) return rc;
+    if (int rc = check_books(to, false)) return rc;
+    if (from->columns != to->columns || from->rows != to->rows) return NEREUS_ERR_MISMATCH;
+    if (!map || !status || (pools->pages > 1 && !moves)) return NEREUS_ERR_ARG;
+    if (misaligned(map) || misaligned(status)) return NEREUS_ERR_ALIGN;
+    if ((uintptr_t)moves & 7) return NEREUS_ERR_ALIGN;
+    const Range written[] = {ints(map, pools->pages), ints(moves, pools->pages / 2 * 2), ints(status, 4)};
+    if (int rc = check_apart(*from, *to, pools->pages, false, nullptr, 0, written, 3)) return rc;
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    const Books    old = books_of(*from, pools->pages);
+    const NewBooks now = new_books_of(*to);
+    const Compact  c = {keep, map, moves, status};
+    cudaLaunchConfig_t  cfg;
+    cudaLaunchAttribute attr;
+    book_launch(&cfg, &attr, pools->pages, 0, (cudaStream_t)cuda_stream);
+    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, compact_kernel, old, now, c));
+    int unit;
+    const Pools p = pools_of(*pools, *pools, &unit);
+    return unit == 16  ? compact_apply<uint4>(p, old, now, c, dev, (cudaStream_t)cuda_stream)
+           : unit == 4 ? compact_apply<uint32_t>(p, old, now, c, dev, (cudaStream_t)cuda_stream)
+                       : compact_apply<unsigned char>(p, old, now, c, dev, (cudaStream_t)cuda_stream);
+}
+
+}  // extern "C"

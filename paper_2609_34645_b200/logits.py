@@ -1,5 +1,5 @@
-"""The model-stages' own steps on the LM head's logits, on torch tensors: ``process`` (generation), ``teacher_top``
-(inference) and the distillation from a teacher's top logits (training), ``distill_forward`` / ``distill_backward`` /
+"""The model-stages' own steps on the LM head's logits, on torch tensors: ``process`` and ``beam_select`` (generation),
+``teacher_top`` (inference) and the distillation from a teacher's top logits (training), ``distill_forward`` / ``distill_backward`` /
 ``distill_step`` and, for autograd, ``distill_loss``.
 
 Logits are one tensor [rows, vocab] or, where the head is cut over tensor-parallel ranks, the list of its column shards
@@ -46,6 +46,19 @@ def process(x, *, vocab=None, out=None, out_dtype=None, history=None, prompt_len
     out: like x, in x's type or fp32 (default: new, of out_dtype); x itself processes in place."""
     return _t.process(x, vocab, out, out_dtype, history, prompt_len, total_len, repetition, presence, frequency, bias_ids,
                       bias_values, mask, mask_row)
+
+
+def beam_select(x, score, k, *, beams, vocab=None, ended=None, norm=None, settle=False):
+    """(score fp32, parent int32, token int32), each [requests, k]: one step of a beam search.  x has requests * beams rows;
+    of all hypotheses score + x - logsumexp(x) of a request's beams the k best, falling, equal ones by rising beam and
+    token.  parent is the row that a hypothesis goes on from, for ``cache.reorder`` and ``cache.fork``; places for which
+    nothing is left get (-inf, -1, -1).
+
+    score [rows] fp32: of the beams so far; a beam of -inf offers nothing (and all but a request's first do on its first
+    step).  ended [rows] int32: the token of a beam that has ended, which offers itself alone, -1 for one that goes on.
+    norm [rows] fp32 > 0: hypotheses are ranked by score / norm, as by their lengths.  settle (k == beams): the best that
+    goes on from a row is put at that row's place, so that only rows that nothing goes on from are overwritten."""
+    return _t.beam_select(x, vocab, score, k, beams, ended, norm, settle)
 
 
 def teacher_top(x, k, *, vocab=None, temperature=1.0):

@@ -1,9 +1,10 @@
-// Argument marshalling of paper_2609_34645_b200/logits.py: from torch tensors to the C ABI's calls on logits, with the
+// Argument marshalling of paper_2609_34645_b200/logits.py and cache.py: from torch tensors to the C ABI's calls, with the
 // checks of types, devices and shapes.  A decode step's calls are a few microseconds of GPU time each; through ctypes their
 // arguments alone took two to three times that.  Host code only; every kernel is in libnereus.so.
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/core/grad_mode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -11,7 +12,9 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
 #include <string>
+#include <vector>
 
 #include "nereus.h"
 
@@ -144,6 +147,11 @@ bool failed(int rc, const char* what) {
     return true;
 }
 
+int64_t int_of(PyObject* o) {
+    const int64_t v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw python_error();
+    return v;
+}
 double double_of(PyObject* o) {
     const double d = PyFloat_AsDouble(o);
     if (d == -1.0 && PyErr_Occurred()) throw python_error();
@@ -310,6 +318,289 @@ PyObject* distill_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     NEREUS_END
 }
 
+// (x, vocab, score, k, beams, ended, norm, settle) -> (score, parent, token)
+PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    NEREUS_BEGIN
+    if (!counted(n, 8)) return nullptr;
+    const View x = view_of(a[0], vocab_of(a[1]), nullptr);
+    const c10::cuda::OptionalCUDAGuard guard(x.device);
+    const int64_t rows = x.v.rows, k = int_of(a[3]), beams = int_of(a[4]);
+    nereus_beams_t how = {};
+    // out of range: refused by the library
+    how.beams = beams < 1 || beams > NEREUS_BEAM_MAX ? 0 : (int32_t)beams;
+    how.k = k < 1 || k > NEREUS_BEAM_MAX_K ? 0 : (int32_t)k;
+    how.settle = PyObject_IsTrue(a[7]);
+    if (a[2] == Py_None) throw Wrong{"score: expected a tensor"};
+    how.score = (const float*)arg_of(a[2], at::kFloat, rows, -1, x, "score");
+    how.ended = (const int32_t*)arg_of(a[5], at::kInt, rows, -1, x, "ended");
+    how.norm = (const float*)arg_of(a[6], at::kFloat, rows, -1, x, "norm");
+    const int64_t requests = how.beams ? rows / how.beams : 0, room = std::max<int64_t>(how.k, 1);
+    at::Tensor score = empty({requests, room}, at::kFloat, x), parent = empty({requests, room}, at::kInt, x), token = empty({requests, room}, at::kInt, x);
+    if (failed(nereus_beam_select(&x.v, &how, (float*)score.data_ptr(), (int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(), stream_of(x)),
+               "nereus_beam_select"))
+        return nullptr;
+    THPObjectPtr s(THPVariable_Wrap(std::move(score))), p(THPVariable_Wrap(std::move(parent))), t(THPVariable_Wrap(std::move(token)));
+    return PyTuple_Pack(3, s.get(), p.get(), t.get());
+    NEREUS_END
+}
+
+// ---- states and cache ------------------------------------------------------------------------------------------
+
+// The tensors of an argument that is one or a sequence of them, with one device, element size, shape and strides.
+struct Buffers {
+    std::vector<const at::Tensor*> t;
+    THPObjectPtr hold;
+    c10::Device  device{c10::DeviceType::CPU};
+};
+void buffers_of(PyObject* x, const char* what, Buffers* b) {
+    if (THPVariable_Check(x)) b->t.push_back(&THPVariable_Unpack(x));
+    else {
+        b->hold = PySequence_Fast(x, "expected a tensor or a sequence of tensors");
+        if (!b->hold) throw python_error();
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(b->hold.get()); ++i) b->t.push_back(&tensor_of(PySequence_Fast_GET_ITEM(b->hold.get(), i), what));
+    }
+    if (b->t.size() > NEREUS_MAX_BUFFERS) throw Wrong{std::string(what) + ": at most " + std::to_string(NEREUS_MAX_BUFFERS) + " buffers"};
+    for (const at::Tensor* t : b->t) {
+        if (!t->is_cuda() || t->dim() < 1 || t->layout() != at::kStrided) throw Wrong{std::string(what) + ": expected tensors [rows, ...] on a CUDA device"};
+        const at::Tensor& u = *b->t[0];
+        if (t->device() != u.device() || t->element_size() != u.element_size() || t->sizes() != u.sizes() || (t->numel() && t->strides() != u.strides()))
+            throw Wrong{std::string(what) + ": the buffers differ in device, element size, shape or strides"};
+    }
+    if (!b->t.empty()) b->device = b->t[0]->device();
+}
+// A tensor that a call writes.
+void writable(const at::Tensor& t, const char* what) {
+    if (t.requires_grad() && at::GradMode::is_enabled()) throw Wrong{std::string(what) + ": written without a gradient; detach it"};
+}
+void written(const Buffers& b) {
+    for (const at::Tensor* t : b.t)
+        if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+// Whether dimensions from `first` on lie one after the other; *elements: their product.
+bool packed(const at::Tensor& t, int64_t first, int64_t* elements) {
+    int64_t step = 1;
+    for (int64_t d = t.dim() - 1; d >= first; --d) {
+        if (t.size(d) != 1 && t.stride(d) != step) return false;
+        step *= t.size(d);
+    }
+    *elements = step;
+    return true;
+}
+
+// States [rows, ..., tokens, ...], tokens at `dim`.
+nereus_states_t states_of(const Buffers& b, int64_t dim, const char* what) {
+    if (b.t.empty()) throw Wrong{std::string(what) + ": expected a tensor at least"};
+    const at::Tensor& t = *b.t[0];
+    if (dim < 0) dim += t.dim();
+    if (dim < 1 || (dim >= t.dim() && !(dim == 1 && t.dim() == 1))) throw Wrong{std::string(what) + ": dim is the tokens' axis, behind that of the rows"};
+    nereus_states_t s = {};
+    const int64_t size = t.element_size();
+    s.buffers = (int32_t)b.t.size();
+    if (t.size(0) > INT32_MAX) throw Wrong{std::string(what) + ": too many rows"};
+    s.rows = (int32_t)t.size(0);
+    s.row_stride = t.stride(0) * size;
+    s.outer = 1;
+    s.tokens = 1;
+    s.token_bytes = size;
+    for (size_t i = 0; i < b.t.size(); ++i) s.buffer[i] = b.t[i]->data_ptr();
+    if (t.numel() == 0) {
+        s.tokens = 0;
+        return s;
+    }
+    if (t.dim() == 1) return s;
+    int64_t token = 1;
+    if (!packed(t, dim + 1, &token) || (t.size(dim) != 1 && t.stride(dim) != token)) throw Wrong{std::string(what) + ": not contiguous from the tokens' axis on"};
+    s.tokens = t.size(dim);
+    s.token_bytes = token * size;
+    // the axes between the rows and the tokens are one, or steps of one stride
+    for (int64_t d = dim - 1; d >= 1; --d) {
+        if (t.size(d) == 1) continue;
+        if (s.outer > 1 && t.stride(d) * size != s.outer * s.outer_stride) throw Wrong{std::string(what) + ": the axes before the tokens' have no common stride"};
+        if (s.outer == 1) s.outer_stride = t.stride(d) * size;
+        s.outer *= t.size(d);
+    }
+    return s;
+}
+
+// Pools [pages, ...]; none: `pages` pages that hold nothing.
+nereus_pages_t pools_of(const Buffers& b, int64_t pages, const char* what) {
+    nereus_pages_t p = {};
+    p.pools = (int32_t)b.t.size();
+    if (b.t.empty()) {
+        p.pages = (int32_t)std::min<int64_t>(pages, INT32_MAX);
+        return p;
+    }
+    const at::Tensor& t = *b.t[0];
+    int64_t page = 1;
+    if (!packed(t, 1, &page)) throw Wrong{std::string(what) + ": a page is not contiguous"};
+    p.pages = (int32_t)std::min<int64_t>(t.size(0), INT32_MAX);
+    p.page_bytes = page * t.element_size();
+    p.page_stride = t.stride(0) * t.element_size();
+    for (size_t i = 0; i < b.t.size(); ++i) p.pool[i] = b.t[i]->data_ptr();
+    return p;
+}
+
+// An int32 vector on `device`; size < 0: any.
+int32_t* ints_of(PyObject* o, int64_t size, c10::Device device, const char* what) {
+    const at::Tensor& t = tensor_of(o, what);
+    if (t.scalar_type() != at::kInt || t.device() != device || t.dim() != 1 || (size >= 0 && t.size(0) != size) || !t.is_contiguous())
+        throw Wrong{std::string(what) + ": expected a contiguous int32 tensor of shape [" + (size < 0 ? "n" : std::to_string(size)) + "] on the same device"};
+    return (int32_t*)t.data_ptr();
+}
+const at::Tensor& table_of(PyObject* o, nereus_page_table_t* b, const char* what) {
+    const at::Tensor& t = tensor_of(o, what);
+    if (t.scalar_type() != at::kInt || !t.is_cuda() || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1) || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)
+        throw Wrong{std::string(what) + ": expected int32 [rows, columns], contiguous along the columns, on a CUDA device"};
+    b->rows = (int32_t)t.size(0);
+    b->columns = (int32_t)t.size(1);
+    b->stride = t.size(0) > 1 ? t.stride(0) : t.size(1);
+    b->table = (int32_t*)t.data_ptr();
+    return t;
+}
+at::Tensor new_ints(c10::IntArrayRef shape, c10::Device device) { return at::empty(shape, at::TensorOptions().dtype(at::kInt).device(device)); }
+void* stream_on(c10::Device d) { return (void*)c10::cuda::getCurrentCUDAStream(d.index()).stream(); }
+// The pools' and the page table's device are one.
+void same_device(const Buffers& b, c10::Device d) {
+    if (!b.t.empty() && b.device != d) throw Wrong{"pools and page table are on different devices"};
+}
+// Item i of the tuple `out`.
+PyObject* item_of(PyObject* out, Py_ssize_t i, Py_ssize_t n) {
+    if (!PyTuple_Check(out) || PyTuple_GET_SIZE(out) != n) throw Wrong{"out: expected a tuple of " + std::to_string(n) + " tensors"};
+    return PyTuple_GET_ITEM(out, i);
+}
+
+// (states, parent, beams, length, dim, out) -> None
+PyObject* reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    NEREUS_BEGIN
+    if (!counted(n, 6)) return nullptr;
+    Buffers from, to;
+    buffers_of(a[0], "states", &from);
+    const bool in_place = a[5] == Py_None;
+    if (!in_place) buffers_of(a[5], "out", &to);
+    const Buffers& dst = in_place ? from : to;
+    const int64_t  dim = int_of(a[4]), beams = a[2] == Py_None ? 0 : int_of(a[2]);
+    const nereus_states_t s = states_of(from, dim, "states"), d = states_of(dst, dim, in_place ? "states" : "out");
+    if (dst.device != from.device) throw Wrong{"out: on another device than the states"};
+    if (dst.t[0]->element_size() != from.t[0]->element_size() || dst.t.size() != from.t.size() || dst.t[0]->sizes().slice(1) != from.t[0]->sizes().slice(1))
+        throw Wrong{"out: other buffers than the states but for their rows"};
+    for (const at::Tensor* t : dst.t) writable(*t, in_place ? "states" : "out");
+    const c10::cuda::OptionalCUDAGuard guard(from.device);
+    const int32_t* parent = ints_of(a[1], d.rows, from.device, "parent");
+    const int32_t* length = a[3] == Py_None ? nullptr : ints_of(a[3], s.rows, from.device, "length");
+    if (failed(nereus_states_reorder(&s, &d, beams < 0 || beams > INT32_MAX ? -1 : (int)beams, parent, length, stream_on(from.device)), "nereus_states_reorder"))
+        return nullptr;
+    written(dst);
+    Py_RETURN_NONE;
+    NEREUS_END
+}
+
+// (pools, src, dst, to) -> None
+PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    NEREUS_BEGIN
+    if (!counted(n, 4)) return nullptr;
+    Buffers from, to;
+    buffers_of(a[0], "pools", &from);
+    const bool within = a[3] == Py_None;
+    if (!within) buffers_of(a[3], "to", &to);
+    const Buffers& dst = within ? from : to;
+    if (from.t.empty() || dst.t.empty()) throw Wrong{"pools: expected a pool at least"};
+    if (dst.device != from.device) throw Wrong{"to: on another device than the pools"};
+    for (const at::Tensor* t : dst.t) writable(*t, within ? "pools" : "to");
+    const c10::cuda::OptionalCUDAGuard guard(from.device);
+    const nereus_pages_t p = pools_of(from, 0, "pools"), q = pools_of(dst, 0, "to");
+    const int64_t pairs = tensor_of(a[1], "src").numel();
+    const int32_t* src = ints_of(a[1], pairs, from.device, "src");
+    const int32_t* at = ints_of(a[2], pairs, from.device, "dst");
+    if (failed(nereus_cache_copy(&p, &q, pairs, src, at, stream_on(from.device)), "nereus_cache_copy")) return nullptr;
+    written(dst);
+    Py_RETURN_NONE;
+    NEREUS_END
+}
+
+// (pools, table, length, refs, parent, page_size, room, out) -> (table, length, refs, copies, status)
+PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    NEREUS_BEGIN
+    if (!counted(n, 8)) return nullptr;
+    Buffers pools;
+    buffers_of(a[0], "pools", &pools);
+    nereus_page_table_t from = {}, to = {};
+    const c10::Device device = table_of(a[1], &from, "table").device();
+    same_device(pools, device);
+    const c10::cuda::OptionalCUDAGuard guard(device);
+    for (const at::Tensor* t : pools.t) writable(*t, "pools");
+    from.length = ints_of(a[2], from.rows, device, "length");
+    const nereus_pages_t p = pools_of(pools, tensor_of(a[3], "refs").numel(), "pools");
+    from.refs = ints_of(a[3], p.pages, device, "refs");
+    const int64_t  rows = tensor_of(a[4], "parent").numel(), page_size = int_of(a[5]);
+    const int32_t* parent = ints_of(a[4], rows, device, "parent");
+    const int32_t* room_of = nullptr;
+    int64_t room = 0;
+    if (THPVariable_Check(a[6])) room_of = ints_of(a[6], rows, device, "room");
+    else room = int_of(a[6]);
+    THPObjectPtr table, length, refs;
+    if (a[7] == Py_None) {
+        table = THPVariable_Wrap(new_ints({rows, from.columns}, device));
+        length = THPVariable_Wrap(new_ints({rows}, device));
+        refs = THPVariable_Wrap(new_ints({p.pages}, device));
+    } else {
+        PyObject* o[3] = {item_of(a[7], 0, 3), item_of(a[7], 1, 3), item_of(a[7], 2, 3)};
+        for (PyObject* x : o) Py_INCREF(x);
+        table = o[0]; length = o[1]; refs = o[2];
+    }
+    if (table_of(table.get(), &to, "out").device() != device || to.rows != rows) throw Wrong{"out: the table has a row for each parent, on the same device"};
+    to.length = ints_of(length.get(), rows, device, "out");
+    to.refs = ints_of(refs.get(), p.pages, device, "out");
+    at::Tensor copies = new_ints({rows, 2}, device), status = new_ints({4}, device);
+    auto narrow = [](int64_t v) { return v < 0 || v > INT32_MAX ? -1 : (int)v; };            // out of range: refused by the library
+    if (failed(nereus_cache_fork(&p, &from, &to, parent, narrow(page_size), narrow(room), room_of, (int32_t*)copies.data_ptr(), (int32_t*)status.data_ptr(),
+                                 stream_on(device)), "nereus_cache_fork"))
+        return nullptr;
+    written(pools);
+    if (a[7] != Py_None)
+        for (PyObject* x : {table.get(), length.get(), refs.get()}) written(x);
+    THPObjectPtr c(THPVariable_Wrap(std::move(copies))), s(THPVariable_Wrap(std::move(status)));
+    return PyTuple_Pack(5, table.get(), length.get(), refs.get(), c.get(), s.get());
+    NEREUS_END
+}
+
+// (pools, table, refs, keep, out) -> (table, refs, map, moves, status)
+PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    NEREUS_BEGIN
+    if (!counted(n, 5)) return nullptr;
+    Buffers pools;
+    buffers_of(a[0], "pools", &pools);
+    nereus_page_table_t from = {}, to = {};
+    const c10::Device device = table_of(a[1], &from, "table").device();
+    same_device(pools, device);
+    const c10::cuda::OptionalCUDAGuard guard(device);
+    for (const at::Tensor* t : pools.t) writable(*t, "pools");
+    const nereus_pages_t p = pools_of(pools, tensor_of(a[2], "refs").numel(), "pools");
+    from.refs = ints_of(a[2], p.pages, device, "refs");
+    int64_t keep = -1;
+    if (a[3] != Py_None && (keep = int_of(a[3])) < 0) throw Wrong{"keep: a number of pages, or None"};
+    THPObjectPtr table, refs;
+    if (a[4] == Py_None) {
+        table = THPVariable_Wrap(new_ints({from.rows, from.columns}, device));
+        refs = THPVariable_Wrap(new_ints({p.pages}, device));
+    } else {
+        PyObject* o[2] = {item_of(a[4], 0, 2), item_of(a[4], 1, 2)};
+        for (PyObject* x : o) Py_INCREF(x);
+        table = o[0]; refs = o[1];
+    }
+    if (table_of(table.get(), &to, "out").device() != device) throw Wrong{"out: on another device"};
+    to.refs = ints_of(refs.get(), p.pages, device, "out");
+    at::Tensor map = new_ints({p.pages}, device), moves = new_ints({p.pages / 2, 2}, device), status = new_ints({4}, device);
+    if (failed(nereus_cache_compact(&p, &from, &to, keep, (int32_t*)map.data_ptr(), (int32_t*)moves.data_ptr(), (int32_t*)status.data_ptr(), stream_on(device)),
+               "nereus_cache_compact"))
+        return nullptr;
+    written(pools);
+    if (a[4] != Py_None)
+        for (PyObject* x : {table.get(), refs.get()}) written(x);
+    THPObjectPtr m(THPVariable_Wrap(std::move(map))), v(THPVariable_Wrap(std::move(moves))), s(THPVariable_Wrap(std::move(status)));
+    return PyTuple_Pack(5, table.get(), refs.get(), m.get(), v.get(), s.get());
+    NEREUS_END
+}
+
 // x -> uninitialised logits like x
 PyObject* empty_like_of(PyObject*, PyObject* x) {
     NEREUS_BEGIN
@@ -326,7 +617,9 @@ PyObject* set_error(PyObject*, PyObject* cls) {
 
 #define NEREUS_FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {NEREUS_FAST(process),         NEREUS_FAST(teacher_top),  NEREUS_FAST(distill_forward),
-                           NEREUS_FAST(distill_backward), NEREUS_FAST(distill_step), {"empty_like", empty_like_of, METH_O, nullptr},
+                           NEREUS_FAST(distill_backward), NEREUS_FAST(distill_step),
+                           NEREUS_FAST(beam_select),     NEREUS_FAST(reorder),     NEREUS_FAST(fork),
+                           NEREUS_FAST(compact),         NEREUS_FAST(copy),        {"empty_like", empty_like_of, METH_O, nullptr},
                            {"set_error", set_error, METH_O, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_nereus_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
