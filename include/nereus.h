@@ -439,8 +439,8 @@ int nereus_static_status(int* device_status);
  * One tensor [rows, vocab] is tp = 1; a tensor cut into column slices is tp slices with the tensor's row_stride.
  * Pointers are aligned to an element.  Any vocab >= 1 and any row_stride work; rows whose starts are congruent
  * modulo 16 bytes on the read and the written side are moved in 16-byte vectors.
- * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace and
- * may be captured into a CUDA graph.  rows = 0 is a call that does nothing.  A row's results are the same, bit for
+ * The calls below enqueue on `cuda_stream`, keep nothing after they return, allocate nothing, need no workspace (but for
+ * nereus_beam_select) and may be captured into a CUDA graph.  rows = 0 is a call that does nothing.  A row's results are the same, bit for
  * bit, whatever other rows the call has and wherever the row stands among them, as long as its shards start alike modulo
  * 16 bytes (nereus_logits_process: in calls with the same parts NULL and the same side of 32768 of history_len, too).
  * Common errors: ARG (null pointer, non-positive size, a shard or stride too small for its columns), UNSUPPORTED
@@ -515,10 +515,15 @@ typedef struct {
     const int32_t* ended;          /* [rows], or NULL: none has; outside [0, vocab): it goes on */
     const float*   norm;           /* [rows], or NULL = 1 */
 } nereus_beams_t;
-/* out_score, out_parent, out_token: [rows / beams, k].  Errors: common, ARG (beams, k, rows, settle), TOO_LARGE (vocab above
- * 2^24). */
-int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, float* out_score, int32_t* out_parent,
-                       int32_t* out_token, void* cuda_stream);
+/* Bytes of the workspace that a call with this view's shape and these beams and k needs on the current device, a few
+ * hundred per row and 64 KiB of logits.  Errors: as below. */
+int nereus_beam_workspace(const nereus_logits_t* in, const nereus_beams_t* how, size_t* bytes);
+/* out_score, out_parent, out_token: [rows / beams, k].  workspace (device, 16-byte aligned) is written and read by the call
+ * alone: calls that may overlap on the device, two captured graphs among them, have one each.  Unlike the other calls' a request's
+ * results are those of any batch but for the order in which the parts of a row's sum are added up, in 64 bits.
+ * Errors: common, ARG (beams, k, rows, settle), TOO_SMALL (workspace). */
+int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, void* workspace, size_t workspace_bytes, float* out_score,
+                       int32_t* out_parent, int32_t* out_token, void* cuda_stream);
 
 /* INFERENCE: what a teacher leaves for the training stage.  values[r, j], ids[r, j] (device, [rows, k]): the k largest
  * logits of row r in falling order, equal ones by rising id; lse[r] (device, [rows]) = log of the sum over the row of

@@ -201,7 +201,8 @@ _SIGS = {
     "nereus_distill_forward": [_P(Logits), _P(Distill), _vp, _vp, _vp],
     "nereus_distill_backward": [_P(Logits), _P(Distill), _vp, _vp, _P(Logits), _vp],
     "nereus_distill_step": [_P(Logits), _P(Distill), _vp, _P(Logits), _vp],
-    "nereus_beam_select": [_P(Logits), _P(Beams), _vp, _vp, _vp, _vp],
+    "nereus_beam_workspace": [_P(Logits), _P(Beams), _P(_sz)],
+    "nereus_beam_select": [_P(Logits), _P(Beams), _vp, _sz, _vp, _vp, _vp, _vp],
     "nereus_states_reorder": [_P(States), _P(States), _i, _vp, _vp, _vp],
     "nereus_cache_fork": [_P(Pages), _P(PageTable), _P(PageTable), _vp, _i, _i, _vp, _vp, _vp, _vp],
     "nereus_cache_compact": [_P(Pages), _P(PageTable), _P(PageTable), ctypes.c_int64, _vp, _vp, _vp, _vp],
@@ -559,9 +560,16 @@ def distill_step(src: Logits, how: Distill, loss, grad: Logits, stream=0) -> Non
     _ck(_lib.nereus_distill_step(src, how, loss, grad, stream), "nereus_distill_step")
 
 
-def beam_select(src: Logits, how: Beams, score, parent, token, stream=0) -> None:
-    """nereus_beam_select; score, parent, token: device addresses."""
-    _ck(_lib.nereus_beam_select(src, how, score, parent, token, stream), "nereus_beam_select")
+def beam_workspace(src: Logits, how: Beams) -> int:
+    """nereus_beam_workspace."""
+    n = _sz()
+    _ck(_lib.nereus_beam_workspace(src, how, ctypes.byref(n)), "nereus_beam_workspace")
+    return n.value
+
+
+def beam_select(src: Logits, how: Beams, workspace, workspace_bytes: int, score, parent, token, stream=0) -> None:
+    """nereus_beam_select; workspace, score, parent, token: device addresses."""
+    _ck(_lib.nereus_beam_select(src, how, workspace, workspace_bytes, score, parent, token, stream), "nereus_beam_select")
 
 
 def states_reorder(src: States, dst: States, beams: int, parent, length=0, stream=0) -> None:

@@ -1,15 +1,16 @@
 // One step of a beam search for sm_100a (nereus_beam_select): of what the beams of a request offer, score + x - log-sum-exp
 // over the vocabulary, the k best.
 //
-// Every logit is read once; the floor is HBM bandwidth, with one exponential an element next.  A cluster takes a request:
-//   * its blocks share every row of it (a few rows of 128256 are a megabyte, which one SM would read for 10 us), each summing
-//     the exponentials of its layers and noting the largest element of every thread's vectors of one or a few layers;
-//   * one exchange through distributed shared memory gives every block the log-sum-exp of every row, so that elements of
-//     different rows can be compared, and the largest elements that the warps have seen: the k-th largest of these bounds
-//     the k-th best hypothesis from below, whatever the order of the rows;
-//   * only vectors whose note reaches the bound are read again (from L2); what is found in them, little more than k
-//     hypotheses, goes to the first block, which ranks it by counting.
-// Where more is found than the lists hold (rows of few distinct values: a mask's lowest value, say), the bound is made exact
+// Every logit is read once; the floor is HBM bandwidth, with one exponential an element next (16 a clock and SM, which is what
+// bf16 from HBM asks three quarters of).  Two launches:
+//   * sum: the rows are cut into parts of a few layers, dealt out evenly to as many blocks as the GPU holds, whatever requests
+//     they belong to.  Of its part of a row a block leaves every warp's sum of exponentials, and of every thread the largest
+//     element that it has seen, in 16 bits rounded up: its note;
+//   * pick: a block for a request puts the sums together to log-sum-exps, so that elements of different rows can be compared.
+//     The notes are worth something then: of 8 sets of them the j-th largest bounds the k-th best hypothesis from below,
+//     whatever the order of the rows.  Only vectors whose note reaches the bound are read again; what is found in them, a
+//     few times k hypotheses, is ranked by counting.
+// Where more is found than the list holds (rows of few distinct values: a mask's lowest value, say), the bound is made exact
 // by counting the keys' bytes, the highest first, a pass over the request for each byte that is needed.
 // Hypotheses are compared in 64 bits, as keys of (total / norm, lower index): within a row these order as the logits do.
 #include "nereus_rows.hpp"
@@ -19,27 +20,154 @@ using namespace nereus;
 namespace nereus {
 namespace {
 
-constexpr int kMaxNotes = 64;                     // of a thread
-constexpr int kMaxItems = 512;                    // layers in the block's table at a time
-constexpr int kFound    = 1024;                   // hypotheses that a list holds
-constexpr int kNoted    = (kStreamRing * kVecs * 16 - kFound * 16) / 4;
+constexpr int kTH       = kThreads;               // of a summing block
+constexpr int kItems    = 256;                    // layers in its table at a time
+constexpr int kPart     = 16;                     // layers of a part, as a rule at most
+constexpr int kParts    = 256;                    // parts of a request's rows, as far as a part's layers fit the table
+constexpr int kPick     = 512;                    // threads of a picking block
+constexpr int kPickWarps = kPick / 32;
+constexpr int kSets     = 8;
+constexpr int kFound    = 1024;                   // hypotheses that its list holds
+constexpr int kNoted    = 2048;
 typedef unsigned long long Key;
 
-struct Found {
-    Key      key;
-    uint32_t index;                               // beam * vocab + token
-    float    total;
+// Sums of exponentials are kept as (K, sum of 2^(x c - K)) with a whole number K near the largest x c, so that sums of different
+// threads go together without another rounding; a thread adds up 2 vectors in 32 bits and these in 64.  c = log2(e) has 24
+// bits, kLog2eLow is the rest: it is put right for the largest element of a row at the end, and an element at a distance of d
+// from that is off by 2e-8 d of itself.  K stays within +-2^22: a row whose largest element lies beyond (a mask's lowest value
+// in all of it, say) is summed again, by differences from it.
+constexpr float  kLargestK = 0x1p22f;
+constexpr double kLog2eLow = 1.4426950408889634 - (double)kLog2e, kLn2 = 0.69314718055994531;
+struct Sum {
+    double sum;
+    float  k, top;                                // and the largest element
 };
-static_assert(sizeof(Found) == 16, "Found is moved as 16 bytes");
+__device__ __forceinline__ double power_of_two(float k) {        // k whole and not above 0
+    return !(k >= -1000.f) ? 0.0 : __longlong_as_double((long long)(1023 + (int)k) << 52);
+}
+// log2 of a positive normal number, 1e-7 off
+__device__ __forceinline__ double log2_of(double x) {
+    const long long u = __double_as_longlong(x);
+    return (double)((int)(u >> 52) - 1023) + (double)log2f((float)__longlong_as_double((u & 0xfffffffffffffll) | 1023ll << 52));
+}
 
 struct Select {
-    int32_t beams, k, settle, per_note, notes;    // layers of a note, notes of a row
+    int32_t beams, k, settle, rows;
+    int32_t parts, of_part;                       // parts of a row, layers of a part (a power of two)
+    float   per_shard_1;                          // 1 / layers of a shard
     const float*   score;
     const int32_t* ended;
     const float*   norm;
+    Sum*      sums;                               // [rows, parts, kWarps]
+    uint16_t* notes;                              // [rows, parts, kTH]
     float*   out_score;
     int32_t *out_parent, *out_token;
 };
+// a / b for a below 2^22, one_by = 1 / b rounded: off by one at most before it is put right.
+__device__ __forceinline__ int quotient(int a, int b, float one_by) {
+    const int q = (int)((float)a * one_by), r = a - q * b;
+    return q + (r >= b) - (r < 0);
+}
+// Whether a beam's row is read: its score and norm are numbers and it has not ended.
+__device__ __forceinline__ bool offers(const Select& s, int64_t row, int vocab, float* score, float* norm, int* ended) {
+    *score = s.score[row];
+    *norm = s.norm ? s.norm[row] : 1.f;
+    *ended = s.ended ? s.ended[row] : -1;
+    return fabsf(*score) < INFINITY && *norm > 0.f && *norm < INFINITY;
+}
+template <class T> __device__ __forceinline__ Layer layer_at(const LogitsCut& in, const Deal& deal, const Select& s, int64_t row, int l) {
+    if (l >= deal.layers) return {nullptr, nullptr, 0, 0, 0, 0};
+    const int shard = quotient(l, deal.per_shard, s.per_shard_1);
+    return layer_in<T, T, kTH>(in, LogitsCut(), row, shard, (l - shard * deal.per_shard) * kPerLayer<T, kTH>);
+}
+
+// ---- sums ----------------------------------------------------------------------------------------------------
+
+template <class T>
+__global__ void __launch_bounds__(kTH, 4) beam_sum_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
+    __shared__ __align__(16) uint4 ring[kStreamRing * kVecs];
+    __shared__ Layer    table[kItems];
+    __shared__ uint32_t unit_of[kItems];
+    __shared__ int      of_warp[kWarps + 1];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    typename Vec<T>::Max top = Vec<T>::lowest();
+    float  k = -kLargestK;
+    double sum = 0.0;
+    int    i = 0;
+    const uint4* from = ring + tid;
+    const Pair   c = pair(kLog2e, kLog2e);
+    const int64_t units = (int64_t)s.rows * s.parts;
+    const int     log_part = __ffs(s.of_part) - 1, slots = kItems >> log_part;
+    for (int64_t first = blockIdx.x; first < units; first += (int64_t)slots * gridDim.x) {
+        // of the next units those whose rows are read, in order
+        const int64_t unit = first + (int64_t)tid * gridDim.x;
+        bool is = tid < slots && unit < units;
+        if (is) {
+            float score, norm;
+            int   ended;
+            is = offers(s, (uint32_t)unit % (uint32_t)s.rows, in.vocab, &score, &norm, &ended) && (uint32_t)ended >= (uint32_t)in.vocab;
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, is);
+        __syncthreads();
+        if (lane == 0) of_warp[warp] = __popc(who);
+        __syncthreads();
+        int before = 0, n = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += of_warp[w];
+            n += of_warp[w];
+        }
+        if (is) unit_of[before + __popc(who & ((1u << lane) - 1))] = (uint32_t)unit;
+        __syncthreads();
+        const int items = n << log_part;
+        if (tid < items) {
+            const uint32_t u = unit_of[tid >> log_part];
+            const int      part = (int)(u / (uint32_t)s.rows);
+            table[tid] = layer_at<T>(in, deal, s, u - (uint32_t)part * (uint32_t)s.rows, (part << log_part) + (tid & (s.of_part - 1)));
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int l = 0; l < kStreamRing; ++l) load_layer<T, kTH>(table, ring, l, l, items);
+        int slot = 0;
+#pragma unroll 1
+        for (int item = 0; item < items; ++item) {
+            copy_wait<kStreamRing - 1>();
+            const uint4 a = from[slot * kVecs], b = from[slot * kVecs + kTH];
+            if (item + kStreamRing < items) load_layer<T, kTH>(table, ring, slot, item + kStreamRing, items);
+            else copy_commit();
+            slot = slot + 1 == kStreamRing ? 0 : slot + 1;
+            top = Vec<T>::join(top, Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b)));
+            const float v = Vec<T>::value(top);
+            // an element ahead of K carries the roundings of the distance: 2^4 at most
+            if (v * kLog2e > k + 4.f) {
+                const float to = fminf(fmaxf(rintf(v * kLog2e), -kLargestK), kLargestK);
+                sum *= power_of_two(k - to);
+                k = to;
+            }
+            const Pair   minus = pair(-k, -k);
+            const float2 h = halves(add2(exp_sum<T, false>(a, c, c, minus), exp_sum<T, false>(b, c, c, minus)));
+            sum += (double)(h.x + h.y);
+            if (++i == s.of_part) {
+                const uint32_t u = unit_of[item >> log_part];
+                const int      part = (int)(u / (uint32_t)s.rows);
+                const int64_t  at = (int64_t)(u - (uint32_t)part * (uint32_t)s.rows) * s.parts + part;
+                s.notes[at * kTH + tid] = note_of(v);
+                const float all = warp_max(k), most = warp_max(v);
+                double      of_lanes = sum * power_of_two(k - all);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) of_lanes += __shfl_xor_sync(0xffffffffu, of_lanes, o);
+                if (lane == 0) s.sums[at * kWarps + warp] = {of_lanes, all, most};
+                top = Vec<T>::lowest();
+                k = -kLargestK;
+                sum = 0.0;
+                i = 0;
+            }
+        }
+    }
+}
+
+// ---- the pick ------------------------------------------------------------------------------------------------
 
 // orders as the values do, -0 as +0
 __device__ __forceinline__ Key key_of_double(double x) {
@@ -48,275 +176,224 @@ __device__ __forceinline__ Key key_of_double(double x) {
 }
 constexpr Key kKeyNone = 0x000fffffffffffffull;   // of -inf
 
-__device__ __forceinline__ uint32_t peer_load(const void* p, int rank) {
-    uint32_t r;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(r) : "r"(peer_address(p, rank)) : "memory");
-    return r;
-}
-__device__ __forceinline__ float2 peer_load2(const void* p, int rank) {
-    float2 r;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(peer_address(p, rank)) : "memory");
-    return r;
-}
-__device__ __forceinline__ uint4 peer_load4(const void* p, int rank) {
-    uint4 r;
-    asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(peer_address(p, rank)) : "memory");
-    return r;
-}
-
-// A row of the request that is read.
-struct Live {
+// A beam of the request.
+struct Beam {
     double   off, norm;                           // score - log-sum-exp; NaN: the row offers nothing
+    float    off_1, inverse;                      // off and 1 / norm in 32 bits
     float    least;                               // elements below are not among the best; NaN: none is
-    int32_t  beam;
+    float    score;
+    int32_t  ended;                               // its token, -1: it goes on
+    int32_t  pad;
 };
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 4) beam_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s, const Scale scale) {
+__global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
     constexpr int E = kPerVec<T>;
-    extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ float2   part[NEREUS_BEAM_MAX][kWarps];     // of every row and warp: largest element, sum of exponentials
-    __shared__ float    quarter[8][kWarps * 4];            // ... of the first rows and every 8 lanes: largest element
-    __shared__ Live     live[NEREUS_BEAM_MAX];
-    __shared__ uint32_t histogram[2][256];
-    __shared__ uint32_t choice[4];
-    __shared__ int      n_live, n_found, n_noted, n_exact;
+    __shared__ Beam     beams[NEREUS_BEAM_MAX];
+    __shared__ __align__(16) Key found[kFound];
+    __shared__ struct { uint32_t index; float total; } rest[kFound];       // index: beam * vocab + token
+    __shared__ uint32_t noted[kNoted];
+    __shared__ uint32_t peak[kPick], histogram[256], at_place[NEREUS_BEAM_MAX_K], choice[4], of_warp[kPickWarps];
+    __shared__ int      n_found, n_noted;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int blocks = 1 << deal.log_c, rank = (int)blockIdx.x & (blocks - 1);
-    const int64_t request = blockIdx.x >> deal.log_c, first_row = request * s.beams;
+    const int64_t request = blockIdx.x, first_row = request * s.beams;
 
-    uint4*    ring = reinterpret_cast<uint4*>(dynamic);
-    Layer*    table = reinterpret_cast<Layer*>(ring + kStreamRing * kVecs);
-    const int room = min(kMaxItems, s.beams * deal.mine);
-    uint16_t* notes = reinterpret_cast<uint16_t*>(table + room) + tid;      // of this thread
-    Found*    found = reinterpret_cast<Found*>(ring);                       // once the rows have gone through
-    uint32_t* noted = reinterpret_cast<uint32_t*>(found + kFound);
-
-    // the rows that are read, in order
-    if (warp < 2) {
-        // both halves' counts on both warps: 64 beams at most
-        int before = 0;
-        for (int half = 0; half <= warp; ++half) {
-            const int b = half * 32 + lane;
-            bool is = b < s.beams;
-            float norm = 1.f;
-            if (is) {
-                const float score = s.score[first_row + b];
-                if (s.norm) norm = s.norm[first_row + b];
-                is = fabsf(score) < INFINITY && norm > 0.f && norm < INFINITY && !(s.ended && (uint32_t)s.ended[first_row + b] < (uint32_t)in.vocab);
-            }
-            const uint32_t who = __ballot_sync(0xffffffffu, is);
-            if (half == warp && is) {
-                Live& l = live[before + __popc(who & ((1u << lane) - 1))];
-                l.beam = b;
-                l.norm = norm;
-            }
-            before += __popc(who);
-        }
-        if (warp == 1 && lane == 0) n_live = before;
+    for (int b = tid; b < s.beams; b += kPick) {
+        Beam  r;
+        float norm;
+        const bool is = offers(s, first_row + b, in.vocab, &r.score, &norm, &r.ended);
+        if ((uint32_t)r.ended >= (uint32_t)in.vocab) r.ended = -1;
+        r.norm = (double)norm;
+        r.inverse = 1.f / norm;
+        r.off = is ? (double)r.score : (double)NAN;
+        r.least = NAN;
+        beams[b] = r;
     }
-    if (tid == 0) n_found = n_noted = n_exact = 0;
+    if (tid == 0) n_found = n_noted = 0;
     __syncthreads();
-    const int n = n_live, mine = deal.mine;
+    asm volatile("griddepcontrol.wait;" ::: "memory");                      // the sums and notes are there
 
-    // which of a row's shares this block has: rows take turns, so that short rows come to all blocks
-    auto share_of = [&](int q) { return (rank + live[q].beam) & (blocks - 1); };
-    auto layer_at = [&](int q, int i) {
-        return layer_of<T, T>(in, LogitsCut(), deal, first_row + live[q].beam, share_of(q), i);
-    };
-
-    {
-        Running<true> running(scale.high, scale.low);
-        typename Vec<T>::Max top = Vec<T>::lowest();
-        float to_note = -INFINITY;
-        int   q = 0, i = 0, in_note = 0;
-        for (int first = 0; first < n * mine; first += room) {
-            const int items = min(room, n * mine - first);
-            if (first) __syncthreads();
-            for (int j = tid; j < items; j += kThreads) table[j] = layer_at((first + j) / mine, (first + j) % mine);
-            __syncthreads();
-            start_stream<T, kThreads, kStreamRing>(table, ring, items);
-            stream<T, kThreads, kStreamRing>(table, ring, items, [&](int item, uint4 a, uint4 b) {
-                const Layer& L = table[item];
-                if (L.hi > L.lo) {                         // the same for the block; else the ring holds another layer's vectors
-                    const typename Vec<T>::Max m = Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b));
-                    const float v = Vec<T>::value(m);
-                    top = Vec<T>::join(top, m);
-                    to_note = fmaxf(to_note, v);
-                    running.see(v);
-                    running.template add<T>(a, b);
-                }
-                const bool end = i + 1 == mine;
-                if (++in_note == s.per_note || end) {
-                    notes[(q * s.notes + i / s.per_note) * kThreads] = note_of(to_note);
-                    to_note = -INFINITY;
-                    in_note = 0;
-                }
-                if (end) {
-                    const float m = Vec<T>::value(top), all = warp_max(m);
-                    const float sum = warp_sum(running.sum * scale_finely(running.base, all, 1.4426950408889634));
-                    if (lane == 0) part[q][warp] = make_float2(all, sum);
-                    if (q < 8) {
-                        float g = m;
-#pragma unroll
-                        for (int o = 1; o < 8; o *= 2) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, o));
-                        if ((lane & 7) == 0) quarter[q][warp * 4 + (lane >> 3)] = g;
-                    }
-                    running = Running<true>(scale.high, scale.low);
-                    top = Vec<T>::lowest();
-                    i = 0;
-                    ++q;
-                } else {
-                    ++i;
-                }
-            });
+    // every row's log-sum-exp, a warp for each
+    const int entries = s.parts * kWarps;
+    for (int b = warp; b < s.beams; b += kPickWarps) {
+        Beam& r = beams[b];
+        if (r.off != r.off || r.ended >= 0) {
+            if (lane == 0) r.off_1 = NAN;
+            continue;
         }
-    }
-    cluster_arrive();
-    cluster_wait();
-
-    // every row's log-sum-exp, the same in every block: its shares in the row's own order
-    for (int q = warp; q < n; q += kWarps) {
-        float2    v[kMaxCtas * kWarps / 32];
-        float     all = -INFINITY;
-        const int entries = blocks * kWarps;
-#pragma unroll
-        for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) {
-            const int e = j * 32 + lane;
-            v[j] = e < entries ? peer_load2(&part[q][e % kWarps], (e / kWarps - live[q].beam) & (blocks - 1)) : make_float2(-INFINITY, 0.f);
-            all = fmaxf(all, v[j].x);
-        }
-        all = warp_max(all);
+        const Sum* sums = s.sums + (first_row + b) * entries;
+        float  k = -INFINITY, top = -INFINITY;
         double sum = 0.0;
-#pragma unroll
-        for (int j = 0; j < kMaxCtas * kWarps / 32; ++j) sum += (double)v[j].y * (double)scale_finely(v[j].x, all, 1.4426950408889634);
+        for (int e = lane; e < entries; e += 32) {
+            const uint4 u = __ldcg(reinterpret_cast<const uint4*>(sums + e));
+            const float of_k = __uint_as_float(u.z), to = fmaxf(k, of_k);
+            sum = fma(__longlong_as_double((long long)((Key)u.y << 32 | u.x)), power_of_two(of_k - to), sum * power_of_two(k - to));
+            k = to;
+            top = fmaxf(top, __uint_as_float(u.w));
+        }
+        const float all = warp_max(k);
+        top = warp_max(top);
+        sum *= power_of_two(k - all);
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        double lse = kLn2 * ((double)all + log2_of(sum) + (double)top * kLog2eLow);
+        if (fabsf(top * kLog2e) >= kLargestK && fabsf(top) < INFINITY) {
+            sum = 0.0;
+            for (int l = 0; l < deal.layers; ++l) {
+                const Layer L = layer_at<T>(in, deal, s, first_row + b, l);
+                for (int vec = lane; vec < kVecs; vec += 64)
+                    sum += (double)exp_sum_far<T>(edge_vector<T>(L, vec), edge_vector<T>(L, vec + 32), top, pair(kLog2e, kLog2e));
+            }
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            lse = (double)top + kLn2 * log2_of(sum);
+        }
         if (lane == 0) {
-            const bool ok = all > -INFINITY && all < INFINITY && sum > 0.0 && sum < (double)INFINITY;
-            live[q].off = ok ? (double)s.score[first_row + live[q].beam] - ((double)all + log(sum)) : NAN;
+            r.off = fabsf(top) < INFINITY && sum == sum ? r.off - lse : (double)NAN;
+            r.off_1 = (float)r.off;
         }
     }
     __syncthreads();
 
-    // what an element is worth: off + x, by the norm; in 64 bits
-    auto worth = [&](const Live& l, float x, double* total) {
-        *total = l.off + (double)x;
-        return s.norm ? *total / l.norm : *total;
+    // What an element is worth: off + x, by the norm; in 64 bits, and in 32 and a little less for the roundings.
+    auto worth = [&](const Beam& r, float x, double* total) {
+        *total = r.off + (double)x;
+        return s.norm ? *total / r.norm : *total;
     };
-
-    // the k-th largest of the groups' largest elements; few rows: groups of 8 lanes, else of a warp
+    auto worth_below = [](const Beam& r, float x) {
+        const float w = fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse;
+        return fmaf(-1e-6f, fabsf(w), w);
+    };
+    // Notes, 8 at a time: those of one row and part.
+    const uint4* const all_notes = reinterpret_cast<const uint4*>(s.notes + first_row * s.parts * kTH);
+    constexpr int kEach = kTH / 8;
+    const int     groups = s.beams * s.parts * kEach;
+    const float   parts_1 = 1.f / (float)(s.parts * kEach);
     {
-        const bool small = n * blocks * kWarps < 4 * s.k && n <= 8;
-        const int  of_row = blocks * (small ? kWarps * 4 : kWarps);
-        float      v = -INFINITY;
-        for (int g = tid; g < n * of_row; g += kThreads) {
-            const int q = g / of_row, e = g - q * of_row;
-            if (live[q].off != live[q].off) continue;
-            const float x = small ? __uint_as_float(peer_load(&quarter[q][e & (kWarps * 4 - 1)], e / (kWarps * 4)))
-                                  : __uint_as_float(peer_load(&part[q][e & (kWarps - 1)].x, e / kWarps));
-            double total;
-            if (x > -INFINITY) v = fmaxf(v, __double2float_rd(worth(live[q], x, &total)));
+        float most = -INFINITY;
+#pragma unroll 4
+        for (int g = tid; g < groups; g += kPick) {
+            const Beam& r = beams[quotient(g, s.parts * kEach, parts_1)];
+            const uint4 v = __ldcg(all_notes + g);
+            // the largest of 8 notes is the largest as bf16; that of a fp32 was rounded up: the next below is not above it
+            const float up = Vec<__nv_bfloat16>::value(Vec<__nv_bfloat16>::max(v));
+            const float x = sizeof(T) == 2 ? up : note_below((uint16_t)(__float_as_uint(up) >> 16));
+            if (up > -INFINITY && r.off_1 == r.off_1) most = fmaxf(most, worth_below(r, x));
         }
-        const uint32_t key = key_of(v);
-        uint32_t       t = 0;
+        peak[tid] = key_of(most);
+    }
+    __syncthreads();
+    // of each set the j-th largest; the least of these bounds the k-th best from below
+    {
+        const int j = (s.k + kSets - 1) / kSets;
+        uint32_t  t = 0xffffffffu;
+        if (warp < kSets) {
+            uint32_t key = 0;
+            // a row's notes are on neighbouring threads: every set has its share of every row's
+            for (int x = lane * kSets + warp; x < kPick; x += kSets * 32) key = max(key, peak[x]);
 #pragma unroll 1
-        for (int bit = 31; bit >= 16; --bit) {
-            const uint32_t u = t | 1u << bit;
-            if (__syncthreads_count(key >= u) >= s.k) t = u;
+            for (int i = 0; i < j; ++i) {
+                t = __reduce_max_sync(0xffffffffu, key);
+                if (lane == __ffs(__ballot_sync(0xffffffffu, key == t)) - 1) key = 0;
+            }
+            if (lane == 0) of_warp[warp] = t;
         }
-        if (tid < n) {
-            Live&       l = live[tid];
-            const float bound = t > kKeyMinusInf ? value_of(t) : -INFINITY;
+        __syncthreads();
+        t = __reduce_min_sync(0xffffffffu, lane < kSets ? of_warp[lane] : 0xffffffffu);
+        const float bound = t > kKeyMinusInf ? value_of(t) : -INFINITY;
+        for (int b = tid; b < s.beams; b += kPick) {
+            Beam& r = beams[b];
             // the least x whose worth reaches the bound, or a little less
-            const double at = (double)bound * l.norm - l.off, slack = 1e-14 * (fabs((double)bound * l.norm) + fabs(l.off));
-            l.least = l.off != l.off ? NAN : bound > -INFINITY ? __double2float_rd(at - slack) : -INFINITY;
+            const float norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
+            r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
+        }
+        __syncthreads();
+        // the notes that reach it
+#pragma unroll 4
+        for (int g = tid; g < groups; g += kPick) {
+            const float least = beams[quotient(g, s.parts * kEach, parts_1)].least;
+            const uint4 v = __ldcg(all_notes + g);
+            const float up = Vec<__nv_bfloat16>::value(Vec<__nv_bfloat16>::max(v));
+            if (!(up >= least && up > -INFINITY)) continue;
+            float x[8];
+            unpack<__nv_bfloat16>(v, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (x[e] >= least && x[e] > -INFINITY) {
+                    const int at = atomicAdd(&n_noted, 1);
+                    if (at < kNoted) noted[at] = (uint32_t)(g * 8 + e);
+                }
         }
     }
     __syncthreads();
 
-    // f(key, total, index) for every element of this thread's vector `vec` of a layer that may be among the best
-    auto look = [&](const Live& l, const Layer& L, int vec, auto f) {
-        const int a = L.lo - vec * E, b = L.hi - vec * E;
-        if (b <= 0 || a >= E) return;
+    // f(key, total, index) for every element of vector `vec` of a layer that may be among the best
+    auto look = [&](int b, const Layer& L, int vec, auto f) {
+        const Beam& r = beams[b];
+        const int   lo = L.lo - vec * E, hi = L.hi - vec * E;
+        if (hi <= 0 || lo >= E) return;
         float x[E];
         unpack<T>(edge_vector<T>(L, vec), x);
-        const uint32_t inside = bits_between(a, b, E);
+        uint32_t hits = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if ((inside >> e & 1u) && x[e] >= l.least && x[e] > -INFINITY) {
-                double    total;
-                const Key key = key_of_double(worth(l, x[e], &total));
-                if (key > kKeyNone) f(key, (float)total, (uint32_t)(l.beam * in.vocab + L.token + vec * E + e));
-            }
+        for (int e = 0; e < E; ++e) hits |= (x[e] >= r.least && x[e] > -INFINITY ? 1u : 0u) << e;
+        hits &= bits_between(lo, hi, E);
+#pragma unroll 1
+        for (; hits; hits &= hits - 1) {
+            const int e = __ffs(hits) - 1;
+            float y = x[0];
+#pragma unroll
+            for (int o = 1; o < E; ++o) y = o == e ? x[o] : y;
+            double    total;
+            const Key key = key_of_double(worth(r, y, &total));
+            if (key > kKeyNone) f(key, (float)total, (uint32_t)(b * in.vocab + L.token + vec * E + e));
+        }
     };
-    auto push = [&](int* count, Key key, float total, uint32_t index) {
-        const int at = atomicAdd(count, 1);
-        if (at < kFound) found[at] = {key, index, total};
+    auto push = [&](Key key, float total, uint32_t index) {
+        const int at = atomicAdd(&n_found, 1);
+        if (at < kFound) {
+            found[at] = key;
+            rest[at] = {index, total};
+        }
     };
-    // the beams that have ended offer themselves; the first block sees to them
+    // the beams that have ended offer themselves
     auto each_ended = [&](auto f) {
-        if (rank || !s.ended || tid >= s.beams) return;
-        const int   token = s.ended[first_row + tid];
-        const float score = s.score[first_row + tid], norm = s.norm ? s.norm[first_row + tid] : 1.f;
-        if ((uint32_t)token >= (uint32_t)in.vocab || !(fabsf(score) < INFINITY) || !(norm > 0.f && norm < INFINITY)) return;
-        f(key_of_double(s.norm ? (double)score / (double)norm : (double)score), score, (uint32_t)(tid * in.vocab + token));
+        if (tid >= s.beams) return;
+        const Beam& r = beams[tid];
+        if (r.ended >= 0 && r.off == r.off) f(key_of_double(s.norm ? r.off / r.norm : r.off), r.score, (uint32_t)(tid * in.vocab + r.ended));
     };
-
-    for (int q = 0; q < n; ++q) {
-        const float least = live[q].least;
-        for (int j = 0; j < s.notes; ++j) {
-            const float top = value_of_note(notes[(q * s.notes + j) * kThreads]);
-            if (top >= least && top > -INFINITY) {
-                const int at = atomicAdd(&n_noted, 1);
-                if (at < kNoted) noted[at] = (uint32_t)((q * s.notes + j) * kThreads + tid);
-            }
+    const int log_part = __ffs(s.of_part) - 1, noted_all = n_noted;
+    if (noted_all <= kNoted) {
+        // every vector of a note on a thread of its own
+        const int log_vecs = log_part + 1, vecs = noted_all << log_vecs;
+        for (int j = tid; j < vecs; j += kPick) {
+            const uint32_t which = noted[j >> log_vecs];
+            const int      row_part = which / kTH, b = quotient(row_part, s.parts, parts_1 * kEach), part = row_part - b * s.parts;
+            const int      l = (part << log_part) + (j >> 1 & (s.of_part - 1));
+            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + (j & 1) * kTH, push);
         }
     }
+    each_ended(push);
     __syncthreads();
-    const bool full = n_noted > kNoted;
-    if (!full) {
-        const int vecs = n_noted * 2 * s.per_note;
-        for (int j = tid; j < vecs; j += kThreads) {
-            const uint32_t which = noted[j / (2 * s.per_note)], note = which / kThreads;
-            const int      q = note / s.notes, i = note % s.notes * s.per_note + j / 2 % s.per_note, vec = which % kThreads + j % 2 * kThreads;
-            if (i < mine) look(live[q], layer_at(q, i), vec, [&](Key key, float total, uint32_t index) { push(&n_found, key, total, index); });
-        }
-    }
-    each_ended([&](Key key, float total, uint32_t index) { push(&n_found, key, total, index); });
-    __syncthreads();
-    if (tid == 0 && full) n_found = kFound + 1;
-    cluster_arrive();
-    cluster_wait();
 
-    int* count = &n_found;
-    int  total = 0;
-    bool crowded = false;
-    for (int r = 0; r < blocks; ++r) {
-        const int c = (int)peer_load(&n_found, r);
-        crowded |= c > kFound;
-        total += c;
-    }
-    if (crowded || total > kFound) {
+    if (noted_all > kNoted || n_found > kFound) {
         // The k-th key exactly, or as much of it as leaves few enough: byte by byte of (key, ~index), the 12 bytes highest
         // first, by the number of hypotheses that share the bytes found so far.
         Key      key_is = 0, key_mask = 0;
         uint32_t index_is = 0, index_mask = 0;
         int      left = s.k, above = 0;
-        bool     done = false;
         auto each = [&](auto f) {
-            for (int q = 0; q < n; ++q) {
-                if (live[q].off != live[q].off) continue;
-                for (int i = 0; i < mine; ++i) {
-                    const Layer L = layer_at(q, i);
-                    for (int vec = tid; vec < kVecs; vec += kThreads) look(live[q], L, vec, f);
+            for (int b = 0; b < s.beams; ++b) {
+                if (beams[b].least != beams[b].least) continue;
+                for (int l = 0; l < deal.layers; ++l) {
+                    const Layer L = layer_at<T>(in, deal, s, first_row + b, l);
+                    for (int vec = tid; vec < kVecs; vec += kPick) look(b, L, vec, f);
                 }
             }
             each_ended(f);
         };
 #pragma unroll 1
-        for (int byte = 0; byte < 12 && !done; ++byte) {
-            uint32_t* const h = histogram[byte & 1];
-            h[tid] = 0;
+        for (int byte = 0; byte < 12; ++byte) {
+            if (tid < 256) histogram[tid] = 0;
+            if (tid == 0) choice[0] = 256;
             __syncthreads();
             int      bin = 0;
             uint32_t run = 0;                              // elements of one bin come one after the other
@@ -324,144 +401,197 @@ __global__ void __launch_bounds__(kThreads, 4) beam_kernel(const __grid_constant
                 if (((key ^ key_is) & key_mask) || ((~index ^ index_is) & index_mask)) return;
                 const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : ~index >> (88 - 8 * byte)) & 255;
                 if (b != bin) {
-                    if (run) atomicAdd(&h[bin], run);
+                    if (run) atomicAdd(&histogram[bin], run);
                     bin = b;
                     run = 0;
                 }
                 ++run;
             });
-            if (run) atomicAdd(&h[bin], run);
-            cluster_arrive();
-            cluster_wait();
-            uint32_t c = 0;
-            for (int r = 0; r < blocks; ++r) c += peer_load(&h[255 - tid], r);
+            if (run) atomicAdd(&histogram[bin], run);
+            __syncthreads();
             // the bins from the highest down: how many there are up to this one
-            uint32_t upto = c;
+            const uint32_t c = tid < 256 ? histogram[255 - tid] : 0;
+            uint32_t       upto = c;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
                 const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
                 if (lane >= o) upto += u;
             }
-            __shared__ uint32_t of_warp[kWarps];
             if (lane == 31) of_warp[warp] = upto;
-            if (tid == 0) choice[0] = 256;
             __syncthreads();
             for (int w = 0; w < warp; ++w) upto += of_warp[w];
-            if (upto >= (uint32_t)left && upto - c < (uint32_t)left) {
+            if (tid < 256 && upto >= (uint32_t)left && upto - c < (uint32_t)left) {
                 choice[0] = 255 - tid;
                 choice[1] = upto - c;
                 choice[2] = c;
             }
             __syncthreads();
-            const uint32_t b = choice[0];
-            if (b == 256) { done = true; break; }          // fewer than k in all: everything is taken
-            above += (int)choice[1];
-            left -= (int)choice[1];
+            const uint32_t b = choice[0], higher = choice[1], same = choice[2];
+            __syncthreads();
+            if (b == 256) break;                           // fewer than k in all: everything is taken
+            above += (int)higher;
+            left -= (int)higher;
             if (byte < 8) { key_is |= (Key)b << (56 - 8 * byte); key_mask |= (Key)255 << (56 - 8 * byte); }
             else { index_is |= b << (88 - 8 * byte); index_mask |= 255u << (88 - 8 * byte); }
-            done = above + (int)choice[2] <= kFound;
-            __syncthreads();
+            if (above + (int)same <= kFound) break;
         }
-        // everything from the bytes found on; this list's counter is another one, since the others may still read the first
-        count = &n_exact;
+        if (tid == 0) n_found = 0;
+        __syncthreads();
+        // everything from the bytes found on
         each([&](Key key, float total, uint32_t index) {
-            const Key k = key & key_mask;
-            if (k > key_is || (k == key_is && (~index & index_mask) >= index_is)) push(&n_exact, key, total, index);
+            const Key top = key & key_mask;
+            if (top > key_is || (top == key_is && (~index & index_mask) >= index_is)) push(key, total, index);
         });
-        cluster_arrive();
-        cluster_wait();
+        __syncthreads();
     }
 
-    if (rank == 0) {
-        // the other blocks' lists behind this one's
-        int at = min(*count, kFound);
-        for (int r = 1; r < blocks; ++r) {
-            const int c = min((int)peer_load(count, r), kFound - at);
-            for (int j = tid; j < c; j += kThreads) *reinterpret_cast<uint4*>(found + at + j) = peer_load4(found + j, r);
-            at += c;
+    // which hypothesis is the j-th, and its beam in the upper half
+    const int total = n_found, quads = (total + 3) / 4;    // keys are read four at a time
+    if (tid < s.k) at_place[tid] = 0xffffffffu;
+    if (tid < 4 * quads - total) found[total + tid] = 0;
+    __syncthreads();
+    // a key on `team` neighbouring threads that share the comparing
+    const int team = total <= 32 ? 16 : total <= 64 ? 8 : total <= 128 ? 4 : total <= 256 ? 2 : 1, sub = tid & (team - 1);
+    for (int j = tid / team; j < (total + 31) / 32 * 32; j += kPick / team) {
+        const Key me = j < total ? found[j] : 0;
+        int place = 0, equal = 0;
+#pragma unroll 2
+        for (int o = sub; o < quads; o += team) {
+            const ulonglong2 a = reinterpret_cast<const ulonglong2*>(found)[2 * o], b = reinterpret_cast<const ulonglong2*>(found)[2 * o + 1];
+            place += (a.x > me) + (a.y > me) + (b.x > me) + (b.y > me);
+            equal += (a.x == me) + (a.y == me) + (b.x == me) + (b.y == me);
         }
-        total = at;
+        for (int o = 1; o < team; o *= 2) {
+            place += __shfl_xor_sync(0xffffffffu, place, o);
+            equal += __shfl_xor_sync(0xffffffffu, equal, o);
+        }
+        if (!me || sub || place >= s.k) continue;
+        const uint32_t index = rest[j].index;
+        if (equal > 1)
+            for (int o = 0; o < total; ++o) place += found[o] == me && rest[o].index < index;
+        if (place < s.k) at_place[place] = (uint32_t)j | index / (uint32_t)in.vocab << 16;
     }
-    cluster_arrive();                                      // nothing is read from the others from here on
-    if (rank == 0) {
-        __syncthreads();
-        uint32_t* const at_place = noted;                  // which hypothesis is the j-th, and its beam in the upper half
-        if (tid < s.k) at_place[tid] = 0xffffffffu;
-        __syncthreads();
-        const int team = total <= 32 ? 8 : total <= 64 ? 4 : total <= 128 ? 2 : 1, sub = tid & (team - 1);
-        for (int j = tid / team; j < (total + 31) / 32 * 32; j += kThreads / team) {
-            const Found me = found[min(j, max(total - 1, 0))];
-            int place = 0;
-            for (int o = sub; o < total; o += team) place += found[o].key > me.key || (found[o].key == me.key && found[o].index < me.index);
-            for (int o = 1; o < team; o *= 2) place += __shfl_xor_sync(0xffffffffu, place, o);
-            if (j < total && sub == 0 && place < s.k) at_place[place] = (uint32_t)j | me.index / (uint32_t)in.vocab << 16;
-        }
-        __syncthreads();
-        if (tid < s.k) {
-            const uint32_t at = at_place[tid], j = at & 0xffffu;
-            const bool     is = at != 0xffffffffu;
-            const int      beam = is ? (int)(at >> 16) : -1;
-            int            to = tid;
-            if (s.settle) {
-                // rows that something goes on from keep their best; the others take the places that are left, in order
-                Key  seen = 0;
-                int  others = 0;
-                bool first = is;
-                for (int o = 0; o < s.k; ++o) {
-                    const uint32_t u = at_place[o];
-                    const bool     leads = u != 0xffffffffu && !(seen >> (u >> 16) & 1);
-                    if (o < tid) {
-                        others += !leads;
-                        if (u != 0xffffffffu && (int)(u >> 16) == beam) first = false;
-                    }
-                    if (leads) seen |= (Key)1 << (u >> 16);
+    __syncthreads();
+    if (tid < s.k) {
+        const uint32_t at = at_place[tid], j = at & 0xffffu;
+        const bool     is = at != 0xffffffffu;
+        const int      beam = is ? (int)(at >> 16) : -1;
+        int            to = tid;
+        if (s.settle) {
+            // rows that something goes on from keep their best; the others take the places that are left, in order
+            Key  seen = 0;
+            int  others = 0;
+            bool first = is;
+            for (int o = 0; o < s.k; ++o) {
+                const uint32_t u = at_place[o];
+                const bool     leads = u != 0xffffffffu && !(seen >> (u >> 16) & 1);
+                if (o < tid) {
+                    others += !leads;
+                    if (u != 0xffffffffu && (int)(u >> 16) == beam) first = false;
                 }
-                if (first) to = beam;
-                else {
-                    to = 0;
-                    for (int skip = others;; ++to)
-                        if (!(seen >> to & 1) && skip-- == 0) break;
-                }
+                if (leads) seen |= (Key)1 << (u >> 16);
             }
-            const int64_t o = request * s.k + to;
-            s.out_score[o] = is ? found[j].total : -INFINITY;
-            s.out_parent[o] = is ? (int32_t)(first_row + beam) : -1;
-            s.out_token[o] = is ? (int32_t)(found[j].index - (uint32_t)beam * (uint32_t)in.vocab) : -1;
+            if (first) to = beam;
+            else {
+                to = 0;
+                for (int skip = others;; ++to)
+                    if (!(seen >> to & 1) && skip-- == 0) break;
+            }
         }
+        const int64_t o = request * s.k + to;
+        s.out_score[o] = is ? rest[j].total : -INFINITY;
+        s.out_parent[o] = is ? (int32_t)(first_row + beam) : -1;
+        s.out_token[o] = is ? (int32_t)(rest[j].index - (uint32_t)beam * (uint32_t)in.vocab) : -1;
     }
-    cluster_wait();
 }
 
-template <class T> int beam_launch(const nereus_logits_t& in, const nereus_beams_t& how, float* score, int32_t* parent, int32_t* token, cudaStream_t stream) {
-    static std::atomic<bool> opted[kMaxDevices];
-    Device dev;
-    if (int rc = device_of(&dev)) return rc;
-    // as many blocks as leave each four layers of the request at least; the number of requests has no part in it
-    Deal d = spread_of(in, kThreads, 0, 0, INT32_MAX);
-    const int64_t e = 16 / size_of(in.dtype), used = (in.vocab + in.shard_cols - 1) / in.shard_cols;
-    const int64_t main = layers_aligned(held_cols(in, 0), e, kThreads) * used;
-    while (d.log_c < 3 && (main * how.beams) >> (d.log_c + 1) >= 4) ++d.log_c;
-    d.mine = (d.layers + (1 << d.log_c) - 1) >> d.log_c;
-    Select s = {how.beams, how.k, how.settle, 0, 0, how.score, how.ended, how.norm, score, parent, token};
-    s.per_note = (d.mine + kMaxNotes / how.beams - 1) / (kMaxNotes / how.beams);
-    s.notes = (d.mine + s.per_note - 1) / s.per_note;
-    const int64_t smem = kStreamRing * kVecs * 16 + std::min<int64_t>(kMaxItems, (int64_t)how.beams * d.mine) * (int64_t)sizeof(Layer) +
-                         (int64_t)how.beams * s.notes * kThreads * 2;
-    return launch(beam_kernel<T>, opted, kThreads, in.rows / how.beams, d, smem, dev, stream, cut_of(in), d, s, scale_of(1.0));
+// ---- host side -----------------------------------------------------------------------------------------------
+
+int check_beams(const nereus_logits_t* in, const nereus_beams_t* how) {
+    if (int rc = check_view(in)) return rc;
+    if (!how || how->beams < 1 || how->beams > NEREUS_BEAM_MAX || how->k < 1 || how->k > NEREUS_BEAM_MAX_K || how->reserved) return NEREUS_ERR_ARG;
+    if (how->settle < 0 || how->settle > 1 || (how->settle && how->k != how->beams) || in->rows % how->beams) return NEREUS_ERR_ARG;
+    return NEREUS_OK;
+}
+
+// How the rows are cut, and where the workspace's arrays are; returns its size.
+size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, int sms, Deal* deal, Select* s, char* workspace) {
+    *deal = spread_of(in, kTH, 0, 0, INT32_MAX);
+    s->beams = how.beams;
+    s->k = how.k;
+    s->settle = how.settle;
+    s->rows = (int32_t)in.rows;
+    s->score = how.score;
+    s->ended = how.ended;
+    s->norm = how.norm;
+    // A few parts for every block that the GPU holds (4 on an SM), so that they end together; no more of a request than one
+    // block puts together in a microsecond.
+    const int64_t all = in.rows * deal->layers;
+    s->of_part = 1;
+    while ((s->of_part < kPart && all / (2 * s->of_part) >= 16 * sms) || (s->of_part < kItems && (int64_t)((deal->layers + s->of_part - 1) / s->of_part) * how.beams > kParts))
+        s->of_part *= 2;
+    s->parts = (deal->layers + s->of_part - 1) / s->of_part;
+    s->per_shard_1 = 1.f / (float)deal->per_shard;
+    const size_t units = (size_t)in.rows * s->parts, sums = units * kWarps * sizeof(Sum);
+    s->sums = reinterpret_cast<Sum*>(workspace);
+    s->notes = reinterpret_cast<uint16_t*>(workspace + sums);
+    return sums + units * kTH * 2;
+}
+
+template <class T> int beam_launch(const LogitsCut& cut, const Deal& deal, const Select& s, const Device& dev, cudaStream_t stream) {
+    const int64_t units = (int64_t)s.rows * s.parts;
+    // an odd number of blocks: beams that offer nothing (all but a request's first on its first step) come to all of them
+    const int64_t most = 4 * dev.sms - 1;
+    beam_sum_kernel<T><<<(unsigned)std::min<int64_t>(units, most), kTH, 0, stream>>>(cut, deal, s);
+    NEREUS_CUDA(cudaGetLastError());
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(s.rows / s.beams));
+    cfg.blockDim = dim3(kPick);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;          // its blocks come while the last sums are made
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, beam_pick_kernel<T>, cut, deal, s));
+    return NEREUS_OK;
 }
 
 }  // namespace
 }  // namespace nereus
 
-extern "C" int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, float* out_score, int32_t* out_parent, int32_t* out_token,
-                                  void* cuda_stream) {
-    if (int rc = check_view(in)) return rc;
-    if (!how || how->beams < 1 || how->beams > NEREUS_BEAM_MAX || how->k < 1 || how->k > NEREUS_BEAM_MAX_K || how->reserved) return NEREUS_ERR_ARG;
-    if (how->settle < 0 || how->settle > 1 || (how->settle && how->k != how->beams) || in->rows % how->beams) return NEREUS_ERR_ARG;
+extern "C" {
+
+int nereus_beam_workspace(const nereus_logits_t* in, const nereus_beams_t* how, size_t* bytes) {
+    if (int rc = check_beams(in, how)) return rc;
+    if (!bytes) return NEREUS_ERR_ARG;
+    if (in->rows == 0) { *bytes = 0; return NEREUS_OK; }
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    Deal   deal;
+    Select s;
+    *bytes = lay_out(*in, *how, dev.sms, &deal, &s, nullptr);
+    return NEREUS_OK;
+}
+
+int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, void* workspace, size_t workspace_bytes, float* out_score,
+                       int32_t* out_parent, int32_t* out_token, void* cuda_stream) {
+    if (int rc = check_beams(in, how)) return rc;
     if (misaligned(how->score) || misaligned(how->ended) || misaligned(how->norm) || misaligned(out_score) || misaligned(out_parent) || misaligned(out_token))
         return NEREUS_ERR_ALIGN;
+    if ((uintptr_t)workspace & 15) return NEREUS_ERR_ALIGN;
     if (in->rows == 0) return NEREUS_OK;
-    if (!how->score || !out_score || !out_parent || !out_token) return NEREUS_ERR_ARG;
+    if (!how->score || !out_score || !out_parent || !out_token || !workspace) return NEREUS_ERR_ARG;
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
+    Deal   deal;
+    Select s;
+    if (lay_out(*in, *how, dev.sms, &deal, &s, (char*)workspace) > workspace_bytes) return NEREUS_ERR_TOO_SMALL;
+    s.out_score = out_score;
+    s.out_parent = out_parent;
+    s.out_token = out_token;
     auto go = in->dtype == NEREUS_BF16 ? beam_launch<__nv_bfloat16> : beam_launch<float>;
-    return go(*in, *how, out_score, out_parent, out_token, (cudaStream_t)cuda_stream);
+    return go(cut_of(*in), deal, s, dev, (cudaStream_t)cuda_stream);
 }
+
+}  // extern "C"

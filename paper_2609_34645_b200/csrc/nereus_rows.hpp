@@ -73,13 +73,10 @@ __device__ __forceinline__ int width_of(const LogitsCut& c, int s) {
     return left <= 0 ? 0 : left < c.cols ? (int)left : c.cols;
 }
 
-// Block `rank`'s i-th layer of a row; hi = 0 where it has none.
-template <class TI, class TO, int TH = kThreads>
-__device__ __forceinline__ Layer layer_of(const LogitsCut& in, const LogitsCut& out, const Deal& d, int64_t row, int rank, int i) {
+// The layer of shard s that begins at vector position `first`, counted in elements; hi = 0 where the row has none there.
+template <class TI, class TO, int TH>
+__device__ __forceinline__ Layer layer_in(const LogitsCut& in, const LogitsCut& out, int64_t row, int s, int first) {
     Layer r = {nullptr, nullptr, 0, 0, 0, 0};
-    const int l = (i << d.log_c) + rank;
-    if (l >= d.layers) return r;
-    const int s = l / d.per_shard, first = (l - s * d.per_shard) * kPerLayer<TI, TH>;
     const int w = width_of(in, s);
     if (!w) return r;
     const uintptr_t a = (uintptr_t)row_of<TI>(in, s, row);
@@ -93,6 +90,14 @@ __device__ __forceinline__ Layer layer_of(const LogitsCut& in, const LogitsCut& 
         r.vec_out = ((uintptr_t)r.out & 15) == 0;
     }
     return r;
+}
+// Block `rank`'s i-th layer of a row.
+template <class TI, class TO, int TH = kThreads>
+__device__ __forceinline__ Layer layer_of(const LogitsCut& in, const LogitsCut& out, const Deal& d, int64_t row, int rank, int i) {
+    const int l = (i << d.log_c) + rank;
+    if (l >= d.layers) return {nullptr, nullptr, 0, 0, 0, 0};
+    const int s = l / d.per_shard;
+    return layer_in<TI, TO, TH>(in, out, row, s, (l - s * d.per_shard) * kPerLayer<TI, TH>);
 }
 
 // Two fp32 in one 64-bit register: sm_100 has add, mul and fma on pairs, which halves the instructions of the loops.
@@ -496,6 +501,10 @@ __device__ __forceinline__ uint16_t note_of(float x) {
     return (uint16_t)((u >> 16) + ((u & 0xffffu) && !(u >> 31) ? 1u : 0u));       // a negative one is cut towards 0: up
 }
 __device__ __forceinline__ float value_of_note(uint16_t n) { return __uint_as_float((uint32_t)n << 16); }
+// ... and the next below it: not above x.
+__device__ __forceinline__ float note_below(uint16_t n) {
+    return n == 0 || n == 0x8000u ? -__uint_as_float(0x00010000u) : __uint_as_float((uint32_t)(n >> 15 ? n + 1 : n - 1) << 16);
+}
 
 // ---- host side ------------------------------------------------------------------------------------------------
 
@@ -539,18 +548,21 @@ constexpr int kMaxDevices = 64;
 constexpr int kSmemShare  = 73 * 1024;      // shared memory per block for which three blocks fit on an SM
 
 struct Device {
-    int id = 0, smem = 0;      // dynamic shared memory that a block may have
+    int id = 0, smem = 0, sms = 0;      // dynamic shared memory that a block may have
 };
-// The current device; its shared memory is looked up once.
+// The current device; its shared memory and SMs are looked up once.
 inline int device_of(Device* d) {
-    static std::atomic<int> smem[kMaxDevices];
+    static std::atomic<int> smem[kMaxDevices], sms[kMaxDevices];
     NEREUS_CUDA(cudaGetDevice(&d->id));
     if (d->id < 0 || d->id >= kMaxDevices) return NEREUS_ERR_UNSUPPORTED;
+    d->sms = sms[d->id].load();
     d->smem = smem[d->id].load();
-    if (!d->smem) {
+    if (!d->smem || !d->sms) {
         int most = 0;
         NEREUS_CUDA(cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, d->id));
         d->smem = most - 16384;                                   // 16 KiB: the kernels' static part
+        NEREUS_CUDA(cudaDeviceGetAttribute(&d->sms, cudaDevAttrMultiProcessorCount, d->id));
+        sms[d->id].store(d->sms);
         smem[d->id].store(d->smem);
     }
     return NEREUS_OK;

@@ -336,8 +336,11 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     how.norm = (const float*)arg_of(a[6], at::kFloat, rows, -1, x, "norm");
     const int64_t requests = how.beams ? rows / how.beams : 0, room = std::max<int64_t>(how.k, 1);
     at::Tensor score = empty({requests, room}, at::kFloat, x), parent = empty({requests, room}, at::kInt, x), token = empty({requests, room}, at::kInt, x);
-    if (failed(nereus_beam_select(&x.v, &how, (float*)score.data_ptr(), (int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(), stream_of(x)),
-               "nereus_beam_select"))
+    size_t bytes = 0;
+    if (failed(nereus_beam_workspace(&x.v, &how, &bytes), "nereus_beam_select")) return nullptr;
+    const at::Tensor workspace = empty({(int64_t)bytes}, at::kByte, x);
+    if (failed(nereus_beam_select(&x.v, &how, workspace.data_ptr(), bytes, (float*)score.data_ptr(), (int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(),
+                                  stream_of(x)), "nereus_beam_select"))
         return nullptr;
     THPObjectPtr s(THPVariable_Wrap(std::move(score))), p(THPVariable_Wrap(std::move(parent))), t(THPVariable_Wrap(std::move(token)));
     return PyTuple_Pack(3, s.get(), p.get(), t.get());

@@ -33,18 +33,20 @@ def beams(beams=2, k=4, settle=0, score=A, ended=None, norm=None, reserved=0):
 
 
 def test_beam_select_refuses():
-    def select(view=None, how=None, out=(A, A, A)):
-        return code(B.beam_select, view or logits(), how or beams(), *out)
-    for how in (beams(beams=0), beams(beams=65), beams(k=0), beams(k=129), beams(settle=2), beams(settle=1, k=4), beams(beams=4), beams(reserved=1),
-                beams(score=None)):
-        assert select(how=how) == B.ERR_ARG
+    def select(view=None, how=None, out=(A, A, A), work=A):
+        return code(B.beam_select, view or logits(), how or beams(), work, 1 << 30, *out)
+    wrong = (beams(beams=0), beams(beams=65), beams(k=0), beams(k=129), beams(settle=2), beams(settle=1, k=4), beams(beams=4), beams(reserved=1))
+    for how in wrong:
+        assert select(how=how) == code(B.beam_workspace, logits(), how) == B.ERR_ARG
+    assert select(how=beams(score=None)) == select(work=None) == B.ERR_ARG and select(work=A + 8) == B.ERR_ALIGN
     assert select(logits(dtype=7)) == B.ERR_UNSUPPORTED
     assert select(logits(vocab=1 << 25)) == B.ERR_TOO_LARGE
     assert select(logits(base=A + 1)) == select(how=beams(score=A + 2)) == select(how=beams(ended=A + 1)) == select(how=beams(norm=A + 3)) == B.ERR_ALIGN
     assert select(out=(A + 1, A, A)) == select(out=(A, A + 2, A)) == select(out=(A, A, A + 3)) == B.ERR_ALIGN
     assert select(out=(None, A, A)) == select(out=(A, None, A)) == select(out=(A, A, None)) == B.ERR_ARG
-    assert B._lib.nereus_beam_select(None, beams(), A, A, A, None) == B._lib.nereus_beam_select(logits(), None, A, A, A, None) == B.ERR_ARG
-    assert select(logits(rows=0)) == B.OK
+    assert B._lib.nereus_beam_select(None, beams(), A, 0, A, A, A, None) == B._lib.nereus_beam_select(logits(), None, A, 0, A, A, A, None) == B.ERR_ARG
+    assert B._lib.nereus_beam_workspace(logits(), beams(), None) == B.ERR_ARG
+    assert select(logits(rows=0)) == B.OK and B.beam_workspace(logits(rows=0), beams()) == 0
 
 
 def states(rows=6, buffers=2, outer=1, tokens=10, token_bytes=8, row=None, step=0, base=A):
