@@ -21,18 +21,21 @@ namespace nereus {
 namespace {
 
 constexpr int kTH       = kThreads;               // of a summing block
-constexpr int kItems    = 256;                    // layers in its table at a time
-constexpr int kPart     = 16;                     // layers of a part, as a rule at most
-constexpr int kParts    = 256;                    // parts of a request's rows, as far as a part's layers fit the table
-constexpr int kPick     = 512;                    // threads of a picking block
+constexpr int kRoom     = 4 * kTH;                // vectors of a layer here: four a thread, for one pass of the loop's overhead
+constexpr int kStages   = 2;                      // layers on their way to a block, 16 KiB each
+constexpr int kItems    = 128;                    // layers in its table at a time
+constexpr int kListed   = 4096;                   // rows that it lists
+constexpr int kPart     = 16;                     // layers of a part, where that leaves no more parts than
+constexpr int kParts    = 256;                    // parts of a request's rows, at most
+constexpr int kPick     = 1024;                   // threads of a picking block
 constexpr int kPickWarps = kPick / 32;
 constexpr int kSets     = 8;
 constexpr int kFound    = 1024;                   // hypotheses that its list holds
-constexpr int kNoted    = 2048;
+constexpr int kNoted    = 1024;                   // notes, or groups of 8, that reach the bound
 typedef unsigned long long Key;
 
 // Sums of exponentials are kept as (K, sum of 2^(x c - K)) with a whole number K near the largest x c, so that sums of different
-// threads go together without another rounding; a thread adds up 2 vectors in 32 bits and these in 64.  c = log2(e) has 24
+// threads go together without another rounding; a thread adds up 4 vectors in 32 bits and these in 64.  c = log2(e) has 24
 // bits, kLog2eLow is the rest: it is put right for the largest element of a row at the end, and an element at a distance of d
 // from that is off by 2e-8 d of itself.  K stays within +-2^22: a row whose largest element lies beyond (a mask's lowest value
 // in all of it, say) is summed again, by differences from it.
@@ -42,8 +45,18 @@ struct Sum {
     double sum;
     float  k, top;                                // and the largest element
 };
+// What a block leaves of a part.
+struct Record {
+    Sum      sum;
+    uint16_t notes[kTH];
+};
 __device__ __forceinline__ double power_of_two(float k) {        // k whole and not above 0
     return !(k >= -1000.f) ? 0.0 : __longlong_as_double((long long)(1023 + (int)k) << 52);
+}
+template <int kLanes> __device__ __forceinline__ double sum_of_lanes(double x) {
+#pragma unroll
+    for (int o = kLanes / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
 }
 // log2 of a positive normal number, 1e-7 off
 __device__ __forceinline__ double log2_of(double x) {
@@ -58,8 +71,7 @@ struct Select {
     const float*   score;
     const int32_t* ended;
     const float*   norm;
-    Sum*      sums;                               // [rows, parts, kWarps]
-    uint16_t* notes;                              // [rows, parts, kTH]
+    Record*  records;                             // [rows, parts]
     float*   out_score;
     int32_t *out_parent, *out_token;
 };
@@ -78,66 +90,109 @@ __device__ __forceinline__ bool offers(const Select& s, int64_t row, int vocab, 
 template <class T> __device__ __forceinline__ Layer layer_at(const LogitsCut& in, const Deal& deal, const Select& s, int64_t row, int l) {
     if (l >= deal.layers) return {nullptr, nullptr, 0, 0, 0, 0};
     const int shard = quotient(l, deal.per_shard, s.per_shard_1);
-    return layer_in<T, T, kTH>(in, LogitsCut(), row, shard, (l - shard * deal.per_shard) * kPerLayer<T, kTH>);
+    return layer_in<T, T, 2 * kTH>(in, LogitsCut(), row, shard, (l - shard * deal.per_shard) * kPerLayer<T, 2 * kTH>);
 }
 
 // ---- sums ----------------------------------------------------------------------------------------------------
 
+// Starts the copies of this thread's vectors of layer l, one commit group; nothing but the group past the last layer.
+template <class T> __device__ __forceinline__ void load_four(const Layer* table, uint4* to, int l, int n) {
+    if (l < n) {
+        const Layer& L = table[l];
+        const char*  from = L.in + threadIdx.x * 16;
+        if (L.hi - L.lo == kPerLayer<T, 2 * kTH>) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
+        } else {
+#pragma unroll 1
+            for (int v = 0; v < 4; ++v) {
+                const int at = ((int)threadIdx.x + v * kTH) * kPerVec<T>;
+                if (at >= L.lo && at + kPerVec<T> <= L.hi) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
+                else to[v * kTH] = edge_vector<T>(L, threadIdx.x + v * kTH);
+            }
+        }
+    }
+    copy_commit();
+}
+
 template <class T>
 __global__ void __launch_bounds__(kTH, 4) beam_sum_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
-    __shared__ __align__(16) uint4 ring[kStreamRing * kVecs];
+    __shared__ __align__(16) uint4 ring[kStages * kRoom];
     __shared__ Layer    table[kItems];
-    __shared__ uint32_t unit_of[kItems];
-    __shared__ int      of_warp[kWarps + 1];
+    __shared__ uint16_t listed[kListed];
+    __shared__ Sum      of_warps[2][kWarps];
+    __shared__ int      of_warp[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // The rows that are read.  They are listed, so that their parts come to all blocks alike; where there are many their
+    // number evens out what each block gets, and rows that are not read are passed over.
+    int  n = s.rows;
+    bool list = s.rows <= kListed;
+    auto read = [&](int row) {
+        float score, norm;
+        int   ended;
+        return offers(s, row, in.vocab, &score, &norm, &ended) && (uint32_t)ended >= (uint32_t)in.vocab;
+    };
+    if (list) {
+        n = 0;
+        uint32_t flags = 0;                                // of rows tid, tid + kTH, ...
+#pragma unroll
+        for (int j = 0; j < kListed / kTH; ++j)
+            if (j * kTH < s.rows) flags |= (j * kTH + tid < s.rows && read(j * kTH + tid) ? 1u : 0u) << j;
+#pragma unroll 1
+        for (int j = 0; j * kTH < s.rows; ++j) {
+            const uint32_t who = __ballot_sync(0xffffffffu, flags >> j & 1u);
+            __syncthreads();
+            if (lane == 0) of_warp[warp] = __popc(who);
+            __syncthreads();
+            int before = n;
+            for (int w = 0; w < kWarps; ++w) {
+                if (w < warp) before += of_warp[w];
+                n += of_warp[w];
+            }
+            if (flags >> j & 1u) listed[before + __popc(who & ((1u << lane) - 1))] = (uint16_t)(j * kTH + tid);
+        }
+        __syncthreads();
+    }
 
     typename Vec<T>::Max top = Vec<T>::lowest();
     float  k = -kLargestK;
     double sum = 0.0;
-    int    i = 0;
-    const uint4* from = ring + tid;
-    const Pair   c = pair(kLog2e, kLog2e);
-    const int64_t units = (int64_t)s.rows * s.parts;
-    const int     log_part = __ffs(s.of_part) - 1, slots = kItems >> log_part;
-    for (int64_t first = blockIdx.x; first < units; first += (int64_t)slots * gridDim.x) {
-        // of the next units those whose rows are read, in order
-        const int64_t unit = first + (int64_t)tid * gridDim.x;
-        bool is = tid < slots && unit < units;
-        if (is) {
-            float score, norm;
-            int   ended;
-            is = offers(s, (uint32_t)unit % (uint32_t)s.rows, in.vocab, &score, &norm, &ended) && (uint32_t)ended >= (uint32_t)in.vocab;
-        }
-        const uint32_t who = __ballot_sync(0xffffffffu, is);
+    int    i = 0, odd = 0;
+    uint4* const  mine = ring + tid;
+    const Pair    c = pair(kLog2e, kLog2e);
+    const int     log_part = __ffs(s.of_part) - 1;
+    const int64_t units = (int64_t)n * s.parts;
+    // the block's x-th unit: a row, and a part of it
+    auto unit_of = [&](int64_t x, int* part) {
+        const uint32_t u = (uint32_t)(blockIdx.x + x * gridDim.x);
+        *part = (int)(u / (uint32_t)n);
+        const int r = (int)(u - (uint32_t)*part * (uint32_t)n);
+        return list ? (int)listed[r] : r;
+    };
+    const int64_t layers = blockIdx.x < units ? ((units - blockIdx.x + gridDim.x - 1) / gridDim.x) << log_part : 0;
+    for (int64_t first = 0; first < layers; first += kItems) {
+        const int items = (int)min((int64_t)kItems, layers - first);
         __syncthreads();
-        if (lane == 0) of_warp[warp] = __popc(who);
-        __syncthreads();
-        int before = 0, n = 0;
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += of_warp[w];
-            n += of_warp[w];
-        }
-        if (is) unit_of[before + __popc(who & ((1u << lane) - 1))] = (uint32_t)unit;
-        __syncthreads();
-        const int items = n << log_part;
         if (tid < items) {
-            const uint32_t u = unit_of[tid >> log_part];
-            const int      part = (int)(u / (uint32_t)s.rows);
-            table[tid] = layer_at<T>(in, deal, s, u - (uint32_t)part * (uint32_t)s.rows, (part << log_part) + (tid & (s.of_part - 1)));
+            int       part;
+            const int row = unit_of((first + tid) >> log_part, &part);
+            table[tid] = list || read(row) ? layer_at<T>(in, deal, s, row, (part << log_part) + ((int)(first + tid) & (s.of_part - 1)))
+                                           : Layer{nullptr, nullptr, 0, 0, 0, 0};
         }
         __syncthreads();
 #pragma unroll 1
-        for (int l = 0; l < kStreamRing; ++l) load_layer<T, kTH>(table, ring, l, l, items);
+        for (int l = 0; l < kStages; ++l) load_four<T>(table, mine + l * kRoom, l, items);
         int slot = 0;
 #pragma unroll 1
         for (int item = 0; item < items; ++item) {
-            copy_wait<kStreamRing - 1>();
-            const uint4 a = from[slot * kVecs], b = from[slot * kVecs + kTH];
-            if (item + kStreamRing < items) load_layer<T, kTH>(table, ring, slot, item + kStreamRing, items);
-            else copy_commit();
-            slot = slot + 1 == kStreamRing ? 0 : slot + 1;
-            top = Vec<T>::join(top, Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b)));
+            copy_wait<kStages - 1>();
+            uint4* const here = mine + slot * kRoom;
+            const uint4 a = here[0], b = here[kTH], d = here[2 * kTH], e = here[3 * kTH];
+            load_four<T>(table, here, item + kStages, items);
+            slot = slot + 1 == kStages ? 0 : slot + 1;
+            top = Vec<T>::join(top, Vec<T>::join(Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b)), Vec<T>::join(Vec<T>::max(d), Vec<T>::max(e))));
             const float v = Vec<T>::value(top);
             // an element ahead of K carries the roundings of the distance: 2^4 at most
             if (v * kLog2e > k + 4.f) {
@@ -146,18 +201,25 @@ __global__ void __launch_bounds__(kTH, 4) beam_sum_kernel(const __grid_constant_
                 k = to;
             }
             const Pair   minus = pair(-k, -k);
-            const float2 h = halves(add2(exp_sum<T, false>(a, c, c, minus), exp_sum<T, false>(b, c, c, minus)));
+            const float2 h = halves(add2(add2(exp_sum<T, false>(a, c, c, minus), exp_sum<T, false>(b, c, c, minus)),
+                                         add2(exp_sum<T, false>(d, c, c, minus), exp_sum<T, false>(e, c, c, minus))));
             sum += (double)(h.x + h.y);
             if (++i == s.of_part) {
-                const uint32_t u = unit_of[item >> log_part];
-                const int      part = (int)(u / (uint32_t)s.rows);
-                const int64_t  at = (int64_t)(u - (uint32_t)part * (uint32_t)s.rows) * s.parts + part;
-                s.notes[at * kTH + tid] = note_of(v);
+                int           part;
+                const int     row = unit_of((first + item) >> log_part, &part);
+                Record* const to = s.records + (int64_t)row * s.parts + part;
+                to->notes[tid] = note_of(v);
                 const float all = warp_max(k), most = warp_max(v);
-                double      of_lanes = sum * power_of_two(k - all);
-#pragma unroll
-                for (int o = 16; o; o >>= 1) of_lanes += __shfl_xor_sync(0xffffffffu, of_lanes, o);
-                if (lane == 0) s.sums[at * kWarps + warp] = {of_lanes, all, most};
+                const Sum   mine = {sum_of_lanes<32>(sum * power_of_two(k - all)), all, most};
+                if (lane == 0) of_warps[odd][warp] = mine;
+                __syncthreads();
+                if (warp == 0) {                           // two sets of sums: the others are at the next part's meanwhile
+                    Sum u = lane < kWarps ? of_warps[odd][lane] : Sum{0.0, -kLargestK, -INFINITY};
+                    const float of_all = warp_max(u.k);
+                    u = {sum_of_lanes<kWarps>(u.sum * power_of_two(u.k - of_all)), of_all, warp_max(u.top)};
+                    if (lane == 0) to->sum = u;
+                }
+                odd ^= 1;
                 top = Vec<T>::lowest();
                 k = -kLargestK;
                 sum = 0.0;
@@ -186,15 +248,39 @@ struct Beam {
     int32_t  pad;
 };
 
+// A hypothesis: the element, later the total, of a token of a beam.
+struct Hit {
+    float   x;
+    int32_t beam, token;
+};
+__device__ __forceinline__ float largest_note(const Record* records, int g) {
+    const uint4 v = reinterpret_cast<const uint4*>(records[g / 32].notes)[g % 32];
+    return Vec<__nv_bfloat16>::value(Vec<__nv_bfloat16>::max(v));
+}
+// The log-sum-exp of a row whose largest element lies far from 0, by a warp.
+template <class T> __device__ __noinline__ double far_row(const LogitsCut& in, const Deal& deal, const Select& s, int64_t row, float top, double* sum) {
+    double all = 0.0;
+    for (int l = 0; l < deal.layers; ++l) {
+        const Layer L = layer_at<T>(in, deal, s, row, l);
+        for (int vec = threadIdx.x & 31; vec < kRoom; vec += 64)
+            all += (double)exp_sum_far<T>(edge_vector<T>(L, vec), edge_vector<T>(L, vec + 32), top, pair(kLog2e, kLog2e));
+    }
+    all = sum_of_lanes<32>(all);
+    *sum = all;
+    return (double)top + kLn2 * log2_of(all);
+}
+
 template <class T>
 __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
     constexpr int E = kPerVec<T>;
+    extern __shared__ __align__(16) unsigned char dynamic[];
+    Record* const records = reinterpret_cast<Record*>(dynamic);
     __shared__ Beam     beams[NEREUS_BEAM_MAX];
     __shared__ __align__(16) Key found[kFound];
-    __shared__ struct { uint32_t index; float total; } rest[kFound];       // index: beam * vocab + token
-    __shared__ uint32_t noted[kNoted];
+    __shared__ Hit      rest[kFound];
+    __shared__ uint32_t noted[kNoted], grouped[kNoted];
     __shared__ uint32_t peak[kPick], histogram[256], at_place[NEREUS_BEAM_MAX_K], choice[4], of_warp[kPickWarps];
-    __shared__ int      n_found, n_noted;
+    __shared__ int      n_found, n_noted, n_grouped;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t request = blockIdx.x, first_row = request * s.beams;
 
@@ -209,43 +295,46 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         r.least = NAN;
         beams[b] = r;
     }
-    if (tid == 0) n_found = n_noted = 0;
+    if (tid == 0) n_found = n_noted = n_grouped = 0;
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");                      // the sums and notes are there
 
+    // what the sums' blocks have left of the request
+    const int   row_parts = s.beams * s.parts, groups = row_parts * (kTH / 8);
+    const float parts_1 = 1.f / (float)s.parts;
+    {
+        const uint4* const from = reinterpret_cast<const uint4*>(s.records + first_row * s.parts);
+#pragma unroll 1
+        for (int x = tid; x < row_parts * (int)(sizeof(Record) / 16); x += kPick)
+            copy_async(smem_address(reinterpret_cast<uint4*>(records) + x), from + x);
+        copy_commit();
+        copy_wait<0>();
+    }
+    __syncthreads();
+
     // every row's log-sum-exp, a warp for each
-    const int entries = s.parts * kWarps;
+#pragma unroll 1
     for (int b = warp; b < s.beams; b += kPickWarps) {
         Beam& r = beams[b];
         if (r.off != r.off || r.ended >= 0) {
             if (lane == 0) r.off_1 = NAN;
             continue;
         }
-        const Sum* sums = s.sums + (first_row + b) * entries;
         float  k = -INFINITY, top = -INFINITY;
         double sum = 0.0;
-        for (int e = lane; e < entries; e += 32) {
-            const uint4 u = __ldcg(reinterpret_cast<const uint4*>(sums + e));
-            const float of_k = __uint_as_float(u.z), to = fmaxf(k, of_k);
-            sum = fma(__longlong_as_double((long long)((Key)u.y << 32 | u.x)), power_of_two(of_k - to), sum * power_of_two(k - to));
+#pragma unroll 1
+        for (int e = lane; e < s.parts; e += 32) {
+            const Sum   u = records[b * s.parts + e].sum;
+            const float to = fmaxf(k, u.k);
+            sum = fma(u.sum, power_of_two(u.k - to), sum * power_of_two(k - to));
             k = to;
-            top = fmaxf(top, __uint_as_float(u.w));
+            top = fmaxf(top, u.top);
         }
         const float all = warp_max(k);
         top = warp_max(top);
-        sum *= power_of_two(k - all);
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        sum = sum_of_lanes<32>(sum * power_of_two(k - all));
         double lse = kLn2 * ((double)all + log2_of(sum) + (double)top * kLog2eLow);
-        if (fabsf(top * kLog2e) >= kLargestK && fabsf(top) < INFINITY) {
-            sum = 0.0;
-            for (int l = 0; l < deal.layers; ++l) {
-                const Layer L = layer_at<T>(in, deal, s, first_row + b, l);
-                for (int vec = lane; vec < kVecs; vec += 64)
-                    sum += (double)exp_sum_far<T>(edge_vector<T>(L, vec), edge_vector<T>(L, vec + 32), top, pair(kLog2e, kLog2e));
-            }
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            lse = (double)top + kLn2 * log2_of(sum);
-        }
+        if (fabsf(top * kLog2e) >= kLargestK && fabsf(top) < INFINITY) lse = far_row<T>(in, deal, s, first_row + b, top, &sum);
         if (lane == 0) {
             r.off = fabsf(top) < INFINITY && sum == sum ? r.off - lse : (double)NAN;
             r.off_1 = (float)r.off;
@@ -253,88 +342,75 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     }
     __syncthreads();
 
-    // What an element is worth: off + x, by the norm; in 64 bits, and in 32 and a little less for the roundings.
-    auto worth = [&](const Beam& r, float x, double* total) {
-        *total = r.off + (double)x;
-        return s.norm ? *total / r.norm : *total;
-    };
-    auto worth_below = [](const Beam& r, float x) {
+    // The notes, 8 at a time; a warp's are of one row and part.  Of each set of threads the j-th largest of what their notes
+    // are worth, off + x, by the norm, in 32 bits and a little less for the roundings: the least of these bounds the k-th
+    // best from below.
+    float most = -INFINITY;
+#pragma unroll 1
+    for (int g = tid; g < groups; g += kPick) {
+        const Beam& r = beams[quotient(g / 32, s.parts, parts_1)];
+        if (r.off_1 != r.off_1) continue;
+        const float up = largest_note(records, g);
+        // a note of a fp32 was rounded up: the next below it is not above the element
+        const float x = sizeof(T) == 2 ? up : note_below((uint16_t)(__float_as_uint(up) >> 16));
         const float w = fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse;
-        return fmaf(-1e-6f, fabsf(w), w);
-    };
-    // Notes, 8 at a time: those of one row and part.
-    const uint4* const all_notes = reinterpret_cast<const uint4*>(s.notes + first_row * s.parts * kTH);
-    constexpr int kEach = kTH / 8;
-    const int     groups = s.beams * s.parts * kEach;
-    const float   parts_1 = 1.f / (float)(s.parts * kEach);
-    {
-        float most = -INFINITY;
-#pragma unroll 4
-        for (int g = tid; g < groups; g += kPick) {
-            const Beam& r = beams[quotient(g, s.parts * kEach, parts_1)];
-            const uint4 v = __ldcg(all_notes + g);
-            // the largest of 8 notes is the largest as bf16; that of a fp32 was rounded up: the next below is not above it
-            const float up = Vec<__nv_bfloat16>::value(Vec<__nv_bfloat16>::max(v));
-            const float x = sizeof(T) == 2 ? up : note_below((uint16_t)(__float_as_uint(up) >> 16));
-            if (up > -INFINITY && r.off_1 == r.off_1) most = fmaxf(most, worth_below(r, x));
+        if (up > -INFINITY) most = fmaxf(most, fmaf(-1e-6f, fabsf(w), w));
+    }
+    peak[tid] = key_of(most);
+    __syncthreads();
+    if (warp < kSets) {
+        uint32_t key = 0, t = 0;
+        // a row's notes are on neighbouring threads: every set has its share of every row's
+#pragma unroll
+        for (int x = 0; x < kPick; x += kSets * 32) key = max(key, peak[x + lane * kSets + warp]);
+#pragma unroll 1
+        for (int i = 0; i < s.k; i += kSets) {
+            t = __reduce_max_sync(0xffffffffu, key);
+            if (lane == __ffs(__ballot_sync(0xffffffffu, key == t)) - 1) key = 0;
         }
-        peak[tid] = key_of(most);
+        if (lane == 0) of_warp[warp] = t;
     }
     __syncthreads();
-    // of each set the j-th largest; the least of these bounds the k-th best from below
-    {
-        const int j = (s.k + kSets - 1) / kSets;
-        uint32_t  t = 0xffffffffu;
-        if (warp < kSets) {
-            uint32_t key = 0;
-            // a row's notes are on neighbouring threads: every set has its share of every row's
-            for (int x = lane * kSets + warp; x < kPick; x += kSets * 32) key = max(key, peak[x]);
-#pragma unroll 1
-            for (int i = 0; i < j; ++i) {
-                t = __reduce_max_sync(0xffffffffu, key);
-                if (lane == __ffs(__ballot_sync(0xffffffffu, key == t)) - 1) key = 0;
-            }
-            if (lane == 0) of_warp[warp] = t;
-        }
-        __syncthreads();
-        t = __reduce_min_sync(0xffffffffu, lane < kSets ? of_warp[lane] : 0xffffffffu);
-        const float bound = t > kKeyMinusInf ? value_of(t) : -INFINITY;
-        for (int b = tid; b < s.beams; b += kPick) {
-            Beam& r = beams[b];
-            // the least x whose worth reaches the bound, or a little less
-            const float norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
-            r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
-        }
-        __syncthreads();
-        // the notes that reach it
-#pragma unroll 4
-        for (int g = tid; g < groups; g += kPick) {
-            const float least = beams[quotient(g, s.parts * kEach, parts_1)].least;
-            const uint4 v = __ldcg(all_notes + g);
-            const float up = Vec<__nv_bfloat16>::value(Vec<__nv_bfloat16>::max(v));
-            if (!(up >= least && up > -INFINITY)) continue;
-            float x[8];
-            unpack<__nv_bfloat16>(v, x);
+    if (tid < s.beams) {
+        Beam&    r = beams[tid];
+        uint32_t t = 0xffffffffu;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (x[e] >= least && x[e] > -INFINITY) {
-                    const int at = atomicAdd(&n_noted, 1);
-                    if (at < kNoted) noted[at] = (uint32_t)(g * 8 + e);
-                }
+        for (int i = 0; i < kSets; ++i) t = min(t, of_warp[i]);
+        const float bound = t > kKeyMinusInf ? value_of(t) : -INFINITY;
+        // the least x whose worth reaches the bound, or a little less
+        const float norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
+        r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
+    }
+    __syncthreads();
+    // the groups of notes that reach it, then the notes
+#pragma unroll 1
+    for (int g = tid; g < groups; g += kPick)
+        if (const float up = largest_note(records, g); up >= beams[quotient(g / 32, s.parts, parts_1)].least && up > -INFINITY) {
+            const int at = atomicAdd(&n_grouped, 1);
+            if (at < kNoted) grouped[at] = (uint32_t)g;
+        }
+    __syncthreads();
+    const int n_groups = n_grouped;
+#pragma unroll 1
+    for (int j = tid; j < min(n_groups, kNoted) * 8; j += kPick) {
+        const int g = (int)grouped[j / 8], row_part = g / 32, thread = g % 32 * 8 + (j & 7);
+        if (value_of_note(records[row_part].notes[thread]) >= beams[quotient(row_part, s.parts, parts_1)].least) {
+            const int at = atomicAdd(&n_noted, 1);
+            if (at < kNoted) noted[at] = (uint32_t)(row_part * kTH + thread);
         }
     }
     __syncthreads();
 
-    // f(key, total, index) for every element of vector `vec` of a layer that may be among the best
+    // f(beam, x, token) for every element of vector `vec` of a layer that may be among the best
     auto look = [&](int b, const Layer& L, int vec, auto f) {
-        const Beam& r = beams[b];
-        const int   lo = L.lo - vec * E, hi = L.hi - vec * E;
+        const int lo = L.lo - vec * E, hi = L.hi - vec * E;
         if (hi <= 0 || lo >= E) return;
+        const float least = beams[b].least;
         float x[E];
         unpack<T>(edge_vector<T>(L, vec), x);
         uint32_t hits = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) hits |= (x[e] >= r.least && x[e] > -INFINITY ? 1u : 0u) << e;
+        for (int e = 0; e < E; ++e) hits |= (x[e] >= least && x[e] > -INFINITY ? 1u : 0u) << e;
         hits &= bits_between(lo, hi, E);
 #pragma unroll 1
         for (; hits; hits &= hits - 1) {
@@ -342,33 +418,35 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             float y = x[0];
 #pragma unroll
             for (int o = 1; o < E; ++o) y = o == e ? x[o] : y;
-            double    total;
-            const Key key = key_of_double(worth(r, y, &total));
-            if (key > kKeyNone) f(key, (float)total, (uint32_t)(b * in.vocab + L.token + vec * E + e));
-        }
-    };
-    auto push = [&](Key key, float total, uint32_t index) {
-        const int at = atomicAdd(&n_found, 1);
-        if (at < kFound) {
-            found[at] = key;
-            rest[at] = {index, total};
+            f(b, y, L.token + vec * E + e);
         }
     };
     // the beams that have ended offer themselves
     auto each_ended = [&](auto f) {
-        if (tid >= s.beams) return;
-        const Beam& r = beams[tid];
-        if (r.ended >= 0 && r.off == r.off) f(key_of_double(s.norm ? r.off / r.norm : r.off), r.score, (uint32_t)(tid * in.vocab + r.ended));
+        if (tid < s.beams && beams[tid].ended >= 0 && beams[tid].off == beams[tid].off) f(tid, 0.f, beams[tid].ended);
     };
-    const int log_part = __ffs(s.of_part) - 1, noted_all = n_noted;
+    auto push = [&](int b, float x, int token) {
+        const int at = atomicAdd(&n_found, 1);
+        if (at < kFound) rest[at] = {x, b, token};
+    };
+    // what a hypothesis is worth, in 64 bits; 0: it is not offered
+    auto key_of_hit = [&](int b, float x, float* total) {
+        const Beam&  r = beams[b];
+        const double sum = r.ended >= 0 ? r.off : r.off + (double)x;
+        const Key    key = key_of_double(s.norm ? sum / r.norm : sum);
+        *total = r.ended >= 0 ? r.score : (float)sum;
+        return key > kKeyNone ? key : 0;
+    };
+    const int log_part = __ffs(s.of_part) - 1, noted_all = max(n_noted, n_groups);
     if (noted_all <= kNoted) {
         // every vector of a note on a thread of its own
-        const int log_vecs = log_part + 1, vecs = noted_all << log_vecs;
+        const int log_vecs = log_part + 2, vecs = n_noted << log_vecs;
+#pragma unroll 1
         for (int j = tid; j < vecs; j += kPick) {
             const uint32_t which = noted[j >> log_vecs];
-            const int      row_part = which / kTH, b = quotient(row_part, s.parts, parts_1 * kEach), part = row_part - b * s.parts;
-            const int      l = (part << log_part) + (j >> 1 & (s.of_part - 1));
-            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + (j & 1) * kTH, push);
+            const int      row_part = which / kTH, b = quotient(row_part, s.parts, parts_1);
+            const int      l = ((row_part - b * s.parts) << log_part) + (j >> 2 & (s.of_part - 1));
+            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + (j & 3) * kTH, push);
         }
     }
     each_ended(push);
@@ -385,7 +463,7 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
                 if (beams[b].least != beams[b].least) continue;
                 for (int l = 0; l < deal.layers; ++l) {
                     const Layer L = layer_at<T>(in, deal, s, first_row + b, l);
-                    for (int vec = tid; vec < kVecs; vec += kPick) look(b, L, vec, f);
+                    for (int vec = tid; vec < kRoom; vec += kPick) look(b, L, vec, f);
                 }
             }
             each_ended(f);
@@ -397,8 +475,11 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             __syncthreads();
             int      bin = 0;
             uint32_t run = 0;                              // elements of one bin come one after the other
-            each([&](Key key, float, uint32_t index) {
-                if (((key ^ key_is) & key_mask) || ((~index ^ index_is) & index_mask)) return;
+            each([&](int beam, float x, int token) {
+                float          unused;
+                const Key      key = key_of_hit(beam, x, &unused);
+                const uint32_t index = (uint32_t)(beam * in.vocab + token);
+                if (!key || ((key ^ key_is) & key_mask) || ((~index ^ index_is) & index_mask)) return;
                 const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : ~index >> (88 - 8 * byte)) & 255;
                 if (b != bin) {
                     if (run) atomicAdd(&histogram[bin], run);
@@ -438,9 +519,10 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         if (tid == 0) n_found = 0;
         __syncthreads();
         // everything from the bytes found on
-        each([&](Key key, float total, uint32_t index) {
-            const Key top = key & key_mask;
-            if (top > key_is || (top == key_is && (~index & index_mask) >= index_is)) push(key, total, index);
+        each([&](int beam, float x, int token) {
+            float     unused;
+            const Key key = key_of_hit(beam, x, &unused), top = key & key_mask;
+            if (key && (top > key_is || (top == key_is && (~(uint32_t)(beam * in.vocab + token) & index_mask) >= index_is))) push(beam, x, token);
         });
         __syncthreads();
     }
@@ -448,28 +530,35 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     // which hypothesis is the j-th, and its beam in the upper half
     const int total = n_found, quads = (total + 3) / 4;    // keys are read four at a time
     if (tid < s.k) at_place[tid] = 0xffffffffu;
-    if (tid < 4 * quads - total) found[total + tid] = 0;
+#pragma unroll 1
+    for (int j = tid; j < 4 * quads; j += kPick) {
+        if (j < total) found[j] = key_of_hit(rest[j].beam, rest[j].x, &rest[j].x);       // its total takes the element's place
+        else found[j] = 0;
+    }
     __syncthreads();
     // a key on `team` neighbouring threads that share the comparing
     const int team = total <= 32 ? 16 : total <= 64 ? 8 : total <= 128 ? 4 : total <= 256 ? 2 : 1, sub = tid & (team - 1);
+#pragma unroll 1
     for (int j = tid / team; j < (total + 31) / 32 * 32; j += kPick / team) {
         const Key me = j < total ? found[j] : 0;
         int place = 0, equal = 0;
-#pragma unroll 2
+#pragma unroll 1
         for (int o = sub; o < quads; o += team) {
             const ulonglong2 a = reinterpret_cast<const ulonglong2*>(found)[2 * o], b = reinterpret_cast<const ulonglong2*>(found)[2 * o + 1];
             place += (a.x > me) + (a.y > me) + (b.x > me) + (b.y > me);
             equal += (a.x == me) + (a.y == me) + (b.x == me) + (b.y == me);
         }
-        for (int o = 1; o < team; o *= 2) {
-            place += __shfl_xor_sync(0xffffffffu, place, o);
-            equal += __shfl_xor_sync(0xffffffffu, equal, o);
-        }
+        int both = place << 16 | equal;                    // of at most 1024 keys
+#pragma unroll 1
+        for (int o = 1; o < team; o *= 2) both += __shfl_xor_sync(0xffffffffu, both, o);
+        place = both >> 16;
         if (!me || sub || place >= s.k) continue;
-        const uint32_t index = rest[j].index;
-        if (equal > 1)
-            for (int o = 0; o < total; ++o) place += found[o] == me && rest[o].index < index;
-        if (place < s.k) at_place[place] = (uint32_t)j | index / (uint32_t)in.vocab << 16;
+        if ((both & 0xffff) > 1) {
+            const Hit mine = rest[j];
+            for (int o = 0; o < total; ++o)
+                place += found[o] == me && (rest[o].beam < mine.beam || (rest[o].beam == mine.beam && rest[o].token < mine.token));
+        }
+        if (place < s.k) at_place[place] = (uint32_t)(j | rest[j].beam << 16);
     }
     __syncthreads();
     if (tid < s.k) {
@@ -499,9 +588,9 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             }
         }
         const int64_t o = request * s.k + to;
-        s.out_score[o] = is ? rest[j].total : -INFINITY;
+        s.out_score[o] = is ? rest[j].x : -INFINITY;
         s.out_parent[o] = is ? (int32_t)(first_row + beam) : -1;
-        s.out_token[o] = is ? (int32_t)(rest[j].index - (uint32_t)beam * (uint32_t)in.vocab) : -1;
+        s.out_token[o] = is ? rest[j].token : -1;
     }
 }
 
@@ -516,7 +605,7 @@ int check_beams(const nereus_logits_t* in, const nereus_beams_t* how) {
 
 // How the rows are cut, and where the workspace's arrays are; returns its size.
 size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, int sms, Deal* deal, Select* s, char* workspace) {
-    *deal = spread_of(in, kTH, 0, 0, INT32_MAX);
+    *deal = spread_of(in, 2 * kTH, 0, 0, INT32_MAX);
     s->beams = how.beams;
     s->k = how.k;
     s->settle = how.settle;
@@ -524,29 +613,36 @@ size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, int sms, De
     s->score = how.score;
     s->ended = how.ended;
     s->norm = how.norm;
-    // A few parts for every block that the GPU holds (4 on an SM), so that they end together; no more of a request than one
-    // block puts together in a microsecond.
-    const int64_t all = in.rows * deal->layers;
+    // The layers of a part that the busiest block is done with first, when the GPU holds 4 on an SM and a part's end takes as
+    // long as half a layer; and no more parts of a request than one block puts together in a microsecond.
+    auto parts = [&](int of_part) { return (int64_t)(deal->layers + of_part - 1) / of_part; };
+    auto takes = [&](int of_part) { return (double)((parts(of_part) * in.rows + 4 * sms - 1) / (4 * sms)) * (of_part + 0.5); };
     s->of_part = 1;
-    while ((s->of_part < kPart && all / (2 * s->of_part) >= 16 * sms) || (s->of_part < kItems && (int64_t)((deal->layers + s->of_part - 1) / s->of_part) * how.beams > kParts))
-        s->of_part *= 2;
+    for (int m = 2; m <= kPart; m *= 2)
+        if (takes(m) < takes(s->of_part)) s->of_part = m;
+    while (parts(s->of_part) * how.beams > kParts) s->of_part *= 2;
     s->parts = (deal->layers + s->of_part - 1) / s->of_part;
     s->per_shard_1 = 1.f / (float)deal->per_shard;
-    const size_t units = (size_t)in.rows * s->parts, sums = units * kWarps * sizeof(Sum);
-    s->sums = reinterpret_cast<Sum*>(workspace);
-    s->notes = reinterpret_cast<uint16_t*>(workspace + sums);
-    return sums + units * kTH * 2;
+    s->records = reinterpret_cast<Record*>(workspace);
+    return (size_t)in.rows * s->parts * sizeof(Record);
 }
 
 template <class T> int beam_launch(const LogitsCut& cut, const Deal& deal, const Select& s, const Device& dev, cudaStream_t stream) {
+    static std::atomic<bool> opted[kMaxDevices];
+    constexpr int kMost = kParts * (int)sizeof(Record);
+    if (!opted[dev.id].load()) {
+        NEREUS_CUDA(cudaFuncSetAttribute(beam_pick_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost));
+        opted[dev.id].store(true);
+    }
     const int64_t units = (int64_t)s.rows * s.parts;
-    // an odd number of blocks: beams that offer nothing (all but a request's first on its first step) come to all of them
+    // an odd number of blocks: rows that are not read (all but a request's first on its first step) come to all alike
     const int64_t most = 4 * dev.sms - 1;
     beam_sum_kernel<T><<<(unsigned)std::min<int64_t>(units, most), kTH, 0, stream>>>(cut, deal, s);
     NEREUS_CUDA(cudaGetLastError());
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(s.rows / s.beams));
     cfg.blockDim = dim3(kPick);
+    cfg.dynamicSmemBytes = (size_t)s.beams * s.parts * sizeof(Record);
     cfg.stream = stream;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;          // its blocks come while the last sums are made
