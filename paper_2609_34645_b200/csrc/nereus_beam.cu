@@ -104,11 +104,11 @@ template <class T> __device__ __forceinline__ void load_four(const Layer* table,
 #pragma unroll
             for (int v = 0; v < 4; ++v) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
         } else {
-#pragma unroll 1
+#pragma unroll
             for (int v = 0; v < 4; ++v) {
                 const int at = ((int)threadIdx.x + v * kTH) * kPerVec<T>;
                 if (at >= L.lo && at + kPerVec<T> <= L.hi) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
-                else to[v * kTH] = edge_vector<T>(L, threadIdx.x + v * kTH);
+                else to[v * kTH] = at + kPerVec<T> <= L.lo || at >= L.hi ? Vec<T>::none() : edge_vector<T>(L, threadIdx.x + v * kTH);
             }
         }
     }

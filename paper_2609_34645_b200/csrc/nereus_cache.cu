@@ -36,9 +36,10 @@ constexpr int64_t kMaxPage  = (int64_t)1 << 30;
 // A warp takes a tile of up to 4 KiB of one page in one pool, loads all of it and stores it.  The number of pairs may be known to the
 // device alone, so the grid is what the GPU holds and every warp goes on by the grid's size.
 
-struct Pools {
-    char*   from[NEREUS_MAX_BUFFERS];
-    char*   to[NEREUS_MAX_BUFFERS];
+constexpr int kFew = 64;                   // buffers of most calls: a kernel's parameters of 4 KiB take 2 us more to hand over
+template <int N> struct Pools {
+    char*   from[N];
+    char*   to[N];
     int64_t from_stride, to_stride, page_bytes;
     int32_t pools, from_pages, to_pages, chunks;
 };
@@ -46,8 +47,8 @@ constexpr int kCopyThreads = 256;
 constexpr int kTileVecs = 8;               // of a thread
 
 // The tiles of `n` pairs, from this warp's first on; src, dst: `step` apart.
-template <class V>
-__device__ __forceinline__ void copy_pages(const Pools& p, int64_t n, const int32_t* src, const int32_t* dst, int step, int64_t warp, int64_t warps) {
+template <class V, class P>
+__device__ __forceinline__ void copy_pages(const P& p, int64_t n, const int32_t* src, const int32_t* dst, int step, int64_t warp, int64_t warps) {
     const int     lane = threadIdx.x & 31;
     const int64_t per_pair = (int64_t)p.pools * p.chunks, vecs = p.page_bytes / (int64_t)sizeof(V);
     // this warp's place as (pair, pool, chunk), and how far it goes on
@@ -57,7 +58,7 @@ __device__ __forceinline__ void copy_pages(const Pools& p, int64_t n, const int3
     const int by_pool = (int)(warps - by_pair * per_pair) / p.chunks, by_chunk = (int)(warps - by_pair * per_pair) % p.chunks;
 #pragma unroll 1
     while (pair < n) {
-        const int s = src[pair * step], d = dst[pair * step];
+        const int s = __ldcg(src + pair * step), d = __ldcg(dst + pair * step);
         if ((unsigned)s < (unsigned)p.from_pages && (unsigned)d < (unsigned)p.to_pages) {
             const int64_t at = (int64_t)chunk * (32 * kTileVecs) + lane;
             const V* a = reinterpret_cast<const V*>(p.from[pool] + s * p.from_stride) + at;
@@ -78,20 +79,24 @@ __device__ __forceinline__ void copy_pages(const Pools& p, int64_t n, const int3
     }
 }
 
-template <class V>
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ Pools p, int64_t n, const int32_t* src, const int32_t* dst) {
-    copy_pages<V>(p, n, src, dst, 1, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+template <class V, class P>
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ P p, int64_t n, const int32_t* src, const int32_t* dst) {
+    copy_pages<V, P>(p, n, src, dst, 1, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
 }
 
 // ---- what the books' kernels share -----------------------------------------------------------------------------
 //
-// The books are worked on by one cluster of `gridDim.x` blocks: its barriers cost what they cost, a microsecond or so, where
-// launches of their own would cost several.  Every block has a slice of the pages, every warp a part of the slice.
+// A call is a chain of launches, each of which is told to come up while the one before it runs and waits for its end only
+// where it needs what that has written: what it can work out from the call's arguments is ready by then.  Free pages are ranked
+// by one cluster, whose barriers cost a microsecond or so: every block has a slice of the pages, every warp a part of the slice.
 
 constexpr int kBookThreads = 1024;
 constexpr int kBookWarps   = kBookThreads / 32;
-constexpr int kMaxCluster  = 8;
+constexpr int kMaxCluster  = 16;
+constexpr int kGroup       = 128;             // pages that a warp looks at at a time, four a lane
 
+__device__ __forceinline__ void let_next_come() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
@@ -146,13 +151,43 @@ __device__ __forceinline__ Wide blocks_before(Wide mine, Wide* totals, int rank,
     *total = all;
     return before;
 }
-// This warp's part [lo, hi) of the pages, by whole groups of 32.
+// This warp's part [lo, hi) of the pages, in whole groups; blocks is a power of two.
 struct Part {
     int lo, hi;
 };
 __device__ __forceinline__ Part part_of(int pages, int rank, int blocks) {
-    const int64_t groups = (pages + 31) / 32, parts = (int64_t)blocks * kBookWarps, i = (int64_t)rank * kBookWarps + (threadIdx.x >> 5);
-    return {(int)min((int64_t)pages, groups * i / parts * 32), (int)min((int64_t)pages, groups * (i + 1) / parts * 32)};
+    const int64_t groups = (pages + kGroup - 1) / kGroup, parts = (int64_t)blocks * kBookWarps, i = (int64_t)rank * kBookWarps + (threadIdx.x >> 5);
+    const int     shift = __ffsll(parts) - 1;
+    return {(int)min((int64_t)pages, (groups * i >> shift) * kGroup), (int)min((int64_t)pages, (groups * (i + 1) >> shift) * kGroup)};
+}
+// Counts of the lane's four pages of the group that begins at p; `none` past hi.
+__device__ __forceinline__ int4 counts_of(const int32_t* refs, int p, int hi, bool aligned, int none) {
+    const int at = p + 4 * (threadIdx.x & 31);
+    if (aligned && at + 4 <= hi) return __ldcg(reinterpret_cast<const int4*>(refs + at));
+    int4 v;
+    v.x = at < hi ? __ldcg(refs + at) : none;
+    v.y = at + 1 < hi ? __ldcg(refs + at + 1) : none;
+    v.z = at + 2 < hi ? __ldcg(refs + at + 2) : none;
+    v.w = at + 3 < hi ? __ldcg(refs + at + 3) : none;
+    return v;
+}
+__device__ __forceinline__ int live_of(int4 v) { return (v.x > 0) + (v.y > 0) + (v.z > 0) + (v.w > 0); }
+// Pages in use of a warp's part, in all its lanes together.
+__device__ __forceinline__ int count_live(const int32_t* refs, Part part, bool aligned) {
+    int n = 0;
+#pragma unroll 4
+    for (int p = part.lo; p < part.hi; p += kGroup) n += live_of(counts_of(refs, p, part.hi, aligned, 0));
+    return __reduce_add_sync(0xffffffffu, n);
+}
+
+// x / d for 0 <= x < 2^52, one_by = 1 / d rounded: off by one at most before it is put right.
+struct Divisor {
+    double  one_by;
+    int32_t d;
+};
+__device__ __forceinline__ int64_t quotient(int64_t x, const Divisor& by) {
+    const int64_t q = __double2ll_rz((double)x * by.one_by), r = x - q * by.d;
+    return r < 0 ? q - 1 : r >= by.d ? q + 1 : q;
 }
 
 struct Books {
@@ -167,11 +202,15 @@ struct NewBooks {
 };
 
 // ---- forking -------------------------------------------------------------------------------------------------
+//
+// Four launches: start (counts copied, the table's plain entries), count (what the rows' old and new holders change), assign
+// (which pages are free, and which row gets which), apply (page copies).
 
 struct Fork {
     const int32_t *parent, *room_of;
     int32_t *copies, *status;
-    int32_t  page_size, room;
+    Divisor  page_size;
+    int32_t  room;
 };
 // What becomes of a row: its parent (-1: it is empty), the tokens and full pages it starts with, and the columns until which it
 // has to have pages.
@@ -180,108 +219,194 @@ struct Heir {
     bool    begun;
     int64_t until;
 };
+__device__ __forceinline__ int tokens_of(const Books& b, const Fork& f, int row) {
+    return (int)min((int64_t)max(b.length[row], 0), (int64_t)b.columns * f.page_size.d);
+}
 __device__ __forceinline__ Heir heir_of(const Books& b, const Fork& f, int row) {
     Heir h = {f.parent[row], 0, 0, false, 0};
     if ((unsigned)h.parent >= (unsigned)b.rows) h.parent = -1;
     else {
-        h.n = (int)min((int64_t)max(b.length[h.parent], 0), (int64_t)b.columns * f.page_size);
-        h.full = h.n / f.page_size;
-        h.begun = h.n % f.page_size != 0;
-        const int64_t room = max(f.room_of ? f.room_of[row] : f.room, 0);
-        h.until = (h.n + room + f.page_size - 1) / f.page_size;
+        h.n = tokens_of(b, f, h.parent);
+        h.full = (int)quotient(h.n, f.page_size);
+        h.begun = h.n != h.full * f.page_size.d;
+        h.until = quotient((int64_t)h.n + max(f.room_of ? f.room_of[row] : f.room, 0) + f.page_size.d - 1, f.page_size);
     }
     return h;
 }
 __device__ __forceinline__ bool is_page(int e, int pages) { return (unsigned)e < (unsigned)pages; }
 
+constexpr int kStartThreads = 256;
+constexpr int kPerThread    = 4;              // entries, or vectors of four counts
+constexpr int kRefsUnit     = kStartThreads * kPerThread * 4;
+constexpr int kTableUnit    = kStartThreads * kPerThread;
+
+// Counts and plain entries, dealt out in units to all blocks: HBM is what bounds them where they are many.
+__global__ void __launch_bounds__(kStartThreads) fork_start_kernel(const Books from, const NewBooks to, const Fork f, int refs_units, int chunks) {
+    const int  tid = threadIdx.x;
+    const bool aligned = (((uintptr_t)from.refs | (uintptr_t)to.refs) & 15) == 0;
+    let_next_come();
+#pragma unroll 1
+    for (int64_t u = blockIdx.x; u < refs_units + (int64_t)to.rows * chunks; u += gridDim.x) {
+        if (u < refs_units) {
+            const int lo = (int)u * kRefsUnit, hi = (int)min((int64_t)lo + kRefsUnit, (int64_t)from.pages);
+            if (aligned && hi - lo == kRefsUnit) {
+                int4 v[kPerThread];
+#pragma unroll
+                for (int j = 0; j < kPerThread; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from.refs + lo) + tid + j * kStartThreads);
+#pragma unroll
+                for (int j = 0; j < kPerThread; ++j) __stcg(reinterpret_cast<int4*>(to.refs + lo) + tid + j * kStartThreads, v[j]);
+            } else {
+                for (int p = lo + tid; p < hi; p += kStartThreads) to.refs[p] = from.refs[p];
+            }
+            continue;
+        }
+        const int  i = (int)((u - refs_units) / chunks), first = (int)((u - refs_units) - (int64_t)i * chunks) * kTableUnit;
+        const int  end = min(first + kTableUnit, from.columns);
+        const Heir h = heir_of(from, f, i);
+        int        before = 0;                         // whether a row above names the same parent
+        if (h.parent >= 0 && end > h.full)
+            for (int j = tid; j < i; j += kStartThreads) before |= f.parent[j] == h.parent;
+        const bool     leads = !__syncthreads_or(before);
+        const int32_t* row = from.table + max(h.parent, 0) * from.stride;
+        int32_t* const out = to.table + i * to.stride;
+        int e[kPerThread];
+#pragma unroll
+        for (int j = 0; j < kPerThread; ++j) {
+            const int c = first + tid + j * kStartThreads;
+            e[j] = h.parent >= 0 && c < end && (c < h.full || leads) ? __ldcg(row + c) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kPerThread; ++j) {
+            const int c = first + tid + j * kStartThreads;
+            // a column that lacks a page gets its entry later
+            if (c < end && !(c >= h.full && c < h.until && !is_page(e[j], from.pages))) __stcg(out + c, e[j]);
+        }
+        if (first == 0 && tid == 0) {
+            to.length[i] = h.n;
+            f.copies[2 * i] = f.copies[2 * i + 1] = -1;
+        }
+    }
+}
+
+// A thread goes down a column over a few rows: beams of one request hold the same pages one above the other, whose changes are
+// added up before they go out.
+constexpr int kCountThreads = 256;
+constexpr int kMostRows     = 64;
+constexpr int kAtATime      = 8;
+__global__ void __launch_bounds__(kCountThreads) fork_count_kernel(const Books from, const NewBooks to, const Fork f, int group) {
+    __shared__ int kids[kMostRows], full[kMostRows];
+    const int tid = threadIdx.x, first = blockIdx.y * group, n = min(group, from.rows - first), c = blockIdx.x * kCountThreads + tid;
+    let_next_come();
+    if (tid < n) {
+        kids[tid] = 0;
+        full[tid] = (int)quotient(tokens_of(from, f, first + tid), f.page_size);
+    }
+    __syncthreads();
+    for (int i = tid; i < to.rows; i += kCountThreads) {
+        const int r = f.parent[i] - first;
+        if ((unsigned)r < (unsigned)n) atomicAdd(&kids[r], 1);
+    }
+    __syncthreads();
+    wait_for_last();                                   // the old counts are there
+    if (c >= from.columns) return;
+    int page = -1, sum = 0;
+#pragma unroll 1
+    for (int first_of = 0; first_of < n; first_of += kAtATime) {
+        int e[kAtATime], change[kAtATime];
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j) {
+            const int r = min(first_of + j, n - 1), k = kids[r];
+            change[j] = first_of + j >= n ? 0 : c < full[r] ? k - 1 : k ? 0 : -1;
+            e[j] = change[j] ? __ldcg(from.table + (first + r) * from.stride + c) : -1;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtATime; ++j) {
+            if (!is_page(e[j], from.pages)) continue;
+            if (e[j] != page) {
+                if (sum) atomicAdd(&to.refs[page], sum);
+                page = e[j];
+                sum = 0;
+            }
+            sum += change[j];
+        }
+    }
+    if (sum) atomicAdd(&to.refs[page], sum);
+}
+
 // A row's need of fresh pages, and 1 << 48 where its first is a copy.
 constexpr Wide kOneCopy = (Wide)1 << 48;
+__device__ __forceinline__ int64_t pages_in(Wide need) { return (int64_t)(need & (kOneCopy - 1)); }
 
-// Books of a fork but for the table's plain entries.  One cluster.  first, kids: of every old row, the lowest new row that names
-// it and how many do; need: of every new row, then its sum over the rows before.
-__global__ void __launch_bounds__(kBookThreads, 1) fork_kernel(const Books from, const NewBooks to, const Fork f) {
+// Of a row that lacks pages: its parent, the columns in which it lacks them, whether it has pages between these.
+struct Lack {
+    int parent, full, until;
+};
+constexpr int kSelf = 8;                      // columns that a row's own thread looks through; a warp takes rows with more
+
+// One cluster.  Of every new row: what it needs, then the sum of that over the rows before; what it lacks.  first: of every old
+// row, the lowest new row that names it.  free_of: free pages of the block's groups, then their sum over the groups before.
+__global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Books from, const NewBooks to, const Fork f, int groups_of_block) {
     extern __shared__ __align__(16) unsigned char dynamic[];
     __shared__ Wide scratch[kBookWarps + 1], totals[kMaxCluster];
     __shared__ Wide lacking_columns;
-    Wide* need  = reinterpret_cast<Wide*>(dynamic);
-    int*  first = reinterpret_cast<int*>(need + to.rows);
-    int*  kids  = first + from.rows;
-    int*  changed = kids + from.rows;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = gridDim.x, rank = blockIdx.x;
-    const Part part = part_of(from.pages, rank, blocks);
+    Wide* need    = reinterpret_cast<Wide*>(dynamic);
+    Lack* lack    = reinterpret_cast<Lack*>(need + to.rows);
+    int*  first   = reinterpret_cast<int*>(lack + to.rows);
+    int*  free_of = first + from.rows;
+    const int  tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = gridDim.x, rank = blockIdx.x;
+    const bool aligned = ((uintptr_t)to.refs & 15) == 0;
 
-    cluster_arrive();                                  // this block has begun: the others may write to it
-    for (int r = tid; r < from.rows; r += kBookThreads) { first[r] = INT_MAX; kids[r] = 0; }
+    let_next_come();
     if (tid == 0) lacking_columns = 0;
+    cluster_arrive();                                  // this block has begun: the others may write to it
+    for (int r = tid; r < from.rows; r += kBookThreads) first[r] = INT_MAX;
     __syncthreads();
     for (int i = tid; i < to.rows; i += kBookThreads) {
         const int p = f.parent[i];
-        if ((unsigned)p < (unsigned)from.rows) {
-            atomicAdd(&kids[p], 1);
-            atomicMin(&first[p], i);
-        }
+        if ((unsigned)p < (unsigned)from.rows) atomicMin(&first[p], i);
     }
-    for (int p = part.lo + lane; p < part.hi; p += 32) to.refs[p] = from.refs[p];
     __syncthreads();
-    cluster_wait();
-    // what the rows need, a warp for each; every block gets it
-    for (int i = rank * kBookWarps + warp; i < to.rows; i += blocks * kBookWarps) {
-        const Heir h = heir_of(from, f, i);
-        Wide       w = 0;
-        if (h.parent >= 0) {
-            const int     until = (int)min(h.until, (int64_t)from.columns);
-            const int32_t* row = from.table + h.parent * from.stride;
-            if (first[h.parent] == i) {
-                for (int c = h.full + lane; c < until; c += 32) w += !is_page(row[c], from.pages);
-                w = __reduce_add_sync(0xffffffffu, (unsigned)w);
-            } else if (h.full < until) {
-                w = until - h.full;
-                if (h.begun && is_page(row[h.full], from.pages)) w += kOneCopy;
-            }
-        }
-        if (lane < blocks) peer_store(peer_address(need + i, lane), w);
-    }
+    // what the rows need: every block goes through all of them
+    bool long_rows = false;
+#pragma unroll 1
     for (int i = tid; i < to.rows; i += kBookThreads) {
         const Heir h = heir_of(from, f, i);
-        if (h.until > from.columns) atomicAdd(&lacking_columns, (Wide)(h.until - from.columns));
-    }
-    // rows whose number of holders changes, in order: every block has the same list
-    int n_changed = 0;
-    for (int r = tid; r - tid < from.rows; r += kBookThreads) {
-        const bool     is = r < from.rows && kids[r] != 1;
-        const unsigned who = __ballot_sync(0xffffffffu, is);
-        Wide           all;
-        const int      before = (int)warps_before(__popc(who), scratch, &all);
-        if (is) changed[n_changed + before + __popc(who & ((1u << lane) - 1))] = r;
-        n_changed += (int)all;
-    }
-    cluster_sync();                                    // the new counts and the needs are there
-
-    // a thread goes down a column: beams of one request hold the same pages one above the other, whose changes are added up
-    // before they go out
-    {
-        const int64_t threads = (int64_t)blocks * kBookThreads, self = (int64_t)rank * kBookThreads + tid;
-        const int64_t lanes = min((int64_t)(from.columns + 31) / 32 * 32, threads), groups = max((int64_t)1, threads / lanes);
-        const int     group = (int)(self / lanes), n = n_changed;
-        if (group < groups)
-            for (int64_t c = self % lanes; c < from.columns; c += lanes) {
-                int page = -1, sum = 0;
-                for (int j = (int)((int64_t)n * group / groups), end = (int)((int64_t)n * (group + 1) / groups); j < end; ++j) {
-                    const int r = changed[j], k = kids[r];
-                    const int tokens = (int)min((int64_t)max(from.length[r], 0), (int64_t)from.columns * f.page_size);
-                    const bool full = c < tokens / f.page_size;
-                    if (!full && k) continue;
-                    const int e = from.table[r * from.stride + c];
-                    if (!is_page(e, from.pages)) continue;
-                    if (e != page) {
-                        if (sum) atomicAdd(&to.refs[page], sum);
-                        page = e;
-                        sum = 0;
-                    }
-                    sum += full ? k - 1 : -1;
-                }
-                if (sum) atomicAdd(&to.refs[page], sum);
+        const int  until = (int)min(h.until, (int64_t)from.columns);
+        Wide       w = 0;
+        if (h.parent >= 0) {
+            const int32_t* row = from.table + h.parent * from.stride;
+            const bool     leads = first[h.parent] == i;
+            if (h.until > from.columns) atomicAdd(&lacking_columns, (Wide)(h.until - from.columns));
+            if (h.full >= until) {
+            } else if (!leads) {
+                w = (Wide)(until - h.full) + (h.begun && is_page(row[h.full], from.pages) ? kOneCopy : 0);
+            } else if (until - h.full <= kSelf) {
+#pragma unroll
+                for (int c = 0; c < kSelf; ++c) w += h.full + c < until && !is_page(row[min(h.full + c, from.columns - 1)], from.pages);
+            } else {
+                long_rows = true;
+                w = ~(Wide)0;
             }
+        }
+        need[i] = w;
+        lack[i] = {h.parent, h.full, until};
+    }
+    const bool some_long = __syncthreads_or(long_rows);
+    cluster_wait();
+    if (some_long) {                                   // in all blocks: their rows are shared out
+        cluster_sync();                                // nobody marks them any more
+        for (int i = rank * kBookWarps + warp; i < to.rows; i += blocks * kBookWarps) {
+            if (need[i] != ~(Wide)0) continue;
+            const Lack     l = lack[i];
+            const int32_t* row = from.table + l.parent * from.stride;
+            unsigned       n = 0;
+#pragma unroll 4
+            for (int c = l.full + lane; c < l.until; c += 32) n += !is_page(__ldcg(row + c), from.pages);
+            n = __reduce_add_sync(0xffffffffu, n);
+            __syncwarp();
+            if (lane < blocks) peer_store(peer_address(need + i, lane), n);
+        }
+        cluster_sync();
     }
     // need: sum over the rows before
     Wide needed = 0;
@@ -293,94 +418,98 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_kernel(const Books from,
         Wide at = warps_before(__shfl_sync(0xffffffffu, upto, 31), scratch, &needed) + upto - sum;
         for (int i = lo; i < hi; ++i) { const Wide w = need[i]; need[i] = at; at += w; }
     }
-    const int64_t fresh = (int64_t)(needed & (kOneCopy - 1));
+    const int64_t fresh = pages_in(needed);
     const int     n_copies = (int)(needed >> 48);
-    cluster_sync();                                    // all changes are in
+    wait_for_last();                                   // all changes are in
 
-    // free pages, in all and before this warp
-    Wide of_warp = 0, of_block, free_pages;
-    for (int p = part.lo; p < part.hi; p += 32) of_warp += __popc(__ballot_sync(0xffffffffu, p + lane < part.hi && __ldcg(to.refs + p + lane) <= 0));
-    Wide rank_of = warps_before(of_warp, scratch, &of_block);
-    rank_of += blocks_before(of_block, totals, rank, blocks, &free_pages);
+    // free pages: of every group, in all, and before the block
+    const int first_group = rank * groups_of_block, n_groups = min(groups_of_block, max(0, (from.pages + kGroup - 1) / kGroup - first_group));
+#pragma unroll 8
+    for (int g = warp; g < n_groups; g += kBookWarps) {
+        const int p = (first_group + g) * kGroup;
+        const int n = __reduce_add_sync(0xffffffffu, 4 - live_of(counts_of(to.refs, p, from.pages, aligned, 1)));
+        if (lane == 0) free_of[g] = n;
+    }
+    __syncthreads();
+    Wide of_block, free_pages;
+    {
+        const int per = (n_groups + kBookThreads - 1) / kBookThreads, lo = min(tid * per, n_groups), hi = min(lo + per, n_groups);
+        int sum = 0;
+        for (int g = lo; g < hi; ++g) sum += free_of[g];
+        const int upto = (int)warp_scan((Wide)sum);
+        int at = (int)warps_before((Wide)__shfl_sync(0xffffffffu, upto, 31), scratch, &of_block) + upto - sum;
+        for (int g = lo; g < hi; ++g) { const int n = free_of[g]; free_of[g] = at; at += n; }
+    }
+    const int64_t before = (int64_t)blocks_before(of_block, totals, rank, blocks, &free_pages);
     const int64_t missing = max((int64_t)0, fresh - (int64_t)free_pages) + (int64_t)lacking_columns;
-    const bool    fine = missing == 0;
-    if (fine) {
-        for (int p = part.lo; p < part.hi && (int64_t)rank_of < fresh; p += 32) {
-            const bool     is = p + lane < part.hi && __ldcg(to.refs + p + lane) <= 0;
-            const unsigned who = __ballot_sync(0xffffffffu, is);
-            const int64_t  j = (int64_t)rank_of + __popc(who & ((1u << lane) - 1));
-            rank_of += __popc(who);
-            if (!is || j >= fresh) continue;
-            int lo = 0, hi = to.rows;                  // the last row whose sum is not above j
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) / 2;
-                if ((int64_t)(need[mid] & (kOneCopy - 1)) <= j) lo = mid;
-                else hi = mid;
-            }
-            const Heir     h = heir_of(from, f, lo);
-            const int      until = (int)min(h.until, (int64_t)from.columns);
-            const int32_t* row = from.table + h.parent * from.stride;
-            int            k = (int)(j - (int64_t)(need[lo] & (kOneCopy - 1))), c = h.full + k;
-            const int64_t  of_row = (int64_t)((lo + 1 < to.rows ? need[lo + 1] : needed) & (kOneCopy - 1)) - (int64_t)(need[lo] & (kOneCopy - 1));
-            if (first[h.parent] == lo && of_row != until - h.full)
-                for (c = h.full; c < until; ++c)       // the row has pages between those it lacks
-                    if (!is_page(row[c], from.pages) && k-- == 0) break;
-            to.table[lo * to.stride + c] = p + lane;
-            to.refs[p + lane] = 1;
-            if (k == 0 && c == h.full && (lo + 1 < to.rows ? need[lo + 1] : needed) >> 48 != need[lo] >> 48) {
-                const int at = (int)(need[lo] >> 48);
-                f.copies[2 * at] = row[c];
-                f.copies[2 * at + 1] = p + lane;
+    if (missing == 0) {
+#pragma unroll 1
+        for (int g = warp; g < n_groups && before + free_of[g] < fresh; g += kBookWarps) {
+            const int      p = (first_group + g) * kGroup;
+            const int4     v = counts_of(to.refs, p, from.pages, aligned, 1);
+            const unsigned below = (1u << lane) - 1;
+            int64_t        j = before + free_of[g];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) j += __popc(__ballot_sync(0xffffffffu, (e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) <= 0) & below);
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                if ((e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) > 0) continue;
+                if (j >= fresh) break;
+                int lo = 0, hi = to.rows;              // the last row whose sum is not above j
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) / 2;
+                    if (pages_in(need[mid]) <= j) lo = mid;
+                    else hi = mid;
+                }
+                const Wide here = need[lo], next = lo + 1 < to.rows ? need[lo + 1] : needed;
+                const Lack l = lack[lo];
+                const int  page = p + 4 * lane + e;
+                int        k = (int)(j - pages_in(here)), c = l.full + k;
+                const int32_t* row = from.table + l.parent * from.stride;
+                if (pages_in(next - here) != l.until - l.full)
+                    for (c = l.full; c < l.until; ++c)         // the row has pages between those it lacks
+                        if (!is_page(row[c], from.pages) && k-- == 0) break;
+                to.table[lo * to.stride + c] = page;
+                to.refs[page] = 1;
+                if (c == l.full && next >> 48 != here >> 48) {
+                    const int at = (int)(here >> 48);
+                    f.copies[2 * at] = row[c];
+                    f.copies[2 * at + 1] = page;
+                }
+                ++j;
             }
         }
     } else {
-        for (int p = part.lo + lane; p < part.hi; p += 32) to.refs[p] = from.refs[p];
+        const int lo = first_group * kGroup, hi = (int)min((int64_t)from.pages, (int64_t)(first_group + n_groups) * kGroup);
+        for (int p = lo + tid; p < hi; p += kBookThreads) to.refs[p] = from.refs[p];
     }
-    int was_free = 0;
-    if (!fine && rank == 0) {
-        for (int p = tid; p < from.pages; p += kBookThreads) was_free += from.refs[p] <= 0;
+    int64_t left = (int64_t)free_pages - fresh;
+    if (missing && rank == 0) {
+        int n = 0;
+        for (int p = tid; p < from.pages; p += kBookThreads) n += from.refs[p] <= 0;
         Wide all;
-        warps_before(__reduce_add_sync(0xffffffffu, was_free), scratch, &all);
-        was_free = (int)all;
+        warps_before(__reduce_add_sync(0xffffffffu, n), scratch, &all);
+        left = (int64_t)all;
     }
-    const int self = rank * kBookThreads + tid;
-    for (int i = self; i < to.rows; i += blocks * kBookThreads) {
-        to.length[i] = fine ? heir_of(from, f, i).n : i < from.rows ? from.length[i] : 0;
-        if (!fine || i >= n_copies) { f.copies[2 * i] = -1; f.copies[2 * i + 1] = -1; }
-    }
-    if (self == 0) {
-        f.status[0] = fine ? (int)((int64_t)free_pages - fresh) : was_free;
+    if (rank == 0 && tid == 0) {
+        f.status[0] = (int)left;
         f.status[1] = (int)min(missing, (int64_t)INT_MAX);
-        f.status[2] = fine ? n_copies : 0;
+        f.status[2] = missing ? 0 : n_copies;
         f.status[3] = 0;
     }
 }
 
-// The table's plain entries, a block for a row at a time, and the copies.
-template <class V>
-__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ Pools p, const Books from, const NewBooks to, const Fork f) {
-    const bool fine = f.status[1] == 0;
-    for (int i = blockIdx.x; i < to.rows; i += gridDim.x) {
-        int32_t* const out = to.table + i * to.stride;
-        if (!fine) {
-            for (int c = threadIdx.x; c < from.columns; c += kCopyThreads) out[c] = i < from.rows ? from.table[i * from.stride + c] : -1;
-            continue;
+// The page copies; where the fork is refused, the old table and lengths.
+template <class V, class P>
+__global__ void __launch_bounds__(kCopyThreads) fork_apply_kernel(const __grid_constant__ P p, const Books from, const NewBooks to, const Fork f) {
+    wait_for_last();
+    const int n = __ldcg(f.status + 2);
+    if (__ldcg(f.status + 1))
+        for (int i = blockIdx.x; i < to.rows; i += gridDim.x) {
+            for (int c = threadIdx.x; c < from.columns; c += kCopyThreads) to.table[i * to.stride + c] = i < from.rows ? from.table[i * from.stride + c] : -1;
+            if (threadIdx.x == 0) to.length[i] = i < from.rows ? from.length[i] : 0;
         }
-        const Heir h = heir_of(from, f, i);
-        int        before = 0;                         // whether a row above names the same parent
-        if (h.parent >= 0)
-            for (int j = threadIdx.x; j < i; j += kCopyThreads) before |= f.parent[j] == h.parent;
-        const bool     leads = !__syncthreads_or(before);
-        const int32_t* row = from.table + max(h.parent, 0) * from.stride;
-        for (int c = threadIdx.x; c < from.columns; c += kCopyThreads) {
-            int e = -1;
-            if (h.parent >= 0 && (c < h.full || leads)) e = row[c];
-            if (c >= h.full && c < h.until && !is_page(e, from.pages)) continue;          // a fresh page, written already
-            out[c] = e;
-        }
-    }
-    const int n = f.status[2];
-    copy_pages<V>(p, n, f.copies, f.copies + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+    copy_pages<V, P>(p, n, f.copies, f.copies + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
 }
 
 // ---- compacting ----------------------------------------------------------------------------------------------
@@ -393,40 +522,58 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const Books fr
     __shared__ Wide scratch[kBookWarps + 1], totals[2][kMaxCluster];
     const int  tid = threadIdx.x, lane = tid & 31, blocks = gridDim.x, rank = blockIdx.x;
     const Part part = part_of(from.pages, rank, blocks);
-    Wide of_warp = 0, of_block, live;
+    const bool aligned = ((uintptr_t)from.refs & 15) == 0;
+    let_next_come();
     cluster_arrive();                                  // this block has begun: the others may write to it
-    for (int p = part.lo; p < part.hi; p += 32) of_warp += __popc(__ballot_sync(0xffffffffu, p + lane < part.hi && from.refs[p + lane] > 0));
-    warps_before(of_warp, scratch, &of_block);
+    const int of_part = count_live(from.refs, part, aligned);
+    Wide of_block, live;
+    warps_before((Wide)of_part, scratch, &of_block);
     cluster_wait();
     blocks_before(of_block, totals[0], rank, blocks, &live);
     const int64_t missing = c.keep < 0 ? 0 : max((int64_t)0, (int64_t)live - c.keep);
     const int     keep = missing ? from.pages : c.keep < 0 ? (int)live : (int)min(c.keep, (int64_t)from.pages);
-    // pages that go (in the upper half) and holes that take them, before this warp and in all
-    of_warp = 0;
-    for (int p = part.lo; p < part.hi; p += 32) {
-        const bool in = p + lane < part.hi, is = in && from.refs[p + lane] > 0, up = p + lane >= keep;
-        of_warp += ((Wide)__popc(__ballot_sync(0xffffffffu, is && up)) << 32) + __popc(__ballot_sync(0xffffffffu, in && !is && !up));
+    // pages that go (in the upper half) and holes that take them, before this warp and in all; one part may lie on both sides
+    Wide of_warp = part.hi <= keep ? (Wide)(part.hi - part.lo - of_part) : (Wide)of_part << 32;
+    if (part.lo < keep && part.hi > keep) {
+        const int low = count_live(from.refs, {part.lo, keep}, aligned);
+        of_warp = ((Wide)(of_part - low) << 32) + (Wide)(keep - part.lo - low);
     }
     Wide all, before = warps_before(of_warp, scratch, &of_block);
     before += blocks_before(of_block, totals[1], rank, blocks, &all);
     const int moves = (int)(all >> 32);
     int goes = (int)(before >> 32), hole = (int)before;
-    for (int p = part.lo; p < part.hi; p += 32) {
-        const int  page = p + lane;
-        const bool in = page < part.hi;
-        const int  r = in ? from.refs[page] : 0;
-        const bool is = r > 0, up = page >= keep;
-        const unsigned who = __ballot_sync(0xffffffffu, is && up), where = __ballot_sync(0xffffffffu, in && !is && !up), below = (1u << lane) - 1;
-        if (is && up) c.moves[2 * (goes + __popc(who & below))] = page;
-        const int h = hole + __popc(where & below);
-        const bool taken = in && !is && !up && h < moves;
-        if (taken) c.moves[2 * h + 1] = page;
-        if (in) {
-            if (!(is && up)) c.map[page] = is ? page : -1;
-            if (!taken) to.refs[page] = is && up ? 0 : r > 0 ? r : 0;
+#pragma unroll 1
+    for (int p = part.lo; p < part.hi; p += kGroup) {
+        const int4     v = counts_of(from.refs, p, part.hi, aligned, 0);
+        const int      r[4] = {v.x, v.y, v.z, v.w}, at = p + 4 * lane;
+        const unsigned below = (1u << lane) - 1;
+        int g = goes, h = hole;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool     in = at + e < part.hi, up = at + e >= keep;
+            const unsigned who = __ballot_sync(0xffffffffu, in && r[e] > 0 && up), where = __ballot_sync(0xffffffffu, in && r[e] <= 0 && !up);
+            g += __popc(who & below);
+            h += __popc(where & below);
+            goes += __popc(who);
+            hole += __popc(where);
         }
-        goes += __popc(who);
-        hole += __popc(where);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int page = at + e;
+            if (page >= part.hi) break;
+            const bool is = r[e] > 0, up = page >= keep;
+            if (is && up) {
+                c.moves[2 * g++] = page;
+                to.refs[page] = 0;
+            } else if (is || up || h >= moves) {
+                c.map[page] = is ? page : -1;
+                to.refs[page] = max(r[e], 0);
+                h += !is && !up;
+            } else {                                   // its count comes with the page
+                c.map[page] = -1;
+                c.moves[2 * h++ + 1] = page;
+            }
+        }
     }
     cluster_sync();
     for (int j = rank * kBookThreads + tid; j < moves; j += blocks * kBookThreads) {
@@ -441,14 +588,16 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const Books fr
         c.status[3] = keep;
     }
 }
-template <class V>
-__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ Pools p, const Books from, const NewBooks to, const Compact c) {
+template <class V, class P>
+__global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __grid_constant__ P p, const Books from, const NewBooks to, const Compact c) {
+    wait_for_last();
     for (int i = blockIdx.x; i < to.rows; i += gridDim.x)
+#pragma unroll 4
         for (int j = threadIdx.x; j < from.columns; j += kCopyThreads) {
-            const int e = from.table[i * from.stride + j];
-            to.table[i * to.stride + j] = is_page(e, from.pages) ? c.map[e] : e;
+            const int e = __ldcg(from.table + i * from.stride + j);
+            __stcg(to.table + i * to.stride + j, is_page(e, from.pages) ? __ldcg(c.map + e) : e);
         }
-    copy_pages<V>(p, c.status[2], c.moves, c.moves + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
+    copy_pages<V, P>(p, __ldcg(c.status + 2), c.moves, c.moves + 1, 2, ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) >> 5, ((int64_t)gridDim.x * kCopyThreads) >> 5);
 }
 
 // ---- reordering rows -----------------------------------------------------------------------------------------
@@ -456,9 +605,9 @@ __global__ void __launch_bounds__(kCopyThreads) compact_apply_kernel(const __gri
 // A thread takes one vector's place in the rows of a group: it loads what moves from every row that something goes on from,
 // then stores.  No other thread touches that place, so that parents may cross in place without a barrier.
 
-struct States {
-    char*   from[NEREUS_MAX_BUFFERS];
-    char*   to[NEREUS_MAX_BUFFERS];
+template <int N> struct States {
+    char*   from[N];
+    char*   to[N];
     int64_t from_row, to_row, from_outer, to_outer;        // strides
     int64_t piece;                                         // bytes of a piece: tokens * token_bytes
     int64_t token_bytes, tokens;
@@ -471,8 +620,8 @@ struct Move {
     int64_t from, to, bytes;
 };
 
-template <class V, int N>
-__global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_constant__ States s, const int32_t* parent, const int32_t* length) {
+template <class V, int N, class S>
+__global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_constant__ S s, const int32_t* parent, const int32_t* length) {
     __shared__ Move moves[N];
     __shared__ int  n_moves;
     __shared__ Wide most_bytes;
@@ -592,6 +741,25 @@ bool apart(const Side& a, const Side& b) {
         return r;
     };
     if (!meet(hull(a), hull(b))) return true;
+    // in the order of their starts, a range meets one of the other side before it or none
+    struct Item {
+        uintptr_t lo, hi;
+        bool second;
+    } all[2 * NEREUS_MAX_BUFFERS];
+    int n = 0;
+    for (const Side* s : {&a, &b})
+        for (int i = 0; i < s->n; ++i) {
+            const uintptr_t lo = (uintptr_t)s->base[i];
+            all[n++] = {lo, lo + (s->count - 1) * s->stride + s->width, s == &b};
+        }
+    std::sort(all, all + n, [](const Item& x, const Item& y) { return x.lo < y.lo; });
+    uintptr_t end[2] = {0, 0};
+    bool      met = false;
+    for (int i = 0; i < n && !met; ++i) {
+        met = all[i].lo < end[!all[i].second];
+        end[all[i].second] = std::max(end[all[i].second], all[i].hi);
+    }
+    if (!met) return true;
     for (int i = 0; i < a.n; ++i)
         for (int j = 0; j < b.n; ++j)
             if (!apart((uintptr_t)a.base[i], a.count, a.stride, a.width, (uintptr_t)b.base[j], b.count, b.stride, b.width)) return false;
@@ -641,72 +809,86 @@ int check_apart(const nereus_page_table_t& a, const nereus_page_table_t& b, int 
     return NEREUS_OK;
 }
 
-Pools pools_of(const nereus_pages_t& a, const nereus_pages_t& b, int* unit) {
-    Pools p;
+// f(a vector of the widest type that divides everything, the parameters), for as many buffers as there are.
+template <int N, class F> int with_pools(const nereus_pages_t& a, const nereus_pages_t& b, F f) {
+    Pools<N> p;
     uint64_t bits = (uint64_t)a.page_bytes | (a.pages > 1 ? a.page_stride : 0) | (b.pages > 1 ? b.page_stride : 0);
     for (int i = 0; i < a.pools; ++i) {
         p.from[i] = (char*)a.pool[i];
         p.to[i] = (char*)b.pool[i];
         bits |= (uintptr_t)a.pool[i] | (uintptr_t)b.pool[i];
     }
-    *unit = a.pools ? unit_of(bits) : 16;
+    const int unit = a.pools ? unit_of(bits) : 16;
     p.from_stride = a.page_stride;
     p.to_stride = b.page_stride;
     p.page_bytes = a.pools ? a.page_bytes : 0;
     p.pools = a.pools;
     p.from_pages = a.pages;
     p.to_pages = b.pages;
-    const int64_t tile = (int64_t)*unit * 32 * kTileVecs;
+    const int64_t tile = (int64_t)unit * 32 * kTileVecs;
     p.chunks = a.pools ? (int32_t)((a.page_bytes + tile - 1) / tile) : 1;
     if (!p.pools) { p.pools = 1; p.from_pages = 0; }       // no pair is in range
-    return p;
+    return unit == 16 ? f(uint4(), p) : unit == 4 ? f(uint32_t(), p) : f((unsigned char)0, p);
+}
+template <class F> int with_pools(const nereus_pages_t& a, const nereus_pages_t& b, F f) {
+    return a.pools <= kFew ? with_pools<kFew>(a, b, f) : with_pools<NEREUS_MAX_BUFFERS>(a, b, f);
 }
 
-void book_launch(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, int64_t work, int64_t smem, cudaStream_t stream) {
-    *cfg = {};
-    // one block where the books are small: what more blocks would save is less than their barriers cost
-    const unsigned blocks = work > 16384 ? kMaxCluster : 1;
-    cfg->gridDim = dim3(blocks);
-    cfg->blockDim = dim3(kBookThreads);
-    cfg->dynamicSmemBytes = (size_t)smem;
-    cfg->stream = stream;
-    attr->id = cudaLaunchAttributeClusterDimension;
-    attr->val.clusterDim.x = blocks;
-    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
-    cfg->attrs = attr;
-    cfg->numAttrs = 1;
+// Launches a kernel; cluster: of all its blocks; chained: it comes up while the launch before it runs, and waits for that itself.
+template <class... P, class... A>
+int launch(void (*kernel)(P...), dim3 grid, int threads, int64_t smem, bool cluster, bool chained, cudaStream_t stream, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2] = {};
+    if (cluster) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = grid.x;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+    }
+    if (chained) {
+        attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+        ++cfg.numAttrs;
+    }
+    cfg.attrs = attr;
+    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return NEREUS_OK;
 }
+// Blocks of the cluster that ranks pages: one where its own pass over them takes no longer than a cluster's barriers.
+unsigned cluster_of(int pages) { return pages <= 32768 ? 1 : kMaxCluster; }
+
 Books    books_of(const nereus_page_table_t& t, int pages) { return {t.table, t.length, t.refs, t.stride, t.rows, t.columns, pages}; }
 NewBooks new_books_of(const nereus_page_table_t& t) { return {t.table, t.length, t.refs, t.stride, t.rows}; }
 
-template <class V> int copy_launch(const Pools& p, int64_t n, const int32_t* src, const int32_t* dst, const Device& dev, cudaStream_t stream) {
+template <class V, class P> int copy_launch(const P& p, int64_t n, const int32_t* src, const int32_t* dst, const Device& dev, cudaStream_t stream) {
     static std::atomic<int> known[kMaxDevices];
     int per_sm;
-    if (int rc = resident(copy_kernel<V>, kCopyThreads, known, dev, &per_sm)) return rc;
+    if (int rc = resident(copy_kernel<V, P>, kCopyThreads, known, dev, &per_sm)) return rc;
     const int64_t warps = kCopyThreads / 32, tiles = n * p.pools * p.chunks;
     const int64_t grid = std::min<int64_t>((tiles + warps - 1) / warps, (int64_t)per_sm * dev.sms);
-    copy_kernel<V><<<(unsigned)grid, kCopyThreads, 0, stream>>>(p, n, src, dst);
-    NEREUS_CUDA(cudaGetLastError());
-    return NEREUS_OK;
+    return launch(copy_kernel<V, P>, dim3((unsigned)grid), kCopyThreads, 0, false, false, stream, p, n, src, dst);
 }
-template <class V, class Work>
-int apply_launch(void (*kernel)(Pools, Books, NewBooks, Work), std::atomic<int>* known, const Pools& p, int64_t most_pairs, const Books& from,
-                 const NewBooks& to, const Work& w, const Device& dev, cudaStream_t stream) {
+// The last launch of a fork or compaction: `most_pairs` page copies at most.
+template <class P, class Work>
+int apply_launch(void (*kernel)(P, Books, NewBooks, Work), std::atomic<int>* known, const P& p, int64_t most_pairs, const Books& from, const NewBooks& to,
+                 const Work& w, const Device& dev, cudaStream_t stream) {
     int per_sm;
     if (int rc = resident(kernel, kCopyThreads, known, dev, &per_sm)) return rc;
     const int64_t warps = kCopyThreads / 32, tiles = p.page_bytes ? most_pairs * p.pools * p.chunks : 0;
     const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>((tiles + warps - 1) / warps, to.rows), (int64_t)per_sm * dev.sms));
-    kernel<<<(unsigned)grid, kCopyThreads, 0, stream>>>(p, from, to, w);
-    NEREUS_CUDA(cudaGetLastError());
-    return NEREUS_OK;
+    return launch(kernel, dim3((unsigned)grid), kCopyThreads, 0, false, true, stream, p, from, to, w);
 }
-template <class V> int fork_apply(const Pools& p, const Books& from, const NewBooks& to, const Fork& f, const Device& dev, cudaStream_t stream) {
+template <class V, class P> int fork_apply(const P& p, const Books& from, const NewBooks& to, const Fork& f, const Device& dev, cudaStream_t stream) {
     static std::atomic<int> known[kMaxDevices];
-    return apply_launch<V>(fork_apply_kernel<V>, known, p, to.rows, from, to, f, dev, stream);
+    return apply_launch(fork_apply_kernel<V, P>, known, p, to.rows, from, to, f, dev, stream);
 }
-template <class V> int compact_apply(const Pools& p, const Books& from, const NewBooks& to, const Compact& c, const Device& dev, cudaStream_t stream) {
+template <class V, class P> int compact_apply(const P& p, const Books& from, const NewBooks& to, const Compact& c, const Device& dev, cudaStream_t stream) {
     static std::atomic<int> known[kMaxDevices];
-    return apply_launch<V>(compact_apply_kernel<V>, known, p, from.pages / 2, from, to, c, dev, stream);
+    return apply_launch(compact_apply_kernel<V, P>, known, p, from.pages / 2, from, to, c, dev, stream);
 }
 
 int check_states(const nereus_states_t* s) {
@@ -723,24 +905,47 @@ int check_states(const nereus_states_t* s) {
     return NEREUS_OK;
 }
 
-template <class V, int N> int reorder_launch(States& s, int64_t groups, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+template <class V, int N, class S> int reorder_launch(S& s, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
     constexpr int64_t kTile = (int64_t)kMoveThreads * sizeof(V);
+    const int64_t groups = ((int64_t)s.to_rows + s.group - 1) / s.group;
     s.tiles = (s.piece + kTile - 1) / kTile;
     s.items = s.tiles * s.outer * s.buffers;
     // a block sees to 8 tiles or so: few enough that the last ones do not keep the GPU waiting
-    int64_t blocks = (s.items + 7) / 8;
-    const int64_t most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / groups);
+    const int64_t blocks = (s.items + 7) / 8, most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / groups);
     s.blocks = (int32_t)std::min<int64_t>(std::min<int64_t>(blocks, most), 1 << 20);
-    reorder_kernel<V, N><<<(unsigned)(groups * s.blocks), kMoveThreads, 0, stream>>>(s, parent, length);
-    NEREUS_CUDA(cudaGetLastError());
-    return NEREUS_OK;
+    return launch(reorder_kernel<V, N, S>, dim3((unsigned)(groups * s.blocks)), kMoveThreads, 0, false, false, stream, s, parent, length);
 }
-template <class V> int reorder_by(States& s, int64_t groups, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+template <class V, class S> int reorder_by(S& s, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
     typedef typename std::conditional<sizeof(V) == 1, unsigned char, uint32_t>::type Small;       // 64 vectors of 16 bytes are no registers
-    return s.group <= 4    ? reorder_launch<V, 4>(s, groups, parent, length, stream)
-           : s.group <= 8  ? reorder_launch<V, 8>(s, groups, parent, length, stream)
-           : s.group <= 16 ? reorder_launch<V, 16>(s, groups, parent, length, stream)
-                           : reorder_launch<Small, 64>(s, groups, parent, length, stream);
+    return s.group <= 4    ? reorder_launch<V, 4>(s, parent, length, stream)
+           : s.group <= 8  ? reorder_launch<V, 8>(s, parent, length, stream)
+           : s.group <= 16 ? reorder_launch<V, 16>(s, parent, length, stream)
+                           : reorder_launch<Small, 64>(s, parent, length, stream);
+}
+template <int N>
+int reorder(const nereus_states_t& from, const nereus_states_t& to, int group, bool in_place, uint64_t bits, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+    States<N> s;
+    for (int i = 0; i < to.buffers; ++i) {
+        s.from[i] = (char*)from.buffer[i];
+        s.to[i] = (char*)to.buffer[i];
+    }
+    s.from_row = from.rows > 1 ? from.row_stride : 0;
+    s.to_row = to.rows > 1 ? to.row_stride : 0;
+    s.from_outer = to.outer > 1 ? from.outer_stride : 0;
+    s.to_outer = to.outer > 1 ? to.outer_stride : 0;
+    s.piece = to.tokens * to.token_bytes;
+    s.token_bytes = to.token_bytes;
+    s.tokens = to.tokens;
+    s.buffers = to.buffers;
+    s.from_rows = from.rows;
+    s.to_rows = to.rows;
+    s.outer = (int32_t)to.outer;
+    s.group = group;
+    s.in_place = in_place;
+    const int unit = unit_of(bits);
+    return unit == 16  ? reorder_by<uint4>(s, parent, length, stream)
+           : unit == 4 ? reorder_by<uint32_t>(s, parent, length, stream)
+                       : reorder_by<unsigned char>(s, parent, length, stream);
 }
 
 }  // namespace
@@ -759,14 +964,11 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
     if (to->rows && !parent) return NEREUS_ERR_ARG;
     const int64_t piece = to->tokens * to->token_bytes;
     if (!to->rows || !from->rows || !piece) return NEREUS_OK;
-    States s;
     uint64_t bits = (from->rows > 1 ? from->row_stride : 0) | (to->rows > 1 ? to->row_stride : 0) | (to->outer > 1 ? from->outer_stride | to->outer_stride : 0);
     bool same = true;
     for (int i = 0; i < to->buffers; ++i) {
-        s.from[i] = (char*)from->buffer[i];
-        s.to[i] = (char*)to->buffer[i];
-        bits |= (uintptr_t)s.from[i] | (uintptr_t)s.to[i];
-        same &= s.from[i] == s.to[i];
+        bits |= (uintptr_t)from->buffer[i] | (uintptr_t)to->buffer[i];
+        same &= from->buffer[i] == to->buffer[i];
     }
     if (same) {
         if (from->rows != to->rows || (to->rows > 1 && from->row_stride != to->row_stride) || (to->outer > 1 && from->outer_stride != to->outer_stride))
@@ -781,24 +983,8 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
         };
         if (!apart(side(*from), side(*to))) return NEREUS_ERR_ALIAS;
     }
-    s.from_row = from->rows > 1 ? from->row_stride : 0;
-    s.to_row = to->rows > 1 ? to->row_stride : 0;
-    s.from_outer = to->outer > 1 ? from->outer_stride : 0;
-    s.to_outer = to->outer > 1 ? to->outer_stride : 0;
-    s.piece = piece;
-    s.token_bytes = to->token_bytes;
-    s.tokens = to->tokens;
-    s.buffers = to->buffers;
-    s.from_rows = from->rows;
-    s.to_rows = to->rows;
-    s.outer = (int32_t)to->outer;
-    s.group = same ? beams : 8;
-    s.in_place = same;
-    const int64_t groups = ((int64_t)to->rows + s.group - 1) / s.group;
-    const int unit = unit_of(bits);
-    return unit == 16  ? reorder_by<uint4>(s, groups, parent, length, (cudaStream_t)cuda_stream)
-           : unit == 4 ? reorder_by<uint32_t>(s, groups, parent, length, (cudaStream_t)cuda_stream)
-                       : reorder_by<unsigned char>(s, groups, parent, length, (cudaStream_t)cuda_stream);
+    auto go = to->buffers <= kFew ? reorder<kFew> : reorder<NEREUS_MAX_BUFFERS>;
+    return go(*from, *to, same ? beams : 8, same, bits, parent, length, (cudaStream_t)cuda_stream);
 }
 
 int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int64_t n, const int32_t* src, const int32_t* dst, void* cuda_stream) {
@@ -817,11 +1003,7 @@ int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int6
     if (!n || !from->pools) return NEREUS_OK;
     Device dev;
     if (int rc = device_of(&dev)) return rc;
-    int unit;
-    const Pools p = pools_of(*from, *to, &unit);
-    return unit == 16  ? copy_launch<uint4>(p, n, src, dst, dev, (cudaStream_t)cuda_stream)
-           : unit == 4 ? copy_launch<uint32_t>(p, n, src, dst, dev, (cudaStream_t)cuda_stream)
-                       : copy_launch<unsigned char>(p, n, src, dst, dev, (cudaStream_t)cuda_stream);
+    return with_pools(*from, *to, [&](auto vector, auto& p) { return copy_launch<decltype(vector)>(p, n, src, dst, dev, (cudaStream_t)cuda_stream); });
 }
 
 int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to, const int32_t* parent,
@@ -840,21 +1022,31 @@ int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* fr
     if (int rc = device_of(&dev)) return rc;
     const Books    old = books_of(*from, pools->pages);
     const NewBooks now = new_books_of(*to);
-    const Fork     f = {parent, room_of, copies, status, page_size, room};
+    const Fork     f = {parent, room_of, copies, status, {1.0 / page_size, page_size}, room};
     static std::atomic<bool> opted[kMaxDevices];
     if (!opted[dev.id].load()) {
-        NEREUS_CUDA(cudaFuncSetAttribute(fork_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - 2048));
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - 2048));
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         opted[dev.id].store(true);
     }
-    cudaLaunchConfig_t  cfg;
-    cudaLaunchAttribute attr;
-    book_launch(&cfg, &attr, pools->pages + (int64_t)from->rows * from->columns, (int64_t)to->rows * 8 + (int64_t)from->rows * 12, (cudaStream_t)cuda_stream);
-    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, fork_kernel, old, now, f));
-    int unit;
-    const Pools p = pools_of(*pools, *pools, &unit);
-    return unit == 16  ? fork_apply<uint4>(p, old, now, f, dev, (cudaStream_t)cuda_stream)
-           : unit == 4 ? fork_apply<uint32_t>(p, old, now, f, dev, (cudaStream_t)cuda_stream)
-                       : fork_apply<unsigned char>(p, old, now, f, dev, (cudaStream_t)cuda_stream);
+    cudaStream_t   stream = (cudaStream_t)cuda_stream;
+    const unsigned blocks = cluster_of(pools->pages);
+    const int      groups = ((pools->pages + kGroup - 1) / kGroup + (int)blocks - 1) / (int)blocks;
+    const int64_t  smem = (int64_t)to->rows * (int64_t)(8 + sizeof(Lack)) + ((int64_t)from->rows + groups) * 4;
+    if (smem > dev.smem - 2048) return NEREUS_ERR_TOO_LARGE;
+    const int     refs_units = (pools->pages + kRefsUnit - 1) / kRefsUnit, chunks = (from->columns + kTableUnit - 1) / kTableUnit;
+    const int64_t units = refs_units + (int64_t)to->rows * chunks;
+    if (int rc = launch(fork_start_kernel, dim3((unsigned)std::min<int64_t>(units, 8 * dev.sms)), kStartThreads, 0, false, false, stream, old, now, f, refs_units, chunks))
+        return rc;
+    if (from->rows) {
+        // rows enough for beams to stand together, few enough for blocks on all SMs
+        const int columns = (from->columns + kCountThreads - 1) / kCountThreads, most = std::max(1, 8 * dev.sms / columns);
+        const int group = std::min(kMostRows, std::max(16, (from->rows + most - 1) / most));
+        if (int rc = launch(fork_count_kernel, dim3((unsigned)columns, (unsigned)((from->rows + group - 1) / group)), kCountThreads, 0, false, true, stream, old, now, f, group))
+            return rc;
+    }
+    if (int rc = launch(fork_assign_kernel, dim3(blocks), kBookThreads, smem, true, true, stream, old, now, f, groups)) return rc;
+    return with_pools(*pools, *pools, [&](auto vector, auto& p) { return fork_apply<decltype(vector)>(p, old, now, f, dev, stream); });
 }
 
 int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to, int64_t keep, int32_t* map,
@@ -873,15 +1065,13 @@ int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t*
     const Books    old = books_of(*from, pools->pages);
     const NewBooks now = new_books_of(*to);
     const Compact  c = {keep, map, moves, status};
-    cudaLaunchConfig_t  cfg;
-    cudaLaunchAttribute attr;
-    book_launch(&cfg, &attr, pools->pages, 0, (cudaStream_t)cuda_stream);
-    NEREUS_CUDA(cudaLaunchKernelEx(&cfg, compact_kernel, old, now, c));
-    int unit;
-    const Pools p = pools_of(*pools, *pools, &unit);
-    return unit == 16  ? compact_apply<uint4>(p, old, now, c, dev, (cudaStream_t)cuda_stream)
-           : unit == 4 ? compact_apply<uint32_t>(p, old, now, c, dev, (cudaStream_t)cuda_stream)
-                       : compact_apply<unsigned char>(p, old, now, c, dev, (cudaStream_t)cuda_stream);
+    static std::atomic<bool> opted[kMaxDevices];
+    if (!opted[dev.id].load()) {
+        NEREUS_CUDA(cudaFuncSetAttribute(compact_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        opted[dev.id].store(true);
+    }
+    if (int rc = launch(compact_kernel, dim3(cluster_of(pools->pages)), kBookThreads, 0, true, false, (cudaStream_t)cuda_stream, old, now, c)) return rc;
+    return with_pools(*pools, *pools, [&](auto vector, auto& p) { return compact_apply<decltype(vector)>(p, old, now, c, dev, (cudaStream_t)cuda_stream); });
 }
 
 }  // extern "C"

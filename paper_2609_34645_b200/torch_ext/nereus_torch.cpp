@@ -5,6 +5,8 @@
 
 #include <ATen/ATen.h>
 #include <ATen/core/grad_mode.h>
+#include <c10/core/StorageImpl.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -136,6 +138,17 @@ void written(PyObject* x) {
 
 at::Tensor empty(c10::IntArrayRef shape, at::ScalarType type, const View& like) {
     return at::empty(shape, at::TensorOptions().dtype(type).device(like.device));
+}
+// The same in half the time: a decode step's calls have several results of a few hundred bytes each.  On the current device, as
+// the caching allocator has it for the current stream.
+template <class T> at::Tensor fresh(c10::IntArrayRef shape) {
+    int64_t n = sizeof(T);
+    for (int64_t d : shape) n *= d;
+    auto*         allocator = c10::cuda::CUDACachingAllocator::get();
+    c10::Storage  storage(c10::make_intrusive<c10::StorageImpl>(c10::StorageImpl::use_byte_size_t(), (size_t)n, allocator->allocate((size_t)n), allocator, true));
+    auto          impl = c10::make_intrusive<c10::TensorImpl>(std::move(storage), c10::DispatchKeySet(c10::DispatchKey::CUDA), caffe2::TypeMeta::Make<T>());
+    impl->set_sizes_contiguous(shape);
+    return at::Tensor(std::move(impl));
 }
 void* stream_of(const View& v) { return (void*)c10::cuda::getCurrentCUDAStream(v.device.index()).stream(); }
 
@@ -335,11 +348,11 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     how.ended = (const int32_t*)arg_of(a[5], at::kInt, rows, -1, x, "ended");
     how.norm = (const float*)arg_of(a[6], at::kFloat, rows, -1, x, "norm");
     const int64_t requests = how.beams ? rows / how.beams : 0, room = std::max<int64_t>(how.k, 1);
-    at::Tensor score = empty({requests, room}, at::kFloat, x), parent = empty({requests, room}, at::kInt, x), token = empty({requests, room}, at::kInt, x);
+    at::Tensor score = fresh<float>({requests, room}), parent = fresh<int32_t>({requests, room}), token = fresh<int32_t>({requests, room});
     size_t bytes = 0;
     if (failed(nereus_beam_workspace(&x.v, &how, &bytes), "nereus_beam_select")) return nullptr;
-    const at::Tensor workspace = empty({(int64_t)bytes}, at::kByte, x);
-    if (failed(nereus_beam_select(&x.v, &how, workspace.data_ptr(), bytes, (float*)score.data_ptr(), (int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(),
+    const c10::DataPtr workspace = c10::cuda::CUDACachingAllocator::get()->allocate(bytes);
+    if (failed(nereus_beam_select(&x.v, &how, workspace.get(), bytes, (float*)score.data_ptr(), (int32_t*)parent.data_ptr(), (int32_t*)token.data_ptr(),
                                   stream_of(x)), "nereus_beam_select"))
         return nullptr;
     THPObjectPtr s(THPVariable_Wrap(std::move(score))), p(THPVariable_Wrap(std::move(parent))), t(THPVariable_Wrap(std::move(token)));
@@ -351,33 +364,42 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // The tensors of an argument that is one or a sequence of them, with one device, element size, shape and strides.
 struct Buffers {
-    std::vector<const at::Tensor*> t;
+    const at::Tensor* t[NEREUS_MAX_BUFFERS];
+    size_t       n = 0;
     THPObjectPtr hold;
     c10::Device  device{c10::DeviceType::CPU};
 };
 void buffers_of(PyObject* x, const char* what, Buffers* b) {
-    if (THPVariable_Check(x)) b->t.push_back(&THPVariable_Unpack(x));
+    if (THPVariable_Check(x)) b->t[b->n++] = &THPVariable_Unpack(x);
     else {
         b->hold = PySequence_Fast(x, "expected a tensor or a sequence of tensors");
         if (!b->hold) throw python_error();
-        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(b->hold.get()); ++i) b->t.push_back(&tensor_of(PySequence_Fast_GET_ITEM(b->hold.get(), i), what));
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(b->hold.get());
+        if (n > NEREUS_MAX_BUFFERS) throw Wrong{std::string(what) + ": at most " + std::to_string(NEREUS_MAX_BUFFERS) + " buffers"};
+        for (Py_ssize_t i = 0; i < n; ++i) b->t[b->n++] = &tensor_of(PySequence_Fast_GET_ITEM(b->hold.get(), i), what);
     }
-    if (b->t.size() > NEREUS_MAX_BUFFERS) throw Wrong{std::string(what) + ": at most " + std::to_string(NEREUS_MAX_BUFFERS) + " buffers"};
-    for (const at::Tensor* t : b->t) {
-        if (!t->is_cuda() || t->dim() < 1 || t->layout() != at::kStrided) throw Wrong{std::string(what) + ": expected tensors [rows, ...] on a CUDA device"};
-        const at::Tensor& u = *b->t[0];
-        if (t->device() != u.device() || t->element_size() != u.element_size() || t->sizes() != u.sizes() || (t->numel() && t->strides() != u.strides()))
+    if (!b->n) return;
+    const at::Tensor& u = *b->t[0];
+    if (!u.is_cuda() || u.dim() < 1) throw Wrong{std::string(what) + ": expected tensors [rows, ...] on a CUDA device"};
+    b->device = u.device();
+    const c10::IntArrayRef sizes = u.sizes(), strides = u.strides();
+    const size_t size = u.itemsize();
+    const bool   empty = u.numel() == 0;
+    for (size_t i = 1; i < b->n; ++i) {
+        const at::Tensor& t = *b->t[i];
+        if (t.device() != b->device || t.itemsize() != size || t.sizes() != sizes || (!empty && t.strides() != strides))
             throw Wrong{std::string(what) + ": the buffers differ in device, element size, shape or strides"};
     }
-    if (!b->t.empty()) b->device = b->t[0]->device();
 }
-// A tensor that a call writes.
-void writable(const at::Tensor& t, const char* what) {
-    if (t.requires_grad() && at::GradMode::is_enabled()) throw Wrong{std::string(what) + ": written without a gradient; detach it"};
+// Tensors that a call writes.
+void writable(const Buffers& b, const char* what) {
+    if (!at::GradMode::is_enabled()) return;
+    for (size_t i = 0; i < b.n; ++i)
+        if (b.t[i]->requires_grad()) throw Wrong{std::string(what) + ": written without a gradient; detach it"};
 }
 void written(const Buffers& b) {
-    for (const at::Tensor* t : b.t)
-        if (!t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+    for (size_t i = 0; i < b.n; ++i)
+        if (!b.t[i]->is_inference()) b.t[i]->unsafeGetTensorImpl()->bump_version();
 }
 // Whether dimensions from `first` on lie one after the other; *elements: their product.
 bool packed(const at::Tensor& t, int64_t first, int64_t* elements) {
@@ -392,20 +414,21 @@ bool packed(const at::Tensor& t, int64_t first, int64_t* elements) {
 
 // States [rows, ..., tokens, ...], tokens at `dim`.
 nereus_states_t states_of(const Buffers& b, int64_t dim, const char* what) {
-    if (b.t.empty()) throw Wrong{std::string(what) + ": expected a tensor at least"};
+    if (!b.n) throw Wrong{std::string(what) + ": expected a tensor at least"};
     const at::Tensor& t = *b.t[0];
     if (dim < 0) dim += t.dim();
     if (dim < 1 || (dim >= t.dim() && !(dim == 1 && t.dim() == 1))) throw Wrong{std::string(what) + ": dim is the tokens' axis, behind that of the rows"};
-    nereus_states_t s = {};
+    nereus_states_t s;
+    s.outer_stride = 0;
     const int64_t size = t.element_size();
-    s.buffers = (int32_t)b.t.size();
+    s.buffers = (int32_t)b.n;
     if (t.size(0) > INT32_MAX) throw Wrong{std::string(what) + ": too many rows"};
     s.rows = (int32_t)t.size(0);
     s.row_stride = t.stride(0) * size;
     s.outer = 1;
     s.tokens = 1;
     s.token_bytes = size;
-    for (size_t i = 0; i < b.t.size(); ++i) s.buffer[i] = b.t[i]->data_ptr();
+    for (size_t i = 0; i < b.n; ++i) s.buffer[i] = b.t[i]->data_ptr();
     if (t.numel() == 0) {
         s.tokens = 0;
         return s;
@@ -427,9 +450,10 @@ nereus_states_t states_of(const Buffers& b, int64_t dim, const char* what) {
 
 // Pools [pages, ...]; none: `pages` pages that hold nothing.
 nereus_pages_t pools_of(const Buffers& b, int64_t pages, const char* what) {
-    nereus_pages_t p = {};
-    p.pools = (int32_t)b.t.size();
-    if (b.t.empty()) {
+    nereus_pages_t p;
+    p.pools = (int32_t)b.n;
+    p.page_bytes = p.page_stride = 0;
+    if (!b.n) {
         p.pages = (int32_t)std::min<int64_t>(pages, INT32_MAX);
         return p;
     }
@@ -439,7 +463,7 @@ nereus_pages_t pools_of(const Buffers& b, int64_t pages, const char* what) {
     p.pages = (int32_t)std::min<int64_t>(t.size(0), INT32_MAX);
     p.page_bytes = page * t.element_size();
     p.page_stride = t.stride(0) * t.element_size();
-    for (size_t i = 0; i < b.t.size(); ++i) p.pool[i] = b.t[i]->data_ptr();
+    for (size_t i = 0; i < b.n; ++i) p.pool[i] = b.t[i]->data_ptr();
     return p;
 }
 
@@ -460,11 +484,10 @@ const at::Tensor& table_of(PyObject* o, nereus_page_table_t* b, const char* what
     b->table = (int32_t*)t.data_ptr();
     return t;
 }
-at::Tensor new_ints(c10::IntArrayRef shape, c10::Device device) { return at::empty(shape, at::TensorOptions().dtype(at::kInt).device(device)); }
 void* stream_on(c10::Device d) { return (void*)c10::cuda::getCurrentCUDAStream(d.index()).stream(); }
 // The pools' and the page table's device are one.
 void same_device(const Buffers& b, c10::Device d) {
-    if (!b.t.empty() && b.device != d) throw Wrong{"pools and page table are on different devices"};
+    if (b.n && b.device != d) throw Wrong{"pools and page table are on different devices"};
 }
 // Item i of the tuple `out`.
 PyObject* item_of(PyObject* out, Py_ssize_t i, Py_ssize_t n) {
@@ -484,9 +507,9 @@ PyObject* reorder(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t  dim = int_of(a[4]), beams = a[2] == Py_None ? 0 : int_of(a[2]);
     const nereus_states_t s = states_of(from, dim, "states"), d = states_of(dst, dim, in_place ? "states" : "out");
     if (dst.device != from.device) throw Wrong{"out: on another device than the states"};
-    if (dst.t[0]->element_size() != from.t[0]->element_size() || dst.t.size() != from.t.size() || dst.t[0]->sizes().slice(1) != from.t[0]->sizes().slice(1))
+    if (dst.t[0]->itemsize() != from.t[0]->itemsize() || dst.n != from.n || dst.t[0]->sizes().slice(1) != from.t[0]->sizes().slice(1))
         throw Wrong{"out: other buffers than the states but for their rows"};
-    for (const at::Tensor* t : dst.t) writable(*t, in_place ? "states" : "out");
+    writable(dst, in_place ? "states" : "out");
     const c10::cuda::OptionalCUDAGuard guard(from.device);
     const int32_t* parent = ints_of(a[1], d.rows, from.device, "parent");
     const int32_t* length = a[3] == Py_None ? nullptr : ints_of(a[3], s.rows, from.device, "length");
@@ -506,9 +529,9 @@ PyObject* copy(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const bool within = a[3] == Py_None;
     if (!within) buffers_of(a[3], "to", &to);
     const Buffers& dst = within ? from : to;
-    if (from.t.empty() || dst.t.empty()) throw Wrong{"pools: expected a pool at least"};
+    if (!from.n || !dst.n) throw Wrong{"pools: expected a pool at least"};
     if (dst.device != from.device) throw Wrong{"to: on another device than the pools"};
-    for (const at::Tensor* t : dst.t) writable(*t, within ? "pools" : "to");
+    writable(dst, within ? "pools" : "to");
     const c10::cuda::OptionalCUDAGuard guard(from.device);
     const nereus_pages_t p = pools_of(from, 0, "pools"), q = pools_of(dst, 0, "to");
     const int64_t pairs = tensor_of(a[1], "src").numel();
@@ -530,7 +553,7 @@ PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::Device device = table_of(a[1], &from, "table").device();
     same_device(pools, device);
     const c10::cuda::OptionalCUDAGuard guard(device);
-    for (const at::Tensor* t : pools.t) writable(*t, "pools");
+    writable(pools, "pools");
     from.length = ints_of(a[2], from.rows, device, "length");
     const nereus_pages_t p = pools_of(pools, tensor_of(a[3], "refs").numel(), "pools");
     from.refs = ints_of(a[3], p.pages, device, "refs");
@@ -542,9 +565,9 @@ PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
     else room = int_of(a[6]);
     THPObjectPtr table, length, refs;
     if (a[7] == Py_None) {
-        table = THPVariable_Wrap(new_ints({rows, from.columns}, device));
-        length = THPVariable_Wrap(new_ints({rows}, device));
-        refs = THPVariable_Wrap(new_ints({p.pages}, device));
+        table = THPVariable_Wrap(fresh<int32_t>({rows, from.columns}));
+        length = THPVariable_Wrap(fresh<int32_t>({rows}));
+        refs = THPVariable_Wrap(fresh<int32_t>({p.pages}));
     } else {
         PyObject* o[3] = {item_of(a[7], 0, 3), item_of(a[7], 1, 3), item_of(a[7], 2, 3)};
         for (PyObject* x : o) Py_INCREF(x);
@@ -553,7 +576,7 @@ PyObject* fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (table_of(table.get(), &to, "out").device() != device || to.rows != rows) throw Wrong{"out: the table has a row for each parent, on the same device"};
     to.length = ints_of(length.get(), rows, device, "out");
     to.refs = ints_of(refs.get(), p.pages, device, "out");
-    at::Tensor copies = new_ints({rows, 2}, device), status = new_ints({4}, device);
+    at::Tensor copies = fresh<int32_t>({rows, 2}), status = fresh<int32_t>({4});
     auto narrow = [](int64_t v) { return v < 0 || v > INT32_MAX ? -1 : (int)v; };            // out of range: refused by the library
     if (failed(nereus_cache_fork(&p, &from, &to, parent, narrow(page_size), narrow(room), room_of, (int32_t*)copies.data_ptr(), (int32_t*)status.data_ptr(),
                                  stream_on(device)), "nereus_cache_fork"))
@@ -576,15 +599,15 @@ PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const c10::Device device = table_of(a[1], &from, "table").device();
     same_device(pools, device);
     const c10::cuda::OptionalCUDAGuard guard(device);
-    for (const at::Tensor* t : pools.t) writable(*t, "pools");
+    writable(pools, "pools");
     const nereus_pages_t p = pools_of(pools, tensor_of(a[2], "refs").numel(), "pools");
     from.refs = ints_of(a[2], p.pages, device, "refs");
     int64_t keep = -1;
     if (a[3] != Py_None && (keep = int_of(a[3])) < 0) throw Wrong{"keep: a number of pages, or None"};
     THPObjectPtr table, refs;
     if (a[4] == Py_None) {
-        table = THPVariable_Wrap(new_ints({from.rows, from.columns}, device));
-        refs = THPVariable_Wrap(new_ints({p.pages}, device));
+        table = THPVariable_Wrap(fresh<int32_t>({from.rows, from.columns}));
+        refs = THPVariable_Wrap(fresh<int32_t>({p.pages}));
     } else {
         PyObject* o[2] = {item_of(a[4], 0, 2), item_of(a[4], 1, 2)};
         for (PyObject* x : o) Py_INCREF(x);
@@ -592,7 +615,7 @@ PyObject* compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (table_of(table.get(), &to, "out").device() != device) throw Wrong{"out: on another device"};
     to.refs = ints_of(refs.get(), p.pages, device, "out");
-    at::Tensor map = new_ints({p.pages}, device), moves = new_ints({p.pages / 2, 2}, device), status = new_ints({4}, device);
+    at::Tensor map = fresh<int32_t>({p.pages}), moves = fresh<int32_t>({p.pages / 2, 2}), status = fresh<int32_t>({4});
     if (failed(nereus_cache_compact(&p, &from, &to, keep, (int32_t*)map.data_ptr(), (int32_t*)moves.data_ptr(), (int32_t*)status.data_ptr(), stream_on(device)),
                "nereus_cache_compact"))
         return nullptr;
