@@ -629,7 +629,7 @@ typedef struct {
     int32_t* refs;                 /* [pages] */
 } nereus_page_table_t;
 #define NEREUS_CACHE_MAX_ROWS 8192
-#define NEREUS_CACHE_MAX_PAGES 16777216
+#define NEREUS_CACHE_MAX_PAGES 8388608
 /* Every row i of `to` becomes a fork of row parent[i] of `from` (device, [to->rows]; outside [0, from->rows): an empty row).
  * This is a beam search's step (parents from nereus_beam_select), a fork (a parent named twice), the freeing of a sequence (a
  * parent named by no row: its pages lose a holder, and those that nothing else holds are free) and the making of room, at

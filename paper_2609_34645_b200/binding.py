@@ -32,7 +32,7 @@ STATIC_MAX_RECTS = 4096
 DEV_OK, DEV_BOUNDS, DEV_TIMEOUT = 0, 1, 2
 VOCAB_MAX_TP, TOP_MAX_K, BIAS_MAX, HISTORY_MAX = 64, 256, 1023, 1048576
 FORWARD_KL, REVERSE_KL, JENSEN = 0, 1, 2
-BEAM_MAX, BEAM_MAX_K, MAX_BUFFERS, CACHE_MAX_ROWS, CACHE_MAX_PAGES = 64, 128, 256, 8192, 16777216
+BEAM_MAX, BEAM_MAX_K, MAX_BUFFERS, CACHE_MAX_ROWS, CACHE_MAX_PAGES = 64, 128, 256, 8192, 8388608
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2609_34645_b200.build` "

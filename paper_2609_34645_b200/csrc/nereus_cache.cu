@@ -56,26 +56,30 @@ __device__ __forceinline__ void copy_pages(const P& p, int64_t n, const int32_t*
     int       pool = (int)(warp - pair * per_pair) / p.chunks, chunk = (int)(warp - pair * per_pair) % p.chunks;
     const int64_t by_pair = warps / per_pair;
     const int by_pool = (int)(warps - by_pair * per_pair) / p.chunks, by_chunk = (int)(warps - by_pair * per_pair) % p.chunks;
+    int s = 0, d = 0;                                  // of the next tile
+    if (pair < n) { s = __ldcg(src + pair * step); d = __ldcg(dst + pair * step); }
 #pragma unroll 1
     while (pair < n) {
-        const int s = __ldcg(src + pair * step), d = __ldcg(dst + pair * step);
-        if ((unsigned)s < (unsigned)p.from_pages && (unsigned)d < (unsigned)p.to_pages) {
-            const int64_t at = (int64_t)chunk * (32 * kTileVecs) + lane;
-            const V* a = reinterpret_cast<const V*>(p.from[pool] + s * p.from_stride) + at;
-            V*       b = reinterpret_cast<V*>(p.to[pool] + d * p.to_stride) + at;
-            V v[kTileVecs];
-#pragma unroll
-            for (int i = 0; i < kTileVecs; ++i)
-                if (at + 32 * i < vecs) v[i] = __ldcg(a + 32 * i);
-#pragma unroll
-            for (int i = 0; i < kTileVecs; ++i)
-                if (at + 32 * i < vecs) __stcg(b + 32 * i, v[i]);
-        }
+        const int     from_page = s, to_page = d;
+        const int64_t at = (int64_t)chunk * (32 * kTileVecs) + lane;
+        const char*   from = p.from[pool];
+        char*         to = p.to[pool];
         chunk += by_chunk;
         if (chunk >= p.chunks) { chunk -= p.chunks; ++pool; }
         pool += by_pool;
         if (pool >= p.pools) { pool -= p.pools; ++pair; }
         pair += by_pair;
+        if (pair < n) { s = __ldcg(src + pair * step); d = __ldcg(dst + pair * step); }
+        if ((unsigned)from_page >= (unsigned)p.from_pages || (unsigned)to_page >= (unsigned)p.to_pages) continue;
+        const V* a = reinterpret_cast<const V*>(from + from_page * p.from_stride) + at;
+        V*       b = reinterpret_cast<V*>(to + to_page * p.to_stride) + at;
+        V v[kTileVecs];
+#pragma unroll
+        for (int i = 0; i < kTileVecs; ++i)
+            if (at + 32 * i < vecs) v[i] = __ldcs(a + 32 * i);
+#pragma unroll
+        for (int i = 0; i < kTileVecs; ++i)
+            if (at + 32 * i < vecs) __stcs(b + 32 * i, v[i]);
     }
 }
 
@@ -122,24 +126,28 @@ __device__ __forceinline__ Wide warp_scan(Wide v) {                  // inclusiv
     }
     return v;
 }
-// Sum over the warps before this one of what their lanes' v is in all, and the block's total.  scratch: kBookWarps + 1.
-__device__ __forceinline__ Wide warps_before(Wide of_warp, Wide* scratch, Wide* total) {
+// Sum over the warps before this one of what their lanes' v is in all, and the block's total.  scratch: kWarps + 1.
+template <int kWarps = kBookWarps> __device__ __forceinline__ Wide warps_before(Wide of_warp, Wide* scratch, Wide* total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
     if (lane == 0) scratch[warp] = of_warp;
     __syncthreads();
     if (warp == 0) {
-        const Wide mine = scratch[lane], upto = warp_scan(mine);
+        const Wide mine = lane < kWarps ? scratch[lane] : 0, upto = warp_scan(mine);
         __syncwarp();
-        scratch[lane] = upto - mine;
-        if (lane == 31) scratch[kBookWarps] = upto;
+        if (lane < kWarps) scratch[lane] = upto - mine;
+        if (lane == kWarps - 1) scratch[kWarps] = upto;
     }
     __syncthreads();
-    *total = scratch[kBookWarps];
+    *total = scratch[kWarps];
     return scratch[warp];
 }
 // What the blocks before this one have, and all of them, of one number each.  Ends in no barrier: `totals` is written once.
 __device__ __forceinline__ Wide blocks_before(Wide mine, Wide* totals, int rank, int blocks, Wide* total) {
+    if (blocks == 1) {
+        *total = mine;
+        return 0;
+    }
     if (threadIdx.x < blocks) peer_store(peer_address(totals + rank, threadIdx.x), mine);
     cluster_sync();
     Wide before = 0, all = 0;
@@ -190,6 +198,9 @@ __device__ __forceinline__ int64_t quotient(int64_t x, const Divisor& by) {
     return r < 0 ? q - 1 : r >= by.d ? q + 1 : q;
 }
 
+// x / d for 0 <= x < 2^31
+__device__ __forceinline__ int64_t quotient64(int x, int64_t d) { return d > x ? 0 : (int64_t)((uint32_t)x / (uint32_t)d); }
+
 struct Books {
     const int32_t *table, *length, *refs;
     int64_t  stride;
@@ -236,8 +247,8 @@ __device__ __forceinline__ Heir heir_of(const Books& b, const Fork& f, int row) 
 __device__ __forceinline__ bool is_page(int e, int pages) { return (unsigned)e < (unsigned)pages; }
 
 constexpr int kStartThreads = 256;
-constexpr int kPerThread    = 4;              // entries, or vectors of four counts
-constexpr int kRefsUnit     = kStartThreads * kPerThread * 4;
+constexpr int kPerThread    = 8;              // entries of a thread
+constexpr int kRefsUnit     = kStartThreads * kPerThread * 2;
 constexpr int kTableUnit    = kStartThreads * kPerThread;
 
 // Counts and plain entries, dealt out in units to all blocks: HBM is what bounds them where they are many.
@@ -250,11 +261,11 @@ __global__ void __launch_bounds__(kStartThreads) fork_start_kernel(const Books f
         if (u < refs_units) {
             const int lo = (int)u * kRefsUnit, hi = (int)min((int64_t)lo + kRefsUnit, (int64_t)from.pages);
             if (aligned && hi - lo == kRefsUnit) {
-                int4 v[kPerThread];
+                int4 v[kPerThread / 2];
 #pragma unroll
-                for (int j = 0; j < kPerThread; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from.refs + lo) + tid + j * kStartThreads);
+                for (int j = 0; j < kPerThread / 2; ++j) v[j] = __ldcg(reinterpret_cast<const int4*>(from.refs + lo) + tid + j * kStartThreads);
 #pragma unroll
-                for (int j = 0; j < kPerThread; ++j) __stcg(reinterpret_cast<int4*>(to.refs + lo) + tid + j * kStartThreads, v[j]);
+                for (int j = 0; j < kPerThread / 2; ++j) __stcg(reinterpret_cast<int4*>(to.refs + lo) + tid + j * kStartThreads, v[j]);
             } else {
                 for (int p = lo + tid; p < hi; p += kStartThreads) to.refs[p] = from.refs[p];
             }
@@ -341,35 +352,51 @@ __device__ __forceinline__ int64_t pages_in(Wide need) { return (int64_t)(need &
 struct Lack {
     int parent, full, until;
 };
+constexpr int64_t kWholeEntries = 8192;       // of both tables: 4 x 256 x 2 in the time of the chain, 128 x 129 x 2 26 us instead of 20
+constexpr int kSmallThreads = 256;
+constexpr int kWindow = 2048;                 // free pages of a block that are handed out at a time
+constexpr int kStaticBooks = 10240;           // shared memory that is not dynamic, with room to spare
 constexpr int kSelf = 8;                      // columns that a row's own thread looks through; a warp takes rows with more
 
 // One cluster.  Of every new row: what it needs, then the sum of that over the rows before; what it lacks.  first: of every old
 // row, the lowest new row that names it.  free_of: free pages of the block's groups, then their sum over the groups before.
-__global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Books from, const NewBooks to, const Fork f, int groups_of_block) {
+// kWhole: small books, whose launches would cost more than one block's work: it does what start and count do, too.
+template <bool kWhole>
+__global__ void __launch_bounds__(kWhole ? kSmallThreads : kBookThreads, 1) fork_assign_kernel(const Books from, const NewBooks to, const Fork f, int groups_of_block) {
+    constexpr int kThreads = kWhole ? kSmallThreads : kBookThreads, kWarps = kThreads / 32;
     extern __shared__ __align__(16) unsigned char dynamic[];
-    __shared__ Wide scratch[kBookWarps + 1], totals[kMaxCluster];
+    __shared__ Wide scratch[kWarps + 1], totals[kMaxCluster];
     __shared__ Wide lacking_columns;
+    __shared__ int  window[kWindow];
     Wide* need    = reinterpret_cast<Wide*>(dynamic);
     Lack* lack    = reinterpret_cast<Lack*>(need + to.rows);
     int*  first   = reinterpret_cast<int*>(lack + to.rows);
     int*  free_of = first + from.rows;
+    int*  kids    = free_of + groups_of_block;         // kWhole: how many rows name an old row
     const int  tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, blocks = gridDim.x, rank = blockIdx.x;
     const bool aligned = ((uintptr_t)to.refs & 15) == 0;
 
     let_next_come();
     if (tid == 0) lacking_columns = 0;
     cluster_arrive();                                  // this block has begun: the others may write to it
-    for (int r = tid; r < from.rows; r += kBookThreads) first[r] = INT_MAX;
+    for (int r = tid; r < from.rows; r += kThreads) {
+        first[r] = INT_MAX;
+        if (kWhole) kids[r] = 0;
+    }
+    if (kWhole)
+        for (int p = tid; p < from.pages; p += kThreads) to.refs[p] = from.refs[p];
     __syncthreads();
-    for (int i = tid; i < to.rows; i += kBookThreads) {
+    for (int i = tid; i < to.rows; i += kThreads) {
         const int p = f.parent[i];
-        if ((unsigned)p < (unsigned)from.rows) atomicMin(&first[p], i);
+        if ((unsigned)p >= (unsigned)from.rows) continue;
+        atomicMin(&first[p], i);
+        if (kWhole) atomicAdd(&kids[p], 1);
     }
     __syncthreads();
     // what the rows need: every block goes through all of them
     bool long_rows = false;
 #pragma unroll 1
-    for (int i = tid; i < to.rows; i += kBookThreads) {
+    for (int i = tid; i < to.rows; i += kThreads) {
         const Heir h = heir_of(from, f, i);
         const int  until = (int)min(h.until, (int64_t)from.columns);
         Wide       w = 0;
@@ -390,12 +417,41 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Book
         }
         need[i] = w;
         lack[i] = {h.parent, h.full, until};
+        if (kWhole) {
+            to.length[i] = h.n;
+            f.copies[2 * i] = f.copies[2 * i + 1] = -1;
+        }
     }
     const bool some_long = __syncthreads_or(long_rows);
     cluster_wait();
+    if (kWhole) {
+        // a warp for a row: what its holders change, then the plain entries
+#pragma unroll 1
+        for (int r = warp; r < from.rows; r += kWarps) {
+            const int k = kids[r], full = k == 1 ? 0 : (int)quotient(tokens_of(from, f, r), f.page_size), end = k == 1 ? 0 : k ? full : from.columns;
+#pragma unroll 4
+            for (int c = lane; c < end; c += 32) {
+                const int e = from.table[r * from.stride + c];
+                if (is_page(e, from.pages)) atomicAdd(&to.refs[e], c < full ? k - 1 : -1);
+            }
+        }
+#pragma unroll 1
+        for (int i = warp; i < to.rows; i += kWarps) {
+            const Lack     l = lack[i];
+            const int      end = l.parent < 0 ? 0 : first[l.parent] == i ? from.columns : l.full;
+            const int32_t* row = from.table + max(l.parent, 0) * from.stride;
+            int32_t* const out = to.table + i * to.stride;
+#pragma unroll 4
+            for (int c = lane; c < from.columns; c += 32) {
+                const int e = c < end ? row[c] : -1;
+                if (!(c >= l.full && c < l.until && !is_page(e, from.pages))) out[c] = e;
+            }
+        }
+        __syncthreads();
+    }
     if (some_long) {                                   // in all blocks: their rows are shared out
         cluster_sync();                                // nobody marks them any more
-        for (int i = rank * kBookWarps + warp; i < to.rows; i += blocks * kBookWarps) {
+        for (int i = rank * kWarps + warp; i < to.rows; i += blocks * kWarps) {
             if (need[i] != ~(Wide)0) continue;
             const Lack     l = lack[i];
             const int32_t* row = from.table + l.parent * from.stride;
@@ -411,11 +467,11 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Book
     // need: sum over the rows before
     Wide needed = 0;
     {
-        const int per = (to.rows + kBookThreads - 1) / kBookThreads, lo = min(tid * per, to.rows), hi = min(lo + per, to.rows);
+        const int per = (to.rows + kThreads - 1) / kThreads, lo = min(tid * per, to.rows), hi = min(lo + per, to.rows);
         Wide sum = 0;
         for (int i = lo; i < hi; ++i) sum += need[i];
         const Wide upto = warp_scan(sum);
-        Wide at = warps_before(__shfl_sync(0xffffffffu, upto, 31), scratch, &needed) + upto - sum;
+        Wide at = warps_before<kWarps>(__shfl_sync(0xffffffffu, upto, 31), scratch, &needed) + upto - sum;
         for (int i = lo; i < hi; ++i) { const Wide w = need[i]; need[i] = at; at += w; }
     }
     const int64_t fresh = pages_in(needed);
@@ -424,37 +480,54 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Book
 
     // free pages: of every group, in all, and before the block
     const int first_group = rank * groups_of_block, n_groups = min(groups_of_block, max(0, (from.pages + kGroup - 1) / kGroup - first_group));
-#pragma unroll 8
-    for (int g = warp; g < n_groups; g += kBookWarps) {
-        const int p = (first_group + g) * kGroup;
-        const int n = __reduce_add_sync(0xffffffffu, 4 - live_of(counts_of(to.refs, p, from.pages, aligned, 1)));
-        if (lane == 0) free_of[g] = n;
+#pragma unroll 1
+    for (int g0 = warp; g0 < n_groups; g0 += 8 * kWarps) {
+        int4 v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = counts_of(to.refs, (first_group + min(g0 + j * kWarps, n_groups - 1)) * kGroup, from.pages, aligned, 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int n = __reduce_add_sync(0xffffffffu, 4 - live_of(v[j]));
+            if (lane == 0 && g0 + j * kWarps < n_groups) free_of[g0 + j * kWarps] = n;
+        }
     }
     __syncthreads();
     Wide of_block, free_pages;
     {
-        const int per = (n_groups + kBookThreads - 1) / kBookThreads, lo = min(tid * per, n_groups), hi = min(lo + per, n_groups);
+        const int per = (n_groups + kThreads - 1) / kThreads, lo = min(tid * per, n_groups), hi = min(lo + per, n_groups);
         int sum = 0;
         for (int g = lo; g < hi; ++g) sum += free_of[g];
         const int upto = (int)warp_scan((Wide)sum);
-        int at = (int)warps_before((Wide)__shfl_sync(0xffffffffu, upto, 31), scratch, &of_block) + upto - sum;
+        int at = (int)warps_before<kWarps>((Wide)__shfl_sync(0xffffffffu, upto, 31), scratch, &of_block) + upto - sum;
         for (int g = lo; g < hi; ++g) { const int n = free_of[g]; free_of[g] = at; at += n; }
     }
     const int64_t before = (int64_t)blocks_before(of_block, totals, rank, blocks, &free_pages);
     const int64_t missing = max((int64_t)0, fresh - (int64_t)free_pages) + (int64_t)lacking_columns;
     if (missing == 0) {
+        // the block's free pages by rank, a window of them at a time, then a thread for each that is handed out
+        const int mine = (int)max((int64_t)0, min((int64_t)of_block, fresh - before));
 #pragma unroll 1
-        for (int g = warp; g < n_groups && before + free_of[g] < fresh; g += kBookWarps) {
-            const int      p = (first_group + g) * kGroup;
-            const int4     v = counts_of(to.refs, p, from.pages, aligned, 1);
-            const unsigned below = (1u << lane) - 1;
-            int64_t        j = before + free_of[g];
+        for (int base = 0; base < mine; base += kWindow) {
+#pragma unroll 1
+            for (int g = warp; g < n_groups && free_of[g] < min(base + kWindow, mine); g += kWarps) {
+                if ((g + 1 < n_groups ? free_of[g + 1] : (int)of_block) <= base) continue;
+                const int      p = (first_group + g) * kGroup;
+                const int4     v = counts_of(to.refs, p, from.pages, aligned, 1);
+                const unsigned below = (1u << lane) - 1;
+                int            j = free_of[g] - base;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) j += __popc(__ballot_sync(0xffffffffu, (e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) <= 0) & below);
+                for (int e = 0; e < 4; ++e) j += __popc(__ballot_sync(0xffffffffu, (e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) <= 0) & below);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if ((e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) > 0) continue;
+                    if ((unsigned)j < (unsigned)kWindow) window[j] = p + 4 * lane + e;
+                    ++j;
+                }
+            }
+            __syncthreads();
 #pragma unroll 1
-            for (int e = 0; e < 4; ++e) {
-                if ((e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) > 0) continue;
-                if (j >= fresh) break;
+            for (int x = tid; x < min(kWindow, mine - base); x += kThreads) {
+                const int64_t j = before + base + x;
                 int lo = 0, hi = to.rows;              // the last row whose sum is not above j
                 while (hi - lo > 1) {
                     const int mid = (lo + hi) / 2;
@@ -463,7 +536,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Book
                 }
                 const Wide here = need[lo], next = lo + 1 < to.rows ? need[lo + 1] : needed;
                 const Lack l = lack[lo];
-                const int  page = p + 4 * lane + e;
+                const int  page = window[x];
                 int        k = (int)(j - pages_in(here)), c = l.full + k;
                 const int32_t* row = from.table + l.parent * from.stride;
                 if (pages_in(next - here) != l.until - l.full)
@@ -476,19 +549,19 @@ __global__ void __launch_bounds__(kBookThreads, 1) fork_assign_kernel(const Book
                     f.copies[2 * at] = row[c];
                     f.copies[2 * at + 1] = page;
                 }
-                ++j;
             }
+            __syncthreads();
         }
     } else {
         const int lo = first_group * kGroup, hi = (int)min((int64_t)from.pages, (int64_t)(first_group + n_groups) * kGroup);
-        for (int p = lo + tid; p < hi; p += kBookThreads) to.refs[p] = from.refs[p];
+        for (int p = lo + tid; p < hi; p += kThreads) to.refs[p] = from.refs[p];
     }
     int64_t left = (int64_t)free_pages - fresh;
     if (missing && rank == 0) {
         int n = 0;
-        for (int p = tid; p < from.pages; p += kBookThreads) n += from.refs[p] <= 0;
+        for (int p = tid; p < from.pages; p += kThreads) n += from.refs[p] <= 0;
         Wide all;
-        warps_before(__reduce_add_sync(0xffffffffu, n), scratch, &all);
+        warps_before<kWarps>(__reduce_add_sync(0xffffffffu, n), scratch, &all);
         left = (int64_t)all;
     }
     if (rank == 0 && tid == 0) {
@@ -522,7 +595,7 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const Books fr
     __shared__ Wide scratch[kBookWarps + 1], totals[2][kMaxCluster];
     const int  tid = threadIdx.x, lane = tid & 31, blocks = gridDim.x, rank = blockIdx.x;
     const Part part = part_of(from.pages, rank, blocks);
-    const bool aligned = ((uintptr_t)from.refs & 15) == 0;
+    const bool aligned = ((uintptr_t)from.refs & 15) == 0, stores = (((uintptr_t)to.refs | (uintptr_t)c.map) & 15) == 0;
     let_next_come();
     cluster_arrive();                                  // this block has begun: the others may write to it
     const int of_part = count_live(from.refs, part, aligned);
@@ -557,21 +630,23 @@ __global__ void __launch_bounds__(kBookThreads, 1) compact_kernel(const Books fr
             goes += __popc(who);
             hole += __popc(where);
         }
+        int now[4], counts[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int page = at + e;
-            if (page >= part.hi) break;
-            const bool is = r[e] > 0, up = page >= keep;
-            if (is && up) {
-                c.moves[2 * g++] = page;
-                to.refs[page] = 0;
-            } else if (is || up || h >= moves) {
-                c.map[page] = is ? page : -1;
-                to.refs[page] = max(r[e], 0);
-                h += !is && !up;
-            } else {                                   // its count comes with the page
-                c.map[page] = -1;
-                c.moves[2 * h++ + 1] = page;
+            const int  page = at + e;
+            const bool in = page < part.hi, is = r[e] > 0, up = page >= keep;
+            now[e] = is && !up ? page : -1;            // pages that go and holes that take them come right below
+            counts[e] = is && !up ? r[e] : 0;
+            if (in && is && up) c.moves[2 * g++] = page;
+            if (in && !is && !up && h++ < moves) c.moves[2 * h - 1] = page;
+        }
+        if (stores && at + 4 <= part.hi) {
+            *reinterpret_cast<int4*>(c.map + at) = make_int4(now[0], now[1], now[2], now[3]);
+            *reinterpret_cast<int4*>(to.refs + at) = make_int4(counts[0], counts[1], counts[2], counts[3]);
+        } else {
+            for (int e = 0; e < 4 && at + e < part.hi; ++e) {
+                c.map[at + e] = e == 0 ? now[0] : e == 1 ? now[1] : e == 2 ? now[2] : now[3];
+                to.refs[at + e] = e == 0 ? counts[0] : e == 1 ? counts[1] : e == 2 ? counts[2] : counts[3];
             }
         }
     }
@@ -612,7 +687,6 @@ template <int N> struct States {
     int64_t piece;                                         // bytes of a piece: tokens * token_bytes
     int64_t token_bytes, tokens;
     int32_t buffers, from_rows, to_rows, outer, group, in_place;
-    int64_t tiles, items;                                  // tiles of a piece; tiles of a group's rows in all buffers
     int32_t blocks;                                        // of a group
 };
 constexpr int kMoveThreads = 128;
@@ -640,17 +714,36 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_cons
         }
     }
     __syncthreads();
-    const int     n = n_moves;
-    const int64_t most = (int64_t)most_bytes;
-    if (!n) return;
     constexpr int kTile = kMoveThreads * (int)sizeof(V);
-    for (int64_t item = block; item < s.items; item += s.blocks) {
-        const int64_t piece = item / s.tiles, tile = item - piece * s.tiles, at = tile * kTile + tid * (int)sizeof(V);
-        if (at >= most) continue;
-        const int   b = (int)(piece / s.outer);
-        const int64_t o = piece - (int64_t)b * s.outer;
+    // few moves: a thread takes several places at a time, one tile apart
+    const int     n_rows = n_moves, places = n_rows ? N / n_rows : 0, n = n_rows * places;
+    const int64_t most = (int64_t)most_bytes, step = (int64_t)places * kTile;
+    if (!n) return;
+    for (int i = n_rows + tid; i < n; i += kMoveThreads) {
+        const Move    m = moves[i % n_rows];
+        const int64_t by = (int64_t)(i / n_rows) * kTile;
+        moves[i] = {m.from + by, m.to + by, m.bytes - by};
+    }
+    __syncthreads();
+    // this block's items: (buffer, piece, stretch of `places` tiles), and how far it goes on
+    const int64_t  tiles = quotient(s.piece + step - 1, Divisor{1.0 / (double)step, (int)step});
+    const uint32_t outer = (uint32_t)s.outer;
+    const int64_t  line = quotient64(block, tiles), by_line = quotient64(s.blocks, tiles);
+    int64_t        tile = block - line * tiles, b = (uint32_t)line / outer;
+    uint32_t       o = (uint32_t)line % outer;
+    const int64_t  by_tile = s.blocks - by_line * tiles, by_b = (uint32_t)by_line / outer;
+    const uint32_t by_o = (uint32_t)by_line % outer;
+#pragma unroll 1
+    while (b < s.buffers) {
+        const int64_t at = tile * step + tid * (int)sizeof(V);
         const char* from = s.from[b] + o * s.from_outer + at;
         char*       to = s.to[b] + o * s.to_outer + at;
+        tile += by_tile;
+        if (tile >= tiles) { tile -= tiles; ++o; }
+        o += by_o;
+        if (o >= outer) { o -= outer; ++b; }
+        b += by_b;
+        if (at >= most) continue;
         V v[N];
         bool edge = false;                                 // the last bytes of a row that are no whole vector
 #pragma unroll
@@ -864,12 +957,16 @@ unsigned cluster_of(int pages) { return pages <= 32768 ? 1 : kMaxCluster; }
 Books    books_of(const nereus_page_table_t& t, int pages) { return {t.table, t.length, t.refs, t.stride, t.rows, t.columns, pages}; }
 NewBooks new_books_of(const nereus_page_table_t& t) { return {t.table, t.length, t.refs, t.stride, t.rows}; }
 
+// Blocks that copy `all` blocks' tiles.
+int64_t copy_blocks(int64_t all, int64_t resident, int64_t each) {
+    return std::min<int64_t>(std::max(std::min(all, resident), (all + each - 1) / each), INT_MAX);
+}
 template <class V, class P> int copy_launch(const P& p, int64_t n, const int32_t* src, const int32_t* dst, const Device& dev, cudaStream_t stream) {
     static std::atomic<int> known[kMaxDevices];
     int per_sm;
     if (int rc = resident(copy_kernel<V, P>, kCopyThreads, known, dev, &per_sm)) return rc;
     const int64_t warps = kCopyThreads / 32, tiles = n * p.pools * p.chunks;
-    const int64_t grid = std::min<int64_t>((tiles + warps - 1) / warps, (int64_t)per_sm * dev.sms);
+    const int64_t grid = copy_blocks((tiles + warps - 1) / warps, (int64_t)per_sm * dev.sms, 2);
     return launch(copy_kernel<V, P>, dim3((unsigned)grid), kCopyThreads, 0, false, false, stream, p, n, src, dst);
 }
 // The last launch of a fork or compaction: `most_pairs` page copies at most.
@@ -879,7 +976,7 @@ int apply_launch(void (*kernel)(P, Books, NewBooks, Work), std::atomic<int>* kno
     int per_sm;
     if (int rc = resident(kernel, kCopyThreads, known, dev, &per_sm)) return rc;
     const int64_t warps = kCopyThreads / 32, tiles = p.page_bytes ? most_pairs * p.pools * p.chunks : 0;
-    const int64_t grid = std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>((tiles + warps - 1) / warps, to.rows), (int64_t)per_sm * dev.sms));
+    const int64_t grid = std::max(copy_blocks((tiles + warps - 1) / warps, (int64_t)per_sm * dev.sms, 4), std::min<int64_t>(std::max(to.rows, 1), (int64_t)per_sm * dev.sms));
     return launch(kernel, dim3((unsigned)grid), kCopyThreads, 0, false, true, stream, p, from, to, w);
 }
 template <class V, class P> int fork_apply(const P& p, const Books& from, const NewBooks& to, const Fork& f, const Device& dev, cudaStream_t stream) {
@@ -905,25 +1002,25 @@ int check_states(const nereus_states_t* s) {
     return NEREUS_OK;
 }
 
-template <class V, int N, class S> int reorder_launch(S& s, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+template <class V, int N, class S> int reorder_launch(S& s, const int32_t* parent, const int32_t* length, const Device& dev, cudaStream_t stream) {
     constexpr int64_t kTile = (int64_t)kMoveThreads * sizeof(V);
-    const int64_t groups = ((int64_t)s.to_rows + s.group - 1) / s.group;
-    s.tiles = (s.piece + kTile - 1) / kTile;
-    s.items = s.tiles * s.outer * s.buffers;
-    // a block sees to 8 tiles or so: few enough that the last ones do not keep the GPU waiting
-    const int64_t blocks = (s.items + 7) / 8, most = std::max<int64_t>(1, (((int64_t)1 << 31) - 1) / groups);
-    s.blocks = (int32_t)std::min<int64_t>(std::min<int64_t>(blocks, most), 1 << 20);
+    const int64_t groups = ((int64_t)s.to_rows + s.group - 1) / s.group, items = (s.piece + kTile - 1) / kTile * s.outer * s.buffers;
+    // Blocks that the GPU holds at a time (6 on an SM), as long as each then has 16 tiles at most: few enough that the last ones do
+    // not keep it waiting.
+    const int64_t each = std::max<int64_t>(1, std::min<int64_t>(16, (items * groups + 6 * dev.sms - 1) / (6 * dev.sms)));
+    s.blocks = (int32_t)std::min<int64_t>(std::min<int64_t>((items + each - 1) / each, (((int64_t)1 << 31) - 1) / groups), 1 << 20);
     return launch(reorder_kernel<V, N, S>, dim3((unsigned)(groups * s.blocks)), kMoveThreads, 0, false, false, stream, s, parent, length);
 }
-template <class V, class S> int reorder_by(S& s, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+template <class V, class S> int reorder_by(S& s, const int32_t* parent, const int32_t* length, const Device& dev, cudaStream_t stream) {
     typedef typename std::conditional<sizeof(V) == 1, unsigned char, uint32_t>::type Small;       // 64 vectors of 16 bytes are no registers
-    return s.group <= 4    ? reorder_launch<V, 4>(s, parent, length, stream)
-           : s.group <= 8  ? reorder_launch<V, 8>(s, parent, length, stream)
-           : s.group <= 16 ? reorder_launch<V, 16>(s, parent, length, stream)
-                           : reorder_launch<Small, 64>(s, parent, length, stream);
+    return s.group <= 4    ? reorder_launch<V, 4>(s, parent, length, dev, stream)
+           : s.group <= 8  ? reorder_launch<V, 8>(s, parent, length, dev, stream)
+           : s.group <= 16 ? reorder_launch<V, 16>(s, parent, length, dev, stream)
+                           : reorder_launch<Small, 64>(s, parent, length, dev, stream);
 }
 template <int N>
-int reorder(const nereus_states_t& from, const nereus_states_t& to, int group, bool in_place, uint64_t bits, const int32_t* parent, const int32_t* length, cudaStream_t stream) {
+int reorder(const nereus_states_t& from, const nereus_states_t& to, int group, bool in_place, uint64_t bits, const int32_t* parent, const int32_t* length, const Device& dev,
+            cudaStream_t stream) {
     States<N> s;
     for (int i = 0; i < to.buffers; ++i) {
         s.from[i] = (char*)from.buffer[i];
@@ -943,9 +1040,9 @@ int reorder(const nereus_states_t& from, const nereus_states_t& to, int group, b
     s.group = group;
     s.in_place = in_place;
     const int unit = unit_of(bits);
-    return unit == 16  ? reorder_by<uint4>(s, parent, length, stream)
-           : unit == 4 ? reorder_by<uint32_t>(s, parent, length, stream)
-                       : reorder_by<unsigned char>(s, parent, length, stream);
+    return unit == 16  ? reorder_by<uint4>(s, parent, length, dev, stream)
+           : unit == 4 ? reorder_by<uint32_t>(s, parent, length, dev, stream)
+                       : reorder_by<unsigned char>(s, parent, length, dev, stream);
 }
 
 }  // namespace
@@ -983,8 +1080,10 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
         };
         if (!apart(side(*from), side(*to))) return NEREUS_ERR_ALIAS;
     }
+    Device dev;
+    if (int rc = device_of(&dev)) return rc;
     auto go = to->buffers <= kFew ? reorder<kFew> : reorder<NEREUS_MAX_BUFFERS>;
-    return go(*from, *to, same ? beams : 8, same, bits, parent, length, (cudaStream_t)cuda_stream);
+    return go(*from, *to, same ? beams : 8, same, bits, parent, length, dev, (cudaStream_t)cuda_stream);
 }
 
 int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int64_t n, const int32_t* src, const int32_t* dst, void* cuda_stream) {
@@ -1025,15 +1124,21 @@ int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* fr
     const Fork     f = {parent, room_of, copies, status, {1.0 / page_size, page_size}, room};
     static std::atomic<bool> opted[kMaxDevices];
     if (!opted[dev.id].load()) {
-        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - 2048));
-        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - kStaticBooks));
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, dev.smem - kStaticBooks));
+        NEREUS_CUDA(cudaFuncSetAttribute(fork_assign_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
         opted[dev.id].store(true);
     }
     cudaStream_t   stream = (cudaStream_t)cuda_stream;
     const unsigned blocks = cluster_of(pools->pages);
     const int      groups = ((pools->pages + kGroup - 1) / kGroup + (int)blocks - 1) / (int)blocks;
     const int64_t  smem = (int64_t)to->rows * (int64_t)(8 + sizeof(Lack)) + ((int64_t)from->rows + groups) * 4;
-    if (smem > dev.smem - 2048) return NEREUS_ERR_TOO_LARGE;
+    if (smem > dev.smem - kStaticBooks) return NEREUS_ERR_TOO_LARGE;
+    auto apply = [&](auto vector, auto& p) { return fork_apply<decltype(vector)>(p, old, now, f, dev, stream); };
+    if (blocks == 1 && ((int64_t)from->rows + to->rows) * from->columns <= kWholeEntries && smem + from->rows * 4 <= dev.smem - kStaticBooks) {
+        if (int rc = launch(fork_assign_kernel<true>, dim3(1), kSmallThreads, smem + from->rows * 4, false, false, stream, old, now, f, groups)) return rc;
+        return with_pools(*pools, *pools, apply);
+    }
     const int     refs_units = (pools->pages + kRefsUnit - 1) / kRefsUnit, chunks = (from->columns + kTableUnit - 1) / kTableUnit;
     const int64_t units = refs_units + (int64_t)to->rows * chunks;
     if (int rc = launch(fork_start_kernel, dim3((unsigned)std::min<int64_t>(units, 8 * dev.sms)), kStartThreads, 0, false, false, stream, old, now, f, refs_units, chunks))
@@ -1045,8 +1150,8 @@ int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* fr
         if (int rc = launch(fork_count_kernel, dim3((unsigned)columns, (unsigned)((from->rows + group - 1) / group)), kCountThreads, 0, false, true, stream, old, now, f, group))
             return rc;
     }
-    if (int rc = launch(fork_assign_kernel, dim3(blocks), kBookThreads, smem, true, true, stream, old, now, f, groups)) return rc;
-    return with_pools(*pools, *pools, [&](auto vector, auto& p) { return fork_apply<decltype(vector)>(p, old, now, f, dev, stream); });
+    if (int rc = launch(fork_assign_kernel<false>, dim3(blocks), kBookThreads, smem, true, true, stream, old, now, f, groups)) return rc;
+    return with_pools(*pools, *pools, apply);
 }
 
 int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t* from, const nereus_page_table_t* to, int64_t keep, int32_t* map,
