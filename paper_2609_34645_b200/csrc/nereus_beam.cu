@@ -3,9 +3,9 @@
 //
 // Every logit is read once; the floor is HBM bandwidth, with one exponential an element next (16 a clock and SM, which is what
 // bf16 from HBM asks three quarters of).  Two launches:
-//   * sum: the rows are cut into parts of a few layers, dealt out evenly to as many blocks as the GPU holds, whatever requests
-//     they belong to.  Of its part of a row a block leaves every warp's sum of exponentials, and of every thread the largest
-//     element that it has seen, in 16 bits rounded up: its note;
+//   * sum: the layers of all rows are dealt out evenly to as many blocks as the GPU holds, whatever requests they belong to, each
+//     block's one after the other.  Of what it has of a row a block leaves the sum of exponentials, and of every part (a layer,
+//     or a few) and thread the largest element, in 16 bits rounded up: a note;
 //   * pick: a block for a request puts the sums together to log-sum-exps, so that elements of different rows can be compared.
 //     The notes are worth something then: of 8 sets of them the j-th largest bounds the k-th best hypothesis from below,
 //     whatever the order of the rows.  Only vectors whose note reaches the bound are read again; what is found in them, a
@@ -21,12 +21,14 @@ namespace nereus {
 namespace {
 
 constexpr int kTH       = kThreads;               // of a summing block
-constexpr int kRoom     = 4 * kTH;                // vectors of a layer here: four a thread, for one pass of the loop's overhead
-constexpr int kStages   = 2;                      // layers on their way to a block, 16 KiB each
+constexpr int kV        = 4;                      // vectors of a layer here, a thread's
+constexpr int kRoom     = kV * kTH;
+constexpr int kHalf     = kRoom / 2;              // a Layer is described as two vectors of so many threads
+constexpr int kStages   = 2;                      // layers on their way to a block
+constexpr int kBlocks   = 4;                      // on an SM
 constexpr int kItems    = 128;                    // layers in its table at a time
 constexpr int kListed   = 4096;                   // rows that it lists
-constexpr int kPart     = 16;                     // layers of a part, where that leaves no more parts than
-constexpr int kParts    = 256;                    // parts of a request's rows, at most
+constexpr int kParts    = 128;                    // parts of a request's rows, at most: a part is a layer, or several
 constexpr int kPick     = 1024;                   // threads of a picking block
 constexpr int kPickWarps = kPick / 32;
 constexpr int kSets     = 8;
@@ -34,25 +36,27 @@ constexpr int kFound    = 1024;                   // hypotheses that its list ho
 constexpr int kNoted    = 1024;                   // notes, or groups of 8, that reach the bound
 typedef unsigned long long Key;
 
-// Sums of exponentials are kept as (K, sum of 2^(x c - K)) with a whole number K near the largest x c, so that sums of different
-// threads go together without another rounding; a thread adds up 4 vectors in 32 bits and these in 64.  c = log2(e) has 24
-// bits, kLog2eLow is the rest: it is put right for the largest element of a row at the end, and an element at a distance of d
-// from that is off by 2e-8 d of itself.  K stays within +-2^22: a row whose largest element lies beyond (a mask's lowest value
-// in all of it, say) is summed again, by differences from it.
-constexpr float  kLargestK = 0x1p22f;
+// Sums of exponentials are kept as (K, sum of 2^(x c - K)) with a whole number K, so that sums go together without another
+// rounding.  A thread adds up a layer's 4 vectors in 32 bits, with K next to the largest x c among them, and layers in 64: how
+// the layers are dealt out shows in the 53rd bit of a sum at most.  c = log2(e) has 24 bits, kLog2eLow is the rest: it is put
+// right for the largest element of a row at the end, and an element at a distance of d from that is off by 2e-8 d of itself.
+// K stays within +-2^21: a row whose largest element lies beyond (a mask's lowest value in all of it, say) is summed again, by
+// differences from it.
+constexpr float  kLargestK = 0x1p21f;
 constexpr double kLog2eLow = 1.4426950408889634 - (double)kLog2e, kLn2 = 0.69314718055994531;
 struct Sum {
-    double sum;
-    float  k, top;                                // and the largest element
+    double  sum;
+    int32_t k;
+    float   top;                                  // the largest element
 };
+__device__ __forceinline__ double power_of_two(int k) {          // k not above 0
+    return __hiloint2double(max(1023 + k, 0) << 20, 0);
+}
 // What a block leaves of a part.
 struct Record {
     Sum      sum;
     uint16_t notes[kTH];
 };
-__device__ __forceinline__ double power_of_two(float k) {        // k whole and not above 0
-    return !(k >= -1000.f) ? 0.0 : __longlong_as_double((long long)(1023 + (int)k) << 52);
-}
 template <int kLanes> __device__ __forceinline__ double sum_of_lanes(double x) {
 #pragma unroll
     for (int o = kLanes / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
@@ -90,22 +94,22 @@ __device__ __forceinline__ bool offers(const Select& s, int64_t row, int vocab, 
 template <class T> __device__ __forceinline__ Layer layer_at(const LogitsCut& in, const Deal& deal, const Select& s, int64_t row, int l) {
     if (l >= deal.layers) return {nullptr, nullptr, 0, 0, 0, 0};
     const int shard = quotient(l, deal.per_shard, s.per_shard_1);
-    return layer_in<T, T, 2 * kTH>(in, LogitsCut(), row, shard, (l - shard * deal.per_shard) * kPerLayer<T, 2 * kTH>);
+    return layer_in<T, T, kHalf>(in, LogitsCut(), row, shard, (l - shard * deal.per_shard) * kPerLayer<T, kHalf>);
 }
 
 // ---- sums ----------------------------------------------------------------------------------------------------
 
 // Starts the copies of this thread's vectors of layer l, one commit group; nothing but the group past the last layer.
-template <class T> __device__ __forceinline__ void load_four(const Layer* table, uint4* to, int l, int n) {
+template <class T> __device__ __forceinline__ void load_layer_of(const Layer* table, uint4* to, int l, int n) {
     if (l < n) {
         const Layer& L = table[l];
         const char*  from = L.in + threadIdx.x * 16;
-        if (L.hi - L.lo == kPerLayer<T, 2 * kTH>) {
+        if (L.hi - L.lo == kPerLayer<T, kHalf>) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
+            for (int v = 0; v < kV; ++v) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
         } else {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
+            for (int v = 0; v < kV; ++v) {
                 const int at = ((int)threadIdx.x + v * kTH) * kPerVec<T>;
                 if (at >= L.lo && at + kPerVec<T> <= L.hi) copy_async(smem_address(to + v * kTH), from + v * kTH * 16);
                 else to[v * kTH] = at + kPerVec<T> <= L.lo || at >= L.hi ? Vec<T>::none() : edge_vector<T>(L, threadIdx.x + v * kTH);
@@ -116,9 +120,10 @@ template <class T> __device__ __forceinline__ void load_four(const Layer* table,
 }
 
 template <class T>
-__global__ void __launch_bounds__(kTH, 4) beam_sum_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
+__global__ void __launch_bounds__(kTH, kBlocks) beam_sum_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
     __shared__ __align__(16) uint4 ring[kStages * kRoom];
     __shared__ Layer    table[kItems];
+    __shared__ uint32_t record_of[kItems];
     __shared__ uint16_t listed[kListed];
     __shared__ Sum      of_warps[2][kWarps];
     __shared__ int      of_warp[kWarps];
@@ -156,74 +161,88 @@ __global__ void __launch_bounds__(kTH, 4) beam_sum_kernel(const __grid_constant_
         __syncthreads();
     }
 
-    typename Vec<T>::Max top = Vec<T>::lowest();
-    float  k = -kLargestK;
+    constexpr int kNone = -(1 << 21);
+    float  top = -INFINITY, row_top = -INFINITY;          // of the part, and of what the block has of the row
+    int    k = kNone;
     double sum = 0.0;
-    int    i = 0, odd = 0;
+    int    odd = 0;
     uint4* const  mine = ring + tid;
     const Pair    c = pair(kLog2e, kLog2e);
+    // the block's units, one after the other: parts of a few layers, all of a row and then the next row's
     const int     log_part = __ffs(s.of_part) - 1;
-    const int64_t units = (int64_t)n * s.parts;
-    // the block's x-th unit: a row, and a part of it
+    const int64_t units = (int64_t)n * s.parts, lo = units * blockIdx.x / gridDim.x, hi = units * (blockIdx.x + 1) / gridDim.x;
     auto unit_of = [&](int64_t x, int* part) {
-        const uint32_t u = (uint32_t)(blockIdx.x + x * gridDim.x);
-        *part = (int)(u / (uint32_t)n);
-        const int r = (int)(u - (uint32_t)*part * (uint32_t)n);
-        return list ? (int)listed[r] : r;
+        const uint32_t u = (uint32_t)(lo + x), q = u / (uint32_t)s.parts;
+        *part = (int)(u - q * (uint32_t)s.parts);
+        return list ? (int)listed[q] : (int)q;
     };
-    const int64_t layers = blockIdx.x < units ? ((units - blockIdx.x + gridDim.x - 1) / gridDim.x) << log_part : 0;
+    const int64_t layers = (hi - lo) << log_part;
     for (int64_t first = 0; first < layers; first += kItems) {
         const int items = (int)min((int64_t)kItems, layers - first);
         __syncthreads();
         if (tid < items) {
             int       part;
-            const int row = unit_of((first + tid) >> log_part, &part);
-            table[tid] = list || read(row) ? layer_at<T>(in, deal, s, row, (part << log_part) + ((int)(first + tid) & (s.of_part - 1)))
-                                           : Layer{nullptr, nullptr, 0, 0, 0, 0};
+            const int row = unit_of((first + tid) >> log_part, &part), in_part = (int)(first + tid) & (s.of_part - 1);
+            const bool last = in_part + 1 == s.of_part;
+            table[tid] = list || read(row) ? layer_at<T>(in, deal, s, row, (part << log_part) + in_part) : Layer{nullptr, nullptr, 0, 0, 0, 0};
+            // where its part's record is; whether the part ends with it, and what the block has of the row
+            record_of[tid] = ((uint32_t)row * (uint32_t)s.parts + (uint32_t)part) << 2 | (last ? 2u : 0u) |
+                             (last && (part + 1 == s.parts || first + tid + 1 == layers) ? 1u : 0u);
         }
         __syncthreads();
 #pragma unroll 1
-        for (int l = 0; l < kStages; ++l) load_four<T>(table, mine + l * kRoom, l, items);
+        for (int l = 0; l < kStages; ++l) load_layer_of<T>(table, mine + l * kRoom, l, items);
         int slot = 0;
 #pragma unroll 1
         for (int item = 0; item < items; ++item) {
             copy_wait<kStages - 1>();
             uint4* const here = mine + slot * kRoom;
-            const uint4 a = here[0], b = here[kTH], d = here[2 * kTH], e = here[3 * kTH];
-            load_four<T>(table, here, item + kStages, items);
+            uint4 x[kV];
+#pragma unroll
+            for (int j = 0; j < kV; ++j) x[j] = here[j * kTH];
+            load_layer_of<T>(table, here, item + kStages, items);
             slot = slot + 1 == kStages ? 0 : slot + 1;
-            top = Vec<T>::join(top, Vec<T>::join(Vec<T>::join(Vec<T>::max(a), Vec<T>::max(b)), Vec<T>::join(Vec<T>::max(d), Vec<T>::max(e))));
-            const float v = Vec<T>::value(top);
-            // an element ahead of K carries the roundings of the distance: 2^4 at most
-            if (v * kLog2e > k + 4.f) {
-                const float to = fminf(fmaxf(rintf(v * kLog2e), -kLargestK), kLargestK);
-                sum *= power_of_two(k - to);
-                k = to;
-            }
-            const Pair   minus = pair(-k, -k);
-            const float2 h = halves(add2(add2(exp_sum<T, false>(a, c, c, minus), exp_sum<T, false>(b, c, c, minus)),
-                                         add2(exp_sum<T, false>(d, c, c, minus), exp_sum<T, false>(e, c, c, minus))));
-            sum += (double)(h.x + h.y);
-            if (++i == s.of_part) {
-                int           part;
-                const int     row = unit_of((first + item) >> log_part, &part);
-                Record* const to = s.records + (int64_t)row * s.parts + part;
-                to->notes[tid] = note_of(v);
-                const float all = warp_max(k), most = warp_max(v);
+            typename Vec<T>::Max m = Vec<T>::max(x[0]);
+#pragma unroll
+            for (int j = 1; j < kV; ++j) m = Vec<T>::join(m, Vec<T>::max(x[j]));
+            const float v = Vec<T>::value(m);              // NaN is passed over
+            top = fmaxf(top, v);
+            // rint by the addition of a number whose last place is 1
+            constexpr float kWhole = 0x1.8p23f;
+            const float  t = fminf(fmaxf(v * kLog2e, -kLargestK), kLargestK) + kWhole, of_k = t - kWhole;
+            const int    now = __float_as_int(t) - __float_as_int(kWhole), next = max(k, now);
+            const Pair   minus = pair(-of_k, -of_k);
+            Pair of_layer = exp_sum<T, false>(x[0], c, c, minus);
+#pragma unroll
+            for (int j = 1; j < kV; ++j) of_layer = add2(of_layer, exp_sum<T, false>(x[j], c, c, minus));
+            const float2 h = halves(of_layer);
+            sum = fma((double)(h.x + h.y), power_of_two(now - next), sum * power_of_two(k - next));
+            k = next;
+            const uint32_t what = record_of[item];
+            if (what & 2u) {
+                Record* const to = s.records + (what >> 2);
+                to->notes[tid] = note_of(top);
+                row_top = fmaxf(row_top, top);
+                top = -INFINITY;
+                if (!(what & 1u)) {
+                    if (tid == 0) to->sum = {0.0, kNone, -INFINITY};
+                    continue;
+                }
+                const int   all = __reduce_max_sync(0xffffffffu, k);
+                const float most = warp_max(row_top);
                 const Sum   mine = {sum_of_lanes<32>(sum * power_of_two(k - all)), all, most};
                 if (lane == 0) of_warps[odd][warp] = mine;
                 __syncthreads();
-                if (warp == 0) {                           // two sets of sums: the others are at the next part's meanwhile
-                    Sum u = lane < kWarps ? of_warps[odd][lane] : Sum{0.0, -kLargestK, -INFINITY};
-                    const float of_all = warp_max(u.k);
+                if (warp == 0) {                           // two sets of sums: the others are at the next row's meanwhile
+                    Sum u = lane < kWarps ? of_warps[odd][lane] : Sum{0.0, kNone, -INFINITY};
+                    const int of_all = __reduce_max_sync(0xffffffffu, u.k);
                     u = {sum_of_lanes<kWarps>(u.sum * power_of_two(u.k - of_all)), of_all, warp_max(u.top)};
                     if (lane == 0) to->sum = u;
                 }
                 odd ^= 1;
-                top = Vec<T>::lowest();
-                k = -kLargestK;
+                row_top = -INFINITY;
+                k = kNone;
                 sum = 0.0;
-                i = 0;
             }
         }
     }
@@ -320,17 +339,18 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             if (lane == 0) r.off_1 = NAN;
             continue;
         }
-        float  k = -INFINITY, top = -INFINITY;
+        int    k = -(1 << 21);
+        float  top = -INFINITY;
         double sum = 0.0;
 #pragma unroll 1
         for (int e = lane; e < s.parts; e += 32) {
-            const Sum   u = records[b * s.parts + e].sum;
-            const float to = fmaxf(k, u.k);
+            const Sum u = records[b * s.parts + e].sum;
+            const int to = max(k, u.k);
             sum = fma(u.sum, power_of_two(u.k - to), sum * power_of_two(k - to));
             k = to;
             top = fmaxf(top, u.top);
         }
-        const float all = warp_max(k);
+        const int all = __reduce_max_sync(0xffffffffu, k);
         top = warp_max(top);
         sum = sum_of_lanes<32>(sum * power_of_two(k - all));
         double lse = kLn2 * ((double)all + log2_of(sum) + (double)top * kLog2eLow);
@@ -440,13 +460,12 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     const int log_part = __ffs(s.of_part) - 1, noted_all = max(n_noted, n_groups);
     if (noted_all <= kNoted) {
         // every vector of a note on a thread of its own
-        const int log_vecs = log_part + 2, vecs = n_noted << log_vecs;
+        const int of_note = kV << log_part, vecs = n_noted * of_note;
 #pragma unroll 1
         for (int j = tid; j < vecs; j += kPick) {
-            const uint32_t which = noted[j >> log_vecs];
-            const int      row_part = which / kTH, b = quotient(row_part, s.parts, parts_1);
-            const int      l = ((row_part - b * s.parts) << log_part) + (j >> 2 & (s.of_part - 1));
-            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + (j & 3) * kTH, push);
+            const int which = (int)noted[j / of_note], row_part = which / kTH, b = quotient(row_part, s.parts, parts_1), v = j % of_note;
+            const int l = ((row_part - b * s.parts) << log_part) + v / kV;
+            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + v % kV * kTH, push);
         }
     }
     each_ended(push);
@@ -604,8 +623,8 @@ int check_beams(const nereus_logits_t* in, const nereus_beams_t* how) {
 }
 
 // How the rows are cut, and where the workspace's arrays are; returns its size.
-size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, int sms, Deal* deal, Select* s, char* workspace) {
-    *deal = spread_of(in, 2 * kTH, 0, 0, INT32_MAX);
+size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, Deal* deal, Select* s, char* workspace) {
+    *deal = spread_of(in, kHalf, 0, 0, INT32_MAX);
     s->beams = how.beams;
     s->k = how.k;
     s->settle = how.settle;
@@ -613,14 +632,9 @@ size_t lay_out(const nereus_logits_t& in, const nereus_beams_t& how, int sms, De
     s->score = how.score;
     s->ended = how.ended;
     s->norm = how.norm;
-    // The layers of a part that the busiest block is done with first, when the GPU holds 4 on an SM and a part's end takes as
-    // long as half a layer; and no more parts of a request than one block puts together in a microsecond.
-    auto parts = [&](int of_part) { return (int64_t)(deal->layers + of_part - 1) / of_part; };
-    auto takes = [&](int of_part) { return (double)((parts(of_part) * in.rows + 4 * sms - 1) / (4 * sms)) * (of_part + 0.5); };
+    // no more parts of a request than one block looks through in a microsecond
     s->of_part = 1;
-    for (int m = 2; m <= kPart; m *= 2)
-        if (takes(m) < takes(s->of_part)) s->of_part = m;
-    while (parts(s->of_part) * how.beams > kParts) s->of_part *= 2;
+    while ((int64_t)((deal->layers + s->of_part - 1) / s->of_part) * how.beams > kParts) s->of_part *= 2;
     s->parts = (deal->layers + s->of_part - 1) / s->of_part;
     s->per_shard_1 = 1.f / (float)deal->per_shard;
     s->records = reinterpret_cast<Record*>(workspace);
@@ -635,9 +649,7 @@ template <class T> int beam_launch(const LogitsCut& cut, const Deal& deal, const
         opted[dev.id].store(true);
     }
     const int64_t units = (int64_t)s.rows * s.parts;
-    // an odd number of blocks: rows that are not read (all but a request's first on its first step) come to all alike
-    const int64_t most = 4 * dev.sms - 1;
-    beam_sum_kernel<T><<<(unsigned)std::min<int64_t>(units, most), kTH, 0, stream>>>(cut, deal, s);
+    beam_sum_kernel<T><<<(unsigned)std::min<int64_t>(units, kBlocks * dev.sms), kTH, 0, stream>>>(cut, deal, s);
     NEREUS_CUDA(cudaGetLastError());
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(s.rows / s.beams));
@@ -666,7 +678,7 @@ int nereus_beam_workspace(const nereus_logits_t* in, const nereus_beams_t* how, 
     if (int rc = device_of(&dev)) return rc;
     Deal   deal;
     Select s;
-    *bytes = lay_out(*in, *how, dev.sms, &deal, &s, nullptr);
+    *bytes = lay_out(*in, *how, &deal, &s, nullptr);
     return NEREUS_OK;
 }
 
@@ -682,7 +694,7 @@ int nereus_beam_select(const nereus_logits_t* in, const nereus_beams_t* how, voi
     if (int rc = device_of(&dev)) return rc;
     Deal   deal;
     Select s;
-    if (lay_out(*in, *how, dev.sms, &deal, &s, (char*)workspace) > workspace_bytes) return NEREUS_ERR_TOO_SMALL;
+    if (lay_out(*in, *how, &deal, &s, (char*)workspace) > workspace_bytes) return NEREUS_ERR_TOO_SMALL;
     s.out_score = out_score;
     s.out_parent = out_parent;
     s.out_token = out_token;
