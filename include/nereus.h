@@ -642,7 +642,7 @@ typedef struct {
  *   - the fresh pages are the lowest ids that are free once the rows' old holders are gone and the shared pages' new ones
  *     counted, in the order of (row, column); length becomes n.  An empty row has length 0 and no pages (-1).
  * `to` shares no byte with `from` (a caller keeps two sets of books and swaps them); its columns are the same.
- * status (device, [4]): pages free after the call; pages missing; page copies made; 0.  Where pages are missing, or columns of
+ * status (device, [4]): pages free after the call; pages missing (2^31 - 1 at most); page copies made; 0.  Where pages are missing, or columns of
  * the table (each counts as one), nothing is forked: length and refs of `to` become those of `from`, and so does the table (rows of
  * `to` past from->rows are empty).
  * copies (device, [to->rows, 2]): source and destination of every page copy, in the order of the rows, then -1.

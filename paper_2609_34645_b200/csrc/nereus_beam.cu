@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         const float up = largest_note(records, g);
         // a note of a fp32 was rounded up: the next below it is not above the element
         const float x = sizeof(T) == 2 ? up : note_below((uint16_t)(__float_as_uint(up) >> 16));
-        const float w = fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse;
+        // (a quotient beyond fp32 counts as the largest number, which it is not below)
+        const float w = fminf(fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse, 3.402823466e38f);
         if (up > -INFINITY) most = fmaxf(most, fmaf(-1e-6f, fabsf(w), w));
     }
     peak[tid] = key_of(most);

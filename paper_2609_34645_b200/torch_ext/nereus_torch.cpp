@@ -476,7 +476,7 @@ int32_t* ints_of(PyObject* o, int64_t size, c10::Device device, const char* what
 }
 const at::Tensor& table_of(PyObject* o, nereus_page_table_t* b, const char* what) {
     const at::Tensor& t = tensor_of(o, what);
-    if (t.scalar_type() != at::kInt || !t.is_cuda() || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1) || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)
+    if (t.scalar_type() != at::kInt || !t.is_cuda() || t.dim() != 2 || (t.numel() && t.size(1) > 1 && t.stride(1) != 1) || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX)
         throw Wrong{std::string(what) + ": expected int32 [rows, columns], contiguous along the columns, on a CUDA device"};
     b->rows = (int32_t)t.size(0);
     b->columns = (int32_t)t.size(1);

@@ -58,7 +58,7 @@ def fork(table, length, refs, parent, page_size, room, rows):
         old[:keep] = table[:keep]
         lengths = np.zeros(rows, np.int64)
         lengths[:keep] = length[:keep]
-        return old, lengths, refs.astype(np.int64), copies, np.array([(refs <= 0).sum(), missing, 0, 0])
+        return old, lengths, refs.astype(np.int64), copies, np.array([(refs <= 0).sum(), min(missing, 2 ** 31 - 1), 0, 0])        # int32
     done = 0
     for (i, c, source), q in zip(fresh, free):
         new[i, c] = q

@@ -248,3 +248,39 @@ def test_no_rows_and_refusals():
             L.beam_select(x, wrong.pop("score", score), 4, beams=2, **wrong)
     with pytest.raises(ValueError):
         L.beam_select(x.half(), score, 4, beams=2)
+
+
+@pytest.mark.parametrize("vocab, rows, beams", [(128256, 5200, 4), (700, 9000, 3)])
+def test_more_rows_than_are_listed(vocab, rows, beams):
+    """More rows than the summing blocks list, and more layers to a block than its table holds; most of them are not read."""
+    gen = torch.Generator("cuda").manual_seed(3)
+    x = torch.randn(rows, vocab, generator=gen, device="cuda").mul_(2).bfloat16()
+    score = -torch.rand(rows, generator=gen, device="cuda")
+    score[torch.rand(rows, generator=gen, device="cuda") < 0.3] = -INF
+    k = 2 * beams
+    value, parent, token = L.beam_select(x, score, k, beams=beams)
+    for a in range(0, rows, 60 * beams):
+        b = min(rows, a + 60 * beams)
+        total = x[a:b].double().log_softmax(1) + score[a:b].double()[:, None]
+        want = total.view(-1, beams * vocab).topk(k, dim=1).values
+        g = slice(a // beams, b // beams)
+        live = want > -INF
+        assert torch.equal(live, parent[g] >= 0)
+        tol = U.sum_error(vocab) + U.EPS * want.abs()
+        assert ((value[g].double() - want).abs()[live] <= tol[live]).all()
+        at = (parent[g].clamp(min=a).long() - a) * vocab + token[g].clamp(min=0).long()
+        got = total.view(-1)[at]
+        assert ((got - want).abs()[live] < NEAR).all()                      # what was picked is worth what it has to be
+        assert all(len(set(r)) == len(r) for r in at[live.all(1)].tolist())
+        assert (value[g][~live] == -INF).all()
+
+
+def test_norms_at_the_ends_of_their_range():
+    """Quotients beyond fp32 and next to 0: the order is theirs in 64 bits."""
+    rng = seed("norms")
+    x = logits(rng, 8, 3000, "fp32")
+    view = U.View(8, 3000, 1, "fp32", "columns").put(torch.as_tensor(x))
+    for norm in (1e-44, 1e-39, 1e-30, 1e30, 3e38):
+        n = np.full(8, norm, np.float32)
+        check(view, x, rng.uniform(-9, 0, 8).astype(np.float32), 8, 4, norm=n)
+        check(view, x, rng.uniform(20, 40, 8).astype(np.float32), 8, 4, norm=n)

@@ -230,6 +230,20 @@ def test_fork_without_enough_pages_changes_nothing(pages):
     check_fork(rng, table, length, refs, np.array([0, 0, 2, 2, 1, 1, -1]), 16, 16 * 5)
 
 
+def test_fork_of_no_rows_and_into_none():
+    """Everything is freed; rows come out of nothing; single columns; room that is refused for one row is refused for all."""
+    rng = seed("none")
+    table, length, refs = books(rng, 12, 6, 8, 30, 3)
+    want = check_fork(rng, table, length, refs, np.array([], np.int64), 8, 4)
+    assert want[4][0] == len(refs)
+    empty = (np.zeros((0, 6), np.int64), np.zeros(0, np.int64), np.zeros(40, np.int64))
+    check_fork(rng, *empty, np.array([0, -1, 5]), 8, 9)
+    check_fork(rng, *empty, np.array([], np.int64), 8, 9)
+    check_fork(rng, np.array([[3]]), np.array([0]), np.array([0, 0, 0, 1]), np.array([0, 0, 0]), 2, 2)
+    check_fork(rng, table, length, refs, np.arange(12), 8, 0, None, np.where(np.arange(12) == 7, 1 << 30, 0))
+    check_fork(rng, table, length, refs, np.arange(12), 8, (1 << 31) - 1)
+
+
 def test_fork_hands_released_pages_out_again():
     """Every page in use, one sequence freed, another forked onto its pages."""
     rng = seed("again")
