@@ -90,8 +90,8 @@ def check(view, x, score, k, beams, ended=None, norm=None, settle=False):
                 assert 0 < gap < NEAR, (g, j, a, b, gap)
         assert len(set(here[here >= 0])) == (here >= 0).sum()
         expect = np.where(here >= 0, total[g][np.maximum(here, 0)], -INF)
-        off = np.abs(value[g][order].astype(np.float64) - expect)[here >= 0]
-        assert (off <= tol + U.EPS * np.abs(expect[here >= 0])).all(), (g, off.max())
+        off = np.abs(value[g][order].astype(np.float64)[here >= 0] - expect[here >= 0])
+        assert (off <= tol + U.EPS * np.abs(expect[here >= 0])).all(), (g, off)
         assert (value[g][order][here < 0] == -INF).all()
     return value, parent, token
 
