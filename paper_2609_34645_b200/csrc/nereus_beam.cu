@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     __shared__ __align__(16) Key found[kFound];
     __shared__ Hit      rest[kFound];
     __shared__ uint32_t noted[kNoted], grouped[kNoted];
-    __shared__ uint32_t peak[kPick], histogram[256], at_place[NEREUS_BEAM_MAX_K], choice[4], of_warp[kPickWarps];
+    __shared__ uint32_t peak[kPick], histogram[256], at_place[NEREUS_BEAM_MAX_K], choice[4], of_warp[kPickWarps], all_of[3], any_of[3];
     __shared__ int      n_found, n_noted, n_grouped;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t request = blockIdx.x, first_row = request * s.beams;
@@ -365,6 +365,11 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     // The notes, 8 at a time; a warp's are of one row and part.  Of each set of threads the j-th largest of what their notes
     // are worth, off + x, by the norm, in 32 bits and a little less for the roundings: the least of these bounds the k-th
     // best from below.
+    auto worth_below = [](const Beam& r, float x) {
+        // a quotient beyond fp32 counts as the largest number, which it is not below
+        const float w = fminf(fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse, 3.402823466e38f);
+        return fmaf(-1e-6f, fabsf(w), w);
+    };
     float most = -INFINITY;
 #pragma unroll 1
     for (int g = tid; g < groups; g += kPick) {
@@ -373,9 +378,7 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         const float up = largest_note(records, g);
         // a note of a fp32 was rounded up: the next below it is not above the element
         const float x = sizeof(T) == 2 ? up : note_below((uint16_t)(__float_as_uint(up) >> 16));
-        // (a quotient beyond fp32 counts as the largest number, which it is not below)
-        const float w = fminf(fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse, 3.402823466e38f);
-        if (up > -INFINITY) most = fmaxf(most, fmaf(-1e-6f, fabsf(w), w));
+        if (up > -INFINITY) most = fmaxf(most, worth_below(r, x));
     }
     peak[tid] = key_of(most);
     __syncthreads();
@@ -392,25 +395,56 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         if (lane == 0) of_warp[warp] = t;
     }
     __syncthreads();
+    // of every row the least x whose worth reaches the bound, or a little less
+    auto set_least = [&](uint32_t key) {
+        if (tid >= s.beams) return;
+        Beam&       r = beams[tid];
+        const float bound = key > kKeyMinusInf ? value_of(key) : -INFINITY, norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
+        r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
+    };
+    // the groups of notes that reach it, then the notes
+    auto list_groups = [&]() {
+#pragma unroll 1
+        for (int g = tid; g < groups; g += kPick)
+            if (const float up = largest_note(records, g); up >= beams[quotient(g / 32, s.parts, parts_1)].least && up > -INFINITY) {
+                const int at = atomicAdd(&n_grouped, 1);
+                if (at < kNoted) grouped[at] = (uint32_t)g;
+            }
+    };
     if (tid < s.beams) {
-        Beam&    r = beams[tid];
         uint32_t t = 0xffffffffu;
 #pragma unroll
         for (int i = 0; i < kSets; ++i) t = min(t, of_warp[i]);
-        const float bound = t > kKeyMinusInf ? value_of(t) : -INFINITY;
-        // the least x whose worth reaches the bound, or a little less
-        const float norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
-        r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
+        set_least(t);
     }
     __syncthreads();
-    // the groups of notes that reach it, then the notes
-#pragma unroll 1
-    for (int g = tid; g < groups; g += kPick)
-        if (const float up = largest_note(records, g); up >= beams[quotient(g / 32, s.parts, parts_1)].least && up > -INFINITY) {
-            const int at = atomicAdd(&n_grouped, 1);
-            if (at < kNoted) grouped[at] = (uint32_t)g;
-        }
+    list_groups();
     __syncthreads();
+    if (n_grouped > kNoted) {
+        // Some set had little to vouch with (what a mask leaves lies on few threads): the k-th largest of all notes, to 16 bits.
+        uint32_t t = 0;
+#pragma unroll 1
+        for (int bit = 31; bit >= 16; --bit) {
+            int reach = 0;
+#pragma unroll 1
+            for (int n = tid; n < groups * 8; n += kPick) {
+                const Beam&    r = beams[quotient(n / kTH, s.parts, parts_1)];
+                const uint16_t note = records[n / kTH].notes[n % kTH];
+                const float    x = sizeof(T) == 2 ? value_of_note(note) : note_below(note);
+                if (value_of_note(note) > -INFINITY && r.off_1 == r.off_1) reach += key_of(worth_below(r, x)) >= (t | 1u << bit);
+            }
+            reach = __reduce_add_sync(0xffffffffu, reach);
+            __syncthreads();
+            if (lane == 0) of_warp[warp] = (uint32_t)reach;
+            __syncthreads();
+            if ((int)__reduce_add_sync(0xffffffffu, of_warp[lane]) >= s.k) t |= 1u << bit;
+        }
+        if (tid == 0) n_grouped = 0;
+        set_least(t);
+        __syncthreads();
+        list_groups();
+        __syncthreads();
+    }
     const int n_groups = n_grouped;
 #pragma unroll 1
     for (int j = tid; j < min(n_groups, kNoted) * 8; j += kPick) {
@@ -474,41 +508,108 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
 
     if (noted_all > kNoted || n_found > kFound) {
         // The k-th key exactly, or as much of it as leaves few enough: byte by byte of (key, ~index), the 12 bytes highest
-        // first, by the number of hypotheses that share the bytes found so far.
+        // first, by the number of hypotheses that share the bytes found so far.  Bytes that all of these have in common are
+        // passed over, and a key is worked out once where neighbours are equal.
         Key      key_is = 0, key_mask = 0;
         uint32_t index_is = 0, index_mask = 0;
         int      left = s.k, above = 0;
+        // f(key, beam, x, token, count) for all that may be among the best, a vector a thread of four layers at a time; `count`
+        // tokens of one key at once where a vector's elements are equal
         auto each = [&](auto f) {
+            auto one = [&](int b, float x, int token) {
+                float     unused;
+                const Key key = key_of_hit(b, x, &unused);
+                if (key) f(key, b, x, token, 1);
+            };
+#pragma unroll 1
             for (int b = 0; b < s.beams; ++b) {
-                if (beams[b].least != beams[b].least) continue;
-                for (int l = 0; l < deal.layers; ++l) {
-                    const Layer L = layer_at<T>(in, deal, s, first_row + b, l);
-                    for (int vec = tid; vec < kRoom; vec += kPick) look(b, L, vec, f);
+                const float least = beams[b].least;
+                if (least != least) continue;
+                float last = NAN;
+                Key   key = 0;
+#pragma unroll 1
+                for (int l = 0; l < deal.layers; l += 4) {
+                    uint4    v[4];
+                    int      token[4];
+                    uint32_t inside[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const Layer L = layer_at<T>(in, deal, s, first_row + b, l + j);
+                        const int   lo = L.lo - tid * E, hi = L.hi - tid * E;
+                        token[j] = L.token + tid * E;
+                        inside[j] = bits_between(lo, hi, E);
+                        v[j] = lo <= 0 && hi >= E ? __ldg(reinterpret_cast<const uint4*>(L.in) + tid) : inside[j] ? edge_vector<T>(L, tid) : Vec<T>::none();
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float top = Vec<T>::value(Vec<T>::max(v[j]));
+                        if (!inside[j] || !(top >= least) || !(top > -INFINITY)) continue;
+                        const bool equal = v[j].x == v[j].y && v[j].x == v[j].z && v[j].x == v[j].w && (sizeof(T) == 4 || v[j].x >> 16 == (v[j].x & 0xffffu));
+                        const int  step = equal && inside[j] == (1u << E) - 1 ? E : 1;
+                        float x[E];
+                        unpack<T>(v[j], x);
+#pragma unroll 1
+                        for (int e = 0; e < E; e += step) {
+                            float y = x[0];
+#pragma unroll
+                            for (int o = 1; o < E; ++o) y = o == e ? x[o] : y;
+                            if (!(inside[j] >> e & 1u) || !(y >= least) || !(y > -INFINITY)) continue;
+                            if (y != last) {
+                                float unused;
+                                key = key_of_hit(b, y, &unused);
+                                last = y;
+                            }
+                            if (key) f(key, b, y, token[j] + e, step);
+                        }
+                    }
                 }
             }
-            each_ended(f);
+            each_ended(one);
         };
+        static_assert(kPick == kRoom && kPickWarps == 32, "a vector of a layer for every thread, a lane for every warp");
+        int byte = 0;
 #pragma unroll 1
-        for (int byte = 0; byte < 12; ++byte) {
+        while (byte < 12) {
             if (tid < 256) histogram[tid] = 0;
-            if (tid == 0) choice[0] = 256;
+            if (tid == 0) {
+                choice[0] = 256;
+                for (int j = 0; j < 3; ++j) { all_of[j] = ~0u; any_of[j] = 0u; }
+            }
             __syncthreads();
             int      bin = 0;
             uint32_t run = 0;                              // elements of one bin come one after the other
-            each([&](int beam, float x, int token) {
-                float          unused;
-                const Key      key = key_of_hit(beam, x, &unused);
-                const uint32_t index = (uint32_t)(beam * in.vocab + token);
-                if (!key || ((key ^ key_is) & key_mask) || ((~index ^ index_is) & index_mask)) return;
-                const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : ~index >> (88 - 8 * byte)) & 255;
-                if (b != bin) {
-                    if (run) atomicAdd(&histogram[bin], run);
-                    bin = b;
-                    run = 0;
+            Key      all_key = ~(Key)0, any_key = 0;
+            uint32_t all_index = ~0u, any_index = 0;
+            each([&](Key key, int beam, float, int token, int count) {
+                if ((key ^ key_is) & key_mask) return;
+                all_key &= key;
+                any_key |= key;
+                // tokens whose index shares this byte and those above it go together
+                const int shift = byte < 8 ? 31 : 88 - 8 * byte;
+#pragma unroll 1
+                for (int done = 0; done < count;) {
+                    const uint32_t first = ~(uint32_t)(beam * in.vocab + token + done), last = first - (uint32_t)(count - done - 1);
+                    const int      n = byte < 8 || first >> shift == last >> shift ? count - done : 1;
+                    done += n;
+                    if ((first ^ index_is) & index_mask) continue;
+                    all_index &= n > 1 ? first & last : first;
+                    any_index |= n > 1 ? first | last : first;
+                    const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : (Key)(first >> shift)) & 255;
+                    if (b != bin) {
+                        if (run) atomicAdd(&histogram[bin], run);
+                        bin = b;
+                        run = 0;
+                    }
+                    run += n;
                 }
-                ++run;
             });
             if (run) atomicAdd(&histogram[bin], run);
+            const uint32_t alls[3] = {(uint32_t)(all_key >> 32), (uint32_t)all_key, all_index}, anys[3] = {(uint32_t)(any_key >> 32), (uint32_t)any_key, any_index};
+#pragma unroll
+            for (int j = 0; j < 3; ++j) {
+                const uint32_t x = __reduce_and_sync(0xffffffffu, alls[j]), y = __reduce_or_sync(0xffffffffu, anys[j]);
+                if (lane == 0) { atomicAnd(&all_of[j], x); atomicOr(&any_of[j], y); }
+            }
             __syncthreads();
             // the bins from the highest down: how many there are up to this one
             const uint32_t c = tid < 256 ? histogram[255 - tid] : 0;
@@ -528,21 +629,32 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             }
             __syncthreads();
             const uint32_t b = choice[0], higher = choice[1], same = choice[2];
-            __syncthreads();
             if (b == 256) break;                           // fewer than k in all: everything is taken
             above += (int)higher;
             left -= (int)higher;
-            if (byte < 8) { key_is |= (Key)b << (56 - 8 * byte); key_mask |= (Key)255 << (56 - 8 * byte); }
-            else { index_is |= b << (88 - 8 * byte); index_mask |= 255u << (88 - 8 * byte); }
+            // this byte, and those behind it that all have in common
+#pragma unroll 1
+            for (bool first = true; byte < 12; first = false) {
+                const int      shift = 24 - 8 * (byte & 3);
+                const uint32_t all = all_of[byte >> 2] >> shift & 255u, any = any_of[byte >> 2] >> shift & 255u;
+                if (!first && all != any) break;
+                const uint32_t is = first ? b : all;
+                if (byte < 8) { key_is |= (Key)is << (56 - 8 * byte); key_mask |= (Key)255 << (56 - 8 * byte); }
+                else { index_is |= is << shift; index_mask |= 255u << shift; }
+                ++byte;
+            }
+            __syncthreads();
             if (above + (int)same <= kFound) break;
         }
         if (tid == 0) n_found = 0;
         __syncthreads();
         // everything from the bytes found on
-        each([&](int beam, float x, int token) {
-            float     unused;
-            const Key key = key_of_hit(beam, x, &unused), top = key & key_mask;
-            if (key && (top > key_is || (top == key_is && (~(uint32_t)(beam * in.vocab + token) & index_mask) >= index_is))) push(beam, x, token);
+        each([&](Key key, int beam, float x, int token, int count) {
+            const Key top = key & key_mask;
+            if (top < key_is) return;
+#pragma unroll 1
+            for (int j = 0; j < count; ++j)
+                if (top > key_is || (~(uint32_t)(beam * in.vocab + token + j) & index_mask) >= index_is) push(beam, x, token + j);
         });
         __syncthreads();
     }
