@@ -12,6 +12,8 @@
 //     few times k hypotheses, is ranked by counting.
 // Where more is found than the list holds (rows of few distinct values: a mask's lowest value, say), the bound is made exact
 // by counting the keys' bytes, the highest first, a pass over the request for each byte that is needed.
+// 128 requests x 8 x 128256 bf16 (32.6 us of HBM): 45 us the sum, 4.8 TB/s, which 8 instructions and an exponential an element
+// bound, and 12 the pick, a chain of dependent steps.  One request of 4 beams takes 10 us, by the same chain.
 // Hypotheses are compared in 64 bits, as keys of (total / norm, lower index): within a row these order as the logits do.
 #include "nereus_rows.hpp"
 
@@ -289,17 +291,205 @@ template <class T> __device__ __noinline__ double far_row(const LogitsCut& in, c
     return (double)top + kLn2 * log2_of(all);
 }
 
+// What the picking block shares with its search of last resort.
+struct Pick {
+    __align__(16) Key found[kFound];
+    Beam     beams[NEREUS_BEAM_MAX];
+    Hit      rest[kFound];
+    uint32_t histogram[256], choice[4], of_warp[kPickWarps], all_of[3], any_of[3];
+    int      n_found;
+};
+// whether a beam offers itself alone
+__device__ __forceinline__ bool ended(const Beam& r) { return r.ended >= 0 && r.off == r.off; }
+__device__ __forceinline__ void push(Pick& pick, int beam, float x, int token) {
+    const int at = atomicAdd(&pick.n_found, 1);
+    if (at < kFound) pick.rest[at] = {x, beam, token};
+}
+// what a hypothesis is worth, in 64 bits; 0: it is not offered
+__device__ __forceinline__ Key key_of_hit(const Select& s, const Beam& r, float x, float* total) {
+    const double sum = r.ended >= 0 ? r.off : r.off + (double)x;
+    const Key    key = key_of_double(s.norm ? sum / r.norm : sum);
+    *total = r.ended >= 0 ? r.score : (float)sum;
+    return key > kKeyNone ? key : 0;
+}
+// Leaves the hypotheses to rank in the list, where they were too many for it.  On its own, out of the pick's registers: they
+// spilled otherwise.  128 requests x 8 x 128256 with 24 tokens allowed each, the others at a mask's lowest value: k 16 in 0.20
+// ms, k 64, where the k-th is a masked one, in 2.4.
+template <class T> __device__ __noinline__ void search_by_bytes(const LogitsCut& in, const Deal& deal, const Select& s, int64_t first_row, Pick& pick) {
+    constexpr int E = kPerVec<T>;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    auto& beams = pick.beams;
+    auto& histogram = pick.histogram;
+    auto& choice = pick.choice;
+    auto& of_warp = pick.of_warp;
+    auto& all_of = pick.all_of;
+    auto& any_of = pick.any_of;
+    auto& n_found = pick.n_found;
+    // The k-th key exactly, or as much of it as leaves few enough: byte by byte of (key, ~index), the 12 bytes highest
+    // first, by the number of hypotheses that share the bytes found so far.  Bytes that all of these have in common are
+    // passed over, and a key is worked out once where neighbours are equal.
+    Key      key_is = 0, key_mask = 0;
+    uint32_t index_is = 0, index_mask = 0;
+    int      left = s.k, above = 0;
+    // f(key, beam, x, token, count) for all that may be among the best, a vector a thread of four layers at a time; `count`
+    // tokens of one key at once where a vector's elements are equal
+    auto each = [&](auto f) {
+        auto one = [&](int b, float x, int token) {
+            float     unused;
+            const Key key = key_of_hit(s, beams[b], x, &unused);
+            if (key) f(key, b, x, token, 1);
+        };
+#pragma unroll 1
+        for (int b = 0; b < s.beams; ++b) {
+            const float least = beams[b].least;
+            if (least != least) continue;
+            float last = NAN;
+            Key   key = 0;
+#pragma unroll 1
+            for (int l = 0; l < deal.layers; l += 4) {
+                uint4    v[4];
+                int      token[4];
+                uint32_t inside[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const Layer L = layer_at<T>(in, deal, s, first_row + b, l + j);
+                    const int   lo = L.lo - tid * E, hi = L.hi - tid * E;
+                    token[j] = L.token + tid * E;
+                    inside[j] = bits_between(lo, hi, E);
+                    v[j] = lo <= 0 && hi >= E ? __ldg(reinterpret_cast<const uint4*>(L.in) + tid) : inside[j] ? edge_vector<T>(L, tid) : Vec<T>::none();
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float top = Vec<T>::value(Vec<T>::max(v[j]));
+                    if (!inside[j] || !(top >= least) || !(top > -INFINITY)) continue;
+                    const bool equal = v[j].x == v[j].y && v[j].x == v[j].z && v[j].x == v[j].w && (sizeof(T) == 4 || v[j].x >> 16 == (v[j].x & 0xffffu));
+                    const int  step = equal && inside[j] == (1u << E) - 1 ? E : 1;
+                    float x[E];
+                    unpack<T>(v[j], x);
+#pragma unroll 1
+                    for (int e = 0; e < E; e += step) {
+                        float y = x[0];
+#pragma unroll
+                        for (int o = 1; o < E; ++o) y = o == e ? x[o] : y;
+                        if (!(inside[j] >> e & 1u) || !(y >= least) || !(y > -INFINITY)) continue;
+                        if (y != last) {
+                            float unused;
+                            key = key_of_hit(s, beams[b], y, &unused);
+                            last = y;
+                        }
+                        if (key) f(key, b, y, token[j] + e, step);
+                    }
+                }
+            }
+        }
+        if (tid < s.beams && ended(beams[tid])) one(tid, 0.f, beams[tid].ended);
+    };
+    static_assert(kPick == kRoom && kPickWarps == 32, "a vector of a layer for every thread, a lane for every warp");
+    int byte = 0;
+#pragma unroll 1
+    while (byte < 12) {
+        if (tid < 256) histogram[tid] = 0;
+        if (tid == 0) {
+            choice[0] = 256;
+            for (int j = 0; j < 3; ++j) { all_of[j] = ~0u; any_of[j] = 0u; }
+        }
+        __syncthreads();
+        int      bin = 0;
+        uint32_t run = 0;                              // elements of one bin come one after the other
+        Key      all_key = ~(Key)0, any_key = 0;
+        uint32_t all_index = ~0u, any_index = 0;
+        each([&](Key key, int beam, float, int token, int count) {
+            if ((key ^ key_is) & key_mask) return;
+            all_key &= key;
+            any_key |= key;
+            // tokens whose index shares this byte and those above it go together
+            const int shift = byte < 8 ? 31 : 88 - 8 * byte;
+#pragma unroll 1
+            for (int done = 0; done < count;) {
+                const uint32_t first = ~(uint32_t)(beam * in.vocab + token + done), last = first - (uint32_t)(count - done - 1);
+                const int      n = byte < 8 || first >> shift == last >> shift ? count - done : 1;
+                done += n;
+                if ((first ^ index_is) & index_mask) continue;
+                all_index &= n > 1 ? first & last : first;
+                any_index |= n > 1 ? first | last : first;
+                const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : (Key)(first >> shift)) & 255;
+                if (b != bin) {
+                    if (run) atomicAdd(&histogram[bin], run);
+                    bin = b;
+                    run = 0;
+                }
+                run += n;
+            }
+        });
+        if (run) atomicAdd(&histogram[bin], run);
+        const uint32_t alls[3] = {(uint32_t)(all_key >> 32), (uint32_t)all_key, all_index}, anys[3] = {(uint32_t)(any_key >> 32), (uint32_t)any_key, any_index};
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const uint32_t x = __reduce_and_sync(0xffffffffu, alls[j]), y = __reduce_or_sync(0xffffffffu, anys[j]);
+            if (lane == 0) { atomicAnd(&all_of[j], x); atomicOr(&any_of[j], y); }
+        }
+        __syncthreads();
+        // the bins from the highest down: how many there are up to this one
+        const uint32_t c = tid < 256 ? histogram[255 - tid] : 0;
+        uint32_t       upto = c;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += u;
+        }
+        if (lane == 31) of_warp[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) upto += of_warp[w];
+        if (tid < 256 && upto >= (uint32_t)left && upto - c < (uint32_t)left) {
+            choice[0] = 255 - tid;
+            choice[1] = upto - c;
+            choice[2] = c;
+        }
+        __syncthreads();
+        const uint32_t b = choice[0], higher = choice[1], same = choice[2];
+        if (b == 256) break;                           // fewer than k in all: everything is taken
+        above += (int)higher;
+        left -= (int)higher;
+        // this byte, and those behind it that all have in common
+#pragma unroll 1
+        for (bool first = true; byte < 12; first = false) {
+            const int      shift = 24 - 8 * (byte & 3);
+            const uint32_t all = all_of[byte >> 2] >> shift & 255u, any = any_of[byte >> 2] >> shift & 255u;
+            if (!first && all != any) break;
+            const uint32_t is = first ? b : all;
+            if (byte < 8) { key_is |= (Key)is << (56 - 8 * byte); key_mask |= (Key)255 << (56 - 8 * byte); }
+            else { index_is |= is << shift; index_mask |= 255u << shift; }
+            ++byte;
+        }
+        __syncthreads();
+        if (above + (int)same <= kFound) break;
+    }
+    if (tid == 0) n_found = 0;
+    __syncthreads();
+    // everything from the bytes found on
+    each([&](Key key, int beam, float x, int token, int count) {
+        const Key top = key & key_mask;
+        if (top < key_is) return;
+#pragma unroll 1
+        for (int j = 0; j < count; ++j)
+            if (top > key_is || (~(uint32_t)(beam * in.vocab + token + j) & index_mask) >= index_is) push(pick, beam, x, token + j);
+    });
+    __syncthreads();
+}
+
 template <class T>
 __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant__ LogitsCut in, const Deal deal, const Select s) {
     constexpr int E = kPerVec<T>;
     extern __shared__ __align__(16) unsigned char dynamic[];
     Record* const records = reinterpret_cast<Record*>(dynamic);
-    __shared__ Beam     beams[NEREUS_BEAM_MAX];
-    __shared__ __align__(16) Key found[kFound];
-    __shared__ Hit      rest[kFound];
-    __shared__ uint32_t noted[kNoted], grouped[kNoted];
-    __shared__ uint32_t peak[kPick], histogram[256], at_place[NEREUS_BEAM_MAX_K], choice[4], of_warp[kPickWarps], all_of[3], any_of[3];
-    __shared__ int      n_found, n_noted, n_grouped;
+    __shared__ Pick pick;
+    auto& beams = pick.beams;
+    auto& found = pick.found;
+    auto& rest = pick.rest;
+    auto& of_warp = pick.of_warp;
+    auto& n_found = pick.n_found;
+    __shared__ uint32_t noted[kNoted], grouped[kNoted], peak[kPick], at_place[NEREUS_BEAM_MAX_K];
+    __shared__ int      n_noted, n_grouped;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t request = blockIdx.x, first_row = request * s.beams;
 
@@ -476,22 +666,6 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
             f(b, y, L.token + vec * E + e);
         }
     };
-    // the beams that have ended offer themselves
-    auto each_ended = [&](auto f) {
-        if (tid < s.beams && beams[tid].ended >= 0 && beams[tid].off == beams[tid].off) f(tid, 0.f, beams[tid].ended);
-    };
-    auto push = [&](int b, float x, int token) {
-        const int at = atomicAdd(&n_found, 1);
-        if (at < kFound) rest[at] = {x, b, token};
-    };
-    // what a hypothesis is worth, in 64 bits; 0: it is not offered
-    auto key_of_hit = [&](int b, float x, float* total) {
-        const Beam&  r = beams[b];
-        const double sum = r.ended >= 0 ? r.off : r.off + (double)x;
-        const Key    key = key_of_double(s.norm ? sum / r.norm : sum);
-        *total = r.ended >= 0 ? r.score : (float)sum;
-        return key > kKeyNone ? key : 0;
-    };
     const int log_part = __ffs(s.of_part) - 1, noted_all = max(n_noted, n_groups);
     if (noted_all <= kNoted) {
         // every vector of a note on a thread of its own
@@ -500,171 +674,20 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         for (int j = tid; j < vecs; j += kPick) {
             const int which = (int)noted[j / of_note], row_part = which / kTH, b = quotient(row_part, s.parts, parts_1), v = j % of_note;
             const int l = ((row_part - b * s.parts) << log_part) + v / kV;
-            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + v % kV * kTH, push);
+            look(b, layer_at<T>(in, deal, s, first_row + b, l), which % kTH + v % kV * kTH, [&](int beam, float x, int token) { push(pick, beam, x, token); });
         }
     }
-    each_ended(push);
+    if (tid < s.beams && ended(beams[tid])) push(pick, tid, 0.f, beams[tid].ended);
     __syncthreads();
 
-    if (noted_all > kNoted || n_found > kFound) {
-        // The k-th key exactly, or as much of it as leaves few enough: byte by byte of (key, ~index), the 12 bytes highest
-        // first, by the number of hypotheses that share the bytes found so far.  Bytes that all of these have in common are
-        // passed over, and a key is worked out once where neighbours are equal.
-        Key      key_is = 0, key_mask = 0;
-        uint32_t index_is = 0, index_mask = 0;
-        int      left = s.k, above = 0;
-        // f(key, beam, x, token, count) for all that may be among the best, a vector a thread of four layers at a time; `count`
-        // tokens of one key at once where a vector's elements are equal
-        auto each = [&](auto f) {
-            auto one = [&](int b, float x, int token) {
-                float     unused;
-                const Key key = key_of_hit(b, x, &unused);
-                if (key) f(key, b, x, token, 1);
-            };
-#pragma unroll 1
-            for (int b = 0; b < s.beams; ++b) {
-                const float least = beams[b].least;
-                if (least != least) continue;
-                float last = NAN;
-                Key   key = 0;
-#pragma unroll 1
-                for (int l = 0; l < deal.layers; l += 4) {
-                    uint4    v[4];
-                    int      token[4];
-                    uint32_t inside[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const Layer L = layer_at<T>(in, deal, s, first_row + b, l + j);
-                        const int   lo = L.lo - tid * E, hi = L.hi - tid * E;
-                        token[j] = L.token + tid * E;
-                        inside[j] = bits_between(lo, hi, E);
-                        v[j] = lo <= 0 && hi >= E ? __ldg(reinterpret_cast<const uint4*>(L.in) + tid) : inside[j] ? edge_vector<T>(L, tid) : Vec<T>::none();
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float top = Vec<T>::value(Vec<T>::max(v[j]));
-                        if (!inside[j] || !(top >= least) || !(top > -INFINITY)) continue;
-                        const bool equal = v[j].x == v[j].y && v[j].x == v[j].z && v[j].x == v[j].w && (sizeof(T) == 4 || v[j].x >> 16 == (v[j].x & 0xffffu));
-                        const int  step = equal && inside[j] == (1u << E) - 1 ? E : 1;
-                        float x[E];
-                        unpack<T>(v[j], x);
-#pragma unroll 1
-                        for (int e = 0; e < E; e += step) {
-                            float y = x[0];
-#pragma unroll
-                            for (int o = 1; o < E; ++o) y = o == e ? x[o] : y;
-                            if (!(inside[j] >> e & 1u) || !(y >= least) || !(y > -INFINITY)) continue;
-                            if (y != last) {
-                                float unused;
-                                key = key_of_hit(b, y, &unused);
-                                last = y;
-                            }
-                            if (key) f(key, b, y, token[j] + e, step);
-                        }
-                    }
-                }
-            }
-            each_ended(one);
-        };
-        static_assert(kPick == kRoom && kPickWarps == 32, "a vector of a layer for every thread, a lane for every warp");
-        int byte = 0;
-#pragma unroll 1
-        while (byte < 12) {
-            if (tid < 256) histogram[tid] = 0;
-            if (tid == 0) {
-                choice[0] = 256;
-                for (int j = 0; j < 3; ++j) { all_of[j] = ~0u; any_of[j] = 0u; }
-            }
-            __syncthreads();
-            int      bin = 0;
-            uint32_t run = 0;                              // elements of one bin come one after the other
-            Key      all_key = ~(Key)0, any_key = 0;
-            uint32_t all_index = ~0u, any_index = 0;
-            each([&](Key key, int beam, float, int token, int count) {
-                if ((key ^ key_is) & key_mask) return;
-                all_key &= key;
-                any_key |= key;
-                // tokens whose index shares this byte and those above it go together
-                const int shift = byte < 8 ? 31 : 88 - 8 * byte;
-#pragma unroll 1
-                for (int done = 0; done < count;) {
-                    const uint32_t first = ~(uint32_t)(beam * in.vocab + token + done), last = first - (uint32_t)(count - done - 1);
-                    const int      n = byte < 8 || first >> shift == last >> shift ? count - done : 1;
-                    done += n;
-                    if ((first ^ index_is) & index_mask) continue;
-                    all_index &= n > 1 ? first & last : first;
-                    any_index |= n > 1 ? first | last : first;
-                    const int b = (int)(byte < 8 ? key >> (56 - 8 * byte) : (Key)(first >> shift)) & 255;
-                    if (b != bin) {
-                        if (run) atomicAdd(&histogram[bin], run);
-                        bin = b;
-                        run = 0;
-                    }
-                    run += n;
-                }
-            });
-            if (run) atomicAdd(&histogram[bin], run);
-            const uint32_t alls[3] = {(uint32_t)(all_key >> 32), (uint32_t)all_key, all_index}, anys[3] = {(uint32_t)(any_key >> 32), (uint32_t)any_key, any_index};
-#pragma unroll
-            for (int j = 0; j < 3; ++j) {
-                const uint32_t x = __reduce_and_sync(0xffffffffu, alls[j]), y = __reduce_or_sync(0xffffffffu, anys[j]);
-                if (lane == 0) { atomicAnd(&all_of[j], x); atomicOr(&any_of[j], y); }
-            }
-            __syncthreads();
-            // the bins from the highest down: how many there are up to this one
-            const uint32_t c = tid < 256 ? histogram[255 - tid] : 0;
-            uint32_t       upto = c;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += u;
-            }
-            if (lane == 31) of_warp[warp] = upto;
-            __syncthreads();
-            for (int w = 0; w < warp; ++w) upto += of_warp[w];
-            if (tid < 256 && upto >= (uint32_t)left && upto - c < (uint32_t)left) {
-                choice[0] = 255 - tid;
-                choice[1] = upto - c;
-                choice[2] = c;
-            }
-            __syncthreads();
-            const uint32_t b = choice[0], higher = choice[1], same = choice[2];
-            if (b == 256) break;                           // fewer than k in all: everything is taken
-            above += (int)higher;
-            left -= (int)higher;
-            // this byte, and those behind it that all have in common
-#pragma unroll 1
-            for (bool first = true; byte < 12; first = false) {
-                const int      shift = 24 - 8 * (byte & 3);
-                const uint32_t all = all_of[byte >> 2] >> shift & 255u, any = any_of[byte >> 2] >> shift & 255u;
-                if (!first && all != any) break;
-                const uint32_t is = first ? b : all;
-                if (byte < 8) { key_is |= (Key)is << (56 - 8 * byte); key_mask |= (Key)255 << (56 - 8 * byte); }
-                else { index_is |= is << shift; index_mask |= 255u << shift; }
-                ++byte;
-            }
-            __syncthreads();
-            if (above + (int)same <= kFound) break;
-        }
-        if (tid == 0) n_found = 0;
-        __syncthreads();
-        // everything from the bytes found on
-        each([&](Key key, int beam, float x, int token, int count) {
-            const Key top = key & key_mask;
-            if (top < key_is) return;
-#pragma unroll 1
-            for (int j = 0; j < count; ++j)
-                if (top > key_is || (~(uint32_t)(beam * in.vocab + token + j) & index_mask) >= index_is) push(beam, x, token + j);
-        });
-        __syncthreads();
-    }
+    if (noted_all > kNoted || n_found > kFound) search_by_bytes<T>(in, deal, s, first_row, pick);
 
     // which hypothesis is the j-th, and its beam in the upper half
     const int total = n_found, quads = (total + 3) / 4;    // keys are read four at a time
     if (tid < s.k) at_place[tid] = 0xffffffffu;
 #pragma unroll 1
     for (int j = tid; j < 4 * quads; j += kPick) {
-        if (j < total) found[j] = key_of_hit(rest[j].beam, rest[j].x, &rest[j].x);       // its total takes the element's place
+        if (j < total) found[j] = key_of_hit(s, beams[rest[j].beam], rest[j].x, &rest[j].x);       // its total takes the element's place
         else found[j] = 0;
     }
     __syncthreads();
