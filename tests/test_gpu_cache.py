@@ -296,6 +296,21 @@ def test_compact(pages, live, keep):
         assert np.array_equal(as_bytes(p), o)
 
 
+def test_compact_of_more_tiles_than_blocks():
+    rng = seed("tiles")
+    pages, pools = 50001, 60
+    refs = np.where((np.arange(pages) > 24000) ^ (rng.random(pages) < 0.01), 1, 0)
+    table = rng.integers(0, pages, (3, 50))
+    whole = noise(rng, (pools, pages, 8), torch.int16)
+    old = as_bytes(whole).reshape(pools, pages, -1)
+    got = C.compact(list(whole.unbind(0)), ints(table), ints(refs))
+    want = U.compact(table, refs, None)
+    moves = np.array(want[3], np.int64).reshape(-1, 2)
+    assert len(moves) > 20000 and np.array_equal(got[3][:len(moves)].cpu().numpy(), moves)
+    old[:, moves[:, 1]] = old[:, moves[:, 0]]
+    assert np.array_equal(as_bytes(whole).reshape(pools, pages, -1), old)
+
+
 # ---- copy ------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("page", [1, 3, 16, 585, 1000, 4096, 9000])
