@@ -510,7 +510,8 @@ __global__ void __launch_bounds__(kWhole ? kSmallThreads : kBookThreads, 1) fork
     const int64_t before = (int64_t)blocks_before(of_block, totals, rank, blocks, &free_pages);
     const int64_t missing = max((int64_t)0, fresh - (int64_t)free_pages) + (int64_t)lacking_columns;
     if (missing == 0) {
-        // the block's free pages by rank, a window of them at a time, then a thread for each that is handed out
+        // The block's free pages by rank, a window of them at a time, then a thread for each that is handed out, which marks it as
+        // taken: a group in which a window ends is read again for the next, and what is left of it begins that one.
         const int mine = (int)max((int64_t)0, min((int64_t)of_block, fresh - before));
 #pragma unroll 1
         for (int base = 0; base < mine; base += kWindow) {
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(kWhole ? kSmallThreads : kBookThreads, 1) fork
                 const int      p = (first_group + g) * kGroup;
                 const int4     v = counts_of(to.refs, p, from.pages, aligned, 1);
                 const unsigned below = (1u << lane) - 1;
-                int            j = free_of[g] - base;
+                int            j = max(free_of[g] - base, 0);      // what the windows before took of the group counts as free no more
 #pragma unroll
                 for (int e = 0; e < 4; ++e) j += __popc(__ballot_sync(0xffffffffu, (e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w) <= 0) & below);
 #pragma unroll
