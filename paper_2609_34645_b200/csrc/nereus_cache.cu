@@ -765,9 +765,7 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_cons
                 if (left >= (int64_t)sizeof(V)) v[i] = __ldcg(reinterpret_cast<const V*>(from + moves[i].from));
                 else edge |= left > 0;
             }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i < n && moves[i].bytes - at >= (int64_t)sizeof(V)) __stcg(reinterpret_cast<V*>(to + moves[i].to), v[i]);
+        // Before any whole vector is stored: that may be where a shorter row's bytes come from, and none is loaded from where these go.
         if (sizeof(V) > 1 && edge)
             for (int k = 0; k < (int)sizeof(V); ++k) {
                 unsigned char c[N];
@@ -778,6 +776,9 @@ __global__ void __launch_bounds__(kMoveThreads) reorder_kernel(const __grid_cons
                 for (int i = 0; i < N; ++i)
                     if (i < n && moves[i].bytes - at < (int64_t)sizeof(V) && moves[i].bytes - at > k) to[moves[i].to + k] = c[i];
             }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < n && moves[i].bytes - at >= (int64_t)sizeof(V)) __stcg(reinterpret_cast<V*>(to + moves[i].to), v[i]);
     }
 }
 
