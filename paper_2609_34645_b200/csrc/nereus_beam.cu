@@ -500,6 +500,7 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         if ((uint32_t)r.ended >= (uint32_t)in.vocab) r.ended = -1;
         r.norm = (double)norm;
         r.inverse = 1.f / norm;
+        if (isinf(r.inverse)) r.inverse = NAN;         // 1 / norm is beyond fp32: its notes are worth nothing for the bound
         r.off = is ? (double)r.score : (double)NAN;
         r.least = NAN;
         beams[b] = r;
@@ -556,9 +557,11 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
     // are worth, off + x, by the norm, in 32 bits and a little less for the roundings: the least of these bounds the k-th
     // best from below.
     auto worth_below = [](const Beam& r, float x) {
-        // a quotient beyond fp32 counts as the largest number, which it is not below
-        const float w = fminf(fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x), r.off_1 + x) * r.inverse, 3.402823466e38f);
-        return fmaf(-1e-6f, fabsf(w), w);
+        // Not a number (an offset or 1 / norm beyond fp32): it vouches for nothing.  A quotient beyond fp32 counts as the largest
+        // number, which it is not below.  1e-38: so that what the smallest floats are rounded by is covered too.
+        const float sum = fmaf(-1e-6f, fabsf(r.off_1) + fabsf(x) + 1e-38f, r.off_1 + x);
+        const float w = fminf(fmaxf(sum * r.inverse, -INFINITY), 3.402823466e38f);
+        return fmaf(-1e-6f, fabsf(w) + 1e-38f, w);
     };
     float most = -INFINITY;
 #pragma unroll 1
@@ -585,12 +588,12 @@ __global__ void __launch_bounds__(kPick) beam_pick_kernel(const __grid_constant_
         if (lane == 0) of_warp[warp] = t;
     }
     __syncthreads();
-    // of every row the least x whose worth reaches the bound, or a little less
+    // of every row the least x whose worth reaches the bound, or a little less; in 64 bits, where nothing overflows
     auto set_least = [&](uint32_t key) {
         if (tid >= s.beams) return;
-        Beam&       r = beams[tid];
-        const float bound = key > kKeyMinusInf ? value_of(key) : -INFINITY, norm = (float)r.norm, at = fmaf(bound, norm, -r.off_1);
-        r.least = r.off_1 != r.off_1 ? NAN : bound > -INFINITY ? fmaf(-1e-6f, fabsf(bound * norm) + fabsf(r.off_1), at) : -INFINITY;
+        Beam&        r = beams[tid];
+        const double reach = (double)value_of(key) * r.norm;
+        r.least = r.off_1 != r.off_1 ? NAN : key > kKeyMinusInf ? __double2float_rd(fma(-1e-6, fabs(reach) + fabs(r.off), reach - r.off)) : -INFINITY;
     };
     // the groups of notes that reach it, then the notes
     auto list_groups = [&]() {
