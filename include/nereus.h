@@ -586,8 +586,8 @@ int nereus_distill_step(const nereus_logits_t* in, const nereus_distill_t* how, 
  * captured into a CUDA graph.  They move bytes: the elements' type does not matter.  Ids that come from device arrays are
  * checked there; what is out of range is left out as said with each call and never read or written.
  * Common errors: ARG (null pointer, negative or zero size, a stride too small), ALIGN (an int32 array that is not aligned to
- * 4 bytes), MISMATCH (the two sides of a call do not fit), ALIAS (what a call writes overlaps what it reads), TOO_LARGE
- * (limits named with each call), CUDA.  The buffers are on the current device. */
+ * 4 bytes), MISMATCH (the two sides of a call do not fit), ALIAS (what a call writes overlaps what it reads, or something else
+ * that it writes), TOO_LARGE (limits named with each call), CUDA.  The buffers are on the current device. */
 
 /* States of sequences: `buffers` buffers of one geometry.  Row r of a buffer is `outer` pieces, `outer_stride` bytes apart, of
  * `tokens` tokens of `token_bytes` contiguous bytes: [rows, tokens, heads, dim] has outer = 1, [rows, heads, tokens, dim]
@@ -605,7 +605,8 @@ typedef struct {
  *   to != from   the two share no byte.  A parent outside [0, from->rows) leaves the row as it was.  beams = 0.
  *   to == from   in place (the same buffers, geometry and strides): rows come in groups of `beams` (1..NEREUS_BEAM_MAX,
  *                rows a multiple); all rows of a group are read before one is written, so that parents may cross.  A
- *                parent outside the row's own group, or the row itself, leaves the row as it was.
+ *                parent outside the row's own group, or the row itself, leaves the row as it was. No two
+ *                buffers share a byte; out of place, two may be one on both sides.
  * Errors: common, ARG (beams), MISMATCH (geometry), TOO_LARGE (rows or outer > 2^24, a buffer of more
  * than 2^46 bytes). */
 int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to, int beams, const int32_t* parent,

@@ -12,6 +12,7 @@
 #include <atomic>
 #include <climits>
 #include <cstdint>
+#include <cstdlib>
 #include <type_traits>
 
 #include "nereus_internal.hpp"
@@ -872,6 +873,51 @@ bool apart(const Side& a, const Side& b) {
     return true;
 }
 
+// Pieces of a buffer: n0 times n1 of `width` bytes, s0 and s1 apart, in the order of their addresses.
+struct Grid {
+    int64_t n0, s0, n1, s1, width;
+    int64_t inner() const { return (n1 - 1) * s1 + width; }
+    int64_t whole() const { return (n0 - 1) * s0 + inner(); }
+};
+// Whether two buffers of such pieces share a byte when one lies `delta` bytes behind the other.  A piece meets those next to its
+// own distance alone.
+bool meet(const Grid& g, int64_t delta) {
+    if (delta < 0) delta = -delta;
+    if (delta >= g.whole()) return false;
+    const int64_t first = g.n0 > 1 ? delta / g.s0 : 0;
+    for (int64_t i = first; i <= first + 1 && i < g.n0; ++i) {
+        const int64_t rest = std::abs(delta - i * g.s0);
+        if (rest >= g.inner()) continue;
+        const int64_t second = g.n1 > 1 ? rest / g.s1 : 0;
+        for (int64_t j = second; j <= second + 1 && j < g.n1; ++j)
+            if (std::abs(rest - j * g.s1) < g.width) return true;
+    }
+    return false;
+}
+// Whether n buffers of such pieces share no byte with one another.  Where `other` is given, two that are the same here and there
+// count as one.  Buffers one after the other, and such whose pieces or inner stretches lie side by side, are seen at a glance.
+bool disjoint(const Grid& g, void* const* base, int n, void* const* other) {
+    struct Item {
+        uintptr_t lo;
+        int       i;
+    } all[NEREUS_MAX_BUFFERS];
+    for (int i = 0; i < n; ++i) all[i] = {(uintptr_t)base[i], i};
+    auto before = [](const Item& a, const Item& b) { return a.lo < b.lo; };
+    if (!std::is_sorted(all, all + n, before)) std::sort(all, all + n, before);
+    uintptr_t least = UINTPTR_MAX;
+    for (int i = 1; i < n; ++i) least = std::min(least, all[i].lo - all[i - 1].lo);
+    if (n < 2 || least >= (uintptr_t)g.whole()) return true;
+    const uintptr_t span = all[n - 1].lo - all[0].lo;
+    if (g.n0 > 1 && least >= (uintptr_t)g.inner() && span + g.inner() <= (uintptr_t)g.s0) return true;
+    if (g.n1 > 1 && least >= (uintptr_t)g.width && span + g.width <= (uintptr_t)g.s1 && (g.n0 < 2 || span + g.inner() <= (uintptr_t)g.s0)) return true;
+    for (int i = 0; i < n; ++i)
+        for (int j = i + 1; j < n && all[j].lo - all[i].lo < (uintptr_t)g.whole(); ++j) {
+            if (other && all[i].lo == all[j].lo && other[all[i].i] == other[all[j].i]) continue;
+            if (meet(g, (int64_t)(all[j].lo - all[i].lo))) return false;
+        }
+    return true;
+}
+
 // The largest of 16, 4 and 1 that divides everything.
 int unit_of(uint64_t bits) { return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 1; }
 
@@ -1016,6 +1062,11 @@ int check_states(const nereus_states_t* s) {
     return NEREUS_OK;
 }
 
+Grid grid_of(const nereus_states_t& t) {
+    const int64_t piece = t.tokens * t.token_bytes, row = t.rows > 1 ? t.row_stride : 0, step = t.outer > 1 ? t.outer_stride : 0;
+    return t.rows < 2 || row >= (t.outer - 1) * step + piece ? Grid{t.rows, row, t.outer, step, piece} : Grid{t.outer, step, t.rows, row, piece};
+}
+
 template <class V, int N, class S> int reorder_launch(S& s, const int32_t* parent, const int32_t* length, const Device& dev, cudaStream_t stream) {
     constexpr int64_t kTile = (int64_t)kMoveThreads * sizeof(V);
     const int64_t groups = ((int64_t)s.to_rows + s.group - 1) / s.group, items = (s.piece + kTile - 1) / kTile * s.outer * s.buffers;
@@ -1085,6 +1136,7 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
         if (from->rows != to->rows || (to->rows > 1 && from->row_stride != to->row_stride) || (to->outer > 1 && from->outer_stride != to->outer_stride))
             return NEREUS_ERR_MISMATCH;
         if (beams < 1 || to->rows % beams) return NEREUS_ERR_ARG;
+        if (!disjoint(grid_of(*to), to->buffer, to->buffers, nullptr)) return NEREUS_ERR_ALIAS;
     } else {
         if (beams) return NEREUS_ERR_ARG;
         // rows whose pieces lie between other rows' are looked at piece by piece
@@ -1092,7 +1144,7 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
             const int64_t row = t.rows > 1 ? t.row_stride : 0, step = t.outer > 1 ? t.outer_stride : 0, whole = (t.outer - 1) * step + piece;
             return row >= whole || t.rows < 2 ? Side{t.buffer, t.buffers, t.rows, row, whole} : Side{t.buffer, t.buffers, t.outer, step, (t.rows - 1) * row + piece};
         };
-        if (!apart(side(*from), side(*to))) return NEREUS_ERR_ALIAS;
+        if (!apart(side(*from), side(*to)) || !disjoint(grid_of(*to), to->buffer, to->buffers, from->buffer)) return NEREUS_ERR_ALIAS;
     }
     Device dev;
     if (int rc = device_of(&dev)) return rc;
