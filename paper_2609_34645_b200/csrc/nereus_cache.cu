@@ -894,6 +894,26 @@ bool meet(const Grid& g, int64_t delta) {
     }
     return false;
 }
+// Whether the bytes of an array meet a piece of the buffer at `base`.
+bool meet(const Grid& g, uintptr_t base, const Range& r) {
+    if (r.lo >= r.hi || r.hi <= base || r.lo >= base + g.whole()) return false;
+    // the first piece that ends behind r.lo
+    const int64_t at = r.lo > base ? (int64_t)(r.lo - base) : 0;
+    int64_t       i = g.n0 > 1 ? at / g.s0 : 0, rest = at - i * g.s0, j = g.n1 > 1 ? rest / g.s1 : 0;
+    if (rest - j * g.s1 >= g.width) ++j;
+    if (j >= g.n1) { ++i; j = 0; }
+    return i < g.n0 && base + i * g.s0 + j * g.s1 < r.hi;
+}
+// Whether n buffers share no byte with any of the arrays.
+bool clear_of(const Grid& g, void* const* base, int n, const Range* arrays, int n_arrays) {
+    Range hull = {UINTPTR_MAX, 0};
+    for (int i = 0; i < n; ++i) hull = {std::min(hull.lo, (uintptr_t)base[i]), std::max(hull.hi, (uintptr_t)base[i] + g.whole())};
+    for (int a = 0; a < n_arrays; ++a)
+        if (arrays[a].lo < arrays[a].hi && meet(hull, arrays[a]))
+            for (int i = 0; i < n; ++i)
+                if (meet(g, (uintptr_t)base[i], arrays[a])) return false;
+    return true;
+}
 // Whether n buffers of such pieces share no byte with one another.  Where `other` is given, two that are the same here and there
 // count as one.  Buffers one after the other, and such whose pieces or inner stretches lie side by side, are seen at a glance.
 bool disjoint(const Grid& g, void* const* base, int n, void* const* other) {
@@ -938,26 +958,28 @@ int check_books(const nereus_page_table_t* t, bool length) {
     if (misaligned(t->refs) || misaligned(t->table) || (length && misaligned(t->length))) return NEREUS_ERR_ALIGN;
     return NEREUS_OK;
 }
-// The old and new books, and arrays of a call, share no byte.
-int check_apart(const nereus_page_table_t& a, const nereus_page_table_t& b, int pages, bool length, const Range* read, int n_read, const Range* written,
-                int n_written) {
-    Range r[8], w[8];
-    int   nr = 0, nw = 0;
-    auto books = [&](const nereus_page_table_t& t, Range* x, int* n) {
-        x[(*n)++] = ints(t.refs, pages);
-        x[(*n)++] = t.rows ? ints(t.table, (t.rows - 1) * t.stride + t.columns) : Range{0, 0};
-        x[(*n)++] = t.rows && length ? ints(t.length, t.rows) : Range{0, 0};
+// The pages of a call's pools.
+Grid grid_of(const nereus_pages_t& p) { return {p.pages, p.page_stride, 1, 0, p.page_bytes}; }
+// The old and new books, arrays of a call and its pools share no byte; two pools are apart, or one.
+int check_apart(const nereus_pages_t& pools, const nereus_page_table_t& a, const nereus_page_table_t& b, bool length, const Range* read, int n_read,
+                const Range* written, int n_written) {
+    Range r[16];                                       // what is read, then what is written
+    int   n = 0;
+    auto books = [&](const nereus_page_table_t& t) {
+        r[n++] = ints(t.refs, pools.pages);
+        r[n++] = t.rows ? ints(t.table, (t.rows - 1) * t.stride + t.columns) : Range{0, 0};
+        r[n++] = t.rows && length ? ints(t.length, t.rows) : Range{0, 0};
     };
-    books(a, r, &nr);
-    books(b, w, &nw);
-    for (int i = 0; i < n_read; ++i) r[nr++] = read[i];
-    for (int i = 0; i < n_written; ++i) w[nw++] = written[i];
-    for (int i = 0; i < nw; ++i) {
-        for (int j = 0; j < nr; ++j)
-            if (meet(w[i], r[j])) return NEREUS_ERR_ALIAS;
+    books(a);
+    for (int i = 0; i < n_read; ++i) r[n++] = read[i];
+    const int first = n;
+    books(b);
+    for (int i = 0; i < n_written; ++i) r[n++] = written[i];
+    for (int i = first; i < n; ++i)
         for (int j = 0; j < i; ++j)
-            if (meet(w[i], w[j])) return NEREUS_ERR_ALIAS;
-    }
+            if (meet(r[i], r[j])) return NEREUS_ERR_ALIAS;
+    const Grid pages = grid_of(pools);
+    if (!disjoint(pages, pools.pool, pools.pools, pools.pool) || !clear_of(pages, pools.pool, pools.pools, r, n)) return NEREUS_ERR_ALIAS;
     return NEREUS_OK;
 }
 
@@ -1146,6 +1168,8 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
         };
         if (!apart(side(*from), side(*to)) || !disjoint(grid_of(*to), to->buffer, to->buffers, from->buffer)) return NEREUS_ERR_ALIAS;
     }
+    const Range arrays[] = {ints(parent, to->rows), ints(length, length ? from->rows : 0)};
+    if (!clear_of(grid_of(*to), to->buffer, to->buffers, arrays, 2)) return NEREUS_ERR_ALIAS;
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     auto go = to->buffers <= kFew ? reorder<kFew> : reorder<NEREUS_MAX_BUFFERS>;
@@ -1166,6 +1190,8 @@ int nereus_cache_copy(const nereus_pages_t* from, const nereus_pages_t* to, int6
                         Side{to->pool, to->pools, to->pages, to->page_stride, to->page_bytes}))
         return NEREUS_ERR_ALIAS;
     if (!n || !from->pools) return NEREUS_OK;
+    const Range arrays[] = {ints(src, n), ints(dst, n)};
+    if (!disjoint(grid_of(*to), to->pool, to->pools, from->pool) || !clear_of(grid_of(*to), to->pool, to->pools, arrays, 2)) return NEREUS_ERR_ALIAS;
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     return with_pools(*from, *to, [&](auto vector, auto& p) { return copy_launch<decltype(vector)>(p, n, src, dst, dev, (cudaStream_t)cuda_stream); });
@@ -1182,7 +1208,7 @@ int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* fr
     if (!status || (to->rows && (!parent || !copies))) return NEREUS_ERR_ARG;
     if (misaligned(parent) || misaligned(room_of) || misaligned(copies) || misaligned(status)) return NEREUS_ERR_ALIGN;
     const Range read[] = {ints(parent, to->rows), ints(room_of, room_of ? to->rows : 0)}, written[] = {ints(copies, 2 * (int64_t)to->rows), ints(status, 4)};
-    if (int rc = check_apart(*from, *to, pools->pages, true, read, 2, written, 2)) return rc;
+    if (int rc = check_apart(*pools, *from, *to, true, read, 2, written, 2)) return rc;
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const Books    old = books_of(*from, pools->pages);
@@ -1230,7 +1256,7 @@ int nereus_cache_compact(const nereus_pages_t* pools, const nereus_page_table_t*
     if (misaligned(map) || misaligned(status)) return NEREUS_ERR_ALIGN;
     if ((uintptr_t)moves & 7) return NEREUS_ERR_ALIGN;
     const Range written[] = {ints(map, pools->pages), ints(moves, pools->pages / 2 * 2), ints(status, 4)};
-    if (int rc = check_apart(*from, *to, pools->pages, false, nullptr, 0, written, 3)) return rc;
+    if (int rc = check_apart(*pools, *from, *to, false, nullptr, 0, written, 3)) return rc;
     Device dev;
     if (int rc = device_of(&dev)) return rc;
     const Books    old = books_of(*from, pools->pages);

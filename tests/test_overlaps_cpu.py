@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2609_34645_b200 import binding as B
-from test_beam_cache_cpu import A, code
+from test_beam_cache_cpu import A, NEW, OLD, REST, book, code, pages
 
 FAR = 1 << 34
 no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="what is not refused would run on addresses that are none")
@@ -77,3 +77,54 @@ def test_overlaps_are_told_byte_by_byte():
         assert in_place(s) == want, (list(s.buffer[:s.buffers]), rows, outer, piece, row, step)
         told[want] += 1
     assert min(told.values()) > 500
+
+
+# ---- arrays within buffers, pools that overlap -------------------------------------------------------------------
+
+def test_arrays_within_the_states_that_are_written():
+    s = states([A, A + (1 << 20)], row=256)
+    for at in (A, A + 4, A + 124, A + 3 * 256 + 120, A + (1 << 20) + 512, A - 12):
+        assert code(B.states_reorder, s, s, 2, at, None) == code(B.states_reorder, s, s, 2, FAR, at) == B.ERR_ALIAS
+    src = states([FAR << 1, (FAR << 1) + (1 << 20)], row=256)
+    assert code(B.states_reorder, src, s, 0, A + 8, None) == B.ERR_ALIAS
+
+
+def test_arrays_within_the_pools():
+    def fork(old=None, new=None, parent=REST, room_of=None, copies=REST + 4096, status=REST + 8192, pool=None):
+        return code(B.cache_fork, pool or pages(), old or book(OLD), new or book(NEW), parent, 16, 0, room_of, copies, status)
+
+    def compact(old=None, new=None, where=REST, moves=REST + 4096, status=REST + 8192, pool=None):
+        return code(B.cache_compact, pool or pages(), old or book(OLD), new or book(NEW), -1, where, moves, status)
+    for at in (A, A + 636, A + (1 << 16) + 64):                                            # pages are 640 bytes of each pool
+        for call in (fork, compact):
+            assert call(old=book(OLD, table=at)) == call(old=book(OLD, refs=at)) == call(new=book(NEW, table=at)) == B.ERR_ALIAS
+            assert call(new=book(NEW, refs=at)) == call(status=at) == B.ERR_ALIAS
+        assert fork(old=book(OLD, length=at)) == fork(new=book(NEW, length=at)) == fork(parent=at) == fork(room_of=at) == fork(copies=at) == B.ERR_ALIAS
+        assert compact(where=at) == compact(moves=at - at % 8) == B.ERR_ALIAS
+        assert code(B.cache_copy, pages(base=OLD), pages(), 3, at, REST) == code(B.cache_copy, pages(), pages(), 3, REST, at) == B.ERR_ALIAS
+
+
+def test_pools_that_overlap():
+    shifted = pages()
+    shifted.pool[1] = shifted.pool[0] + 64                                                 # page p of one is page p + 1 of the other
+    assert code(B.cache_fork, shifted, book(OLD), book(NEW), REST, 16, 0, None, REST + 4096, REST + 8192) == B.ERR_ALIAS
+    assert code(B.cache_compact, shifted, book(OLD), book(NEW), -1, REST, REST + 4096, REST + 8192) == B.ERR_ALIAS
+    assert code(B.cache_copy, shifted, shifted, 3, REST, REST + 4096) == code(B.cache_copy, pages(base=OLD), shifted, 3, REST, REST + 4096) == B.ERR_ALIAS
+    twice = pages()
+    twice.pool[1] = twice.pool[0]
+    assert code(B.cache_copy, pages(base=OLD), twice, 3, REST, REST + 4096) == B.ERR_ALIAS
+
+
+@no_gpu
+def test_arrays_and_pools_that_do_not_meet():
+    twice = pages()
+    twice.pool[1] = twice.pool[0]                                                          # one pool, named twice
+    assert code(B.cache_copy, twice, twice, 3, REST, REST + 4096) == B.ERR_CUDA
+    wide = pages(stride=128)
+    wide.pool[1] = wide.pool[0] + 64                                                       # keys and values of a page side by side
+    assert code(B.cache_fork, wide, book(OLD), book(NEW), REST, 16, 0, None, REST + 4096, REST + 8192) == B.ERR_CUDA
+    gap = pages(stride=128)
+    assert code(B.cache_copy, gap, gap, 3, A + 64, A + 128 + 64) == B.ERR_CUDA             # arrays between two pages
+    assert code(B.cache_copy, gap, gap, 17, A + 64, REST) == B.ERR_ALIAS                   # 17 numbers reach the next
+    s = states([A], row=256)
+    assert code(B.states_reorder, s, s, 2, A + 128, A + 256 + 128) == B.ERR_CUDA
