@@ -960,14 +960,15 @@ int check_books(const nereus_page_table_t* t, bool length) {
 }
 // The pages of a call's pools.
 Grid grid_of(const nereus_pages_t& p) { return {p.pages, p.page_stride, 1, 0, p.page_bytes}; }
+// The rows of a page table.
+Grid grid_of(const nereus_page_table_t& t) { return {std::max(t.rows, 1), t.rows > 1 ? 4 * t.stride : 0, 1, 0, 4 * (int64_t)t.columns}; }
 // The old and new books, arrays of a call and its pools share no byte; two pools are apart, or one.
 int check_apart(const nereus_pages_t& pools, const nereus_page_table_t& a, const nereus_page_table_t& b, bool length, const Range* read, int n_read,
                 const Range* written, int n_written) {
-    Range r[16];                                       // what is read, then what is written
+    Range r[16];                                       // what is read, then what is written; the tables on their own
     int   n = 0;
     auto books = [&](const nereus_page_table_t& t) {
         r[n++] = ints(t.refs, pools.pages);
-        r[n++] = t.rows ? ints(t.table, (t.rows - 1) * t.stride + t.columns) : Range{0, 0};
         r[n++] = t.rows && length ? ints(t.length, t.rows) : Range{0, 0};
     };
     books(a);
@@ -978,6 +979,13 @@ int check_apart(const nereus_pages_t& pools, const nereus_page_table_t& a, const
     for (int i = first; i < n; ++i)
         for (int j = 0; j < i; ++j)
             if (meet(r[i], r[j])) return NEREUS_ERR_ALIAS;
+    // tables may be columns of one wider tensor
+    const Grid at = grid_of(a), bt = grid_of(b);
+    if (a.rows && b.rows && !apart((uintptr_t)a.table, at.n0, at.s0, at.width, (uintptr_t)b.table, bt.n0, bt.s0, bt.width)) return NEREUS_ERR_ALIAS;
+    for (int i = 0; i < n; ++i)
+        if ((i >= first && a.rows && meet(at, (uintptr_t)a.table, r[i])) || (b.rows && meet(bt, (uintptr_t)b.table, r[i]))) return NEREUS_ERR_ALIAS;
+    r[n++] = ints(a.table, a.rows ? (a.rows - 1) * a.stride + a.columns : 0);
+    r[n++] = ints(b.table, b.rows ? (b.rows - 1) * b.stride + b.columns : 0);
     const Grid pages = grid_of(pools);
     if (!disjoint(pages, pools.pool, pools.pools, pools.pool) || !clear_of(pages, pools.pool, pools.pools, r, n)) return NEREUS_ERR_ALIAS;
     return NEREUS_OK;

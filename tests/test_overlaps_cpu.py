@@ -128,3 +128,30 @@ def test_arrays_and_pools_that_do_not_meet():
     assert code(B.cache_copy, gap, gap, 17, A + 64, REST) == B.ERR_ALIAS                   # 17 numbers reach the next
     s = states([A], row=256)
     assert code(B.states_reorder, s, s, 2, A + 128, A + 256 + 128) == B.ERR_CUDA
+
+
+# ---- tables that are columns of one tensor -----------------------------------------------------------------------
+
+def fork_of(old, new, parent=REST, copies=REST + 4096):
+    return code(B.cache_fork, pages(), old, new, parent, 16, 0, None, copies, REST + 8192)
+
+
+def compact_of(old, new):
+    return code(B.cache_compact, pages(), old, new, -1, REST, REST + 4096, REST + 8192)
+
+
+def test_tables_that_share_columns():
+    for at, stride in ((OLD + 12, 8), (OLD + 32 * 2 + 12, 8), (OLD + 20, 8), (OLD + 16, 9), (OLD + 8, 4), (OLD + 64, 8)):
+        new = book(NEW, table=at, stride=stride)
+        assert fork_of(book(OLD, stride=8), new) == compact_of(book(OLD, stride=8), new) == B.ERR_ALIAS
+    # an array within a row of either table
+    assert fork_of(book(OLD, stride=8), book(NEW, stride=8), copies=OLD + 32) == fork_of(book(OLD, stride=8), book(NEW, stride=8), parent=NEW + 12) == B.ERR_ALIAS
+
+
+@no_gpu
+def test_tables_side_by_side():
+    for at in (OLD + 16, OLD - 16, OLD + 32 + 16):
+        new = book(NEW, table=at, stride=8)
+        assert fork_of(book(OLD, stride=8), new) == compact_of(book(OLD, stride=8), new) == B.ERR_CUDA
+    assert fork_of(book(OLD, rows=1), book(NEW, rows=1, table=OLD + 16)) == B.ERR_CUDA
+    assert fork_of(book(OLD, stride=8), book(NEW, stride=8), parent=NEW + 16) == B.ERR_CUDA
