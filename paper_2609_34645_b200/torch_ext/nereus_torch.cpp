@@ -343,6 +343,7 @@ PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     how.beams = beams < 1 || beams > NEREUS_BEAM_MAX ? 0 : (int32_t)beams;
     how.k = k < 1 || k > NEREUS_BEAM_MAX_K ? 0 : (int32_t)k;
     how.settle = PyObject_IsTrue(a[7]);
+    if (how.settle < 0) throw python_error();
     if (a[2] == Py_None) throw Wrong{"score: expected a tensor"};
     how.score = (const float*)arg_of(a[2], at::kFloat, rows, -1, x, "score");
     how.ended = (const int32_t*)arg_of(a[5], at::kInt, rows, -1, x, "ended");
