@@ -515,8 +515,9 @@ typedef struct {
     const int32_t* ended;          /* [rows], or NULL: none has; outside [0, vocab): it goes on */
     const float*   norm;           /* [rows], or NULL = 1 */
 } nereus_beams_t;
-/* Bytes of the workspace that a call with this view's shape and these beams and k needs on the current device, a few
- * hundred per row and 64 KiB of logits.  Errors: as below. */
+/* Bytes of the workspace that a call with this view's shape and these beams and k needs on the current device: 528 for each
+ * piece of up to 16 KiB of a row's logits, or for a few such pieces together where a request has more than 128 (4 rows
+ * of 128256 bf16: 33 KB; 1024 such rows, 8 a request: 8.6 MB).  Errors: as below. */
 int nereus_beam_workspace(const nereus_logits_t* in, const nereus_beams_t* how, size_t* bytes);
 /* out_score, out_parent, out_token: [rows / beams, k].  workspace (device, 16-byte aligned) is written and read by the call
  * alone: calls that may overlap on the device, two captured graphs among them, have one each.  Unlike the other calls' a request's
@@ -655,8 +656,8 @@ int nereus_cache_fork(const nereus_pages_t* pools, const nereus_page_table_t* fr
                       int32_t* status, void* cuda_stream);
 /* Moves the pages in use to the front, so that the pools can be cut to their first `keep` pages (keep < 0: to as many as
  * are in use), e.g. to have room for a plan transition: the j-th page in use at or past `keep` goes to the j-th free page below
- * it.  map (device, [pages]): where each page is now, -1 for free ones.  moves (device, [pages / 2, 2]): source and destination of
- * the moves; what lies behind the last is left as it was.  `to` gets the table and refs by the new ids (entries that are no page
+ * it.  map (device, [pages]): where each page is now, -1 for free ones.  moves (device, [pages / 2, 2], aligned to 8 bytes): source
+ * and destination of the moves; what lies behind the last is left as it was.  `to` gets the table and refs by the new ids (entries that are no page
  * stay as they are, entries of free pages become -1); length is neither read nor written and may be NULL.
  * status (device, [4]): pages in use; pages in use beyond `keep`, where they are more than that: nothing is moved then; moves
  * made; pages that hold everything now (keep, or the pools' size where nothing could be moved).
