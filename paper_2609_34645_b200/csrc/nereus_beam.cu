@@ -12,8 +12,11 @@
 //     few times k hypotheses, is ranked by counting.
 // Where more is found than the list holds (rows of few distinct values: a mask's lowest value, say), the bound is made exact
 // by counting the keys' bytes, the highest first, a pass over the request for each byte that is needed.
-// 128 requests x 8 x 128256 bf16 (32.6 us of HBM): 45 us the sum, 4.8 TB/s, which 8 instructions and an exponential an element
-// bound, and 12 the pick, a chain of dependent steps.  One request of 4 beams takes 10 us, by the same chain.
+// 128 requests x 8 x 128256 bf16 (32.6 us of HBM): 45 us the sum, 4.8 TB/s, and 12 the pick, a chain of dependent steps.  No unit is
+// full while the sum runs: instructions are issued in 61% of the cycles, 8 an element, of which 3.3 are on whole numbers where opening
+// a bf16 asks for one; the exponentials' unit is at 56%, DRAM at 59%.  A scheduler has 6.4 warps, 1.7 of them ready; the others wait
+// for fixed latencies, for the queue of exponentials and shared memory, and for the next layer, in about equal parts.  One
+// request of 4 beams takes 10 us, by the pick's chain.
 // Hypotheses are compared in 64 bits, as keys of (total / norm, lower index): within a row these order as the logits do.
 #include "nereus_rows.hpp"
 
