@@ -7,6 +7,8 @@ States are one tensor [rows, ...] or a list of them (keys and values of every la
 tensors: table [rows, columns] (the page of every page_size tokens of a sequence, -1 for none), length [rows] (tokens of a
 sequence) and refs [pages] (how often a page is held; 0: it is free).
 
+What a call writes shares no memory with anything else that it reads or writes; a pool that is named twice counts as one.
+
 Everything runs in the CUDA library on torch's current stream and synchronises nothing; what is returned was allocated on that
 stream unless the caller passed it in.  Wrong types, devices or shapes raise ValueError, everything the library refuses raises
 NereusError.  What device arrays say (parents, lengths, page ids) is checked on the device: what is out of range is left

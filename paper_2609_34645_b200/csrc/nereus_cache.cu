@@ -879,18 +879,17 @@ struct Grid {
     int64_t inner() const { return (n1 - 1) * s1 + width; }
     int64_t whole() const { return (n0 - 1) * s0 + inner(); }
 };
-// Whether two buffers of such pieces share a byte when one lies `delta` bytes behind the other.  A piece meets those next to its
-// own distance alone.
-bool meet(const Grid& g, int64_t delta) {
-    if (delta < 0) delta = -delta;
-    if (delta >= g.whole()) return false;
-    const int64_t first = g.n0 > 1 ? delta / g.s0 : 0;
-    for (int64_t i = first; i <= first + 1 && i < g.n0; ++i) {
-        const int64_t rest = std::abs(delta - i * g.s0);
-        if (rest >= g.inner()) continue;
-        const int64_t second = g.n1 > 1 ? rest / g.s1 : 0;
-        for (int64_t j = second; j <= second + 1 && j < g.n1; ++j)
-            if (std::abs(rest - j * g.s1) < g.width) return true;
+// Whether a buffer of such pieces and one of the same strides, of n0 times n1, share a byte when the second lies `delta` bytes behind
+// the first.  A piece meets those next to its own distance alone.
+bool meet(const Grid& g, int64_t delta, int64_t n0, int64_t n1) {
+    auto below = [](int64_t x, int64_t step) { return x >= 0 ? x / step : -((step - 1 - x) / step); };
+    const int64_t first = g.s0 > 0 ? below(delta, g.s0) : 0;
+    for (int64_t i = first; i <= first + 1; ++i) {
+        const int64_t rest = delta - i * g.s0;
+        if (i <= -n0 || i >= g.n0 || rest >= g.inner() || -rest >= (n1 - 1) * g.s1 + g.width) continue;
+        const int64_t second = g.s1 > 0 ? below(rest, g.s1) : 0;
+        for (int64_t j = second; j <= second + 1; ++j)
+            if (j > -n1 && j < g.n1 && std::abs(rest - j * g.s1) < g.width) return true;
     }
     return false;
 }
@@ -933,7 +932,7 @@ bool disjoint(const Grid& g, void* const* base, int n, void* const* other) {
     for (int i = 0; i < n; ++i)
         for (int j = i + 1; j < n && all[j].lo - all[i].lo < (uintptr_t)g.whole(); ++j) {
             if (other && all[i].lo == all[j].lo && other[all[i].i] == other[all[j].i]) continue;
-            if (meet(g, (int64_t)(all[j].lo - all[i].lo))) return false;
+            if (meet(g, (int64_t)(all[j].lo - all[i].lo), g.n0, g.n1)) return false;
         }
     return true;
 }
@@ -1097,6 +1096,26 @@ Grid grid_of(const nereus_states_t& t) {
     return t.rows < 2 || row >= (t.outer - 1) * step + piece ? Grid{t.rows, row, t.outer, step, piece} : Grid{t.outer, step, t.rows, row, piece};
 }
 
+// Whether no buffer of one side shares a byte with one of the other.
+bool apart(const nereus_states_t& a, const nereus_states_t& b) {
+    const int64_t piece = a.tokens * a.token_bytes;
+    // rows whose pieces lie between other rows' are looked at piece by piece
+    auto side = [&](const nereus_states_t& t) {
+        const Grid g = grid_of(t);
+        return Side{t.buffer, t.buffers, g.n0, g.s0, g.inner()};
+    };
+    if (apart(side(a), side(b))) return true;
+    if ((a.rows > 1 && b.rows > 1 && a.row_stride != b.row_stride) || (a.outer > 1 && a.outer_stride != b.outer_stride)) return false;
+    // buffers that interleave, as keys and values of every head do
+    const int64_t row = a.rows > 1 ? a.row_stride : b.rows > 1 ? b.row_stride : 0, step = a.outer > 1 ? a.outer_stride : 0;
+    const bool    by_row = std::max(a.rows, b.rows) < 2 || row >= (a.outer - 1) * step + piece;
+    const Grid    g = by_row ? Grid{a.rows, row, a.outer, step, piece} : Grid{a.outer, step, a.rows, row, piece};
+    for (int i = 0; i < a.buffers; ++i)
+        for (int j = 0; j < b.buffers; ++j)
+            if (meet(g, (int64_t)((uintptr_t)b.buffer[j] - (uintptr_t)a.buffer[i]), by_row ? b.rows : b.outer, by_row ? b.outer : b.rows)) return false;
+    return true;
+}
+
 template <class V, int N, class S> int reorder_launch(S& s, const int32_t* parent, const int32_t* length, const Device& dev, cudaStream_t stream) {
     constexpr int64_t kTile = (int64_t)kMoveThreads * sizeof(V);
     const int64_t groups = ((int64_t)s.to_rows + s.group - 1) / s.group, items = (s.piece + kTile - 1) / kTile * s.outer * s.buffers;
@@ -1169,12 +1188,7 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
         if (!disjoint(grid_of(*to), to->buffer, to->buffers, nullptr)) return NEREUS_ERR_ALIAS;
     } else {
         if (beams) return NEREUS_ERR_ARG;
-        // rows whose pieces lie between other rows' are looked at piece by piece
-        auto side = [&](const nereus_states_t& t) {
-            const int64_t row = t.rows > 1 ? t.row_stride : 0, step = t.outer > 1 ? t.outer_stride : 0, whole = (t.outer - 1) * step + piece;
-            return row >= whole || t.rows < 2 ? Side{t.buffer, t.buffers, t.rows, row, whole} : Side{t.buffer, t.buffers, t.outer, step, (t.rows - 1) * row + piece};
-        };
-        if (!apart(side(*from), side(*to)) || !disjoint(grid_of(*to), to->buffer, to->buffers, from->buffer)) return NEREUS_ERR_ALIAS;
+        if (!apart(*from, *to) || !disjoint(grid_of(*to), to->buffer, to->buffers, from->buffer)) return NEREUS_ERR_ALIAS;
     }
     const Range arrays[] = {ints(parent, to->rows), ints(length, length ? from->rows : 0)};
     if (!clear_of(grid_of(*to), to->buffer, to->buffers, arrays, 2)) return NEREUS_ERR_ALIAS;

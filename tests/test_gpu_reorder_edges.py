@@ -50,3 +50,20 @@ def test_groups_whose_parents_cross(beams, token, unit):
         gaps = torch.ones(flat.shape[0], dtype=torch.bool, device="cuda")
         torch.as_strided(gaps, x.shape, x.stride(), x.storage_offset()).fill_(False)
         assert torch.equal(flat[gaps], before[gaps])                     # nothing between the rows is written
+
+
+def test_keys_and_values_of_every_head_side_by_side():
+    """Both in place at once, then one to the other's place in the same tensor."""
+    rng = seed("side by side")
+    whole = noise(rng, (6, 3, 2, 9, 10), torch.bfloat16)                 # rows, heads, keys and values, tokens, width
+    states = [whole[:, :, 0], whole[:, :, 1]]
+    move = lambda a: a.transpose(0, 2, 1, 3)                             # noqa: E731
+    parent, length = [1, 2, 0, 4, 3, 3], np.array([9, 4, 7, 0, 3, 5])
+    old = [move(as_bytes(t)) for t in states]
+    C.reorder(states, ints(parent), beams=3, length=ints(length), dim=2)
+    now = [U.reorder(o, o, parent, length, 3) for o in old]
+    for t, w in zip(states, now):
+        assert np.array_equal(move(as_bytes(t)), w)
+    C.reorder(states[0], ints([5, 5, 0, 1, 2, -1]), length=ints(length), dim=2, out=states[1])
+    assert np.array_equal(move(as_bytes(states[0])), now[0])
+    assert np.array_equal(move(as_bytes(states[1])), U.reorder(now[0], now[1], [5, 5, 0, 1, 2, -1], length, 0))

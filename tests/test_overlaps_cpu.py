@@ -155,3 +155,38 @@ def test_tables_side_by_side():
         assert fork_of(book(OLD, stride=8), new) == compact_of(book(OLD, stride=8), new) == B.ERR_CUDA
     assert fork_of(book(OLD, rows=1), book(NEW, rows=1, table=OLD + 16)) == B.ERR_CUDA
     assert fork_of(book(OLD, stride=8), book(NEW, stride=8), parent=NEW + 16) == B.ERR_CUDA
+
+
+# ---- out of place, between buffers of one tensor -------------------------------------------------------------------
+
+@no_gpu
+def test_from_one_buffer_to_another_between_its_pieces():
+    def move(src, dst):
+        return code(B.states_reorder, src, dst, 0, FAR, None)
+    keys, values = states([A], outer=2, row=512, step=256), states([A + 128], outer=2, row=512, step=256)      # of every head
+    assert move(keys, values) == move(values, keys) == B.ERR_CUDA
+    assert move(keys, states([A + 128], rows=2, outer=2, row=512, step=256)) == move(states([A], rows=1, outer=2, step=256), values) == B.ERR_CUDA
+    assert move(keys, states([A + 127], outer=2, row=512, step=256)) == move(keys, states([A + 129], outer=2, row=512, step=256)) == B.ERR_ALIAS
+    assert move(keys, states([A + 512], outer=2, row=512, step=256)) == B.ERR_ALIAS                              # a row further on
+    import random
+    rng = random.Random(9)
+    told = {B.ERR_ALIAS: 0, B.ERR_CUDA: 0}
+    for _ in range(4000):
+        rows, more, outer, piece = rng.randint(1, 4), rng.randint(1, 4), rng.randint(1, 4), rng.choice([1, 2, 5])
+        if rng.random() < 0.5:
+            step = rng.randint(piece, 3 * piece)
+            row = rng.randint((outer - 1) * step + piece, 3 * outer * step)
+        else:
+            row = rng.randint(piece, 3 * piece)
+            step = rng.randint((max(rows, more) - 1) * row + piece, 3 * max(rows, more) * row)
+        hull = (rows - 1) * row + (outer - 1) * step + piece
+        far = rng.choice([piece * 4, hull * 2])
+        src = states([A + rng.randint(0, far) for _ in range(2)], rows, outer, 1, piece, row, step)
+        dst = states([A + rng.randint(0, far), A + (1 << 20)], more, outer, 1, piece, row, step)
+        if src.buffer[0] == dst.buffer[0]:
+            continue
+        held = bytes_of(src, src.buffer[0]) | bytes_of(src, src.buffer[1])
+        want = B.ERR_ALIAS if held & bytes_of(dst, dst.buffer[0]) else B.ERR_CUDA
+        assert move(src, dst) == want, (src.buffer[0], src.buffer[1], dst.buffer[0], rows, more, outer, piece, row, step)
+        told[want] += 1
+    assert min(told.values()) > 500
