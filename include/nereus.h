@@ -614,7 +614,7 @@ int nereus_states_reorder(const nereus_states_t* from, const nereus_states_t* to
                           const int32_t* length, void* cuda_stream);
 
 /* A paged cache: `pools` pools (keys and values of every layer, of every virtual rank), all of `pages` pages; page p of pool q
- * is page_bytes contiguous bytes at pool[q] + p * page_stride.  Any sizes and alignment work. */
+ * is page_bytes contiguous bytes at pool[q] + p * page_stride.  Any sizes and alignment work.  Two pools share no byte, or are one. */
 typedef struct {
     int32_t pools, pages;          /* pools 0..NEREUS_MAX_BUFFERS; 0: the calls keep the books and move nothing */
     int64_t page_bytes, page_stride;
